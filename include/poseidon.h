@@ -13,7 +13,8 @@
  * schemes on payloads that are already in device memory, and the choice.
  *
  * General conventions
- *  - All array arguments are device pointers to fp32 data owned by the caller.
+ *  - All array arguments are device pointers to fp32 data owned by the caller
+ *    (the operators at a network's end name their own types).
  *    The library allocates no device memory and keeps no pointer past a call,
  *    except a KV store, which keeps its tensors' pointers for its lifetime and
  *    each received update's pointer until the work it triggers has been
@@ -597,8 +598,142 @@ typedef struct poseidon_launch_record {
 int poseidon_pool_launch_times(poseidon_stream_pool* pool, poseidon_launch_record* records,
                                int32_t capacity, int32_t* count);
 
+/*
+ * The operators at the end of a network.  What the updates above consume is
+ * made by a worker's backward pass: the factors (u, v) of a fully-connected
+ * layer's gradient, dense gradients of everything else.  These make the
+ * payloads of a large classifier (softmax cross entropy fused with its
+ * product) and of normalisation layers, and the dropout between them.
+ *
+ * Activations and the classifier's weight are fp32 or bf16 (`dtype`, one for
+ * all of a call's untyped arrays); what is synchronised or accumulated -- U,
+ * dW, dgamma, dbeta, and gamma, beta, losses and statistics -- is fp32.  Sums
+ * and statistics are fp32 whatever the type; a bf16 result is rounded once.
+ * Arrays are row-major without gaps, on any boundary of their own type.
+ * A workspace is caller-owned device memory on a 16-byte boundary of at least
+ * the size its query returns, whose contents mean nothing before or after the
+ * call; it may be shared by calls that run one after the other.  No result
+ * depends on timing: the same call gives the same bits.
+ */
+#define POSEIDON_F32  0
+#define POSEIDON_BF16 1
+
+/*
+ * Dropout (inverted): y = residual + keep * x / (1 - p), element by element on
+ * rows x cols values; residual may be NULL (0).  The backward pass is the same
+ * call on the gradient.
+ *
+ * The mask is not stored: element (r, c) is dropped when its 16 random bits
+ * are below t = floor(65536 p + 1/2), and the scale is 65536 / (65536 - t), so
+ * that p counts as rounded to 2^-16.  The bits come from Philox4x32 with seven
+ * rounds (Salmon et al., SC 2011): rng[0] is the 64-bit key, the counter's
+ * low 64 bits are the group r * ceil(cols / 8) + c / 8, its high 64 bits
+ * rng[1]; within the 128 bits of a group, element c takes bits
+ * 16 (c mod 8) .. + 15.  rng (two values in device memory, read when the work
+ * runs, so that a captured graph's replays can each have their own) is the
+ * caller's to advance: equal rng, rows and cols give equal masks.  t = 0 drops
+ * nothing and reads no rng (NULL allowed); t = 65536 drops everything.  A
+ * dropped element leaves nothing even where x is infinite or NaN.
+ * Returns POSEIDON_OK, POSEIDON_ERR_INVALID_ARG (negative sizes, an unknown
+ * dtype, p outside 0..1, NULL arrays with work, y overlapping an input) or
+ * POSEIDON_ERR_HIP.
+ */
+int poseidon_dropout(const void* x, const void* residual, int64_t rows, int64_t cols, int32_t dtype, double p,
+                     const int64_t* rng, void* y, hipStream_t stream);
+
+/*
+ * Layer norm over rows of cols values, with the dropout and the residual sum
+ * that come before it in the same pass:
+ *
+ *     h = residual + dropout(x)       (as poseidon_dropout; either may be absent)
+ *     mean = avg(h), rstd = 1 / sqrt(avg((h - mean)^2) + eps)      (per row)
+ *     y = (h - mean) * rstd * gamma + beta
+ *
+ * h (may be NULL) and y are rows x cols of `dtype`; mean and rstd have rows
+ * values, gamma and beta cols.  Statistics and y come from h before it is
+ * rounded.  Returns POSEIDON_OK, POSEIDON_ERR_INVALID_ARG (as
+ * poseidon_dropout; also cols < 1 with rows > 0, cols above 2^28, a negative
+ * or NaN eps, outputs overlapping each other or an input) or POSEIDON_ERR_HIP.
+ */
+int poseidon_norm_forward(const void* x, const void* residual, const float* gamma, const float* beta,
+                          int64_t rows, int64_t cols, int32_t dtype, float eps, double p, const int64_t* rng,
+                          void* h, void* y, float* mean, float* rstd, hipStream_t stream);
+
+/* Bytes of workspace for poseidon_norm_backward.  Host-only. */
+int poseidon_norm_workspace(int64_t rows, int64_t cols, int64_t* bytes);
+
+/*
+ * Its backward pass, from h, mean and rstd as the forward pass left them; with
+ * g = dy * gamma and n = (h - mean) * rstd:
+ *
+ *     dh = rstd * (g - avg(g) - n * avg(g * n)) + dresidual
+ *     dx = dropout(dh)                 (the forward's p and rng)
+ *     dgamma = sum over rows of dy * n,   dbeta = sum over rows of dy
+ *
+ * dh is the gradient of the residual input; dresidual (may be NULL) is what
+ * arrives at h by another way.  dx may be NULL when p drops nothing (it is dh
+ * then).  dgamma and dbeta (cols values, replaced) may lie in a gradient
+ * shard; with rows = 0 they are 0.  Returns POSEIDON_OK,
+ * POSEIDON_ERR_INVALID_ARG (as poseidon_norm_forward; also a workspace too
+ * small or off its boundary) or POSEIDON_ERR_HIP.
+ */
+int poseidon_norm_backward(const void* dy, const void* h, const float* gamma, const float* mean, const float* rstd,
+                           const void* dresidual, int64_t rows, int64_t cols, int32_t dtype, double p,
+                           const int64_t* rng, void* dx, void* dh, float* dgamma, float* dbeta,
+                           void* workspace, int64_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Softmax cross entropy of a classifier, fused with its product: T rows X
+ * (T x D), V classes W (V x D, an FC layer with M = V and N = D), both of
+ * `dtype`, one target class per row:
+ *
+ *     s_tv = sum_d X_td W_vd,  lse_t = log sum_v exp(s_tv),
+ *     loss_t = lse_t - s_t,target
+ *     G_tv = (exp(s_tv - lse_t) - [v = target_t]) * dloss_t
+ *     dX = G W  (T x D),   dW = G^T X  (V x D)
+ *
+ * A row whose target is outside 0..V-1 (padding) has loss 0 and G = 0, and
+ * whatever its X and dloss hold reaches no gradient; its lse is still given.
+ * dloss_t is the gradient of the whole loss with respect to loss_t (1 / rows
+ * for a mean).
+ *
+ * poseidon_xent_forward and poseidon_xent_backward keep no logits: the
+ * backward pass makes them again, a piece of the vocabulary at a time, from
+ * the lse that the forward pass left.  dW is the dense payload of the
+ * parameter server (it may lie in a shard), replaced, exact to fp32 whatever
+ * the type; with T = 0 it is 0.  poseidon_xent_factor is for a layer that is
+ * synchronised by sufficient factors: it leaves the layer's factor U = G
+ * (T x V fp32; the layer's V factor is X), the losses and dX in one call.
+ * fp32 inputs are multiplied as fp32; bf16 inputs on the bf16 matrix cores,
+ * with G rounded to bf16 for a bf16 dX and in three exact parts for dW.
+ * Returns POSEIDON_OK, POSEIDON_ERR_INVALID_ARG (negative T; V or D < 1; T, V
+ * above 2^24, T*V above 2^37, D above 2^20; an unknown dtype; NULL arrays with
+ * work; outputs overlapping each other, the workspace or an input; a workspace
+ * too small or off its boundary) or POSEIDON_ERR_HIP.
+ */
+#define POSEIDON_XENT_FORWARD  0
+#define POSEIDON_XENT_BACKWARD 1
+#define POSEIDON_XENT_FACTOR   2
+
+/* Bytes of workspace for the call `op` on these arrays (their boundaries
+ * decide whether they are laid out again).  Host-only. */
+int poseidon_xent_workspace(int32_t op, const void* X, const void* W, int64_t T, int64_t V, int64_t D,
+                            int32_t dtype, int64_t* bytes);
+
+int poseidon_xent_forward(const void* X, const void* W, const int64_t* target, int64_t T, int64_t V, int64_t D,
+                          int32_t dtype, float* loss, float* lse, void* workspace, int64_t workspace_bytes,
+                          hipStream_t stream);
+
+int poseidon_xent_backward(const void* X, const void* W, const int64_t* target, const float* lse, const float* dloss,
+                           int64_t T, int64_t V, int64_t D, int32_t dtype, void* dX, float* dW,
+                           void* workspace, int64_t workspace_bytes, hipStream_t stream);
+
+int poseidon_xent_factor(const void* X, const void* W, const int64_t* target, const float* dloss,
+                         int64_t T, int64_t V, int64_t D, int32_t dtype, float* loss, float* U, void* dX,
+                         void* workspace, int64_t workspace_bytes, hipStream_t stream);
+
 /* Library version, for the binding's load check: returns POSEIDON_ABI_VERSION. */
-#define POSEIDON_ABI_VERSION 3
+#define POSEIDON_ABI_VERSION 4
 int poseidon_abi_version(void);
 
 #ifdef __cplusplus

@@ -9,7 +9,7 @@ import os
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libposeidon.so")
-ABI_VERSION = 3
+ABI_VERSION = 4
 
 OK = 0
 ERR_INVALID_ARG = -1
@@ -26,6 +26,11 @@ WFBP_EACH = 2
 WFBP_SERIAL = 3
 SF_BF16X6 = 0
 SF_FP32 = 1
+F32 = 0
+BF16 = 1
+XENT_FORWARD = 0
+XENT_BACKWARD = 1
+XENT_FACTOR = 2
 
 EXPORTS = ("poseidon_sf_apply", "poseidon_sf_apply_momentum", "poseidon_sf_apply_batch",
            "poseidon_ps_apply", "poseidon_ps_apply_batch",
@@ -37,7 +42,9 @@ EXPORTS = ("poseidon_sf_apply", "poseidon_sf_apply_momentum", "poseidon_sf_apply
            "poseidon_kv_layout", "poseidon_kv_create", "poseidon_kv_destroy", "poseidon_kv_begin",
            "poseidon_kv_receive", "poseidon_kv_pair_count", "poseidon_kv_receive_message",
            "poseidon_kv_message_size", "poseidon_kv_pack", "poseidon_sf_set_arithmetic",
-           "poseidon_sf_arithmetic")
+           "poseidon_sf_arithmetic", "poseidon_dropout", "poseidon_norm_forward", "poseidon_norm_workspace",
+           "poseidon_norm_backward", "poseidon_xent_workspace", "poseidon_xent_forward", "poseidon_xent_backward",
+           "poseidon_xent_factor")
 
 
 class PoseidonTensor(ctypes.Structure):
@@ -123,6 +130,15 @@ def lib() -> ctypes.CDLL:
     L.poseidon_kv_message_size.argtypes = [vp, ctypes.POINTER(i64)]
     L.poseidon_kv_pack.argtypes = [ctypes.POINTER(i64), ctypes.POINTER(vp), i32, i64, i32, i32, vp, i64,
                                    ctypes.POINTER(i64), vp]
+    f64 = ctypes.c_double
+    L.poseidon_dropout.argtypes = [vp, vp, i64, i64, i32, f64, vp, vp, vp]
+    L.poseidon_norm_forward.argtypes = [vp] * 4 + [i64, i64, i32, f32, f64] + [vp] * 6
+    L.poseidon_norm_workspace.argtypes = [i64, i64, ctypes.POINTER(i64)]
+    L.poseidon_norm_backward.argtypes = [vp] * 6 + [i64, i64, i32, f64] + [vp] * 6 + [i64, vp]
+    L.poseidon_xent_workspace.argtypes = [i32, vp, vp, i64, i64, i64, i32, ctypes.POINTER(i64)]
+    L.poseidon_xent_forward.argtypes = [vp] * 3 + [i64] * 3 + [i32] + [vp] * 3 + [i64, vp]
+    L.poseidon_xent_backward.argtypes = [vp] * 5 + [i64] * 3 + [i32] + [vp] * 3 + [i64, vp]
+    L.poseidon_xent_factor.argtypes = [vp] * 4 + [i64] * 3 + [i32] + [vp] * 4 + [i64, vp]
     for name in EXPORTS:
         getattr(L, name).restype = ctypes.c_int
     if L.poseidon_abi_version() != ABI_VERSION:

@@ -14,7 +14,7 @@ import ctypes
 import torch
 
 from . import _lib as L
-from ._lib import (ADAM, ERR_HIP, ERR_INVALID_ARG, ERR_PAYLOAD, KIND_FC, KIND_OTHER, PS, SFB,  # noqa: F401
+from ._lib import (ADAM, BF16, ERR_HIP, ERR_INVALID_ARG, ERR_PAYLOAD, F32, KIND_FC, KIND_OTHER, PS, SFB,  # noqa: F401
                    SF_BF16X6, SF_FP32, WFBP_ALL_LAST, WFBP_EACH, WFBP_SERIAL, WFBP_SFB_LAST)
 
 
@@ -548,3 +548,236 @@ class KVStore:
             self.close()
         except Exception:
             pass
+
+
+# --------------------------------------------------------------------------
+# Operators at a network's end
+# --------------------------------------------------------------------------
+
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _dev(name: str, t: torch.Tensor, dtype: torch.dtype, shape=None) -> torch.Tensor:
+    """A contiguous device tensor of the given type (and shape)."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on a HIP device (no host path exists)")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t
+
+
+def _typed(name: str, t: torch.Tensor) -> int:
+    """The type code of an activation or weight tensor."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype not in _DTYPES:
+        raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}")
+    _dev(name, t, t.dtype)
+    return _DTYPES[t.dtype]
+
+
+def _out(name: str, t, shape, dtype: torch.dtype, device) -> torch.Tensor:
+    """The caller's result tensor, checked, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    return _dev(name, t, dtype, shape)
+
+
+def _work_on(stream, device):
+    """The context in which a call allocates its results and workspace: its
+    stream's own memory, so that no earlier work of another stream can still be
+    using it and none of it is handed out again before the call's work is done."""
+    if stream is None:
+        return _on(device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(_stream_handle(stream, device), device=device)
+    return torch.cuda.stream(stream)
+
+
+def _drops(p: float) -> bool:
+    """Whether p, rounded to 2^-16, drops anything."""
+    return p * 65536 + 0.5 >= 1.0
+
+
+def _rng(rng, p: float):
+    """The generator's state, checked: needed when p drops anything."""
+    if not 0.0 <= p <= 1.0:
+        raise ValueError(f"p must lie in 0..1, got {p}")
+    if rng is None:
+        if _drops(p):
+            raise ValueError("dropout needs rng: two int64 values (seed, offset) on the device")
+        return None
+    return _dev("rng", rng, torch.int64, (2,))
+
+
+def _workspace(size, device) -> torch.Tensor:
+    return torch.empty(max(1, size.value), dtype=torch.uint8, device=device)
+
+
+def _rows_cols(x: torch.Tensor) -> tuple[int, int]:
+    if x.dim() < 1:
+        raise ValueError("x must have at least one dimension")
+    cols = x.shape[-1]
+    return (x.numel() // cols if cols else 0), cols
+
+
+def dropout(x: torch.Tensor, p: float, rng: torch.Tensor | None, residual: torch.Tensor | None = None,
+            y: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """y = residual + keep * x / (1 - p) (poseidon_dropout); the backward pass
+    is dropout(dy, p, rng).  ``rng`` holds (seed, offset) as two int64 values on
+    the device; the mask follows from them, the row length x.shape[-1] and an
+    element's place, and is never stored."""
+    dt = _typed("x", x)
+    rng = _rng(rng, p)
+    if residual is not None:
+        _dev("residual", residual, x.dtype, x.shape)
+    rows, cols = _rows_cols(x)
+    with _work_on(stream, x.device):
+        y = _out("y", y, x.shape, x.dtype, x.device)
+        _same_device(x, residual, rng, y)
+        _uses(stream, x, residual, rng, y)
+        _check("poseidon_dropout", L.lib().poseidon_dropout(
+            x.data_ptr(), _ptr(residual), rows, cols, dt, float(p), _ptr(rng), y.data_ptr(),
+            _stream_handle(stream, x.device)))
+    return y
+
+
+def norm_forward(x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor, eps: float = 1e-5,
+                 residual: torch.Tensor | None = None, p: float = 0.0, rng: torch.Tensor | None = None,
+                 y: torch.Tensor | None = None, stream=None):
+    """h = residual + dropout(x); y = (h - mean) * rstd * gamma + beta over the
+    last dimension (poseidon_norm_forward).  Returns (y, h, mean, rstd), h, mean
+    and rstd being what norm_backward needs; without residual and dropout h is
+    x itself."""
+    dt = _typed("x", x)
+    rng = _rng(rng, p)
+    rows, cols = _rows_cols(x)
+    _dev("gamma", gamma, torch.float32, (cols,)), _dev("beta", beta, torch.float32, (cols,))
+    if residual is not None:
+        _dev("residual", residual, x.dtype, x.shape)
+    with _work_on(stream, x.device):
+        y = _out("y", y, x.shape, x.dtype, x.device)
+        h = x if residual is None and not _drops(p) else torch.empty_like(x)
+        mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device)
+        _same_device(x, gamma, beta, residual, rng, y)
+        _uses(stream, x, gamma, beta, residual, rng, y)
+        _check("poseidon_norm_forward", L.lib().poseidon_norm_forward(
+            x.data_ptr(), _ptr(residual), gamma.data_ptr(), beta.data_ptr(), rows, cols, dt, float(eps), float(p),
+            _ptr(rng), None if h is x else h.data_ptr(), y.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+            _stream_handle(stream, x.device)))
+    shape = x.shape[:-1]
+    return y, h, mean.view(shape), rstd.view(shape)
+
+
+def norm_backward(dy: torch.Tensor, h: torch.Tensor, gamma: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                  dresidual: torch.Tensor | None = None, p: float = 0.0, rng: torch.Tensor | None = None,
+                  dgamma: torch.Tensor | None = None, dbeta: torch.Tensor | None = None, stream=None):
+    """The backward pass of norm_forward (poseidon_norm_backward): returns (dx,
+    dh, dgamma, dbeta), dh being the gradient of the residual input (plus
+    ``dresidual``, what arrives at h by another way) and dx that of x (dh itself
+    when p drops nothing).  dgamma and dbeta may be given, e.g. as this worker's
+    gradient shards."""
+    dt = _typed("dy", dy)
+    rng = _rng(rng, p)
+    rows, cols = _rows_cols(dy)
+    _dev("h", h, dy.dtype, dy.shape), _dev("gamma", gamma, torch.float32, (cols,))
+    _dev("mean", mean, torch.float32, dy.shape[:-1]), _dev("rstd", rstd, torch.float32, dy.shape[:-1])
+    if dresidual is not None:
+        _dev("dresidual", dresidual, dy.dtype, dy.shape)
+    size = ctypes.c_int64()
+    with _work_on(stream, dy.device):
+        _check("poseidon_norm_workspace", L.lib().poseidon_norm_workspace(rows, cols, ctypes.byref(size)))
+        dgamma = _out("dgamma", dgamma, (cols,), torch.float32, dy.device)
+        dbeta = _out("dbeta", dbeta, (cols,), torch.float32, dy.device)
+        dh = torch.empty_like(dy)
+        dx = torch.empty_like(dy) if _drops(p) else dh
+        ws = _workspace(size, dy.device)
+        _same_device(dy, h, gamma, mean, rstd, dresidual, rng, dgamma, dbeta)
+        _uses(stream, dy, h, gamma, mean, rstd, dresidual, rng, dgamma, dbeta)
+        _check("poseidon_norm_backward", L.lib().poseidon_norm_backward(
+            dy.data_ptr(), h.data_ptr(), gamma.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _ptr(dresidual), rows,
+            cols, dt, float(p), _ptr(rng), None if dx is dh else dx.data_ptr(), dh.data_ptr(), dgamma.data_ptr(),
+            dbeta.data_ptr(), ws.data_ptr(), size.value, _stream_handle(stream, dy.device)))
+    return dx, dh, dgamma, dbeta
+
+
+def _xent_args(X, W, target):
+    dt = _typed("X", X)
+    if X.dim() != 2:
+        raise ValueError("X must be 2-D")
+    T, D = X.shape
+    _dev("W", W, X.dtype)
+    if W.dim() != 2 or W.shape[1] != D:
+        raise ValueError(f"W must be V x {D}, got {tuple(W.shape)}")
+    _dev("target", target, torch.int64, (T,))
+    _same_device(X, W, target)
+    return dt, T, W.shape[0], D
+
+
+def _xent_workspace(op, X, W, T, V, D, dt):
+    size = ctypes.c_int64()
+    _check("poseidon_xent_workspace", L.lib().poseidon_xent_workspace(
+        op, X.data_ptr(), W.data_ptr(), T, V, D, dt, ctypes.byref(size)))
+    return _workspace(size, X.device), size.value
+
+
+def xent_forward(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, stream=None):
+    """Softmax cross entropy of the logits X @ W.T against the target classes,
+    the logits never stored (poseidon_xent_forward).  X is T x D, W V x D, target
+    T int64 values; a target outside 0..V-1 marks a row without a loss.  Returns
+    (loss, lse), T fp32 values each."""
+    dt, T, V, D = _xent_args(X, W, target)
+    with _work_on(stream, X.device):
+        ws, size = _xent_workspace(L.XENT_FORWARD, X, W, T, V, D, dt)
+        loss, lse = torch.empty((2, T), dtype=torch.float32, device=X.device)
+        _uses(stream, X, W, target)
+        _check("poseidon_xent_forward", L.lib().poseidon_xent_forward(
+            X.data_ptr(), W.data_ptr(), target.data_ptr(), T, V, D, dt, loss.data_ptr(), lse.data_ptr(),
+            ws.data_ptr(), size, _stream_handle(stream, X.device)))
+    return loss, lse
+
+
+def xent_backward(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, lse: torch.Tensor, dloss: torch.Tensor,
+                  dW: torch.Tensor | None = None, stream=None):
+    """Gradients of sum(dloss * loss) (poseidon_xent_backward): returns (dX, dW),
+    dX in X's type and dW V x D fp32 -- it may be given, e.g. as this worker's
+    gradient shard."""
+    dt, T, V, D = _xent_args(X, W, target)
+    _dev("lse", lse, torch.float32, (T,)), _dev("dloss", dloss, torch.float32, (T,))
+    with _work_on(stream, X.device):
+        dW = _out("dW", dW, (V, D), torch.float32, X.device)
+        _same_device(X, lse, dloss, dW)
+        ws, size = _xent_workspace(L.XENT_BACKWARD, X, W, T, V, D, dt)
+        dX = torch.empty_like(X)
+        _uses(stream, X, W, target, lse, dloss, dW)
+        _check("poseidon_xent_backward", L.lib().poseidon_xent_backward(
+            X.data_ptr(), W.data_ptr(), target.data_ptr(), lse.data_ptr(), dloss.data_ptr(), T, V, D, dt,
+            dX.data_ptr(), dW.data_ptr(), ws.data_ptr(), size, _stream_handle(stream, X.device)))
+    return dX, dW
+
+
+def xent_factor(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, dloss: torch.Tensor,
+                U: torch.Tensor | None = None, stream=None):
+    """Loss and gradients of a classifier that is synchronised by sufficient
+    factors (poseidon_xent_factor): returns (loss, U, dX), U = the T x V fp32
+    gradient of the logits -- the layer's factor beside V = X; it may be given,
+    e.g. as this worker's rows of the factor payload."""
+    dt, T, V, D = _xent_args(X, W, target)
+    _dev("dloss", dloss, torch.float32, (T,))
+    with _work_on(stream, X.device):
+        U = _out("U", U, (T, V), torch.float32, X.device)
+        _same_device(X, dloss, U)
+        ws, size = _xent_workspace(L.XENT_FACTOR, X, W, T, V, D, dt)
+        dX = torch.empty_like(X)
+        loss = torch.empty(T, dtype=torch.float32, device=X.device)
+        _uses(stream, X, W, target, dloss, U)
+        _check("poseidon_xent_factor", L.lib().poseidon_xent_factor(
+            X.data_ptr(), W.data_ptr(), target.data_ptr(), dloss.data_ptr(), T, V, D, dt, loss.data_ptr(),
+            U.data_ptr(), dX.data_ptr(), ws.data_ptr(), size, _stream_handle(stream, X.device)))
+    return loss, U, dX

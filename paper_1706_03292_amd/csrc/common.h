@@ -141,6 +141,28 @@ constexpr int KV_PACK_MAX = 64;
 hipError_t launch_kv_pack(const float* const* src, const int64_t* dst, const int64_t* length, int32_t count,
                           float* message, hipStream_t stream);
 
+// The operators at a network's end (arguments validated; nonzero sizes;
+// `thr`: dropped are the elements whose 16 random bits are below it).
+hipError_t launch_dropout(const void* x, const void* res, int64_t rows, int64_t cols, int32_t dtype, uint32_t thr,
+                          const int64_t* rng, void* y, hipStream_t stream);
+hipError_t launch_norm_forward(const void* x, const void* res, const float* gamma, const float* beta, int64_t rows,
+                               int64_t cols, int32_t dtype, float eps, uint32_t thr, const int64_t* rng, void* h,
+                               void* y, float* mean, float* rstd, hipStream_t stream);
+int64_t norm_backward_workspace(int64_t rows, int64_t cols);
+hipError_t launch_norm_backward(const void* dy, const void* h, const float* gamma, const float* mean,
+                                const float* rstd, const void* dres, int64_t rows, int64_t cols, int32_t dtype,
+                                uint32_t thr, const int64_t* rng, void* dx, void* dh, float* dgamma, float* dbeta,
+                                void* workspace, hipStream_t stream);
+int64_t xent_workspace(int32_t op, const void* X, const void* W, int64_t T, int64_t V, int64_t D, int32_t dtype);
+hipError_t launch_xent_forward(const void* X, const void* W, const int64_t* target, int64_t T, int64_t V, int64_t D,
+                               int32_t dtype, float* loss, float* lse, void* ws, hipStream_t stream);
+hipError_t launch_xent_backward(const void* X, const void* W, const int64_t* target, const float* lse,
+                                const float* dloss, int64_t T, int64_t V, int64_t D, int32_t dtype, void* dX,
+                                float* dW, void* ws, hipStream_t stream);
+hipError_t launch_xent_factor(const void* X, const void* W, const int64_t* target, const float* dloss, int64_t T,
+                              int64_t V, int64_t D, int32_t dtype, float* loss, float* U, void* dX, void* ws,
+                              hipStream_t stream);
+
 // Argument checks of the public entry points (no device work).
 int check_sf_args(const float* W, const float* U, const float* V,
                   int64_t M, int64_t N, int64_t K);

@@ -1,0 +1,352 @@
+// The tiled matrix product of the classifier loss: one BM x BN tile of
+//
+//     C[m][n] = sum_k A(m, k) * B(n, k)
+//
+// with A and B in bf16 or fp32 in memory, products on the matrix cores
+// (16x16x32 bf16, 16x16x4 fp32) and sums in fp32 registers.  Each operand is
+// stored either with k along its rows ("k-major": row m holds A(m, 0..K)) or
+// with k as the row index ("r-major": row k holds A(0..M, k)), so the three
+// products logits = X W^T, dX = G W and dW = G^T X read X, W and G as they are
+// and nothing is transposed in memory.
+//
+// A step takes 128 bytes of k per row (64 bf16 or 32 fp32 values) from each
+// operand straight into LDS (gfx950's 16-byte LDS-direct buffer loads; what is
+// outside the operand reads 0 by the buffer's range check), STAGES - 1 steps
+// ahead.  Each stage is an LDS object of its own, so that reading one does not
+// wait for the loads in flight into another.
+//
+// LDS layout.  An LDS-direct load writes 16 bytes per lane to consecutive
+// addresses, so a permutation of the tile is made by choosing which 16 bytes a
+// lane fetches.  k-major: row r's chunk c sits in slot c ^ (r mod 8) ^ (r/8 mod 2),
+// which spreads the 16 rows of an operand read over all banks.  r-major, bf16:
+// operand reads are gfx950's transposing LDS reads (16 lanes name four k rows
+// of 16 columns, lane i receives column i's four values); chunk pairs are
+// exchanged by a function of the k row so that the rows read together lie in
+// different banks.  r-major, fp32: a lane reads single values; groups of four
+// chunks are exchanged.
+//
+// Operands enter the matrix instruction exchanged (B's rows first), so a lane
+// ends up with four neighbouring n of one row m: wide stores, and row
+// statistics that stay in a lane but for the last two steps.
+#pragma once
+
+#include "elements.h"
+
+namespace poseidon {
+namespace {
+
+typedef float acc4 __attribute__((ext_vector_type(4)));
+typedef short h4 __attribute__((ext_vector_type(4)));
+typedef short h8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(3))) h4 lds_h4;
+
+constexpr int XCDS = 8;              // MI355X: eight dies, each with an L2 of its own
+constexpr int RSRC_RAW = 0x00020000; // buffer resource word 3: raw 32-bit accesses
+constexpr int64_t RSRC_MOST = 0x7fff0000;
+constexpr int OUTSIDE = 0x7ffffff0;  // an offset no resource here contains
+constexpr int STEP_BYTES = 128;      // k per row and step
+
+// One operand: `rows` x `cols` values of type E from p, ld values apart.
+// k-major: cols = K (a multiple of 16 bytes); r-major: rows = K.  `plane`: the
+// distance between the bf16 parts of one matrix, for products of parts.
+struct Operand {
+    const void* p;
+    int64_t ld;
+    int64_t rows;
+    int64_t plane;
+};
+
+// Which parts the products take, in order: A part sel & 3, B part
+// (sel >> 2) & 3, four bits a product.
+struct Parts {
+    int count;
+    uint32_t sel;
+};
+
+template <typename E, int R, int NT, bool KMAJOR>
+struct Panel {
+    static constexpr int SZ = sizeof(E);
+    static constexpr int BYTES = R * STEP_BYTES;
+    static constexpr int LOADS = BYTES / 16 / NT;
+    static constexpr int BK = STEP_BYTES / SZ;
+    static constexpr int PER_ROW = R * SZ / 16;   // r-major: chunks of a k row
+    static_assert(BYTES % (16 * NT) == 0, "whole loads");
+
+    static __device__ __forceinline__ int swz_k(int r) { return (r & 7) ^ ((r >> 3) & 1); }
+
+    // r-major: which chunk of a k row sits in slot s is s ^ swz_r(k).
+    static __device__ __forceinline__ int swz_r(int k)
+    {
+        if constexpr (SZ == 2) {
+            if constexpr (PER_ROW >= 16)   // rows of 256 bytes and more: eight pairs
+                return (((k & 3) | (((k >> 3) & 1) << 2)) << 1);
+            else if constexpr (PER_ROW == 8)   // 128 bytes: two rows span the banks
+                return ((((k >> 1) & 1) | (((k >> 3) & 1) << 1)) << 1);
+            else
+                return 0;
+        } else {
+            if constexpr (PER_ROW >= 16)
+                return ((k >> 2) & 3) << 2;
+            else
+                return 0;
+        }
+    }
+
+    int off[LOADS];      // this lane's offsets from the step's base
+    int kchunk[LOADS];   // k-major: first k of the lane's chunk within the step
+    const char* base;
+    int64_t left;        // bytes from base to the operand's end
+    int64_t advance;     // bytes from one step to the next
+
+    __device__ __forceinline__ void init(const Operand& o, int64_t r0, int64_t k0, int tid)
+    {
+        const int64_t ldb = o.ld * SZ;
+        const int lane = tid & 63, w = tid >> 6;
+        if constexpr (KMAJOR) {
+            const int64_t rows = o.rows - r0 < R ? o.rows - r0 : R;
+            base = static_cast<const char*>(o.p) + r0 * ldb + k0 * SZ;
+            left = rows * ldb - k0 * SZ;
+            advance = STEP_BYTES;
+        } else {
+            base = static_cast<const char*>(o.p) + k0 * ldb + r0 * SZ;
+            left = (o.rows - k0) * ldb - r0 * SZ;
+            advance = BK * ldb;
+        }
+#pragma unroll
+        for (int q = 0; q < LOADS; ++q) {
+            const int b = q * (NT / 64) + w;   // 1 KB block of the stage
+            if constexpr (KMAJOR) {
+                const int r = 8 * b + (lane >> 3), c = (lane & 7) ^ swz_k(r);
+                off[q] = static_cast<int>(r * ldb) + c * 16;
+                kchunk[q] = c * (16 / SZ);
+            } else {
+                const int s = 64 * b + lane, k = s / PER_ROW, c = (s % PER_ROW) ^ swz_r(k);
+                off[q] = static_cast<int>(k * ldb) + c * 16;
+                kchunk[q] = 0;
+            }
+        }
+    }
+
+    // Load step `step` of part offset `part` into the stage; k_left: values of
+    // k from the step's first on (k-major chunks past it read 0; r-major rows
+    // past it lie outside the operand).
+    __device__ __forceinline__ void issue(char* stage, int64_t step, int64_t part, int64_t k_left, int tid) const
+    {
+        const int64_t at = step * advance;
+        int64_t n = left - at;
+        n = n < 0 || k_left <= 0 ? 0 : n > RSRC_MOST ? RSRC_MOST : n;
+        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<char*>(base) + part + at, static_cast<short>(0), static_cast<int>(n), RSRC_RAW);
+        const int w = tid >> 6;
+#pragma unroll
+        for (int q = 0; q < LOADS; ++q) {
+            int v = off[q];
+            if (KMAJOR && k_left < BK)
+                v = kchunk[q] < k_left ? v : OUTSIDE;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                rs, (lds_void*)(stage + __builtin_amdgcn_readfirstlane((q * (NT / 64) + w) * 1024)), 16, v, 0, 0, 0);
+        }
+    }
+
+    // The operand fragment of 16 rows from r0, sub-step kk (two a step): for
+    // bf16 eight k from 32 kk + 8 (lane / 16), for fp32 four from 16 kk + 4
+    // (lane / 16), of row r0 + lane % 16.
+    static __device__ __forceinline__ h8 frag(const char* stage, int r0, int kk, int lane)
+    {
+        const int g = lane >> 4, i = lane & 15;
+        if constexpr (KMAJOR) {
+            const int r = r0 + i;
+            return *reinterpret_cast<const h8*>(stage + r * STEP_BYTES + (((4 * kk + g) ^ swz_k(r)) << 4));
+        } else if constexpr (SZ == 2) {
+            h8 v;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int k = 32 * kk + 8 * g + 4 * half + (i >> 2);
+                const int byte = r0 * 2 + (i & 3) * 8;
+                const char* at = stage + k * (R * 2) + (((byte >> 4) ^ swz_r(k)) << 4) + (byte & 15);
+                const h4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_h4*)at);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    v[4 * half + e] = x[e];
+            }
+            return v;
+        } else {
+            acc4 v;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int k = 16 * kk + 4 * g + j;
+                const int byte = (r0 + i) * 4;
+                v[j] = *reinterpret_cast<const float*>(stage + k * (R * 4) + (((byte >> 4) ^ swz_r(k)) << 4) +
+                                                       (byte & 15));
+            }
+            return __builtin_bit_cast(h8, v);
+        }
+    }
+};
+
+template <typename E>
+__device__ __forceinline__ acc4 mfma(h8 a, h8 b, acc4 c)
+{
+    if constexpr (sizeof(E) == 2) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8e, a), __builtin_bit_cast(bf8e, b), c, 0,
+                                                       0, 0);
+    } else {
+        const acc4 x = __builtin_bit_cast(acc4, a), y = __builtin_bit_cast(acc4, b);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], c, 0, 0, 0);
+        return c;
+    }
+}
+
+// An LDS stage of its own per (size, number, use).
+template <int SIZE, int S, int USE>
+struct Stage {
+    static __device__ __forceinline__ char* ptr()
+    {
+        __shared__ __align__(1024) char a[SIZE];
+        return a;
+    }
+};
+
+constexpr int vmcnt_imm(int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); }
+
+template <typename E_, bool AK_, bool BK_, int BM_, int BN_, int WM_, int WN_, int STAGES_>
+struct Tile {
+    typedef E_ E;
+    static constexpr bool AK = AK_, BKM = BK_;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_;
+    static constexpr int NWN = BN / WN, WAVES = (BM / WM) * NWN, NT = 64 * WAVES;
+    static constexpr int TM = WM / 16, TN = WN / 16;
+    using PA = Panel<E, BM, NT, AK>;
+    using PB = Panel<E, BN, NT, BKM>;
+    static constexpr int LOADS = PA::LOADS + PB::LOADS;
+    static constexpr int STEP = PA::BK;
+
+    template <int S>
+    static __device__ __forceinline__ char* a_stage() { return Stage<PA::BYTES, S, 0>::ptr(); }
+    template <int S>
+    static __device__ __forceinline__ char* b_stage() { return Stage<PB::BYTES, S, 1>::ptr(); }
+
+    PA pa;
+    PB pb;
+    Parts parts;
+    int64_t a_plane, b_plane, K;
+    int nsteps;
+    int step, part;   // the next to load
+
+    template <int S>
+    __device__ __forceinline__ void issue(int tid)
+    {
+        const uint32_t sel = parts.sel >> (4 * part);
+        const int64_t k_left = step < nsteps ? K - static_cast<int64_t>(step) * STEP : 0;
+        pa.issue(a_stage<S>(), step, (sel & 3) * a_plane, k_left, tid);
+        pb.issue(b_stage<S>(), step, ((sel >> 2) & 3) * b_plane, k_left, tid);
+        if (++part == parts.count) {
+            part = 0;
+            ++step;
+        }
+    }
+
+    template <int S>
+    static __device__ __forceinline__ void multiply(acc4 (&acc)[TM][TN], int wm, int wn, int lane)
+    {
+        const char* as = a_stage<S>();
+        const char* bs = b_stage<S>();
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            h8 a[TM], b[TN];
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+                b[j] = PB::frag(bs, wn + 16 * j, kk, lane);
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+                a[i] = PA::frag(as, wm + 16 * i, kk, lane);
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+                    acc[i][j] = mfma<E>(b[j], a[i], acc[i][j]);
+        }
+    }
+
+    template <int S>
+    __device__ __forceinline__ void turn(acc4 (&acc)[TM][TN], int wm, int wn, int lane, int tid)
+    {
+        // Every wave waits for its own loads of this stage, then for the others'.
+        __builtin_amdgcn_s_waitcnt(vmcnt_imm((STAGES - 2) * LOADS));
+        __builtin_amdgcn_s_barrier();
+        // Keeps the loads ahead of the products and the reads behind the barrier.
+        __builtin_amdgcn_sched_barrier(0);
+        issue<(S + STAGES - 1) % STAGES>(tid);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply<S>(acc, wm, wn, lane);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+
+    template <int S>
+    __device__ __forceinline__ void turns(acc4 (&acc)[TM][TN], int left, int wm, int wn, int lane, int tid)
+    {
+        if constexpr (S < STAGES) {
+            if (left > S) {
+                turn<S>(acc, wm, wn, lane, tid);
+                turns<S + 1>(acc, left, wm, wn, lane, tid);
+            }
+        }
+    }
+
+    template <int S>
+    __device__ __forceinline__ void first_loads(int tid)
+    {
+        if constexpr (S < STAGES - 1) {
+            issue<S>(tid);
+            first_loads<S + 1>(tid);
+        }
+    }
+
+    // The tile from (m0, n0) over k from k0, K_ values of it.
+    __device__ __forceinline__ void run(acc4 (&acc)[TM][TN], const Operand& a, const Operand& b, const Parts& p,
+                                        int64_t m0, int64_t n0, int64_t k0, int64_t K_)
+    {
+        const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+        const int wm = (w / NWN) * WM, wn = (w % NWN) * WN;
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+                acc[i][j] = acc4{0.f, 0.f, 0.f, 0.f};
+        pa.init(a, m0, k0, tid);
+        pb.init(b, n0, k0, tid);
+        parts = p;
+        a_plane = a.plane * static_cast<int64_t>(sizeof(E));
+        b_plane = b.plane * static_cast<int64_t>(sizeof(E));
+        K = K_;
+        nsteps = static_cast<int>((K_ + STEP - 1) / STEP);
+        step = part = 0;
+        first_loads<0>(tid);
+        // Past the last step `issue` loads nothing (every lane outside), which
+        // keeps the count of loads in flight the same to the end.
+        for (int left = nsteps * p.count; left > 0; left -= STAGES)
+            turns<0>(acc, left, wm, wn, lane, tid);
+        // No load may still be writing LDS when the workgroup ends.
+        __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    }
+};
+
+// Workgroup number -> tile: consecutive workgroups go to the eight dies in
+// turn, so each die gets a contiguous run of tiles, walked `group` tile rows at
+// a time: what it runs at one time shares operand panels in its L2.
+__device__ __forceinline__ void tile_of(int64_t id, int64_t tiles_m, int64_t tiles_n, int group, int64_t& tm,
+                                        int64_t& tn)
+{
+    const int64_t tiles = tiles_m * tiles_n, q = tiles / XCDS, r = tiles % XCDS;
+    const int64_t x = id % XCDS, t = x * q + (x < r ? x : r) + id / XCDS;
+    const int64_t per = group * tiles_n, g = t / per, first = g * group;
+    const int64_t rows = tiles_m - first < group ? tiles_m - first : group, in = t - g * per;
+    tm = first + in % rows;
+    tn = in / rows;
+}
+
+}  // namespace
+}  // namespace poseidon
