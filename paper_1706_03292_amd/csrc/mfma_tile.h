@@ -47,6 +47,24 @@ constexpr int64_t RSRC_MOST = 0x7fff0000;
 constexpr int OUTSIDE = 0x7ffffff0;  // an offset no resource here contains
 constexpr int STEP_BYTES = 128;      // k per row and step
 
+typedef int i4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ uint32_t lds_address(const char* p)
+{
+    return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void*)p));
+}
+
+// 16 bytes per lane from rs + v to LDS, lane after lane from `to`.  Written as
+// an instruction, not as the builtin: the compiler makes every transposing LDS
+// read after the builtin wait for all loads in flight, whichever stage they
+// go to (dW of a 4097 x 50001 x 1024 product: see the tile shapes below).  It has no
+// result register; whoever reads the stage waits for it (Tile::turn).
+__device__ __forceinline__ void load_to_lds(i4 rs, int v, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(v), "s"(rs)
+                 : "memory");
+}
+
 // One operand: `rows` x `cols` values of type E from p, ld values apart.
 // k-major: cols = K (a multiple of 16 bytes); r-major: rows = K.  `plane`: the
 // distance between the bf16 parts of one matrix, for products of parts.
@@ -95,9 +113,10 @@ struct Panel {
 
     int off[LOADS];      // this lane's offsets from the step's base
     int kchunk[LOADS];   // k-major: first k of the lane's chunk within the step
-    const char* base;
+    uint64_t base;       // of the next step's first part
     int64_t left;        // bytes from base to the operand's end
     int64_t advance;     // bytes from one step to the next
+    i4 rs;               // the next load's resource
 
     __device__ __forceinline__ void init(const Operand& o, int64_t r0, int64_t k0, int tid)
     {
@@ -105,11 +124,11 @@ struct Panel {
         const int lane = tid & 63, w = tid >> 6;
         if constexpr (KMAJOR) {
             const int64_t rows = o.rows - r0 < R ? o.rows - r0 : R;
-            base = static_cast<const char*>(o.p) + r0 * ldb + k0 * SZ;
+            base = reinterpret_cast<uint64_t>(o.p) + r0 * ldb + k0 * SZ;
             left = rows * ldb - k0 * SZ;
             advance = STEP_BYTES;
         } else {
-            base = static_cast<const char*>(o.p) + k0 * ldb + r0 * SZ;
+            base = reinterpret_cast<uint64_t>(o.p) + k0 * ldb + r0 * SZ;
             left = (o.rows - k0) * ldb - r0 * SZ;
             advance = BK * ldb;
         }
@@ -128,25 +147,28 @@ struct Panel {
         }
     }
 
-    // Load step `step` of part offset `part` into the stage; k_left: values of
-    // k from the step's first on (k-major chunks past it read 0; r-major rows
-    // past it lie outside the operand).
-    __device__ __forceinline__ void issue(char* stage, int64_t step, int64_t part, int64_t k_left, int tid) const
+    // The resource of the next step's part at `part` bytes; `any`: whether
+    // there is such a step (else every lane is outside).
+    __device__ __forceinline__ void aim(int64_t part, bool any)
     {
-        const int64_t at = step * advance;
-        int64_t n = left - at;
-        n = n < 0 || k_left <= 0 ? 0 : n > RSRC_MOST ? RSRC_MOST : n;
-        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-            const_cast<char*>(base) + part + at, static_cast<short>(0), static_cast<int>(n), RSRC_RAW);
-        const int w = tid >> 6;
-#pragma unroll
-        for (int q = 0; q < LOADS; ++q) {
-            int v = off[q];
-            if (KMAJOR && k_left < BK)
-                v = kchunk[q] < k_left ? v : OUTSIDE;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                rs, (lds_void*)(stage + __builtin_amdgcn_readfirstlane((q * (NT / 64) + w) * 1024)), 16, v, 0, 0, 0);
-        }
+        const uint64_t from = base + static_cast<uint64_t>(part);
+        const int64_t n = !any || left < 0 ? 0 : left > RSRC_MOST ? RSRC_MOST : left;
+        rs = i4{static_cast<int>(from), static_cast<int>(from >> 32) & 0xffff, static_cast<int>(n), RSRC_RAW};
+    }
+
+    __device__ __forceinline__ void next()
+    {
+        base += static_cast<uint64_t>(advance);
+        left -= advance;
+    }
+
+    // Load q of the aimed step into the stage; k_left: values of k from the
+    // step's first on (k-major chunks past it read 0; r-major rows past it lie
+    // outside the operand).
+    __device__ __forceinline__ void load(const char* stage, int q, int k_left, int tid) const
+    {
+        const int v = KMAJOR && kchunk[q] >= k_left ? OUTSIDE : off[q];
+        load_to_lds(rs, v, lds_address(stage) + __builtin_amdgcn_readfirstlane((tid >> 6) * 1024) + q * (NT / 64) * 1024);
     }
 
     // The operand fragment of 16 rows from r0, sub-step kk (two a step): for
@@ -210,7 +232,8 @@ struct Stage {
     }
 };
 
-constexpr int vmcnt_imm(int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); }
+// s_waitcnt's operand: at most so many vector loads and LDS operations left.
+constexpr int wait_imm(int vm, int lgkm) { return 0x0070 | (lgkm << 8) | (vm & 15) | ((vm >> 4) << 14); }
 
 template <typename E_, bool AK_, bool BK_, int BM_, int BN_, int WM_, int WN_, int STAGES_>
 struct Tile {
@@ -232,105 +255,161 @@ struct Tile {
     PA pa;
     PB pb;
     Parts parts;
-    int64_t a_plane, b_plane, K;
-    int nsteps;
-    int step, part;   // the next to load
+    int64_t a_plane, b_plane;
+    int k_left;        // values of k from the next step on (none left: 0 or less)
+    int part;          // the next product of it
+    int wm, wn, lane, tid;
 
-    template <int S>
-    __device__ __forceinline__ void issue(int tid)
+    // The operands that the next products need first.
+    struct Ahead {
+        h8 a[2], b[TN];
+    };
+
+    __device__ __forceinline__ void aim()
     {
         const uint32_t sel = parts.sel >> (4 * part);
-        const int64_t k_left = step < nsteps ? K - static_cast<int64_t>(step) * STEP : 0;
-        pa.issue(a_stage<S>(), step, (sel & 3) * a_plane, k_left, tid);
-        pb.issue(b_stage<S>(), step, ((sel >> 2) & 3) * b_plane, k_left, tid);
+        pa.aim((sel & 3) * a_plane, k_left > 0);
+        pb.aim(((sel >> 2) & 3) * b_plane, k_left > 0);
+    }
+
+    // Load q of the aimed step (A's, then B's) into stage S.
+    template <int S>
+    __device__ __forceinline__ void load(int q)
+    {
+        if (q < PA::LOADS)
+            pa.load(a_stage<S>(), q, k_left, tid);
+        else
+            pb.load(b_stage<S>(), q - PA::LOADS, k_left, tid);
+    }
+
+    __device__ __forceinline__ void after_loads()
+    {
         if (++part == parts.count) {
             part = 0;
-            ++step;
+            k_left -= STEP;
+            pa.next();
+            pb.next();
         }
     }
 
     template <int S>
-    static __device__ __forceinline__ void multiply(acc4 (&acc)[TM][TN], int wm, int wn, int lane)
+    __device__ __forceinline__ void read_ahead(Ahead& f) const
     {
-        const char* as = a_stage<S>();
-        const char* bs = b_stage<S>();
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            h8 a[TM], b[TN];
+        for (int j = 0; j < TN; ++j)
+            f.b[j] = PB::frag(b_stage<S>(), wn + 16 * j, 0, lane);
+        f.a[0] = PA::frag(a_stage<S>(), wm, 0, lane);
+        f.a[1] = PA::frag(a_stage<S>(), wm + 16 * (1 % TM), 1 / TM, lane);
+    }
+
+    // The products of stage S, in 2 TM groups (sub-step, row block), operands
+    // read two groups before their products.  Two groups before the end every
+    // operand of the stage has been read: there the waves meet, the stage's
+    // next loads start and the next stage's first operands are read while the
+    // last two groups run, so that the matrix cores need not wait for either.
+    template <int S>
+    __device__ __forceinline__ void turn(acc4 (&acc)[TM][TN], Ahead& f)
+    {
+        constexpr int G = 2 * TM, FIRST_B = TM - 2 - TN > 0 ? TM - 2 - TN : 0;
+        h8 a[G], b[2][TN];
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+            b[0][j] = f.b[j];
+        a[0] = f.a[0];
+        a[1] = f.a[1];
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            if (g + 2 < G)
+                a[g + 2] = PA::frag(a_stage<S>(), wm + 16 * ((g + 2) % TM), (g + 2) / TM, lane);
+            if (g >= FIRST_B && g - FIRST_B < TN && g < TM)
+                b[1][g - FIRST_B] = PB::frag(b_stage<S>(), wn + 16 * (g - FIRST_B), 1, lane);
+            if (TN > TM - FIRST_B && g == TM - 1)
+#pragma unroll
+                for (int j = TM - FIRST_B; j < TN; ++j)
+                    b[1][j] = PB::frag(b_stage<S>(), wn + 16 * j, 1, lane);
+            if (g == G - 2) {
+                // All of this wave's reads of the stage are done, and its own
+                // loads of the next stage; then the other waves'.
+                __builtin_amdgcn_s_waitcnt(wait_imm((STAGES - 2) * LOADS, 0));
+                __builtin_amdgcn_s_barrier();
+                __builtin_amdgcn_sched_barrier(0);
+                read_ahead<(S + 1) % STAGES>(f);
+                aim();
+#pragma unroll
+                for (int q = 0; q < (LOADS + 1) / 2; ++q)
+                    load<S>(q);
+            }
+            if (g == G - 1) {
+#pragma unroll
+                for (int q = (LOADS + 1) / 2; q < LOADS; ++q)
+                    load<S>(q);
+                after_loads();
+            }
 #pragma unroll
             for (int j = 0; j < TN; ++j)
-                b[j] = PB::frag(bs, wn + 16 * j, kk, lane);
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-                a[i] = PA::frag(as, wm + 16 * i, kk, lane);
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int j = 0; j < TN; ++j)
-                    acc[i][j] = mfma<E>(b[j], a[i], acc[i][j]);
+                acc[g % TM][j] = mfma<E>(b[g / TM][j], a[g], acc[g % TM][j]);
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
 
     template <int S>
-    __device__ __forceinline__ void turn(acc4 (&acc)[TM][TN], int wm, int wn, int lane, int tid)
-    {
-        // Every wave waits for its own loads of this stage, then for the others'.
-        __builtin_amdgcn_s_waitcnt(vmcnt_imm((STAGES - 2) * LOADS));
-        __builtin_amdgcn_s_barrier();
-        // Keeps the loads ahead of the products and the reads behind the barrier.
-        __builtin_amdgcn_sched_barrier(0);
-        issue<(S + STAGES - 1) % STAGES>(tid);
-        __builtin_amdgcn_sched_barrier(0);
-        multiply<S>(acc, wm, wn, lane);
-        __builtin_amdgcn_sched_barrier(0);
-    }
-
-    template <int S>
-    __device__ __forceinline__ void turns(acc4 (&acc)[TM][TN], int left, int wm, int wn, int lane, int tid)
+    __device__ __forceinline__ void turns(acc4 (&acc)[TM][TN], Ahead& f, int left)
     {
         if constexpr (S < STAGES) {
             if (left > S) {
-                turn<S>(acc, wm, wn, lane, tid);
-                turns<S + 1>(acc, left, wm, wn, lane, tid);
+                turn<S>(acc, f);
+                turns<S + 1>(acc, f, left);
             }
         }
     }
 
     template <int S>
-    __device__ __forceinline__ void first_loads(int tid)
+    __device__ __forceinline__ void first_loads()
     {
-        if constexpr (S < STAGES - 1) {
-            issue<S>(tid);
-            first_loads<S + 1>(tid);
+        if constexpr (S < STAGES) {
+            aim();
+#pragma unroll
+            for (int q = 0; q < LOADS; ++q)
+                load<S>(q);
+            after_loads();
+            first_loads<S + 1>();
         }
     }
 
-    // The tile from (m0, n0) over k from k0, K_ values of it.
+    // The tile from (m0, n0) over k from k0, K of it.
     __device__ __forceinline__ void run(acc4 (&acc)[TM][TN], const Operand& a, const Operand& b, const Parts& p,
-                                        int64_t m0, int64_t n0, int64_t k0, int64_t K_)
+                                        int64_t m0, int64_t n0, int64_t k0, int64_t K)
     {
-        const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-        const int wm = (w / NWN) * WM, wn = (w % NWN) * WN;
+        tid = threadIdx.x;
+        lane = tid & 63;
+        wm = ((tid >> 6) / NWN) * WM;
+        wn = ((tid >> 6) % NWN) * WN;
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int j = 0; j < TN; ++j)
                 acc[i][j] = acc4{0.f, 0.f, 0.f, 0.f};
+        if (K <= 0)
+            return;
         pa.init(a, m0, k0, tid);
         pb.init(b, n0, k0, tid);
         parts = p;
         a_plane = a.plane * static_cast<int64_t>(sizeof(E));
         b_plane = b.plane * static_cast<int64_t>(sizeof(E));
-        K = K_;
-        nsteps = static_cast<int>((K_ + STEP - 1) / STEP);
-        step = part = 0;
-        first_loads<0>(tid);
-        // Past the last step `issue` loads nothing (every lane outside), which
+        k_left = static_cast<int>(K);
+        part = 0;
+        // Past the last step `load` fetches nothing (every lane outside), which
         // keeps the count of loads in flight the same to the end.
-        for (int left = nsteps * p.count; left > 0; left -= STAGES)
-            turns<0>(acc, left, wm, wn, lane, tid);
+        first_loads<0>();
+        __builtin_amdgcn_s_waitcnt(wait_imm((STAGES - 1) * LOADS, 15));
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        Ahead f;
+        read_ahead<0>(f);
+        for (int left = static_cast<int>((K + STEP - 1) / STEP) * p.count; left > 0; left -= STAGES)
+            turns<0>(acc, f, left);
         // No load may still be writing LDS when the workgroup ends.
-        __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+        __builtin_amdgcn_s_waitcnt(wait_imm(0, 0));
     }
 };
 

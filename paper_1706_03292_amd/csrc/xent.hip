@@ -225,7 +225,7 @@ __device__ __forceinline__ void finish(acc4 (&acc)[T::TM][T::TN], const Out& o, 
 // M x N tiles over k split gridDim.y ways (k_split values each, a multiple of
 // the step).
 template <typename T, Use USE>
-__global__ __launch_bounds__(T::NT) void product_kernel(Operand a, Operand b, Parts parts, Out o, int64_t M, int64_t N,
+__global__ __launch_bounds__(T::NT, 2) void product_kernel(Operand a, Operand b, Parts parts, Out o, int64_t M, int64_t N,
                                                         int64_t K, int64_t k_split, int64_t tiles_m, int64_t tiles_n,
                                                         int group)
 {
@@ -388,30 +388,51 @@ struct Arena {
 };
 
 // Tile shapes: 32 rows where there are no more (bound by reading the other
-// operand), else 128 x 128.
+// operand), 256 x 256 (one workgroup a CU) where enough of them fill the GPU,
+// else 128 x 128 (two a CU).
 template <typename E, bool AK, bool BK>
 using Thin = Tile<E, AK, BK, 32, 64, 32, 16, 4>;
 template <typename E, bool AK, bool BK>
 using Square = Tile<E, AK, BK, 128, 128, 64, 64, 2>;
+template <typename E, bool AK, bool BK>
+using Large = Tile<E, AK, BK, 256, 256, 128, 64, 2>;
+
+enum ShapeKind { THIN, SQUARE, LARGE };
 
 struct Shape {
-    bool thin;
+    ShapeKind kind;
     int64_t bm, bn, waves_n;
 };
 
-Shape shape_for(int64_t M) { return M <= 32 ? Shape{true, 32, 64, 4} : Shape{false, 128, 128, 2}; }
+template <typename E>
+Shape shape_for(int64_t M, int64_t N)
+{
+    if (M <= 32)
+        return Shape{THIN, 32, 64, 4};
+    if (sizeof(E) == 2) {
+        const int64_t cus = device_cu_count();
+        const int64_t large = ceil_div(ceil_div(M, 256) * ceil_div(N, 256), cus) * 4;
+        const int64_t square = ceil_div(ceil_div(M, 128) * ceil_div(N, 128), 2 * cus) * 2;
+        if (4 * large <= 5 * square)
+            return Shape{LARGE, 256, 256, 4};
+    }
+    return Shape{SQUARE, 128, 128, 2};
+}
 
+template <typename E>
 int64_t parts_of(int64_t M, int64_t N)
 {
-    const Shape s = shape_for(M);
+    const Shape s = shape_for<E>(M, N);
     return ceil_div(N, s.bn) * s.waves_n;
 }
 
 // How many ways to split k so that the tiles fill the GPU: about two
 // workgroups a CU, at least eight steps each.
-int64_t splits_for(int64_t M, int64_t N, int64_t K, int64_t step)
+template <typename E>
+int64_t splits_for(int64_t M, int64_t N, int64_t K)
 {
-    const Shape s = shape_for(M);
+    const Shape s = shape_for<E>(M, N);
+    const int64_t step = STEP_BYTES / sizeof(E);
     const int64_t tiles = ceil_div(M, s.bm) * ceil_div(N, s.bn), steps = ceil_div(K, step);
     return std::max<int64_t>(1, std::min<int64_t>(2 * device_cu_count() / std::max<int64_t>(tiles, 1), steps / 8));
 }
@@ -431,8 +452,12 @@ template <typename E, bool AK, bool BK, Use USE>
 hipError_t product(const Operand& a, const Operand& b, const Parts& p, const Out& o, int64_t M, int64_t N, int64_t K,
                    int64_t splits, hipStream_t s)
 {
-    if (shape_for(M).thin)
+    const ShapeKind kind = shape_for<E>(M, N).kind;
+    if (kind == THIN)
         return launch_product<Thin<E, AK, BK>, USE>(a, b, p, o, M, N, K, splits, s);
+    if constexpr (sizeof(E) == 2)
+        if (kind == LARGE)
+            return launch_product<Large<E, AK, BK>, USE>(a, b, p, o, M, N, K, splits, s);
     return launch_product<Square<E, AK, BK>, USE>(a, b, p, o, M, N, K, splits, s);
 }
 
@@ -486,7 +511,7 @@ struct Plan {
 template <typename E>
 Plan make_plan(int op, int64_t T, int64_t V, int64_t D, bool copy_x, bool copy_w, char* base)
 {
-    constexpr int64_t SZ = sizeof(E), STEP = STEP_BYTES / SZ;
+    constexpr int64_t SZ = sizeof(E);
     Plan p;
     Arena a{base};
     p.ldd = round_up(D, GROUP);
@@ -495,7 +520,7 @@ Plan make_plan(int op, int64_t T, int64_t V, int64_t D, bool copy_x, bool copy_w
     if (copy_w)
         p.w = a.take(V * p.ldd * SZ);
     if (op != POSEIDON_XENT_BACKWARD) {
-        p.nparts = parts_of(T, V);
+        p.nparts = parts_of<E>(T, V);
         p.part = static_cast<Run*>(a.take(T * p.nparts * sizeof(Run)));
         p.target_logit = static_cast<float*>(a.take(T * 4));
     }
@@ -511,12 +536,12 @@ Plan make_plan(int op, int64_t T, int64_t V, int64_t D, bool copy_x, bool copy_w
     p.ldg = p.piece;
     p.g = a.take(T * p.ldg * g_value);
     p.target_rest = static_cast<float*>(a.take(T * 4));
-    p.dx_splits = splits_for(T, D, std::min(p.piece, V), STEP);
+    p.dx_splits = splits_for<E>(T, D, std::min(p.piece, V));
     const int64_t pieces = ceil_div(V, p.piece);
     if (p.dx_splits > 1 || (pieces > 1 && SZ == 2))
         p.dx = static_cast<float*>(a.take(p.dx_splits * T * D * 4));
     if (op == POSEIDON_XENT_BACKWARD) {
-        p.dw_splits = splits_for(std::min(p.piece, V), D, T, STEP);
+        p.dw_splits = splits_for<E>(std::min(p.piece, V), D, T);
         if (p.dw_splits > 1)
             p.dw = static_cast<float*>(a.take(p.dw_splits * std::min(p.piece, V) * D * 4));
     }
