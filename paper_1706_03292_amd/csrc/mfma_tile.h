@@ -9,16 +9,16 @@
 // products logits = X W^T, dX = G W and dW = G^T X read X, W and G as they are
 // and nothing is transposed in memory.
 //
-// A step takes 128 bytes of k per row (64 bf16 or 32 fp32 values) from each
-// operand straight into LDS (gfx950's 16-byte LDS-direct buffer loads; what is
-// outside the operand reads 0 by the buffer's range check), STAGES - 1 steps
-// ahead.  Each stage is an LDS object of its own, so that reading one does not
+// A step takes 64 or 128 bytes of k per row (32 or 64 bf16 values, half as many
+// fp32) from each operand straight into LDS (gfx950's 16-byte LDS-direct buffer loads; what is
+// outside the operand reads 0 by the buffer's range check), up to STAGES
+// steps ahead.  Each stage is an LDS object of its own, so that reading one does not
 // wait for the loads in flight into another.
 //
 // LDS layout.  An LDS-direct load writes 16 bytes per lane to consecutive
 // addresses, so a permutation of the tile is made by choosing which 16 bytes a
-// lane fetches.  k-major: row r's chunk c sits in slot c ^ (r mod 8) ^ (r/8 mod 2),
-// which spreads the 16 rows of an operand read over all banks.  r-major, bf16:
+// lane fetches.  k-major: chunks are exchanged within a row so that the
+// 16 rows of an operand read lie in different banks.  r-major, bf16:
 // operand reads are gfx950's transposing LDS reads (16 lanes name four k rows
 // of 16 columns, lane i receives column i's four values); chunk pairs are
 // exchanged by a function of the k row so that the rows read together lie in
@@ -45,7 +45,7 @@ constexpr int XCDS = 8;              // MI355X: eight dies, each with an L2 of i
 constexpr int RSRC_RAW = 0x00020000; // buffer resource word 3: raw 32-bit accesses
 constexpr int64_t RSRC_MOST = 0x7fff0000;
 constexpr int OUTSIDE = 0x7ffffff0;  // an offset no resource here contains
-constexpr int STEP_BYTES = 128;      // k per row and step
+constexpr int SUB_BYTES = 64;        // k per row and sub-step: one operand fragment of 16 rows is 1 KB
 
 typedef int i4 __attribute__((ext_vector_type(4)));
 
@@ -82,16 +82,30 @@ struct Parts {
     uint32_t sel;
 };
 
-template <typename E, int R, int NT, bool KMAJOR>
+template <typename E, int R, int NT, bool KMAJOR, int KSUB, bool SPREAD>
 struct Panel {
     static constexpr int SZ = sizeof(E);
+    static constexpr int STEP_BYTES = KSUB * SUB_BYTES;
     static constexpr int BYTES = R * STEP_BYTES;
     static constexpr int LOADS = BYTES / 16 / NT;
     static constexpr int BK = STEP_BYTES / SZ;
     static constexpr int PER_ROW = R * SZ / 16;   // r-major: chunks of a k row
     static_assert(BYTES % (16 * NT) == 0, "whole loads");
 
-    static __device__ __forceinline__ int swz_k(int r) { return (r & 7) ^ ((r >> 3) & 1); }
+    static constexpr int CHUNKS = STEP_BYTES / 16;   // k-major: of a row
+
+    // k-major: which chunk of row r sits in slot s is s ^ swz_k(r).  The rows
+    // read together are 16 neighbours, or (SPREAD) four neighbours each from
+    // four blocks of 16; eight of them in the order of their lanes, and all 16,
+    // lie in different banks.
+    static __device__ __forceinline__ int swz_k(int r)
+    {
+        if constexpr (CHUNKS == 8)
+            return SPREAD ? ((r & 3) ^ ((r >> 5) & 1)) | (((r >> 4) & 1) << 2) : (r & 7) ^ ((r >> 3) & 1);
+        else
+            return SPREAD ? (((r >> 4) & 1) << 1) | (((r >> 1) ^ (r >> 5)) & 1)
+                          : (((r >> 2) & 1) << 1) | (((r >> 1) ^ (r >> 3)) & 1);
+    }
 
     // r-major: which chunk of a k row sits in slot s is s ^ swz_r(k).
     static __device__ __forceinline__ int swz_r(int k)
@@ -136,7 +150,7 @@ struct Panel {
         for (int q = 0; q < LOADS; ++q) {
             const int b = q * (NT / 64) + w;   // 1 KB block of the stage
             if constexpr (KMAJOR) {
-                const int r = 8 * b + (lane >> 3), c = (lane & 7) ^ swz_k(r);
+                const int r = (64 / CHUNKS) * b + lane / CHUNKS, c = (lane % CHUNKS) ^ swz_k(r);
                 off[q] = static_cast<int>(r * ldb) + c * 16;
                 kchunk[q] = c * (16 / SZ);
             } else {
@@ -171,21 +185,22 @@ struct Panel {
         load_to_lds(rs, v, lds_address(stage) + __builtin_amdgcn_readfirstlane((tid >> 6) * 1024) + q * (NT / 64) * 1024);
     }
 
-    // The operand fragment of 16 rows from r0, sub-step kk (two a step): for
-    // bf16 eight k from 32 kk + 8 (lane / 16), for fp32 four from 16 kk + 4
-    // (lane / 16), of row r0 + lane % 16.
-    static __device__ __forceinline__ h8 frag(const char* stage, int r0, int kk, int lane)
+    // The operand fragment of 16 rows, sub-step kk: for bf16 eight k from
+    // 32 kk + 8 (lane / 16), for fp32 four from 16 kk + 4 (lane / 16).  Lane l
+    // takes row r0 + l % 16 of block j = (row - r0) / 16; SPREAD: of the four
+    // blocks from r0 on, rows 16 (i / 4) + 4 j + i % 4, i = l % 16.
+    static __device__ __forceinline__ h8 frag(const char* stage, int r0, int j, int kk, int lane)
     {
         const int g = lane >> 4, i = lane & 15;
         if constexpr (KMAJOR) {
-            const int r = r0 + i;
+            const int r = SPREAD ? r0 + 16 * (i >> 2) + 4 * j + (i & 3) : r0 + 16 * j + i;
             return *reinterpret_cast<const h8*>(stage + r * STEP_BYTES + (((4 * kk + g) ^ swz_k(r)) << 4));
         } else if constexpr (SZ == 2) {
             h8 v;
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const int k = 32 * kk + 8 * g + 4 * half + (i >> 2);
-                const int byte = r0 * 2 + (i & 3) * 8;
+                const int byte = (r0 + 16 * j) * 2 + (i & 3) * 8;
                 const char* at = stage + k * (R * 2) + (((byte >> 4) ^ swz_r(k)) << 4) + (byte & 15);
                 const h4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_h4*)at);
 #pragma unroll
@@ -196,10 +211,10 @@ struct Panel {
         } else {
             acc4 v;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int k = 16 * kk + 4 * g + j;
-                const int byte = (r0 + i) * 4;
-                v[j] = *reinterpret_cast<const float*>(stage + k * (R * 4) + (((byte >> 4) ^ swz_r(k)) << 4) +
+            for (int e = 0; e < 4; ++e) {
+                const int k = 16 * kk + 4 * g + e;
+                const int byte = (r0 + 16 * j + i) * 4;
+                v[e] = *reinterpret_cast<const float*>(stage + k * (R * 4) + (((byte >> 4) ^ swz_r(k)) << 4) +
                                                        (byte & 15));
             }
             return __builtin_bit_cast(h8, v);
@@ -235,15 +250,18 @@ struct Stage {
 // s_waitcnt's operand: at most so many vector loads and LDS operations left.
 constexpr int wait_imm(int vm, int lgkm) { return 0x0070 | (lgkm << 8) | (vm & 15) | ((vm >> 4) << 14); }
 
-template <typename E_, bool AK_, bool BK_, int BM_, int BN_, int WM_, int WN_, int STAGES_>
+template <typename E_, bool AK_, bool BK_, int BM_, int BN_, int WM_, int WN_, int STAGES_, int KSUB_,
+          bool SPREAD_ = false>
 struct Tile {
     typedef E_ E;
     static constexpr bool AK = AK_, BKM = BK_;
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_;
     static constexpr int NWN = BN / WN, WAVES = (BM / WM) * NWN, NT = 64 * WAVES;
-    static constexpr int TM = WM / 16, TN = WN / 16;
-    using PA = Panel<E, BM, NT, AK>;
-    using PB = Panel<E, BN, NT, BKM>;
+    static constexpr int TM = WM / 16, TN = WN / 16, KSUB = KSUB_;
+    static constexpr bool SPREAD = SPREAD_;   // a lane's sums are 16 neighbours of a row, not four of each block
+    static_assert(!SPREAD || (TN == 4 && BKM), "four blocks of k-major rows");
+    using PA = Panel<E, BM, NT, AK, KSUB, false>;
+    using PB = Panel<E, BN, NT, BKM, KSUB, SPREAD>;
     static constexpr int LOADS = PA::LOADS + PB::LOADS;
     static constexpr int STEP = PA::BK;
 
@@ -292,26 +310,33 @@ struct Tile {
         }
     }
 
+    // Group g's A operand, and the B operands of sub-step kk.
+    template <int S>
+    __device__ __forceinline__ h8 a_frag(int g) const { return PA::frag(a_stage<S>(), wm, g % TM, g / TM, lane); }
+    template <int S>
+    __device__ __forceinline__ h8 b_frag(int j, int kk) const { return PB::frag(b_stage<S>(), wn, j, kk, lane); }
+
     template <int S>
     __device__ __forceinline__ void read_ahead(Ahead& f) const
     {
 #pragma unroll
         for (int j = 0; j < TN; ++j)
-            f.b[j] = PB::frag(b_stage<S>(), wn + 16 * j, 0, lane);
-        f.a[0] = PA::frag(a_stage<S>(), wm, 0, lane);
-        f.a[1] = PA::frag(a_stage<S>(), wm + 16 * (1 % TM), 1 / TM, lane);
+            f.b[j] = b_frag<S>(j, 0);
+        f.a[0] = a_frag<S>(0);
+        f.a[1] = a_frag<S>(1);
     }
 
-    // The products of stage S, in 2 TM groups (sub-step, row block), operands
-    // read two groups before their products.  Two groups before the end every
+    // The products of stage S, in groups (sub-step, row block), operands read
+    // two groups before their products.  Two groups before the end every
     // operand of the stage has been read: there the waves meet, the stage's
     // next loads start and the next stage's first operands are read while the
     // last two groups run, so that the matrix cores need not wait for either.
     template <int S>
     __device__ __forceinline__ void turn(acc4 (&acc)[TM][TN], Ahead& f)
     {
-        constexpr int G = 2 * TM, FIRST_B = TM - 2 - TN > 0 ? TM - 2 - TN : 0;
-        h8 a[G], b[2][TN];
+        constexpr int G = KSUB * TM, FIRST_B = TM - 2 - TN > 0 ? TM - 2 - TN : 0;
+        static_assert(G > 2 && TN <= TM, "groups to read in");
+        h8 a[G], b[KSUB][TN];
 #pragma unroll
         for (int j = 0; j < TN; ++j)
             b[0][j] = f.b[j];
@@ -320,13 +345,9 @@ struct Tile {
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             if (g + 2 < G)
-                a[g + 2] = PA::frag(a_stage<S>(), wm + 16 * ((g + 2) % TM), (g + 2) / TM, lane);
-            if (g >= FIRST_B && g - FIRST_B < TN && g < TM)
-                b[1][g - FIRST_B] = PB::frag(b_stage<S>(), wn + 16 * (g - FIRST_B), 1, lane);
-            if (TN > TM - FIRST_B && g == TM - 1)
-#pragma unroll
-                for (int j = TM - FIRST_B; j < TN; ++j)
-                    b[1][j] = PB::frag(b_stage<S>(), wn + 16 * j, 1, lane);
+                a[g + 2] = a_frag<S>(g + 2);
+            if (KSUB > 1 && g >= FIRST_B && g - FIRST_B < TN)
+                b[KSUB - 1][g - FIRST_B] = b_frag<S>(g - FIRST_B, 1);
             if (g == G - 2) {
                 // All of this wave's reads of the stage are done, and its own
                 // loads of the next stage; then the other waves'.

@@ -21,17 +21,9 @@
 namespace poseidon {
 namespace {
 
-// e^x for x <= 0 or near it: 2^(x log2 e) with the product's rounding error put
-// back, so that a small probability keeps fp32's relative accuracy.
-__device__ __forceinline__ float exp_f(float x)
-{
-    const float y = x * 1.44269504f;
-    const float r = fmaf(x, 1.44269504f, -y) + x * 1.92596299e-8f;   // the product's error, and log2(e)'s
-    const float e = __builtin_amdgcn_exp2f(y);
-    return y > -126.f && y < 128.f ? fmaf(e, r * 0.693147181f, e) : e;
-}
+constexpr float LOG2E = 1.44269504f, LOG2E_REST = 1.92596299e-8f, LN2 = 0.693147181f;
 
-// A running maximum and the sum of exponentials below it.
+// A running maximum, in units of log2 e, and the sum of powers of two below it.
 struct Run {
     float m, s;
 };
@@ -40,8 +32,16 @@ __device__ __forceinline__ Run join(Run a, Run b)
 {
     const float m = fmaxf(a.m, b.m);
     // A side without a finite maximum (no column, or all -inf) adds nothing.
-    const float ea = a.m == -INFINITY ? 0.f : exp_f(a.m - m), eb = b.m == -INFINITY ? 0.f : exp_f(b.m - m);
+    const float ea = a.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(a.m - m);
+    const float eb = b.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(b.m - m);
     return Run{m, fmaf(a.s, ea, b.s * eb)};
+}
+
+__device__ __forceinline__ float lse_of(Run r)
+{
+    // m ln 2 to fp32's accuracy: ln 2 in two parts.
+    return r.m == -INFINITY && r.s == 0.f ? -INFINITY
+                                          : fmaf(r.m, 0.693147182f, fmaf(r.m, -1.90465421e-9f, logf(r.s)));
 }
 
 __device__ __forceinline__ bool counts(int64_t target, int64_t V) { return target >= 0 && target < V; }
@@ -59,13 +59,12 @@ struct Out {
     int64_t nparts;
     float* target_logit;
     const int64_t* target;
-    // GRAD: the piece's G from lse and dloss, as bf16 parts (planes apart) or
-    // fp32, columns v0 onwards of V.
+    // GRAD: the piece's G from lse and dloss, in three bf16 parts (planes apart)
+    // or fp32, columns v0 onwards of V.
     const float* lse;
     const float* dloss;
     void* g;
     int64_t ldg, g_plane;
-    int32_t g_parts;      // bf16 parts written (1..3), or 0: fp32
     int64_t v0, V;
     // GRAD writes, and STORE of a bf16 dX reads, what rounding G to bf16 left of
     // each row's entry at its target: that entry is near -dloss where all others
@@ -81,8 +80,14 @@ struct Out {
     int32_t bf16, add;
 };
 
-// One row's four neighbours at p (any 4- or 2-byte boundary), n of them.
-__device__ __forceinline__ void put4(float* p, acc4 v, int64_t n)
+typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+typedef __bf16 b4a __attribute__((ext_vector_type(4), aligned(2)));
+typedef float f2 __attribute__((ext_vector_type(2)));
+typedef unsigned u2 __attribute__((ext_vector_type(2)));
+
+// One row's four neighbours at p (any boundary of their type), n of them.
+__device__ __forceinline__ void put4(float* p, acc4 v, int n)
 {
     if (n >= 4) {
         *reinterpret_cast<f4a*>(p) = v;
@@ -94,10 +99,7 @@ __device__ __forceinline__ void put4(float* p, acc4 v, int64_t n)
     }
 }
 
-typedef __bf16 b4 __attribute__((ext_vector_type(4)));
-typedef __bf16 b4a __attribute__((ext_vector_type(4), aligned(2)));
-
-__device__ __forceinline__ void put4(__bf16* p, b4 v, int64_t n)
+__device__ __forceinline__ void put4(__bf16* p, b4 v, int n)
 {
     if (n >= 4) {
         *reinterpret_cast<b4a*>(p) = v;
@@ -109,116 +111,217 @@ __device__ __forceinline__ void put4(__bf16* p, b4 v, int64_t n)
     }
 }
 
+// Two values rounded to bf16, the first in the low half; and what that leaves.
+__device__ __forceinline__ unsigned bf16_pair(float a, float b)
+{
+    return __builtin_bit_cast(unsigned, __builtin_convertvector((f2){a, b}, b2));
+}
+__device__ __forceinline__ f2 rest_of_pair(float a, float b, unsigned p)
+{
+    return f2{a - __builtin_bit_cast(float, p << 16), b - __builtin_bit_cast(float, p & 0xffff0000u)};
+}
+
+// STATS, LOGITS.  A row's maximum and the sum of exponentials below it over
+// the wave's columns: in a lane first, then across the four lanes that share
+// the row.
+template <typename T, bool EDGE, bool KEEP>
+__device__ __forceinline__ void finish_stats(acc4 (&acc)[T::TM][T::TN], const Out& o, int64_t m0, int64_t n0,
+                                             int64_t block, int rows, int cols, int wm, int wn, int lane)
+{
+    const int first = wn + 4 * (lane >> 4);   // the lane's columns: first + 16 j + r
+#pragma unroll
+    for (int i = 0; i < T::TM; ++i) {
+        const int m = wm + 16 * i + (lane & 15);
+        const bool row = m < rows;
+        const int64_t at = m0 + m;
+        float top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (!EDGE || first + 16 * j + r < cols)
+                    top = fmaxf(top, acc[i][j][r]);
+        // A NaN logit is no maximum, but makes the sum NaN.
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float from = top == -INFINITY ? 0.f : top * LOG2E;
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (!EDGE || first + 16 * j + r < cols)
+                    sum += __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], LOG2E, -from));
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        if (row) {
+            // The sum is of 2^(s log2 e - from); `from` is the maximum's
+            // multiple as rounded, so the maximum that belongs to the sum is
+            // from / log2 e: join() and the last logarithm put it back.
+            if (lane < 16)
+                o.part[at * o.nparts + block] = Run{top == -INFINITY ? -INFINITY : from, sum};
+            const int64_t t = o.target[at] - n0 - first;
+            if (t >= 0 && t < T::WN) {
+#pragma unroll
+                for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (t == 16 * j + r && (!EDGE || first + 16 * j + r < cols))
+                            o.target_logit[at] = acc[i][j][r];
+            }
+            if constexpr (KEEP)
+#pragma unroll
+                for (int j = 0; j < T::TN; ++j)
+                    if (!EDGE || first + 16 * j < cols)
+                        put4(static_cast<float*>(o.c) + at * o.ldc + n0 + first + 16 * j, acc[i][j],
+                             EDGE ? cols - first - 16 * j : 4);
+        }
+    }
+}
+
+// GRAD.  p = 2^(s log2 e - lse log2 e): the product of lse is rounded once a
+// row, and what that (and log2 e's own rounding) leaves goes into the row's
+// factor, so that a probability is as exact as its logit.
+template <typename T, bool EDGE>
+__device__ __forceinline__ void finish_grad(acc4 (&acc)[T::TM][T::TN], const Out& o, int64_t m0, int64_t n0, int rows,
+                                            int cols, int wm, int wn, int lane)
+{
+    // The lane's columns: first + STRIDE j + r.
+    constexpr int STRIDE = T::SPREAD ? 4 : 16;
+    const int first = wn + (T::SPREAD ? 16 : 4) * (lane >> 4);
+#pragma unroll
+    for (int i = 0; i < T::TM; ++i) {
+        const int m = wm + 16 * i + (lane & 15);
+        if (m >= rows)
+            continue;
+        const int64_t at = m0 + m, t = o.target[at];
+        const bool has = counts(t, o.V);
+        const float lse = has ? o.lse[at] : 0.f, d = has ? o.dloss[at] : 0.f;
+        const float from = lse * LOG2E;
+        const float rest = fmaf(lse, LOG2E, -from) + lse * LOG2E_REST;
+        const float scale = has ? fmaf(d, -rest * LN2, d) : 0.f;
+#pragma unroll
+        for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float g = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], LOG2E, -from)) * scale;
+                acc[i][j][r] = EDGE && first + STRIDE * j + r >= cols ? 0.f : g;   // past V: zeros
+            }
+        const int64_t tl = t - o.v0 - n0 - first;
+        if (has && tl >= 0 && tl < T::WN) {
+#pragma unroll
+            for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (tl == STRIDE * j + r) {
+                        acc[i][j][r] -= d;
+                        if (o.target_rest)
+                            o.target_rest[at] = acc[i][j][r] - static_cast<float>(static_cast<__bf16>(acc[i][j][r]));
+                    }
+        }
+        const int64_t to = at * o.ldg + n0 + first;
+        // Runs of values that lie together (SPREAD: eight, else four).
+        constexpr int RUN = T::SPREAD ? 2 : 1;
+        typedef unsigned uw __attribute__((ext_vector_type(2 * RUN)));
+#pragma unroll
+        for (int j = 0; j < T::TN; j += RUN) {
+            const bool in = !EDGE || n0 + first + STRIDE * j < o.ldg;   // ldg: a multiple of eight
+            if constexpr (sizeof(typename T::E) == 4) {
+                if (in)
+                    *reinterpret_cast<acc4*>(static_cast<float*>(o.g) + to + STRIDE * j) = acc[i][j];
+            } else {
+                // bf16 parts: h and m rounded to nearest, l what is left, exactly.
+                __bf16* g = static_cast<__bf16*>(o.g) + to + STRIDE * j;
+                uw part[3];
+#pragma unroll
+                for (int q = 0; q < 2 * RUN; ++q) {
+                    f2 x = {acc[i][j + q / 2][2 * (q % 2)], acc[i][j + q / 2][2 * (q % 2) + 1]};
+                    part[0][q] = bf16_pair(x[0], x[1]);
+                    x = rest_of_pair(x[0], x[1], part[0][q]);
+                    part[1][q] = bf16_pair(x[0], x[1]);
+                    x = rest_of_pair(x[0], x[1], part[1][q]);
+                    part[2][q] = bf16_pair(x[0], x[1]);
+                }
+#pragma unroll
+                for (int p = 0; p < 3; ++p)
+                    if (in)
+                        *reinterpret_cast<uw*>(g + p * o.g_plane) = part[p];
+            }
+        }
+    }
+}
+
+template <typename T, bool EDGE>
+__device__ __forceinline__ void finish_store(acc4 (&acc)[T::TM][T::TN], const Out& o, int64_t m0, int64_t n0, int rows,
+                                             int cols, int wm, int wn, int lane, int z)
+{
+    const int first = wn + 4 * (lane >> 4);
+#pragma unroll
+    for (int i = 0; i < T::TM; ++i) {
+        const int m = wm + 16 * i + (lane & 15);
+        if (m >= rows)
+            continue;
+        const int64_t at = m0 + m;
+        float rest = 0.f;
+        const typename T::E* w = nullptr;
+        if (o.target_rest && z == 0 && counts(o.target[at], o.V)) {
+            rest = o.target_rest[at];
+            w = static_cast<const typename T::E*>(o.W) + o.target[at] * o.ldw + n0 + first;
+        }
+#pragma unroll
+        for (int j = 0; j < T::TN; ++j) {
+            const int left = EDGE ? cols - first - 16 * j : 4;
+            if (left <= 0)
+                continue;
+            acc4 v = acc[i][j];
+            if (w) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (r < left)
+                        v[r] = fmaf(rest, static_cast<float>(w[16 * j + r]), v[r]);
+            }
+            const int64_t to = at * o.ldc + n0 + first + 16 * j;
+            if (o.bf16) {
+                put4(static_cast<__bf16*>(o.c) + to, __builtin_convertvector(v, b4), left);
+            } else {
+                float* c = static_cast<float*>(o.c) + z * o.split_stride + to;
+                if (o.add) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (r < left)
+                            v[r] += c[r];
+                }
+                put4(c, v, left);
+            }
+        }
+    }
+}
+
 template <typename T, Use USE>
 __device__ __forceinline__ void finish(acc4 (&acc)[T::TM][T::TN], const Out& o, int64_t m0, int64_t n0, int64_t tile_n,
                                        int64_t M, int64_t N, int z)
 {
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int wm = (w / T::NWN) * T::WM, wn = (w % T::NWN) * T::WN;
-    const int64_t n_lane = n0 + wn + 4 * (lane >> 4);
-#pragma unroll
-    for (int i = 0; i < T::TM; ++i) {
-        const int64_t m = m0 + wm + 16 * i + (lane & 15);
-        const bool row = m < M;
-        if constexpr (USE == STATS || USE == LOGITS) {
-            const int64_t t = row ? o.target[m] : -1;
-            Run run{-INFINITY, 0.f};
-#pragma unroll
-            for (int j = 0; j < T::TN; ++j) {
-                const int64_t n = n_lane + 16 * j;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float x = n + r < N ? acc[i][j][r] : -INFINITY;
-                    run.m = fmaxf(run.m, x);
-                }
-            }
-            // A NaN logit is not a maximum, but makes the sum one.
-            run.m = fmaxf(run.m, __shfl_xor(run.m, 16));
-            run.m = fmaxf(run.m, __shfl_xor(run.m, 32));
-            const float from = run.m == -INFINITY ? 0.f : run.m;
-#pragma unroll
-            for (int j = 0; j < T::TN; ++j) {
-                const int64_t n = n_lane + 16 * j;
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (n + r < N) {
-                        run.s += exp_f(acc[i][j][r] - from);
-                        if (n + r == t)
-                            o.target_logit[m] = acc[i][j][r];
-                    }
-                if constexpr (USE == LOGITS)
-                    if (row && n < N)
-                        put4(static_cast<float*>(o.c) + m * o.ldc + n, acc[i][j], N - n);
-            }
-            run.s += __shfl_xor(run.s, 16);
-            run.s += __shfl_xor(run.s, 32);
-            if (row && lane < 16)
-                o.part[m * o.nparts + tile_n * T::NWN + w % T::NWN] = run;
-        } else if constexpr (USE == GRAD) {
-            const int64_t t = row ? o.target[m] : -1;
-            const bool has = row && counts(t, o.V);
-            const float lse = row ? o.lse[m] : 0.f, d = row ? o.dloss[m] : 0.f;
-#pragma unroll
-            for (int j = 0; j < T::TN; ++j) {
-                const int64_t n = n_lane + 16 * j;
-                acc4 g;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float p = exp_f(acc[i][j][r] - lse) - (n + r + o.v0 == t ? 1.f : 0.f);
-                    g[r] = has && n + r < N ? p * d : 0.f;   // past V: zeros up to the row's end
-                }
-                if (!row || n >= o.ldg)
-                    continue;
-                if (o.target_rest && has) {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (n + r + o.v0 == t)
-                            o.target_rest[m] = g[r] - static_cast<float>(static_cast<__bf16>(g[r]));
-                }
-                if (o.g_parts == 0) {
-                    put4(static_cast<float*>(o.g) + m * o.ldg + n, g, 4);
-                } else {
-                    __bf16* at = static_cast<__bf16*>(o.g) + m * o.ldg + n;
-                    for (int p = 0; p < o.g_parts; ++p) {
-                        const b4 h = __builtin_convertvector(g, b4);
-                        put4(at + p * o.g_plane, h, 4);
-                        g -= __builtin_convertvector(h, acc4);
-                    }
-                }
-            }
-        } else {
-            float rest = 0.f;
-            const typename T::E* w = nullptr;
-            if (o.target_rest && z == 0 && row && counts(o.target[m], o.V)) {
-                rest = o.target_rest[m];
-                w = static_cast<const typename T::E*>(o.W) + o.target[m] * o.ldw;
-            }
-#pragma unroll
-            for (int j = 0; j < T::TN; ++j) {
-                const int64_t n = n_lane + 16 * j;
-                if (!row || n >= N)
-                    continue;
-                if (w) {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (n + r < N)
-                            acc[i][j][r] = fmaf(rest, static_cast<float>(w[n + r]), acc[i][j][r]);
-                }
-                if (o.bf16) {
-                    put4(static_cast<__bf16*>(o.c) + m * o.ldc + n, __builtin_convertvector(acc[i][j], b4), N - n);
-                } else {
-                    float* at = static_cast<float*>(o.c) + z * o.split_stride + m * o.ldc + n;
-                    acc4 v = acc[i][j];
-                    if (o.add) {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (n + r < N)
-                                v[r] += at[r];
-                    }
-                    put4(at, v, N - n);
-                }
-            }
-        }
+    const int rows = static_cast<int>(M - m0 < T::BM ? M - m0 : T::BM);
+    const int cols = static_cast<int>(N - n0 < T::BN ? N - n0 : T::BN);
+    const bool edge = cols < T::BN;
+    if constexpr (USE == STATS || USE == LOGITS) {
+        const int64_t block = tile_n * T::NWN + w % T::NWN;
+        if (edge)
+            finish_stats<T, true, USE == LOGITS>(acc, o, m0, n0, block, rows, cols, wm, wn, lane);
+        else
+            finish_stats<T, false, USE == LOGITS>(acc, o, m0, n0, block, rows, cols, wm, wn, lane);
+    } else if constexpr (USE == GRAD) {
+        if (edge)
+            finish_grad<T, true>(acc, o, m0, n0, rows, cols, wm, wn, lane);
+        else
+            finish_grad<T, false>(acc, o, m0, n0, rows, cols, wm, wn, lane);
+    } else {
+        if (edge)
+            finish_store<T, true>(acc, o, m0, n0, rows, cols, wm, wn, lane, z);
+        else
+            finish_store<T, false>(acc, o, m0, n0, rows, cols, wm, wn, lane, z);
     }
 }
 
@@ -267,55 +370,149 @@ __global__ __launch_bounds__(THREADS) void loss_kernel(const Run* __restrict__ p
         r = join(r, part[row * nparts + p]);
     r = wave_join(r);
     if (lane == 0) {
-        const float lse = r.m == -INFINITY && r.s == 0.f ? -INFINITY : r.m + logf(r.s);
+        const float lse = lse_of(r);
         lse_out[row] = lse;
         loss[row] = counts(target[row], V) ? lse - target_logit[row] : 0.f;
     }
 }
 
-// The factor form's second step: a workgroup joins its row's runs, then turns
-// its share of the row's logits into G, in place and as the operand of dX
-// (bf16 or fp32, ldg apart, zeros past V).
-constexpr int FACTOR_COLS = 4096;
+// One workgroup a row, where the rows are few: the row's logits are the sums of
+// the product's splits of k; their loss, lse and (given U) G, as U and as the
+// operand of dX (bf16 or fp32, ldg apart, zeros past V).  The summed logits
+// stay in registers where the row has at most ROW_HELD, else they are written
+// to the first split and read again.
+constexpr int ROW_THREADS = 1024, ROW_EACH = 32;
+constexpr int64_t ROW_HELD = int64_t(ROW_THREADS) * ROW_EACH;
 
-template <typename E>
-__global__ __launch_bounds__(THREADS) void factor_kernel(const Run* __restrict__ part, int64_t nparts,
-                                                         const float* __restrict__ target_logit,
+template <typename G, bool HELD, bool FACTOR>
+__global__ __launch_bounds__(ROW_THREADS) void row_kernel(float* __restrict__ logits, int splits, int64_t stride,
+                                                          const int64_t* __restrict__ target,
+                                                          const float* __restrict__ dloss, int64_t V,
+                                                          float* __restrict__ loss, float* __restrict__ lse_out,
+                                                          float* __restrict__ U, G* __restrict__ g, int64_t ldg,
+                                                          float* __restrict__ target_rest)
+{
+    __shared__ Run runs[ROW_THREADS / 64];
+    const int64_t row = blockIdx.x;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    float* s = logits + row * V;
+    const int64_t t = target[row];
+    const bool has = counts(t, V);
+    float held[HELD ? ROW_EACH : 1];
+    Run r{-INFINITY, 0.f};
+    auto summed = [&](int64_t v) {
+        float x = s[v];
+        for (int z = 1; z < splits; ++z)
+            x += s[z * stride + v];
+        return x;
+    };
+    if constexpr (HELD) {
+#pragma unroll
+        for (int e = 0; e < ROW_EACH; ++e) {
+            const int64_t v = threadIdx.x + static_cast<int64_t>(e) * ROW_THREADS;
+            held[e] = v < V ? summed(v) : -INFINITY;
+        }
+#pragma unroll
+        for (int e = 0; e < ROW_EACH; ++e)
+            r.m = fmaxf(r.m, held[e]);
+        r.m *= LOG2E;
+        const float from = r.m == -INFINITY ? 0.f : r.m;
+#pragma unroll
+        for (int e = 0; e < ROW_EACH; ++e)
+            r.s += __builtin_amdgcn_exp2f(fmaf(held[e], LOG2E, -from));   // past V: 0
+    } else {
+        for (int64_t v = threadIdx.x; v < V; v += ROW_THREADS) {
+            const float x = summed(v);
+            s[v] = x;
+            const float y = x * LOG2E;
+            r = join(r, Run{y, x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(x, LOG2E, -y))});
+        }
+    }
+    r = wave_join(r);
+    if (lane == 0)
+        runs[w] = r;
+    __syncthreads();   // and the summed logits are written
+    r = runs[0];
+#pragma unroll
+    for (int i = 1; i < ROW_THREADS / 64; ++i)
+        r = join(r, runs[i]);
+    const float lse = lse_of(r);
+    float hit = 0.f;   // the target's logit, where this thread has it
+    const bool mine = has && t % ROW_THREADS == threadIdx.x;
+    if constexpr (HELD) {
+#pragma unroll
+        for (int e = 0; e < ROW_EACH; ++e)
+            if (mine && t / ROW_THREADS == e)
+                hit = held[e];
+    } else if (mine) {
+        hit = s[t];
+    }
+    if (mine || (!has && threadIdx.x == 0))
+        loss[row] = has ? lse - hit : 0.f;
+    if (lse_out && threadIdx.x == 0)
+        lse_out[row] = lse;
+    if constexpr (FACTOR) {
+        const float d = has ? dloss[row] : 0.f;
+        const float from = has ? lse * LOG2E : 0.f;
+        const float rest = fmaf(lse, LOG2E, -from) + lse * LOG2E_REST;
+        const float scale = has ? fmaf(d, -rest * LN2, d) : 0.f;
+        auto put = [&](int64_t v, float x) {
+            if (v < V) {
+                x = has ? __builtin_amdgcn_exp2f(fmaf(x, LOG2E, -from)) * scale : 0.f;
+                if (has && v == t) {
+                    x -= d;
+                    target_rest[row] = x - static_cast<float>(static_cast<G>(x));
+                }
+                U[row * V + v] = x;
+                g[row * ldg + v] = static_cast<G>(x);
+            } else if (v < ldg) {
+                g[row * ldg + v] = static_cast<G>(0.f);
+            }
+        };
+        if constexpr (HELD) {
+#pragma unroll
+            for (int e = 0; e < ROW_EACH; ++e)
+                put(threadIdx.x + static_cast<int64_t>(e) * ROW_THREADS, held[e]);
+        } else {
+            for (int64_t v = threadIdx.x; v < ldg; v += ROW_THREADS)
+                put(v, v < V ? s[v] : 0.f);
+        }
+    }
+}
+
+// Many rows: G from the logits in U and their lse, in place and as the operand
+// of dX (PARTS bf16 parts, or fp32; ldg apart, zeros past V).
+template <typename E, int PARTS>
+__global__ __launch_bounds__(THREADS) void factor_kernel(const float* __restrict__ lse,
                                                          const int64_t* __restrict__ target,
                                                          const float* __restrict__ dloss, int64_t T, int64_t V,
-                                                         float* __restrict__ loss, float* __restrict__ U,
-                                                         E* __restrict__ g, int64_t ldg,
+                                                         float* __restrict__ U, E* __restrict__ g, int64_t ldg,
                                                          float* __restrict__ target_rest)
 {
-    __shared__ Run runs[THREADS / 64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    for (int64_t row = blockIdx.y; row < T; row += gridDim.y) {
-        Run r{-INFINITY, 0.f};
-        for (int64_t p = threadIdx.x; p < nparts; p += THREADS)
-            r = join(r, part[row * nparts + p]);
-        r = wave_join(r);
-        __syncthreads();   // the row before has read its runs
-        if (lane == 0)
-            runs[w] = r;
-        __syncthreads();
-        r = join(join(runs[0], runs[1]), join(runs[2], runs[3]));
-        const float lse = r.m == -INFINITY && r.s == 0.f ? -INFINITY : r.m + logf(r.s);
-        const int64_t t = target[row];
+    const int64_t per_row = ldg / GROUP, step = static_cast<int64_t>(gridDim.x) * THREADS;
+    for (int64_t q = static_cast<int64_t>(blockIdx.x) * THREADS + threadIdx.x; q < T * per_row; q += step) {
+        const int64_t row = q / per_row, c = (q - row * per_row) * GROUP, t = target[row];
         const bool has = counts(t, V);
-        const float d = dloss[row];
-        if (blockIdx.x == 0 && threadIdx.x == 0)
-            loss[row] = has ? lse - target_logit[row] : 0.f;
-        const int64_t from = static_cast<int64_t>(blockIdx.x) * FACTOR_COLS;
-        for (int64_t v = from + threadIdx.x; v < from + FACTOR_COLS && v < ldg; v += THREADS) {
-            float x = 0.f;
-            if (v < V) {
-                if (has)
-                    x = (exp_f(U[row * V + v] - lse) - (v == t ? 1.f : 0.f)) * d;
-                U[row * V + v] = x;
+        const float l = has ? lse[row] : 0.f, d = has ? dloss[row] : 0.f, from = l * LOG2E;
+        const float rest = fmaf(l, LOG2E, -from) + l * LOG2E_REST, scale = has ? fmaf(d, -rest * LN2, d) : 0.f;
+        float v[GROUP];
+        load_some(U + row * V + c, V - c, v);
+#pragma unroll
+        for (int i = 0; i < GROUP; ++i) {
+            v[i] = has && c + i < V ? __builtin_amdgcn_exp2f(fmaf(v[i], LOG2E, -from)) * scale : 0.f;
+            if (has && c + i == t) {
+                v[i] -= d;
+                target_rest[row] = v[i] - static_cast<float>(static_cast<E>(v[i]));
             }
-            g[row * ldg + v] = static_cast<E>(x);
-            if (has && v == t)
-                target_rest[row] = x - static_cast<float>(static_cast<E>(x));
+        }
+        store_some(U + row * V + c, V - c, v);
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+            store_group(g + p * (T * ldg) + row * ldg + c, v);
+            if (p + 1 < PARTS)
+#pragma unroll
+                for (int i = 0; i < GROUP; ++i)
+                    v[i] -= static_cast<float>(static_cast<__bf16>(v[i]));
         }
     }
 }
@@ -387,54 +584,59 @@ struct Arena {
     }
 };
 
-// Tile shapes: 32 rows where there are no more (bound by reading the other
-// operand), 256 x 256 (one workgroup a CU) where enough of them fill the GPU,
-// else 128 x 128 (two a CU).
-template <typename E, bool AK, bool BK>
-using Thin = Tile<E, AK, BK, 32, 64, 32, 16, 4>;
-template <typename E, bool AK, bool BK>
-using Square = Tile<E, AK, BK, 128, 128, 64, 64, 2>;
-template <typename E, bool AK, bool BK>
-using Large = Tile<E, AK, BK, 256, 256, 128, 64, 2>;
-
+// Tile shapes: 256 x 256 (one workgroup a CU), 128 x 128 (two), and 32 x 64
+// (three) for few rows or few tiles.
 enum ShapeKind { THIN, SQUARE, LARGE };
 
+template <typename E, bool AK, bool BK>
+using Thin = Tile<E, AK, BK, 32, 64, 32, 16, 4, 2>;
+template <typename E, bool AK, bool BK>
+using Square = Tile<E, AK, BK, 128, 128, 64, 64, 2, 2, false>;
+template <typename E, bool AK, bool BK, bool SPREAD = false>
+using Large = Tile<E, AK, BK, 256, 256, 128, 64, 2, 2, SPREAD>;
+
+// What a shape costs, as measured: microseconds of a step of 128 bytes of k
+// with the CU full, and of a tile's start and end; workgroups a CU runs.
 struct Shape {
-    ShapeKind kind;
-    int64_t bm, bn, waves_n;
+    int64_t bm, bn, waves_n, per_cu;
+    double step_us[2], tile_us;   // step: bf16, fp32
+};
+constexpr Shape SHAPES[] = {
+    {32, 64, 4, 3, {0.50, 0.65}, 4.0},
+    {128, 128, 2, 2, {1.05, 4.3}, 6.0},
+    {256, 256, 4, 1, {1.55, 0.0}, 9.0},
 };
 
+struct Choice {
+    ShapeKind kind;
+    int64_t splits;
+    double us;
+};
+
+// The shape, and the ways to split k (whose sums are then added by a kernel of
+// their own), that finish M x N tiles over K values of k first: whole rounds of
+// workgroups over the GPU, and the splits' sums at 4 TB/s.
 template <typename E>
-Shape shape_for(int64_t M, int64_t N)
+Choice choose(int64_t M, int64_t N, int64_t K, int count, bool may_split)
 {
-    if (M <= 32)
-        return Shape{THIN, 32, 64, 4};
-    if (sizeof(E) == 2) {
-        const int64_t cus = device_cu_count();
-        const int64_t large = ceil_div(ceil_div(M, 256) * ceil_div(N, 256), cus) * 4;
-        const int64_t square = ceil_div(ceil_div(M, 128) * ceil_div(N, 128), 2 * cus) * 2;
-        if (4 * large <= 5 * square)
-            return Shape{LARGE, 256, 256, 4};
+    const int64_t steps = ceil_div(std::max<int64_t>(K, 1), 128 / static_cast<int64_t>(sizeof(E))) * count;
+    const int64_t cus = device_cu_count();
+    Choice best{SQUARE, 1, 1e30};
+    for (int k = THIN; k <= LARGE; ++k) {
+        if (k == LARGE && sizeof(E) == 4)
+            continue;
+        const Shape& s = SHAPES[k];
+        const int64_t tiles = ceil_div(M, s.bm) * ceil_div(N, s.bn);
+        const int64_t most = may_split ? std::max<int64_t>(1, std::min<int64_t>(32, steps / count / 4)) : 1;
+        for (int64_t z = 1; z <= most; ++z) {
+            const double rounds = static_cast<double>(ceil_div(tiles * z, s.per_cu * cus));
+            const double us = rounds * (static_cast<double>(ceil_div(steps, z)) * s.step_us[sizeof(E) / 4] + s.tile_us) +
+                              (z > 1 ? 3.0 + 8.0 * static_cast<double>(z * M * N) / 4e6 : 0.0);
+            if (us < best.us)
+                best = Choice{static_cast<ShapeKind>(k), z, us};
+        }
     }
-    return Shape{SQUARE, 128, 128, 2};
-}
-
-template <typename E>
-int64_t parts_of(int64_t M, int64_t N)
-{
-    const Shape s = shape_for<E>(M, N);
-    return ceil_div(N, s.bn) * s.waves_n;
-}
-
-// How many ways to split k so that the tiles fill the GPU: about two
-// workgroups a CU, at least eight steps each.
-template <typename E>
-int64_t splits_for(int64_t M, int64_t N, int64_t K)
-{
-    const Shape s = shape_for<E>(M, N);
-    const int64_t step = STEP_BYTES / sizeof(E);
-    const int64_t tiles = ceil_div(M, s.bm) * ceil_div(N, s.bn), steps = ceil_div(K, step);
-    return std::max<int64_t>(1, std::min<int64_t>(2 * device_cu_count() / std::max<int64_t>(tiles, 1), steps / 8));
+    return best;
 }
 
 template <typename T, Use USE>
@@ -449,20 +651,20 @@ hipError_t launch_product(const Operand& a, const Operand& b, const Parts& p, co
 }
 
 template <typename E, bool AK, bool BK, Use USE>
-hipError_t product(const Operand& a, const Operand& b, const Parts& p, const Out& o, int64_t M, int64_t N, int64_t K,
-                   int64_t splits, hipStream_t s)
+hipError_t product(const Choice& c, const Operand& a, const Operand& b, const Parts& p, const Out& o, int64_t M,
+                   int64_t N, int64_t K, hipStream_t s)
 {
-    const ShapeKind kind = shape_for<E>(M, N).kind;
-    if (kind == THIN)
-        return launch_product<Thin<E, AK, BK>, USE>(a, b, p, o, M, N, K, splits, s);
+    if (c.kind == THIN)
+        return launch_product<Thin<E, AK, BK>, USE>(a, b, p, o, M, N, K, c.splits, s);
     if constexpr (sizeof(E) == 2)
-        if (kind == LARGE)
-            return launch_product<Large<E, AK, BK>, USE>(a, b, p, o, M, N, K, splits, s);
-    return launch_product<Square<E, AK, BK>, USE>(a, b, p, o, M, N, K, splits, s);
+        if (c.kind == LARGE)
+            return launch_product<Large<E, AK, BK, USE == GRAD>, USE>(a, b, p, o, M, N, K, c.splits, s);
+    return launch_product<Square<E, AK, BK>, USE>(a, b, p, o, M, N, K, c.splits, s);
 }
 
-constexpr Parts ONE{1, 0};
-constexpr Parts THREE_A{3, 0x210};   // A in three parts, B in one
+// Products of parts, four bits each (A's, then B's): one; three of A with one
+// of B; the six of 3 x 3 that fp32 needs.
+constexpr Parts ONE{1, 0}, THREE_A{3, 0x210}, SIX{6, 0x528140};
 
 template <typename O>
 hipError_t join_splits(const float* part, int64_t splits, int64_t n, O* out, hipStream_t s)
@@ -472,79 +674,120 @@ hipError_t join_splits(const float* part, int64_t splits, int64_t n, O* out, hip
     return hipGetLastError();
 }
 
-// X or W as an operand: as it is where its rows lie on 16-byte boundaries,
-// else a copy with padded rows (and, given targets, the rows without one
-// cleared).
-template <typename E>
+// X or W as the caller has it is an operand where its rows lie on 16-byte
+// boundaries; else it is laid out again.
+template <typename I>
 bool needs_copy(const void* p, int64_t D)
 {
-    return !aligned16(p) || D * static_cast<int64_t>(sizeof(E)) % 16 != 0;
+    return !aligned16(p) || D * static_cast<int64_t>(sizeof(I)) % 16 != 0;
 }
 
-template <typename E>
-hipError_t copy_rows(const E* x, int64_t rows, int64_t D, int64_t ldo, const int64_t* target, int64_t V, E* out,
-                     hipStream_t s)
+template <typename I, typename O, int PARTS>
+hipError_t lay_out(const I* x, int64_t rows, int64_t D, int64_t ldo, const int64_t* target, int64_t V, O* out,
+                   hipStream_t s)
 {
-    lay_out_kernel<E, E, 1><<<grid_for(ceil_div(rows * (ldo / GROUP), THREADS)), THREADS, 0, s>>>(x, rows, D, ldo,
-                                                                                               target, V, out, 0);
+    if (rows > 0)
+        lay_out_kernel<I, O, PARTS><<<grid_for(ceil_div(rows * (ldo / GROUP), THREADS)), THREADS, 0, s>>>(
+            x, rows, D, ldo, target, V, out, rows * ldo);
     return hipGetLastError();
 }
 
-// Arrays of a call in its workspace; sized with a null base.
+// How a call computes: I, the type of X and W in memory; E, the operands'
+// (bf16, or fp32 multiplied as fp32); fp32 in bf16 parts (I = float, E = bf16)
+// where the products outweigh the splitting.
+//
+// Rows of which the logits of all classes are fewer than this are few: their
+// logits go through memory once (they are small beside W), which lets k be
+// split so that the GPU is full.
+constexpr int64_t FEW_ROWS = 32;
 constexpr int64_t PIECE_BYTES = int64_t(512) << 20;   // of G at a time
 
 struct Plan {
-    int64_t ldd = 0;                      // row length of copies
+    bool few = false, own_x = false, own_w = false;
+    int64_t ldd = 0;   // row length of what is laid out
     void* x = nullptr;
     void* w = nullptr;
-    Run* part = nullptr;
+    Parts logits_parts = ONE, dx_parts = ONE, dw_parts = ONE;
+    Choice logits{}, dx_choice{}, dw_choice{};
+    float* row_logits = nullptr;   // few rows: splits x T x V
+    Run* part = nullptr;           // many: a run per row and column block
     int64_t nparts = 0;
     float* target_logit = nullptr;
+    float* lse = nullptr;
     void* g = nullptr;
-    int64_t piece = 0, ldg = 0, g_parts = 0, dx_splits = 1, dw_splits = 1;
+    int64_t piece = 0, ldg = 0;
     float* target_rest = nullptr;
     float* dx = nullptr;
     float* dw = nullptr;
     int64_t bytes = 0;
 };
 
-template <typename E>
-Plan make_plan(int op, int64_t T, int64_t V, int64_t D, bool copy_x, bool copy_w, char* base)
+template <typename I, typename E>
+Plan make_plan(int op, const void* X, const void* W, int64_t T, int64_t V, int64_t D, char* base)
 {
-    constexpr int64_t SZ = sizeof(E);
+    constexpr bool SPLIT = sizeof(I) == 4 && sizeof(E) == 2;   // fp32 in bf16 parts
+    constexpr int64_t SZ = sizeof(E), COPIES = SPLIT ? 3 : 1;
     Plan p;
     Arena a{base};
     p.ldd = round_up(D, GROUP);
-    if (op == POSEIDON_XENT_BACKWARD || copy_x)
-        p.x = a.take(T * p.ldd * SZ);
-    if (copy_w)
-        p.w = a.take(V * p.ldd * SZ);
-    if (op != POSEIDON_XENT_BACKWARD) {
-        p.nparts = parts_of<E>(T, V);
-        p.part = static_cast<Run*>(a.take(T * p.nparts * sizeof(Run)));
+    p.own_x = SPLIT || op == POSEIDON_XENT_BACKWARD || needs_copy<I>(X, D);
+    p.own_w = SPLIT || needs_copy<I>(W, D);
+    if (p.own_x)
+        p.x = a.take(T * p.ldd * SZ * COPIES);
+    if (p.own_w)
+        p.w = a.take(V * p.ldd * SZ * COPIES);
+    if (SPLIT)
+        p.logits_parts = p.dx_parts = p.dw_parts = SIX;
+    else if (SZ == 2)
+        p.dw_parts = THREE_A;
+    p.few = op != POSEIDON_XENT_BACKWARD && T <= FEW_ROWS;
+    p.logits = choose<E>(T, V, D, p.logits_parts.count, p.few);
+    if (p.few) {
+        p.row_logits = static_cast<float*>(a.take(p.logits.splits * T * V * 4));
+    } else if (op != POSEIDON_XENT_BACKWARD) {
+        const Shape& s = SHAPES[p.logits.kind];
+        p.nparts = ceil_div(V, s.bn) * s.waves_n;
+        p.part = static_cast<Run*>(a.take(T * p.nparts * static_cast<int64_t>(sizeof(Run))));
         p.target_logit = static_cast<float*>(a.take(T * 4));
+        p.lse = static_cast<float*>(a.take(T * 4));
     }
     if (op == POSEIDON_XENT_FORWARD) {
         p.bytes = a.at;
         return p;
     }
-    p.g_parts = SZ == 4 ? 0 : op == POSEIDON_XENT_BACKWARD ? 3 : 1;
-    const int64_t g_value = SZ == 4 ? 4 : 2 * p.g_parts;
+    // G: fp32, or in bf16 parts (for a factor's bf16 dX one of them).
+    const int64_t g_value = SZ == 4 ? 4 : op == POSEIDON_XENT_FACTOR && !SPLIT ? 2 : 6;
     p.piece = round_up(V, GROUP);
-    if (op == POSEIDON_XENT_BACKWARD)
-        p.piece = std::min(p.piece, std::max<int64_t>(PIECE_BYTES / g_value / std::max<int64_t>(T, 1) / 256, 1) * 256);
+    p.dx_choice = choose<E>(T, D, V, p.dx_parts.count, true);
+    if (op == POSEIDON_XENT_BACKWARD) {
+        // Pieces of the vocabulary, as equal as tiles allow: the number of them
+        // (from what the budget asks for) that is cheapest by the choices' own
+        // estimates.
+        const int64_t most = std::max<int64_t>(PIECE_BYTES / g_value / std::max<int64_t>(T, 1) / 256, 1) * 256;
+        const int64_t fewest = ceil_div(V, most);
+        double best = 1e30;
+        for (int64_t n = fewest; n < fewest + 4; ++n) {
+            const int64_t piece = n == 1 ? round_up(V, GROUP) : round_up(ceil_div(V, n), 256);
+            const int64_t count = ceil_div(V, piece), rows = std::min(piece, V);
+            const Choice l = choose<E>(T, rows, D, p.logits_parts.count, false);
+            const Choice x = choose<E>(T, D, rows, p.dx_parts.count, true);
+            const Choice w = choose<E>(rows, D, T, p.dw_parts.count, true);
+            if (static_cast<double>(count) * (l.us + x.us + w.us) < best) {
+                best = static_cast<double>(count) * (l.us + x.us + w.us);
+                p.piece = piece;
+                p.logits = l;
+                p.dx_choice = x;
+                p.dw_choice = w;
+            }
+        }
+        if (p.dw_choice.splits > 1)
+            p.dw = static_cast<float*>(a.take(p.dw_choice.splits * std::min(p.piece, V) * D * 4));
+    }
     p.ldg = p.piece;
     p.g = a.take(T * p.ldg * g_value);
     p.target_rest = static_cast<float*>(a.take(T * 4));
-    p.dx_splits = splits_for<E>(T, D, std::min(p.piece, V));
-    const int64_t pieces = ceil_div(V, p.piece);
-    if (p.dx_splits > 1 || (pieces > 1 && SZ == 2))
-        p.dx = static_cast<float*>(a.take(p.dx_splits * T * D * 4));
-    if (op == POSEIDON_XENT_BACKWARD) {
-        p.dw_splits = splits_for<E>(std::min(p.piece, V), D, T);
-        if (p.dw_splits > 1)
-            p.dw = static_cast<float*>(a.take(p.dw_splits * std::min(p.piece, V) * D * 4));
-    }
+    if (p.dx_choice.splits > 1 || (p.piece < V && sizeof(I) == 2))
+        p.dx = static_cast<float*>(a.take(p.dx_choice.splits * T * D * 4));
     p.bytes = a.at;
     return p;
 }
@@ -556,35 +799,88 @@ Plan make_plan(int op, int64_t T, int64_t V, int64_t D, bool copy_x, bool copy_w
             return rc_;              \
     } while (0)
 
-template <typename E>
-hipError_t forward_typed(const E* X, const E* W, const int64_t* target, int64_t T, int64_t V, int64_t D, float* loss,
-                         float* lse, char* ws, hipStream_t s)
+// X and W as operands, laid out where the plan says so (given `target`, X
+// without the rows that have none: whatever they hold must not reach dW).
+template <typename I, typename E>
+hipError_t operands(const Plan& p, const I* X, const I* W, const int64_t* target, int64_t T, int64_t V, int64_t D,
+                    Operand& x, Operand& w, hipStream_t s)
 {
-    const bool cx = needs_copy<E>(X, D), cw = needs_copy<E>(W, D);
-    const Plan p = make_plan<E>(POSEIDON_XENT_FORWARD, T, V, D, cx, cw, ws);
-    if (cx)
-        POSEIDON_TRY(copy_rows(X, T, D, p.ldd, nullptr, V, static_cast<E*>(p.x), s));
-    if (cw)
-        POSEIDON_TRY(copy_rows(W, V, D, p.ldd, nullptr, V, static_cast<E*>(p.w), s));
+    constexpr int PARTS = sizeof(I) == 4 && sizeof(E) == 2 ? 3 : 1;
+    if (p.own_x)
+        POSEIDON_TRY((lay_out<I, E, PARTS>(X, T, D, p.ldd, target, V, static_cast<E*>(p.x), s)));
+    if (p.own_w)
+        POSEIDON_TRY((lay_out<I, E, PARTS>(W, V, D, p.ldd, nullptr, V, static_cast<E*>(p.w), s)));
+    x = Operand{p.own_x ? p.x : X, p.own_x ? p.ldd : D, T, T * p.ldd};
+    w = Operand{p.own_w ? p.w : W, p.own_w ? p.ldd : D, V, V * p.ldd};
+    return hipSuccess;
+}
+
+// k-major operands end on 16 bytes.
+template <typename E>
+int64_t whole_chunks(int64_t k)
+{
+    return round_up(k, 16 / static_cast<int64_t>(sizeof(E)));
+}
+
+template <typename E>
+hipError_t row_logits(const Plan& p, const Operand& x, const Operand& w, int64_t T, int64_t V, int64_t D,
+                      hipStream_t s)
+{
+    Out o{};
+    o.c = p.row_logits;
+    o.ldc = V;
+    o.split_stride = T * V;
+    return product<E, true, true, STORE>(p.logits, x, w, p.logits_parts, o, T, V, whole_chunks<E>(D), s);
+}
+
+template <typename G, bool FACTOR>
+hipError_t rows_done(const Plan& p, const int64_t* target, const float* dloss, int64_t T, int64_t V, float* loss,
+                     float* lse, float* U, hipStream_t s)
+{
+    auto* k = round_up(V, GROUP) <= ROW_HELD ? row_kernel<G, true, FACTOR> : row_kernel<G, false, FACTOR>;
+    k<<<static_cast<unsigned>(T), ROW_THREADS, 0, s>>>(p.row_logits, static_cast<int>(p.logits.splits), T * V, target,
+                                                       dloss, V, loss, lse, U, static_cast<G*>(p.g), p.ldg,
+                                                       p.target_rest);
+    return hipGetLastError();
+}
+
+// Losses and lse without keeping logits.
+template <typename E>
+hipError_t losses(const Plan& p, const Operand& x, const Operand& w, const int64_t* target, int64_t T, int64_t V,
+                  int64_t D, float* loss, float* lse, hipStream_t s)
+{
     Out o{};
     o.part = p.part;
     o.nparts = p.nparts;
     o.target_logit = p.target_logit;
     o.target = target;
-    const Operand a{cx ? p.x : X, cx ? p.ldd : D, T, 0}, b{cw ? p.w : W, cw ? p.ldd : D, V, 0};
-    POSEIDON_TRY((product<E, true, true, STATS>(a, b, ONE, o, T, V, round_up(D, 16 / sizeof(E)), 1, s)));
+    POSEIDON_TRY((product<E, true, true, STATS>(p.logits, x, w, p.logits_parts, o, T, V, whole_chunks<E>(D), s)));
     loss_kernel<<<static_cast<unsigned>(ceil_div(T, THREADS / 64)), THREADS, 0, s>>>(p.part, p.nparts, p.target_logit,
                                                                                     target, T, V, loss, lse);
     return hipGetLastError();
 }
 
-// dX = G W for one piece of the vocabulary (the first replaces, the others add).
-template <typename E>
-hipError_t input_gradient(const Plan& p, const Operand& g, const Operand& w, const E* W, const int64_t* target,
-                          int64_t T, int64_t V, int64_t D, int64_t v0, int64_t vp, E* dX, hipStream_t s)
+template <typename I, typename E>
+hipError_t forward_typed(const I* X, const I* W, const int64_t* target, int64_t T, int64_t V, int64_t D, float* loss,
+                         float* lse, char* ws, hipStream_t s)
 {
+    const Plan p = make_plan<I, E>(POSEIDON_XENT_FORWARD, X, W, T, V, D, ws);
+    Operand x, w;
+    POSEIDON_TRY((operands<I, E>(p, X, W, nullptr, T, V, D, x, w, s)));
+    if (!p.few)
+        return losses<E>(p, x, w, target, T, V, D, loss, lse, s);
+    POSEIDON_TRY(row_logits<E>(p, x, w, T, V, D, s));
+    return rows_done<E, false>(p, target, nullptr, T, V, loss, lse, nullptr, s);
+}
+
+// dX = G W for one piece of the vocabulary (the first replaces, the others add).
+template <typename I, typename E>
+hipError_t input_gradient(const Plan& p, const Operand& g, const Operand& w, const Operand& whole_w,
+                          const int64_t* target, int64_t T, int64_t V, int64_t D, int64_t v0, int64_t vp, I* dX,
+                          hipStream_t s)
+{
+    constexpr bool BF16 = sizeof(I) == 2;
     const bool first = v0 == 0, last = v0 + vp == V;
-    constexpr bool BF16 = sizeof(E) == 2;
     Out o{};
     o.c = p.dx ? static_cast<void*>(p.dx) : static_cast<void*>(dX);
     o.ldc = D;
@@ -595,92 +891,106 @@ hipError_t input_gradient(const Plan& p, const Operand& g, const Operand& w, con
         o.target_rest = p.target_rest;
         o.target = target;
         o.V = V;
-        o.W = W;
-        o.ldw = w.ld;
+        o.W = whole_w.p;
+        o.ldw = whole_w.ld;
     }
-    POSEIDON_TRY((product<E, true, false, STORE>(g, w, ONE, o, T, D, round_up(vp, GROUP), p.dx_splits, s)));
-    return last && p.dx ? join_splits(p.dx, p.dx_splits, T * D, dX, s) : hipSuccess;
+    POSEIDON_TRY((product<E, true, false, STORE>(p.dx_choice, g, w, p.dx_parts, o, T, D, whole_chunks<E>(vp), s)));
+    return last && p.dx ? join_splits(p.dx, p.dx_choice.splits, T * D, dX, s) : hipSuccess;
 }
 
-template <typename E>
-hipError_t backward_typed(const E* X, const E* W, const int64_t* target, const float* lse, const float* dloss,
-                          int64_t T, int64_t V, int64_t D, E* dX, float* dW, char* ws, hipStream_t s)
+// G of the classes v0 .. v0 + vp.
+template <typename I, typename E>
+hipError_t logit_gradient(const Plan& p, const Operand& x, const Operand& w, const int64_t* target, const float* lse,
+                          const float* dloss, int64_t T, int64_t V, int64_t D, int64_t v0, int64_t vp, hipStream_t s)
 {
-    const bool cw = needs_copy<E>(W, D);
-    const Plan p = make_plan<E>(POSEIDON_XENT_BACKWARD, T, V, D, true, cw, ws);
-    // X without the rows that have no target: whatever they hold must not
-    // reach dW.
-    if (T > 0)
-        POSEIDON_TRY(copy_rows(X, T, D, p.ldd, target, V, static_cast<E*>(p.x), s));
-    if (cw)
-        POSEIDON_TRY(copy_rows(W, V, D, p.ldd, nullptr, V, static_cast<E*>(p.w), s));
-    const E* w = cw ? static_cast<const E*>(p.w) : W;
-    const int64_t ldw = cw ? p.ldd : D;
-    const Operand x{p.x, p.ldd, T, 0};
+    Out o{};
+    o.target = target;
+    o.lse = lse;
+    o.dloss = dloss;
+    o.g = p.g;
+    o.ldg = p.ldg;
+    o.g_plane = T * p.ldg;
+    o.v0 = v0;
+    o.V = V;
+    o.target_rest = sizeof(I) == 2 ? p.target_rest : nullptr;
+    return product<E, true, true, GRAD>(p.logits, x, w, p.logits_parts, o, T, vp, whole_chunks<E>(D), s);
+}
+
+template <typename I, typename E>
+hipError_t backward_typed(const I* X, const I* W, const int64_t* target, const float* lse, const float* dloss,
+                          int64_t T, int64_t V, int64_t D, I* dX, float* dW, char* ws, hipStream_t s)
+{
+    const Plan p = make_plan<I, E>(POSEIDON_XENT_BACKWARD, X, W, T, V, D, ws);
+    Operand x, w;
+    POSEIDON_TRY((operands<I, E>(p, X, W, target, T, V, D, x, w, s)));
+    const Operand g{p.g, p.ldg, T, T * p.ldg};
     for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
         const int64_t vp = std::min(p.piece, V - v0);
-        const Operand wp{w + v0 * ldw, ldw, vp, 0};
-        const Operand g{p.g, p.ldg, T, T * p.ldg};
+        const Operand wp{static_cast<const E*>(w.p) + v0 * w.ld, w.ld, vp, w.plane};
         if (T > 0) {
-            Out o{};
-            o.target = target;
-            o.lse = lse;
-            o.dloss = dloss;
-            o.g = p.g;
-            o.ldg = p.ldg;
-            o.g_plane = T * p.ldg;
-            o.g_parts = static_cast<int32_t>(p.g_parts);
-            o.v0 = v0;
-            o.V = V;
-            o.target_rest = sizeof(E) == 2 ? p.target_rest : nullptr;
-            POSEIDON_TRY((product<E, true, true, GRAD>(x, wp, ONE, o, T, vp, round_up(D, 16 / sizeof(E)), 1, s)));
-            POSEIDON_TRY(input_gradient(p, g, wp, w, target, T, V, D, v0, vp, dX, s));
+            POSEIDON_TRY((logit_gradient<I, E>(p, x, wp, target, lse, dloss, T, V, D, v0, vp, s)));
+            POSEIDON_TRY((input_gradient<I, E>(p, g, wp, w, target, T, V, D, v0, vp, dX, s)));
         }
         Out o{};
         o.c = p.dw ? p.dw : dW + v0 * D;
         o.ldc = D;
         o.split_stride = vp * D;
-        POSEIDON_TRY((product<E, false, false, STORE>(g, x, p.g_parts == 3 ? THREE_A : ONE, o, vp, D, T, p.dw_splits,
-                                                      s)));
+        POSEIDON_TRY((product<E, false, false, STORE>(p.dw_choice, g, x, p.dw_parts, o, vp, D, T, s)));
         if (p.dw)
-            POSEIDON_TRY(join_splits(p.dw, p.dw_splits, vp * D, dW + v0 * D, s));
+            POSEIDON_TRY(join_splits(p.dw, p.dw_choice.splits, vp * D, dW + v0 * D, s));
     }
     return hipSuccess;
 }
 
-template <typename E>
-hipError_t factor_typed(const E* X, const E* W, const int64_t* target, const float* dloss, int64_t T, int64_t V,
-                        int64_t D, float* loss, float* U, E* dX, char* ws, hipStream_t s)
+template <typename I, typename E>
+hipError_t factor_typed(const I* X, const I* W, const int64_t* target, const float* dloss, int64_t T, int64_t V,
+                        int64_t D, float* loss, float* U, I* dX, char* ws, hipStream_t s)
 {
-    const bool cx = needs_copy<E>(X, D), cw = needs_copy<E>(W, D);
-    const Plan p = make_plan<E>(POSEIDON_XENT_FACTOR, T, V, D, cx, cw, ws);
-    if (cx)
-        POSEIDON_TRY(copy_rows(X, T, D, p.ldd, nullptr, V, static_cast<E*>(p.x), s));
-    if (cw)
-        POSEIDON_TRY(copy_rows(W, V, D, p.ldd, nullptr, V, static_cast<E*>(p.w), s));
-    Out o{};
-    o.part = p.part;
-    o.nparts = p.nparts;
-    o.target_logit = p.target_logit;
-    o.target = target;
-    o.c = U;
-    o.ldc = V;
-    const Operand a{cx ? p.x : X, cx ? p.ldd : D, T, 0}, b{cw ? p.w : W, cw ? p.ldd : D, V, 0};
-    POSEIDON_TRY((product<E, true, true, LOGITS>(a, b, ONE, o, T, V, round_up(D, 16 / sizeof(E)), 1, s)));
-    const dim3 grid(static_cast<unsigned>(ceil_div(p.ldg, FACTOR_COLS)), static_cast<unsigned>(std::min<int64_t>(T, 32768)));
-    factor_kernel<E><<<grid, THREADS, 0, s>>>(p.part, p.nparts, p.target_logit, target, dloss, T, V, loss, U,
-                                              static_cast<E*>(p.g), p.ldg, p.target_rest);
-    POSEIDON_TRY(hipGetLastError());
-    return input_gradient(p, Operand{p.g, p.ldg, T, 0}, b, static_cast<const E*>(b.p), target, T, V, D, 0, V, dX, s);
+    const Plan p = make_plan<I, E>(POSEIDON_XENT_FACTOR, X, W, T, V, D, ws);
+    Operand x, w;
+    POSEIDON_TRY((operands<I, E>(p, X, W, nullptr, T, V, D, x, w, s)));
+    if (p.few) {
+        POSEIDON_TRY(row_logits<E>(p, x, w, T, V, D, s));
+        POSEIDON_TRY((rows_done<E, true>(p, target, dloss, T, V, loss, nullptr, U, s)));
+    } else {
+        // The payload is G whole: the logits go to it, and G replaces them.
+        Out o{};
+        o.part = p.part;
+        o.nparts = p.nparts;
+        o.target_logit = p.target_logit;
+        o.target = target;
+        o.c = U;
+        o.ldc = V;
+        POSEIDON_TRY((product<E, true, true, LOGITS>(p.logits, x, w, p.logits_parts, o, T, V, whole_chunks<E>(D), s)));
+        loss_kernel<<<static_cast<unsigned>(ceil_div(T, THREADS / 64)), THREADS, 0, s>>>(
+            p.part, p.nparts, p.target_logit, target, T, V, loss, p.lse);
+        POSEIDON_TRY(hipGetLastError());
+        factor_kernel<E, sizeof(I) == 4 && sizeof(E) == 2 ? 3 : 1>
+            <<<grid_for(ceil_div(T * (p.ldg / GROUP), THREADS)), THREADS, 0, s>>>(
+                p.lse, target, dloss, T, V, U, static_cast<E*>(p.g), p.ldg, p.target_rest);
+        POSEIDON_TRY(hipGetLastError());
+    }
+    return input_gradient<I, E>(p, Operand{p.g, p.ldg, T, T * p.ldg}, w, w, target, T, V, D, 0, V, dX, s);
+}
+
+// fp32 by six bf16 products at 1250 TFLOP/s (the splitting of X and W, ten
+// bytes a value, at 4 TB/s) or as it is at 125.
+bool in_parts(int op, int64_t T, int64_t V, int64_t D)
+{
+    const double flops = 2.0 * static_cast<double>(T) * static_cast<double>(V) * static_cast<double>(D) *
+                         (op == POSEIDON_XENT_FORWARD ? 1 : op == POSEIDON_XENT_BACKWARD ? 3 : 2);
+    const double bytes = 10.0 * static_cast<double>(T + V) * static_cast<double>(D);
+    return T > FEW_ROWS && flops * (6 / 1.25e15) + bytes / 4e12 < flops / 1.25e14;
 }
 
 }  // namespace
 
 int64_t xent_workspace(int32_t op, const void* X, const void* W, int64_t T, int64_t V, int64_t D, int32_t dtype)
 {
-    return dtype == POSEIDON_BF16
-               ? make_plan<__bf16>(op, T, V, D, needs_copy<__bf16>(X, D), needs_copy<__bf16>(W, D), nullptr).bytes
-               : make_plan<float>(op, T, V, D, needs_copy<float>(X, D), needs_copy<float>(W, D), nullptr).bytes;
+    if (dtype == POSEIDON_BF16)
+        return make_plan<__bf16, __bf16>(op, X, W, T, V, D, nullptr).bytes;
+    return in_parts(op, T, V, D) ? make_plan<float, __bf16>(op, X, W, T, V, D, nullptr).bytes
+                                 : make_plan<float, float>(op, X, W, T, V, D, nullptr).bytes;
 }
 
 hipError_t launch_xent_forward(const void* X, const void* W, const int64_t* target, int64_t T, int64_t V, int64_t D,
@@ -688,10 +998,10 @@ hipError_t launch_xent_forward(const void* X, const void* W, const int64_t* targ
 {
     char* w = static_cast<char*>(ws);
     if (dtype == POSEIDON_BF16)
-        return forward_typed(static_cast<const __bf16*>(X), static_cast<const __bf16*>(W), target, T, V, D, loss, lse,
-                             w, stream);
-    return forward_typed(static_cast<const float*>(X), static_cast<const float*>(W), target, T, V, D, loss, lse, w,
-                         stream);
+        return forward_typed<__bf16, __bf16>(static_cast<const __bf16*>(X), static_cast<const __bf16*>(W), target, T,
+                                             V, D, loss, lse, w, stream);
+    auto* f = in_parts(POSEIDON_XENT_FORWARD, T, V, D) ? forward_typed<float, __bf16> : forward_typed<float, float>;
+    return f(static_cast<const float*>(X), static_cast<const float*>(W), target, T, V, D, loss, lse, w, stream);
 }
 
 hipError_t launch_xent_backward(const void* X, const void* W, const int64_t* target, const float* lse,
@@ -700,10 +1010,11 @@ hipError_t launch_xent_backward(const void* X, const void* W, const int64_t* tar
 {
     char* w = static_cast<char*>(ws);
     if (dtype == POSEIDON_BF16)
-        return backward_typed(static_cast<const __bf16*>(X), static_cast<const __bf16*>(W), target, lse, dloss, T, V,
-                              D, static_cast<__bf16*>(dX), dW, w, stream);
-    return backward_typed(static_cast<const float*>(X), static_cast<const float*>(W), target, lse, dloss, T, V, D,
-                          static_cast<float*>(dX), dW, w, stream);
+        return backward_typed<__bf16, __bf16>(static_cast<const __bf16*>(X), static_cast<const __bf16*>(W), target,
+                                              lse, dloss, T, V, D, static_cast<__bf16*>(dX), dW, w, stream);
+    auto* f = in_parts(POSEIDON_XENT_BACKWARD, T, V, D) ? backward_typed<float, __bf16> : backward_typed<float, float>;
+    return f(static_cast<const float*>(X), static_cast<const float*>(W), target, lse, dloss, T, V, D,
+             static_cast<float*>(dX), dW, w, stream);
 }
 
 hipError_t launch_xent_factor(const void* X, const void* W, const int64_t* target, const float* dloss, int64_t T,
@@ -712,10 +1023,11 @@ hipError_t launch_xent_factor(const void* X, const void* W, const int64_t* targe
 {
     char* w = static_cast<char*>(ws);
     if (dtype == POSEIDON_BF16)
-        return factor_typed(static_cast<const __bf16*>(X), static_cast<const __bf16*>(W), target, dloss, T, V, D, loss,
-                            U, static_cast<__bf16*>(dX), w, stream);
-    return factor_typed(static_cast<const float*>(X), static_cast<const float*>(W), target, dloss, T, V, D, loss, U,
-                        static_cast<float*>(dX), w, stream);
+        return factor_typed<__bf16, __bf16>(static_cast<const __bf16*>(X), static_cast<const __bf16*>(W), target,
+                                            dloss, T, V, D, loss, U, static_cast<__bf16*>(dX), w, stream);
+    auto* f = in_parts(POSEIDON_XENT_FACTOR, T, V, D) ? factor_typed<float, __bf16> : factor_typed<float, float>;
+    return f(static_cast<const float*>(X), static_cast<const float*>(W), target, dloss, T, V, D, loss, U,
+             static_cast<float*>(dX), w, stream);
 }
 
 }  // namespace poseidon
