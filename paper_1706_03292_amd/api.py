@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 
 import torch
 
@@ -557,36 +558,54 @@ class KVStore:
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 
-def _dev(name: str, t: torch.Tensor, dtype: torch.dtype, shape=None) -> torch.Tensor:
-    """A contiguous device tensor of the given type (and shape)."""
+def _dev(name: str, t: torch.Tensor, dtype: torch.dtype, device: int, shape) -> None:
+    """Checks a contiguous tensor of the given type and shape on the device."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == device and t.shape == shape
+            and t.is_contiguous()):
+        _refuse(name, t, dtype, device, shape)
+
+
+def _refuse(name, t, dtype, device, shape):
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if not t.is_cuda:
         raise ValueError(f"{name} must be on a HIP device (no host path exists)")
+    if t.get_device() != device:
+        raise ValueError(f"tensors on different devices: {name} on {t.device}, others on cuda:{device}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    return t
+    raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
 
 
-def _typed(name: str, t: torch.Tensor) -> int:
-    """The type code of an activation or weight tensor."""
+def _typed(name: str, t: torch.Tensor) -> tuple[int, int]:
+    """The type code and the device of a call's first activation tensor."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.dtype not in _DTYPES:
         raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}")
-    _dev(name, t, t.dtype)
-    return _DTYPES[t.dtype]
+    device = t.get_device()
+    if device < 0 or not t.is_contiguous():
+        _refuse(name, t, t.dtype, device, t.shape)
+    return _DTYPES[t.dtype], device
 
 
-def _out(name: str, t, shape, dtype: torch.dtype, device) -> torch.Tensor:
-    """The caller's result tensor, checked, or a new one."""
-    if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    return _dev(name, t, dtype, shape)
+def _drops(p: float) -> bool:
+    """Whether p, rounded to 2^-16, drops anything."""
+    return p * 65536 + 0.5 >= 1.0
+
+
+def _rng(rng, p: float, device: int = 0) -> bool:
+    """Checks p and the generator's state; whether p drops anything (it needs
+    the generator then)."""
+    if not 0.0 <= p <= 1.0:
+        raise ValueError(f"p must lie in 0..1, got {p}")
+    if rng is not None:
+        _dev("rng", rng, torch.int64, device, (2,))
+    elif _drops(p):
+        raise ValueError("dropout needs rng: two int64 values (seed, offset) on the device")
+    return _drops(p)
 
 
 def _work_on(stream, device):
@@ -598,26 +617,6 @@ def _work_on(stream, device):
     if not isinstance(stream, torch.cuda.Stream):
         stream = torch.cuda.ExternalStream(_stream_handle(stream, device), device=device)
     return torch.cuda.stream(stream)
-
-
-def _drops(p: float) -> bool:
-    """Whether p, rounded to 2^-16, drops anything."""
-    return p * 65536 + 0.5 >= 1.0
-
-
-def _rng(rng, p: float):
-    """The generator's state, checked: needed when p drops anything."""
-    if not 0.0 <= p <= 1.0:
-        raise ValueError(f"p must lie in 0..1, got {p}")
-    if rng is None:
-        if _drops(p):
-            raise ValueError("dropout needs rng: two int64 values (seed, offset) on the device")
-        return None
-    return _dev("rng", rng, torch.int64, (2,))
-
-
-def _workspace(size, device) -> torch.Tensor:
-    return torch.empty(max(1, size.value), dtype=torch.uint8, device=device)
 
 
 def _rows_cols(x: torch.Tensor) -> tuple[int, int]:
@@ -633,17 +632,19 @@ def dropout(x: torch.Tensor, p: float, rng: torch.Tensor | None, residual: torch
     is dropout(dy, p, rng).  ``rng`` holds (seed, offset) as two int64 values on
     the device; the mask follows from them, the row length x.shape[-1] and an
     element's place, and is never stored."""
-    dt = _typed("x", x)
-    rng = _rng(rng, p)
+    dt, dev = _typed("x", x)
+    _rng(rng, p, dev)
     if residual is not None:
-        _dev("residual", residual, x.dtype, x.shape)
+        _dev("residual", residual, x.dtype, dev, x.shape)
+    if y is not None:
+        _dev("y", y, x.dtype, dev, x.shape)
     rows, cols = _rows_cols(x)
     with _work_on(stream, x.device):
-        y = _out("y", y, x.shape, x.dtype, x.device)
-        _same_device(x, residual, rng, y)
+        if y is None:
+            y = torch.empty_like(x)
         _uses(stream, x, residual, rng, y)
         _check("poseidon_dropout", L.lib().poseidon_dropout(
-            x.data_ptr(), _ptr(residual), rows, cols, dt, float(p), _ptr(rng), y.data_ptr(),
+            x.data_ptr(), _ptr(residual), rows, cols, dt, p, _ptr(rng), y.data_ptr(),
             _stream_handle(stream, x.device)))
     return y
 
@@ -655,24 +656,27 @@ def norm_forward(x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor, eps: 
     last dimension (poseidon_norm_forward).  Returns (y, h, mean, rstd), h, mean
     and rstd being what norm_backward needs; without residual and dropout h is
     x itself."""
-    dt = _typed("x", x)
-    rng = _rng(rng, p)
+    dt, dev = _typed("x", x)
+    drops = _rng(rng, p, dev)
     rows, cols = _rows_cols(x)
-    _dev("gamma", gamma, torch.float32, (cols,)), _dev("beta", beta, torch.float32, (cols,))
+    _dev("gamma", gamma, torch.float32, dev, (cols,))
+    _dev("beta", beta, torch.float32, dev, (cols,))
     if residual is not None:
-        _dev("residual", residual, x.dtype, x.shape)
+        _dev("residual", residual, x.dtype, dev, x.shape)
+    if y is not None:
+        _dev("y", y, x.dtype, dev, x.shape)
     with _work_on(stream, x.device):
-        y = _out("y", y, x.shape, x.dtype, x.device)
-        h = x if residual is None and not _drops(p) else torch.empty_like(x)
-        mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device)
-        _same_device(x, gamma, beta, residual, rng, y)
+        if y is None:
+            y = torch.empty_like(x)
+        h = torch.empty_like(x) if drops or residual is not None else x
+        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+        rstd = torch.empty_like(mean)
         _uses(stream, x, gamma, beta, residual, rng, y)
         _check("poseidon_norm_forward", L.lib().poseidon_norm_forward(
-            x.data_ptr(), _ptr(residual), gamma.data_ptr(), beta.data_ptr(), rows, cols, dt, float(eps), float(p),
-            _ptr(rng), None if h is x else h.data_ptr(), y.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+            x.data_ptr(), _ptr(residual), gamma.data_ptr(), beta.data_ptr(), rows, cols, dt, eps, p, _ptr(rng),
+            None if h is x else h.data_ptr(), y.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
             _stream_handle(stream, x.device)))
-    shape = x.shape[:-1]
-    return y, h, mean.view(shape), rstd.view(shape)
+    return y, h, mean, rstd
 
 
 def norm_backward(dy: torch.Tensor, h: torch.Tensor, gamma: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
@@ -683,59 +687,75 @@ def norm_backward(dy: torch.Tensor, h: torch.Tensor, gamma: torch.Tensor, mean: 
     ``dresidual``, what arrives at h by another way) and dx that of x (dh itself
     when p drops nothing).  dgamma and dbeta may be given, e.g. as this worker's
     gradient shards."""
-    dt = _typed("dy", dy)
-    rng = _rng(rng, p)
+    dt, dev = _typed("dy", dy)
+    drops = _rng(rng, p, dev)
     rows, cols = _rows_cols(dy)
-    _dev("h", h, dy.dtype, dy.shape), _dev("gamma", gamma, torch.float32, (cols,))
-    _dev("mean", mean, torch.float32, dy.shape[:-1]), _dev("rstd", rstd, torch.float32, dy.shape[:-1])
+    _dev("h", h, dy.dtype, dev, dy.shape)
+    _dev("gamma", gamma, torch.float32, dev, (cols,))
+    _dev("mean", mean, torch.float32, dev, dy.shape[:-1])
+    _dev("rstd", rstd, torch.float32, dev, dy.shape[:-1])
     if dresidual is not None:
-        _dev("dresidual", dresidual, dy.dtype, dy.shape)
-    size = ctypes.c_int64()
+        _dev("dresidual", dresidual, dy.dtype, dev, dy.shape)
+    if dgamma is not None:
+        _dev("dgamma", dgamma, torch.float32, dev, (cols,))
+    if dbeta is not None:
+        _dev("dbeta", dbeta, torch.float32, dev, (cols,))
+    lib, size = L.lib(), ctypes.c_int64()
     with _work_on(stream, dy.device):
-        _check("poseidon_norm_workspace", L.lib().poseidon_norm_workspace(rows, cols, ctypes.byref(size)))
-        dgamma = _out("dgamma", dgamma, (cols,), torch.float32, dy.device)
-        dbeta = _out("dbeta", dbeta, (cols,), torch.float32, dy.device)
+        _check("poseidon_norm_workspace", lib.poseidon_norm_workspace(rows, cols, ctypes.byref(size)))
+        if dgamma is None:
+            dgamma = torch.empty_like(gamma)
+        if dbeta is None:
+            dbeta = torch.empty_like(gamma)
         dh = torch.empty_like(dy)
-        dx = torch.empty_like(dy) if _drops(p) else dh
-        ws = _workspace(size, dy.device)
-        _same_device(dy, h, gamma, mean, rstd, dresidual, rng, dgamma, dbeta)
+        dx = torch.empty_like(dy) if drops else dh
+        ws = torch.empty(size.value, dtype=torch.uint8, device=dy.device)
         _uses(stream, dy, h, gamma, mean, rstd, dresidual, rng, dgamma, dbeta)
-        _check("poseidon_norm_backward", L.lib().poseidon_norm_backward(
+        _check("poseidon_norm_backward", lib.poseidon_norm_backward(
             dy.data_ptr(), h.data_ptr(), gamma.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _ptr(dresidual), rows,
-            cols, dt, float(p), _ptr(rng), None if dx is dh else dx.data_ptr(), dh.data_ptr(), dgamma.data_ptr(),
+            cols, dt, p, _ptr(rng), None if dx is dh else dx.data_ptr(), dh.data_ptr(), dgamma.data_ptr(),
             dbeta.data_ptr(), ws.data_ptr(), size.value, _stream_handle(stream, dy.device)))
     return dx, dh, dgamma, dbeta
 
 
 def _xent_args(X, W, target):
-    dt = _typed("X", X)
+    dt, dev = _typed("X", X)
     if X.dim() != 2:
         raise ValueError("X must be 2-D")
     T, D = X.shape
-    _dev("W", W, X.dtype)
-    if W.dim() != 2 or W.shape[1] != D:
-        raise ValueError(f"W must be V x {D}, got {tuple(W.shape)}")
-    _dev("target", target, torch.int64, (T,))
-    _same_device(X, W, target)
-    return dt, T, W.shape[0], D
+    if not isinstance(W, torch.Tensor) or W.dim() != 2:
+        raise ValueError(f"W must be V x {D}")
+    V = W.shape[0]
+    _dev("W", W, X.dtype, dev, (V, D))
+    _dev("target", target, torch.int64, dev, (T,))
+    return dt, dev, T, V, D
+
+
+@functools.lru_cache(maxsize=4096)
+def _xent_size(op, T, V, D, dt, device, x_off, w_off) -> int:
+    """poseidon_xent_workspace, which depends on the arrays' places only by
+    their offsets from 16-byte boundaries, and on the device's size."""
+    size = ctypes.c_int64()
+    _check("poseidon_xent_workspace", L.lib().poseidon_xent_workspace(
+        op, 4096 + x_off, 4096 + w_off, T, V, D, dt, ctypes.byref(size)))
+    return size.value
 
 
 def _xent_workspace(op, X, W, T, V, D, dt):
-    size = ctypes.c_int64()
-    _check("poseidon_xent_workspace", L.lib().poseidon_xent_workspace(
-        op, X.data_ptr(), W.data_ptr(), T, V, D, dt, ctypes.byref(size)))
-    return _workspace(size, X.device), size.value
+    size = _xent_size(op, T, V, D, dt, X.get_device(), X.data_ptr() & 15, W.data_ptr() & 15)
+    return torch.empty(size, dtype=torch.uint8, device=X.device), size
 
 
 def xent_forward(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, stream=None):
     """Softmax cross entropy of the logits X @ W.T against the target classes,
-    the logits never stored (poseidon_xent_forward).  X is T x D, W V x D, target
-    T int64 values; a target outside 0..V-1 marks a row without a loss.  Returns
+    the logits not kept (poseidon_xent_forward).  X is T x D, W V x D, target T
+    int64 values; a target outside 0..V-1 marks a row without a loss.  Returns
     (loss, lse), T fp32 values each."""
-    dt, T, V, D = _xent_args(X, W, target)
+    dt, dev, T, V, D = _xent_args(X, W, target)
     with _work_on(stream, X.device):
         ws, size = _xent_workspace(L.XENT_FORWARD, X, W, T, V, D, dt)
-        loss, lse = torch.empty((2, T), dtype=torch.float32, device=X.device)
+        loss = torch.empty(T, dtype=torch.float32, device=X.device)
+        lse = torch.empty_like(loss)
         _uses(stream, X, W, target)
         _check("poseidon_xent_forward", L.lib().poseidon_xent_forward(
             X.data_ptr(), W.data_ptr(), target.data_ptr(), T, V, D, dt, loss.data_ptr(), lse.data_ptr(),
@@ -748,12 +768,15 @@ def xent_backward(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, lse: t
     """Gradients of sum(dloss * loss) (poseidon_xent_backward): returns (dX, dW),
     dX in X's type and dW V x D fp32 -- it may be given, e.g. as this worker's
     gradient shard."""
-    dt, T, V, D = _xent_args(X, W, target)
-    _dev("lse", lse, torch.float32, (T,)), _dev("dloss", dloss, torch.float32, (T,))
+    dt, dev, T, V, D = _xent_args(X, W, target)
+    _dev("lse", lse, torch.float32, dev, (T,))
+    _dev("dloss", dloss, torch.float32, dev, (T,))
+    if dW is not None:
+        _dev("dW", dW, torch.float32, dev, (V, D))
     with _work_on(stream, X.device):
-        dW = _out("dW", dW, (V, D), torch.float32, X.device)
-        _same_device(X, lse, dloss, dW)
         ws, size = _xent_workspace(L.XENT_BACKWARD, X, W, T, V, D, dt)
+        if dW is None:
+            dW = torch.empty((V, D), dtype=torch.float32, device=X.device)
         dX = torch.empty_like(X)
         _uses(stream, X, W, target, lse, dloss, dW)
         _check("poseidon_xent_backward", L.lib().poseidon_xent_backward(
@@ -768,12 +791,14 @@ def xent_factor(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, dloss: t
     factors (poseidon_xent_factor): returns (loss, U, dX), U = the T x V fp32
     gradient of the logits -- the layer's factor beside V = X; it may be given,
     e.g. as this worker's rows of the factor payload."""
-    dt, T, V, D = _xent_args(X, W, target)
-    _dev("dloss", dloss, torch.float32, (T,))
+    dt, dev, T, V, D = _xent_args(X, W, target)
+    _dev("dloss", dloss, torch.float32, dev, (T,))
+    if U is not None:
+        _dev("U", U, torch.float32, dev, (T, V))
     with _work_on(stream, X.device):
-        U = _out("U", U, (T, V), torch.float32, X.device)
-        _same_device(X, dloss, U)
         ws, size = _xent_workspace(L.XENT_FACTOR, X, W, T, V, D, dt)
+        if U is None:
+            U = torch.empty((T, V), dtype=torch.float32, device=X.device)
         dX = torch.empty_like(X)
         loss = torch.empty(T, dtype=torch.float32, device=X.device)
         _uses(stream, X, W, target, dloss, U)

@@ -111,14 +111,14 @@ struct Panel {
     static __device__ __forceinline__ int swz_r(int k)
     {
         if constexpr (SZ == 2) {
-            if constexpr (PER_ROW >= 16)   // rows of 256 bytes and more: eight pairs
+            if constexpr (PER_ROW % 16 == 0)   // rows of a multiple of 256 bytes: eight pairs
                 return (((k & 3) | (((k >> 3) & 1) << 2)) << 1);
-            else if constexpr (PER_ROW == 8)   // 128 bytes: two rows span the banks
+            else if constexpr (PER_ROW % 8 == 0)   // of 128: the row's parity is half of the bank, four pairs
                 return ((((k >> 1) & 1) | (((k >> 3) & 1) << 1)) << 1);
             else
                 return 0;
         } else {
-            if constexpr (PER_ROW >= 16)
+            if constexpr (PER_ROW % 16 == 0)
                 return ((k >> 2) & 3) << 2;
             else
                 return 0;

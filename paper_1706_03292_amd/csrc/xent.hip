@@ -325,20 +325,22 @@ __device__ __forceinline__ void finish(acc4 (&acc)[T::TM][T::TN], const Out& o, 
     }
 }
 
-// M x N tiles over k split gridDim.y ways (k_split values each, a multiple of
+// Rows m_first to M in tiles over k split gridDim.y ways (k_split values each, a multiple of
 // the step).
 template <typename T, Use USE>
-__global__ __launch_bounds__(T::NT, 2) void product_kernel(Operand a, Operand b, Parts parts, Out o, int64_t M, int64_t N,
-                                                        int64_t K, int64_t k_split, int64_t tiles_m, int64_t tiles_n,
-                                                        int group)
+__global__ __launch_bounds__(T::NT, 2) void product_kernel(Operand a, Operand b, Parts parts, Out o,
+                                                           int64_t m_first, int64_t M, int64_t N, int64_t K,
+                                                           int64_t k_split, int64_t tiles_m, int64_t tiles_n,
+                                                           int group)
 {
     int64_t tm, tn;
     tile_of(blockIdx.x, tiles_m, tiles_n, group, tm, tn);
     const int64_t k0 = blockIdx.y * k_split;
+    const int64_t m0 = m_first + tm * T::BM, n0 = tn * T::BN;
     T tile;
     acc4 acc[T::TM][T::TN];
-    tile.run(acc, a, b, parts, tm * T::BM, tn * T::BN, k0, K - k0 < k_split ? K - k0 : k_split);
-    finish<T, USE>(acc, o, tm * T::BM, tn * T::BN, tn, M, N, static_cast<int>(blockIdx.y));
+    tile.run(acc, a, b, parts, m0, n0, k0, K - k0 < k_split ? K - k0 : k_split);
+    finish<T, USE>(acc, o, m0, n0, tn, M, N, static_cast<int>(blockIdx.y));
 }
 
 // ---------------------------------------------------------------------------
@@ -354,9 +356,11 @@ __device__ __forceinline__ Run wave_join(Run r)
     return r;
 }
 
-// One wave a row: lse and loss from the tiles' partial runs, each lane taking
+// One wave a row: lse and loss from the tiles' partial runs (main_count of them
+// for the first main_rows rows, rest_count for the others), each lane taking
 // every 64th, then joined across the wave in a fixed order.
 __global__ __launch_bounds__(THREADS) void loss_kernel(const Run* __restrict__ part, int64_t nparts,
+                                                       int64_t main_rows, int64_t main_count, int64_t rest_count,
                                                        const float* __restrict__ target_logit,
                                                        const int64_t* __restrict__ target, int64_t T, int64_t V,
                                                        float* __restrict__ loss, float* __restrict__ lse_out)
@@ -366,7 +370,8 @@ __global__ __launch_bounds__(THREADS) void loss_kernel(const Run* __restrict__ p
     if (row >= T)
         return;
     Run r{-INFINITY, 0.f};
-    for (int64_t p = lane; p < nparts; p += 64)
+    const int64_t count = row < main_rows ? main_count : rest_count;
+    for (int64_t p = lane; p < count; p += 64)
         r = join(r, part[row * nparts + p]);
     r = wave_join(r);
     if (lane == 0) {
@@ -378,13 +383,25 @@ __global__ __launch_bounds__(THREADS) void loss_kernel(const Run* __restrict__ p
 
 // One workgroup a row, where the rows are few: the row's logits are the sums of
 // the product's splits of k; their loss, lse and (given U) G, as U and as the
-// operand of dX (bf16 or fp32, ldg apart, zeros past V).  The summed logits
-// stay in registers where the row has at most ROW_HELD, else they are written
-// to the first split and read again.
-constexpr int ROW_THREADS = 1024, ROW_EACH = 32;
-constexpr int64_t ROW_HELD = int64_t(ROW_THREADS) * ROW_EACH;
+// operand of dX (bf16 or fp32, ldg apart, zeros past V).  A thread holds EACH
+// groups of four neighbours; rows longer than 32768 go through memory: the
+// sums replace the first split's and are read again.  What bounds it is one
+// CU's reading of its row: all loads of a split are in flight together.
+constexpr int ROW_THREADS = 1024;
 
-template <typename G, bool HELD, bool FACTOR>
+// n values at p, past them -inf (logits) or 0.
+__device__ __forceinline__ acc4 get4(const float* p, int64_t n, float past)
+{
+    if (n >= 4)
+        return *reinterpret_cast<const f4a*>(p);
+    acc4 v;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+        v[r] = r < n ? p[r] : past;
+    return v;
+}
+
+template <typename G, int EACH, bool FACTOR>
 __global__ __launch_bounds__(ROW_THREADS) void row_kernel(float* __restrict__ logits, int splits, int64_t stride,
                                                           const int64_t* __restrict__ target,
                                                           const float* __restrict__ dloss, int64_t V,
@@ -392,91 +409,102 @@ __global__ __launch_bounds__(ROW_THREADS) void row_kernel(float* __restrict__ lo
                                                           float* __restrict__ U, G* __restrict__ g, int64_t ldg,
                                                           float* __restrict__ target_rest)
 {
+    constexpr bool HELD = EACH > 0;
     __shared__ Run runs[ROW_THREADS / 64];
     const int64_t row = blockIdx.x;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     float* s = logits + row * V;
     const int64_t t = target[row];
     const bool has = counts(t, V);
-    float held[HELD ? ROW_EACH : 1];
+    const float d = FACTOR && has ? dloss[row] : 0.f;
+    acc4 held[HELD ? EACH : 1];
     Run r{-INFINITY, 0.f};
-    auto summed = [&](int64_t v) {
-        float x = s[v];
-        for (int z = 1; z < splits; ++z)
-            x += s[z * stride + v];
-        return x;
+    auto place = [&](int e) { return 4 * (threadIdx.x + static_cast<int64_t>(e) * ROW_THREADS); };
+    auto add = [&](acc4& x) {
+        float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) * LOG2E;
+        const float from = top == -INFINITY ? 0.f : top;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            sum += __builtin_amdgcn_exp2f(fmaf(x[i], LOG2E, -from));   // past V: 0
+        r = join(r, Run{top, sum});
     };
     if constexpr (HELD) {
 #pragma unroll
-        for (int e = 0; e < ROW_EACH; ++e) {
-            const int64_t v = threadIdx.x + static_cast<int64_t>(e) * ROW_THREADS;
-            held[e] = v < V ? summed(v) : -INFINITY;
+        for (int e = 0; e < EACH; ++e)
+            held[e] = get4(s + place(e), V - place(e), -INFINITY);
+#pragma unroll 2
+        for (int z = 1; z < splits; ++z) {
+            acc4 x[EACH];
+#pragma unroll
+            for (int e = 0; e < EACH; ++e)
+                x[e] = get4(s + z * stride + place(e), V - place(e), 0.f);
+#pragma unroll
+            for (int e = 0; e < EACH; ++e)
+                held[e] += x[e];
         }
 #pragma unroll
-        for (int e = 0; e < ROW_EACH; ++e)
-            r.m = fmaxf(r.m, held[e]);
-        r.m *= LOG2E;
-        const float from = r.m == -INFINITY ? 0.f : r.m;
-#pragma unroll
-        for (int e = 0; e < ROW_EACH; ++e)
-            r.s += __builtin_amdgcn_exp2f(fmaf(held[e], LOG2E, -from));   // past V: 0
+        for (int e = 0; e < EACH; ++e)
+            add(held[e]);
     } else {
-        for (int64_t v = threadIdx.x; v < V; v += ROW_THREADS) {
-            const float x = summed(v);
-            s[v] = x;
-            const float y = x * LOG2E;
-            r = join(r, Run{y, x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(x, LOG2E, -y))});
+        for (int64_t v = place(0); v < V; v += 4 * ROW_THREADS) {
+            acc4 x = get4(s + v, V - v, -INFINITY);
+            for (int z = 1; z < splits; ++z)
+                x += get4(s + z * stride + v, V - v, 0.f);
+            put4(s + v, x, static_cast<int>(V - v < 4 ? V - v : 4));
+            add(x);
         }
     }
     r = wave_join(r);
     if (lane == 0)
         runs[w] = r;
-    __syncthreads();   // and the summed logits are written
-    r = runs[0];
-#pragma unroll
-    for (int i = 1; i < ROW_THREADS / 64; ++i)
-        r = join(r, runs[i]);
+    __syncthreads();
+    r = lane < ROW_THREADS / 64 ? runs[lane] : Run{-INFINITY, 0.f};
+    r = wave_join(r);
     const float lse = lse_of(r);
-    float hit = 0.f;   // the target's logit, where this thread has it
-    const bool mine = has && t % ROW_THREADS == threadIdx.x;
+    if (threadIdx.x == 0) {
+        if (lse_out)
+            lse_out[row] = lse;
+        if (!has)
+            loss[row] = 0.f;
+    }
+    const float from = has ? lse * LOG2E : 0.f;
+    const float rest = fmaf(lse, LOG2E, -from) + lse * LOG2E_REST;
+    const float scale = has ? fmaf(d, -rest * LN2, d) : 0.f;
+    auto done = [&](int64_t v, acc4 x) {
+        const bool hit = has && t >= v && t < v + 4;
+        if (hit) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (t == v + i)
+                    loss[row] = lse - x[i];
+        }
+        if constexpr (FACTOR) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                x[i] = has && v + i < V ? __builtin_amdgcn_exp2f(fmaf(x[i], LOG2E, -from)) * scale : 0.f;
+                if (hit && t == v + i) {
+                    x[i] -= d;
+                    target_rest[row] = x[i] - static_cast<float>(static_cast<G>(x[i]));
+                }
+            }
+            if (v < V)
+                put4(U + row * V + v, x, static_cast<int>(V - v < 4 ? V - v : 4));
+            if (v < ldg) {   // ldg: a multiple of eight
+                if constexpr (sizeof(G) == 2)
+                    *reinterpret_cast<b4*>(g + row * ldg + v) = __builtin_convertvector(x, b4);
+                else
+                    *reinterpret_cast<acc4*>(g + row * ldg + v) = x;
+            }
+        }
+    };
     if constexpr (HELD) {
 #pragma unroll
-        for (int e = 0; e < ROW_EACH; ++e)
-            if (mine && t / ROW_THREADS == e)
-                hit = held[e];
-    } else if (mine) {
-        hit = s[t];
-    }
-    if (mine || (!has && threadIdx.x == 0))
-        loss[row] = has ? lse - hit : 0.f;
-    if (lse_out && threadIdx.x == 0)
-        lse_out[row] = lse;
-    if constexpr (FACTOR) {
-        const float d = has ? dloss[row] : 0.f;
-        const float from = has ? lse * LOG2E : 0.f;
-        const float rest = fmaf(lse, LOG2E, -from) + lse * LOG2E_REST;
-        const float scale = has ? fmaf(d, -rest * LN2, d) : 0.f;
-        auto put = [&](int64_t v, float x) {
-            if (v < V) {
-                x = has ? __builtin_amdgcn_exp2f(fmaf(x, LOG2E, -from)) * scale : 0.f;
-                if (has && v == t) {
-                    x -= d;
-                    target_rest[row] = x - static_cast<float>(static_cast<G>(x));
-                }
-                U[row * V + v] = x;
-                g[row * ldg + v] = static_cast<G>(x);
-            } else if (v < ldg) {
-                g[row * ldg + v] = static_cast<G>(0.f);
-            }
-        };
-        if constexpr (HELD) {
-#pragma unroll
-            for (int e = 0; e < ROW_EACH; ++e)
-                put(threadIdx.x + static_cast<int64_t>(e) * ROW_THREADS, held[e]);
-        } else {
-            for (int64_t v = threadIdx.x; v < ldg; v += ROW_THREADS)
-                put(v, v < V ? s[v] : 0.f);
-        }
+        for (int e = 0; e < EACH; ++e)
+            done(place(e), held[e]);
+    } else {
+        for (int64_t v = place(0); v < V || (FACTOR && v < ldg); v += 4 * ROW_THREADS)
+            done(v, v < V ? get4(s + v, V - v, -INFINITY) : acc4{0.f, 0.f, 0.f, 0.f});
     }
 }
 
@@ -584,82 +612,161 @@ struct Arena {
     }
 };
 
-// Tile shapes: 256 x 256 (one workgroup a CU), 128 x 128 (two), and 32 x 64
-// (three) for few rows or few tiles.
-enum ShapeKind { THIN, SQUARE, LARGE };
+// Tile shapes: rows x columns of a workgroup, of a wave, stages.  All take 128
+// bytes of k a step.  THIN is for 32 rows or fewer; of the others the larger
+// read less per product and the smaller fill the GPU with fewer tiles.
+enum ShapeKind { THIN, SMALL, HALF, SQUARE, TALL, LARGE };
 
 template <typename E, bool AK, bool BK>
 using Thin = Tile<E, AK, BK, 32, 64, 32, 16, 4, 2>;
 template <typename E, bool AK, bool BK>
-using Square = Tile<E, AK, BK, 128, 128, 64, 64, 2, 2, false>;
+using Small = Tile<E, AK, BK, 64, 64, 32, 32, 3, 2>;
+template <typename E, bool AK, bool BK>
+using Half = Tile<E, AK, BK, 64, 128, 64, 32, 3, 2>;
+template <typename E, bool AK, bool BK>
+using Square = Tile<E, AK, BK, 128, 128, 64, 64, 2, 2>;
+template <typename E, bool AK, bool BK>
+using Tall = Tile<E, AK, BK, 256, 192, 128, 48, 2, 2>;
 template <typename E, bool AK, bool BK, bool SPREAD = false>
 using Large = Tile<E, AK, BK, 256, 256, 128, 64, 2, 2, SPREAD>;
 
-// What a shape costs, as measured: microseconds of a step of 128 bytes of k
-// with the CU full, and of a tile's start and end; workgroups a CU runs.
+// What a shape costs, as measured (products over K = 4096, 512 and 64 on 256, 512
+// and 768 tiles): microseconds of a step with one, two, three workgroups on a
+// CU, bf16 and fp32, and of a tile's start; a CU writes 24 KB of results per
+// microsecond.
 struct Shape {
-    int64_t bm, bn, waves_n, per_cu;
-    double step_us[2], tile_us;   // step: bf16, fp32
+    int bm, bn, waves_n, per_cu;
+    double step_us[2][3], tile_us;
 };
 constexpr Shape SHAPES[] = {
-    {32, 64, 4, 3, {0.50, 0.65}, 4.0},
-    {128, 128, 2, 2, {1.05, 4.3}, 6.0},
-    {256, 256, 4, 1, {1.55, 0.0}, 9.0},
+    {32, 64, 4, 3, {{0.29, 0.46, 0.66}, {0.50, 0.74, 1.02}}, 3.5},
+    {64, 64, 2, 3, {{0.30, 0.42, 0.58}, {0.65, 1.09, 1.56}}, 4.0},
+    {64, 128, 4, 2, {{0.42, 0.63, 0.}, {1.12, 2.03, 0.}}, 4.5},
+    {128, 128, 2, 2, {{0.78, 1.00, 0.}, {2.17, 3.96, 0.}}, 5.0},
+    {256, 192, 4, 1, {{1.25, 0., 0.}, {0., 0., 0.}}, 6.0},
+    {256, 256, 4, 1, {{1.57, 0., 0.}, {0., 0., 0.}}, 6.0},
 };
 
+// A value's end in a tile, in bytes written or the like: G in bf16 parts counts
+// its arithmetic too.
+template <typename E, Use USE>
+constexpr double OUT_BYTES = USE == STATS ? 0.5 : USE == GRAD && sizeof(E) == 2 ? 8.0 : 4.0;
+
+// How a product of M rows is computed: the first `rows` of them in tiles of
+// `kind`, a rest that would leave most of a tile empty in tiles of `rest`; k
+// split `splits` ways, whose sums a kernel of their own adds.
 struct Choice {
     ShapeKind kind;
     int64_t splits;
     double us;
+    int64_t rows;
+    ShapeKind rest;
 };
 
-// The shape, and the ways to split k (whose sums are then added by a kernel of
-// their own), that finish M x N tiles over K values of k first: whole rounds of
-// workgroups over the GPU, and the splits' sums at 4 TB/s.
-template <typename E>
+// Whole rounds of workgroups over the GPU and a last one that is not full.
+inline double tiles_us(const Shape& s, int type, int64_t M, int64_t N, double steps, int z, double out_bytes)
+{
+    const int cus = device_cu_count();
+    const int64_t tiles = ceil_div(M, s.bm) * ceil_div(N, s.bn) * z;
+    const int64_t full = tiles / (s.per_cu * cus);
+    const int over = static_cast<int>(tiles - full * (s.per_cu * cus));
+    const double out = out_bytes * s.bm * s.bn / 24e3;
+    double us = static_cast<double>(full) * (steps * s.step_us[type][s.per_cu - 1] + s.tile_us + s.per_cu * out);
+    if (over > 0) {
+        const int n = (over - 1) / cus;
+        us += steps * s.step_us[type][n] + s.tile_us + (n + 1) * out;
+    }
+    return us;
+}
+
+// The choice that finishes M x N values over K of k first, by these estimates;
+// never less than reading both operands takes.
+template <typename E, Use USE>
 Choice choose(int64_t M, int64_t N, int64_t K, int count, bool may_split)
 {
-    const int64_t steps = ceil_div(std::max<int64_t>(K, 1), 128 / static_cast<int64_t>(sizeof(E))) * count;
+    constexpr int TYPE = sizeof(E) / 4;
+    constexpr double OUT = OUT_BYTES<E, USE>;
+    const int64_t steps = ceil_div(std::max<int64_t>(K, 1), 128 / static_cast<int64_t>(sizeof(E)));
     const int64_t cus = device_cu_count();
-    Choice best{SQUARE, 1, 1e30};
-    for (int k = THIN; k <= LARGE; ++k) {
-        if (k == LARGE && sizeof(E) == 4)
-            continue;
+    const double reading = static_cast<double>((M + N) * K) * sizeof(E) / 4.8e6;
+    const double sums = 4.0 * static_cast<double>(M * N) / 4e6;   // written or read once, at 4 TB/s
+    Choice best{SMALL, 1, 1e30, M, SMALL};
+    for (int k = M <= 32 ? THIN : SMALL; k <= LARGE; ++k) {
         const Shape& s = SHAPES[k];
-        const int64_t tiles = ceil_div(M, s.bm) * ceil_div(N, s.bn);
-        const int64_t most = may_split ? std::max<int64_t>(1, std::min<int64_t>(32, steps / count / 4)) : 1;
-        for (int64_t z = 1; z <= most; ++z) {
-            const double rounds = static_cast<double>(ceil_div(tiles * z, s.per_cu * cus));
-            const double us = rounds * (static_cast<double>(ceil_div(steps, z)) * s.step_us[sizeof(E) / 4] + s.tile_us) +
-                              (z > 1 ? 3.0 + 8.0 * static_cast<double>(z * M * N) / 4e6 : 0.0);
+        if (s.step_us[TYPE][0] == 0.0)
+            continue;
+        const int64_t tiles = std::max<int64_t>(ceil_div(M, s.bm) * ceil_div(N, s.bn), 1), slots = s.per_cu * cus;
+        const int64_t most = may_split ? std::max<int64_t>(1, std::min<int64_t>(32, steps / 4)) : 1;
+        // Splits worth a look: none, and those that come to whole rounds.
+        for (int round = 0; round <= 4; ++round) {
+            const int z = round == 0 ? 1 : static_cast<int>(std::min(most, round * slots / tiles));
+            if (z < 1 || (round > 0 && z == 1))
+                continue;
+            const double each = static_cast<double>((steps + z - 1) / z * count);
+            // The splits' sums are written (once is counted), read and written, and take a launch.
+            const double joined = z > 1 ? 5.0 + (z + 1) * sums : 0.0;
+            const double us = std::max(tiles_us(s, TYPE, M, N, each, z, OUT), reading) + joined;
             if (us < best.us)
-                best = Choice{static_cast<ShapeKind>(k), z, us};
+                best = Choice{static_cast<ShapeKind>(k), z, us, M, SMALL};
+            const int64_t over = M % s.bm;
+            if (k < SQUARE || over == 0 || over > s.bm / 2 || M < s.bm)
+                continue;
+            const double main = tiles_us(s, TYPE, M - over, N, each, z, OUT);
+            for (int r = over <= 32 ? THIN : SMALL; r <= HALF && main + joined < best.us; ++r) {
+                const double both = main + 2.0 + tiles_us(SHAPES[r], TYPE, over, N, each, z, OUT);
+                if (std::max(both, reading) + joined < best.us)
+                    best = Choice{static_cast<ShapeKind>(k), z, std::max(both, reading) + joined, M - over,
+                                  static_cast<ShapeKind>(r)};
+            }
         }
     }
     return best;
 }
 
 template <typename T, Use USE>
-hipError_t launch_product(const Operand& a, const Operand& b, const Parts& p, const Out& o, int64_t M, int64_t N,
-                          int64_t K, int64_t splits, hipStream_t s)
+hipError_t launch_product(const Operand& a, const Operand& b, const Parts& p, const Out& o, int64_t m_first,
+                          int64_t M, int64_t N, int64_t K, int64_t splits, hipStream_t s)
 {
-    const int64_t tm = ceil_div(M, T::BM), tn = ceil_div(N, T::BN);
+    const int64_t tm = ceil_div(M - m_first, T::BM), tn = ceil_div(N, T::BN);
     const int64_t k_split = round_up(ceil_div(std::max<int64_t>(K, 1), splits), T::STEP);
     product_kernel<T, USE><<<dim3(static_cast<unsigned>(tm * tn), static_cast<unsigned>(splits)), T::NT, 0, s>>>(
-        a, b, p, o, M, N, K, k_split, tm, tn, 1024 / T::BM);
+        a, b, p, o, m_first, M, N, K, k_split, tm, tn, 1024 / T::BM);
     return hipGetLastError();
+}
+
+template <typename E, bool AK, bool BK, Use USE>
+hipError_t product_rows(ShapeKind kind, const Operand& a, const Operand& b, const Parts& p, const Out& o,
+                        int64_t m_first, int64_t M, int64_t N, int64_t K, int64_t splits, hipStream_t s)
+{
+    switch (kind) {
+    case THIN:
+        return launch_product<Thin<E, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s);
+    case SMALL:
+        return launch_product<Small<E, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s);
+    case HALF:
+        return launch_product<Half<E, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s);
+    case SQUARE:
+        return launch_product<Square<E, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s);
+    case TALL:
+        if constexpr (sizeof(E) == 2)
+            return launch_product<Tall<E, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s);
+        break;
+    case LARGE:
+        if constexpr (sizeof(E) == 2)
+            return launch_product<Large<E, AK, BK, USE == GRAD>, USE>(a, b, p, o, m_first, M, N, K, splits, s);
+        break;
+    }
+    return hipErrorInvalidValue;
 }
 
 template <typename E, bool AK, bool BK, Use USE>
 hipError_t product(const Choice& c, const Operand& a, const Operand& b, const Parts& p, const Out& o, int64_t M,
                    int64_t N, int64_t K, hipStream_t s)
 {
-    if (c.kind == THIN)
-        return launch_product<Thin<E, AK, BK>, USE>(a, b, p, o, M, N, K, c.splits, s);
-    if constexpr (sizeof(E) == 2)
-        if (c.kind == LARGE)
-            return launch_product<Large<E, AK, BK, USE == GRAD>, USE>(a, b, p, o, M, N, K, c.splits, s);
-    return launch_product<Square<E, AK, BK>, USE>(a, b, p, o, M, N, K, c.splits, s);
+    const hipError_t rc = product_rows<E, AK, BK, USE>(c.kind, a, b, p, o, 0, c.rows, N, K, c.splits, s);
+    if (rc != hipSuccess || c.rows == M)
+        return rc;
+    return product_rows<E, AK, BK, USE>(c.rest, a, b, p, o, c.rows, M, N, K, c.splits, s);
 }
 
 // Products of parts, four bits each (A's, then B's): one; three of A with one
@@ -702,13 +809,23 @@ hipError_t lay_out(const I* x, int64_t rows, int64_t D, int64_t ldo, const int64
 constexpr int64_t FEW_ROWS = 32;
 constexpr int64_t PIECE_BYTES = int64_t(512) << 20;   // of G at a time
 
+// Runs that a row of N columns leaves, one a wave.
+int64_t column_blocks(ShapeKind kind, int64_t N) { return ceil_div(N, SHAPES[kind].bn) * SHAPES[kind].waves_n; }
+
+// How the three products of one piece are computed.
+struct Pieces {
+    Choice logits{}, dx{}, dw{};
+    double us() const { return logits.us + dx.us + dw.us; }
+};
+
 struct Plan {
     bool few = false, own_x = false, own_w = false;
     int64_t ldd = 0;   // row length of what is laid out
     void* x = nullptr;
     void* w = nullptr;
     Parts logits_parts = ONE, dx_parts = ONE, dw_parts = ONE;
-    Choice logits{}, dx_choice{}, dw_choice{};
+    Choice logits{};      // forward and factor form
+    Pieces full, last;    // backward: of the full pieces and the last one
     float* row_logits = nullptr;   // few rows: splits x T x V
     Run* part = nullptr;           // many: a run per row and column block
     int64_t nparts = 0;
@@ -721,6 +838,14 @@ struct Plan {
     float* dw = nullptr;
     int64_t bytes = 0;
 };
+
+template <typename E>
+Pieces pieces(const Plan& p, int64_t T, int64_t rows, int64_t D)
+{
+    return Pieces{choose<E, GRAD>(T, rows, D, p.logits_parts.count, false),
+                  choose<E, STORE>(T, D, rows, p.dx_parts.count, true),
+                  choose<E, STORE>(rows, D, T, p.dw_parts.count, true)};
+}
 
 template <typename I, typename E>
 Plan make_plan(int op, const void* X, const void* W, int64_t T, int64_t V, int64_t D, char* base)
@@ -741,12 +866,15 @@ Plan make_plan(int op, const void* X, const void* W, int64_t T, int64_t V, int64
     else if (SZ == 2)
         p.dw_parts = THREE_A;
     p.few = op != POSEIDON_XENT_BACKWARD && T <= FEW_ROWS;
-    p.logits = choose<E>(T, V, D, p.logits_parts.count, p.few);
+    p.logits = p.few                         ? choose<E, STORE>(T, V, D, p.logits_parts.count, true)
+               : op == POSEIDON_XENT_FACTOR ? choose<E, LOGITS>(T, V, D, p.logits_parts.count, false)
+                                            : choose<E, STATS>(T, V, D, p.logits_parts.count, false);
     if (p.few) {
         p.row_logits = static_cast<float*>(a.take(p.logits.splits * T * V * 4));
     } else if (op != POSEIDON_XENT_BACKWARD) {
-        const Shape& s = SHAPES[p.logits.kind];
-        p.nparts = ceil_div(V, s.bn) * s.waves_n;
+        p.nparts = column_blocks(p.logits.kind, V);
+        if (p.logits.rows < T)
+            p.nparts = std::max(p.nparts, column_blocks(p.logits.rest, V));
         p.part = static_cast<Run*>(a.take(T * p.nparts * static_cast<int64_t>(sizeof(Run))));
         p.target_logit = static_cast<float*>(a.take(T * 4));
         p.lse = static_cast<float*>(a.take(T * 4));
@@ -758,36 +886,45 @@ Plan make_plan(int op, const void* X, const void* W, int64_t T, int64_t V, int64
     // G: fp32, or in bf16 parts (for a factor's bf16 dX one of them).
     const int64_t g_value = SZ == 4 ? 4 : op == POSEIDON_XENT_FACTOR && !SPLIT ? 2 : 6;
     p.piece = round_up(V, GROUP);
-    p.dx_choice = choose<E>(T, D, V, p.dx_parts.count, true);
+    p.full.dx = choose<E, STORE>(T, D, V, p.dx_parts.count, true);
     if (op == POSEIDON_XENT_BACKWARD) {
-        // Pieces of the vocabulary, as equal as tiles allow: the number of them
-        // (from what the budget asks for) that is cheapest by the choices' own
-        // estimates.
+        // Pieces of the vocabulary within the budget: equal ones, or as many
+        // classes as make whole rounds of dW's largest tiles and a rest;
+        // whichever the choices' estimates make cheapest.
         const int64_t most = std::max<int64_t>(PIECE_BYTES / g_value / std::max<int64_t>(T, 1) / 256, 1) * 256;
-        const int64_t fewest = ceil_div(V, most);
+        const int64_t fewest = ceil_div(V, most), across = ceil_div(D, 256);
+        const int64_t rounds = most / 256 * across / device_cu_count();
         double best = 1e30;
-        for (int64_t n = fewest; n < fewest + 4; ++n) {
-            const int64_t piece = n == 1 ? round_up(V, GROUP) : round_up(ceil_div(V, n), 256);
-            const int64_t count = ceil_div(V, piece), rows = std::min(piece, V);
-            const Choice l = choose<E>(T, rows, D, p.logits_parts.count, false);
-            const Choice x = choose<E>(T, D, rows, p.dx_parts.count, true);
-            const Choice w = choose<E>(rows, D, T, p.dw_parts.count, true);
-            if (static_cast<double>(count) * (l.us + x.us + w.us) < best) {
-                best = static_cast<double>(count) * (l.us + x.us + w.us);
+        for (int i = 0; i < (fewest > 1 ? 6 : 1); ++i) {
+            const int64_t even = round_up(ceil_div(V, fewest + i), 256);
+            const int64_t piece = fewest == 1 ? round_up(V, GROUP)
+                                  : i < 4     ? even
+                                              : (rounds - (i - 4)) * device_cu_count() / across * 256;
+            if (piece < 256 && fewest > 1)
+                continue;
+            const int64_t rows = std::min(piece, V), over = V % rows;
+            const Pieces full = pieces<E>(p, T, rows, D), last = over ? pieces<E>(p, T, over, D) : Pieces{};
+            const double us = static_cast<double>(V / rows) * full.us() + last.us();
+            if (us < best) {
+                best = us;
                 p.piece = piece;
-                p.logits = l;
-                p.dx_choice = x;
-                p.dw_choice = w;
+                p.full = full;
+                p.last = over ? last : full;
             }
         }
-        if (p.dw_choice.splits > 1)
-            p.dw = static_cast<float*>(a.take(p.dw_choice.splits * std::min(p.piece, V) * D * 4));
+        // The rest adds to the full pieces' sums: to no more of them than there are.
+        p.last.dx.splits = std::min(p.last.dx.splits, p.full.dx.splits);
+        const int64_t rows = std::min(p.piece, V);
+        const int64_t dw_sums = std::max(p.full.dw.splits > 1 ? p.full.dw.splits * rows : 0,
+                                         p.last.dw.splits > 1 ? p.last.dw.splits * (V % rows) : 0);
+        if (dw_sums > 0)
+            p.dw = static_cast<float*>(a.take(dw_sums * D * 4));
     }
     p.ldg = p.piece;
     p.g = a.take(T * p.ldg * g_value);
     p.target_rest = static_cast<float*>(a.take(T * 4));
-    if (p.dx_choice.splits > 1 || (p.piece < V && sizeof(I) == 2))
-        p.dx = static_cast<float*>(a.take(p.dx_choice.splits * T * D * 4));
+    if (p.full.dx.splits > 1 || (p.piece < V && sizeof(I) == 2))
+        p.dx = static_cast<float*>(a.take(p.full.dx.splits * T * D * 4));
     p.bytes = a.at;
     return p;
 }
@@ -837,10 +974,24 @@ template <typename G, bool FACTOR>
 hipError_t rows_done(const Plan& p, const int64_t* target, const float* dloss, int64_t T, int64_t V, float* loss,
                      float* lse, float* U, hipStream_t s)
 {
-    auto* k = round_up(V, GROUP) <= ROW_HELD ? row_kernel<G, true, FACTOR> : row_kernel<G, false, FACTOR>;
+    const int64_t each = ceil_div(round_up(V, GROUP), 4 * ROW_THREADS);
+    auto* k = each <= 1   ? row_kernel<G, 1, FACTOR>
+              : each <= 2 ? row_kernel<G, 2, FACTOR>
+              : each <= 4 ? row_kernel<G, 4, FACTOR>
+              : each <= 8 ? row_kernel<G, 8, FACTOR>
+                          : row_kernel<G, 0, FACTOR>;
     k<<<static_cast<unsigned>(T), ROW_THREADS, 0, s>>>(p.row_logits, static_cast<int>(p.logits.splits), T * V, target,
                                                        dloss, V, loss, lse, U, static_cast<G*>(p.g), p.ldg,
                                                        p.target_rest);
+    return hipGetLastError();
+}
+
+hipError_t join_runs(const Plan& p, const int64_t* target, int64_t T, int64_t V, float* loss, float* lse,
+                     hipStream_t s)
+{
+    loss_kernel<<<static_cast<unsigned>(ceil_div(T, THREADS / 64)), THREADS, 0, s>>>(
+        p.part, p.nparts, p.logits.rows, column_blocks(p.logits.kind, V), column_blocks(p.logits.rest, V),
+        p.target_logit, target, T, V, loss, lse);
     return hipGetLastError();
 }
 
@@ -855,9 +1006,7 @@ hipError_t losses(const Plan& p, const Operand& x, const Operand& w, const int64
     o.target_logit = p.target_logit;
     o.target = target;
     POSEIDON_TRY((product<E, true, true, STATS>(p.logits, x, w, p.logits_parts, o, T, V, whole_chunks<E>(D), s)));
-    loss_kernel<<<static_cast<unsigned>(ceil_div(T, THREADS / 64)), THREADS, 0, s>>>(p.part, p.nparts, p.target_logit,
-                                                                                    target, T, V, loss, lse);
-    return hipGetLastError();
+    return join_runs(p, target, T, V, loss, lse, s);
 }
 
 template <typename I, typename E>
@@ -881,6 +1030,7 @@ hipError_t input_gradient(const Plan& p, const Operand& g, const Operand& w, con
 {
     constexpr bool BF16 = sizeof(I) == 2;
     const bool first = v0 == 0, last = v0 + vp == V;
+    const Choice& c = vp == std::min(p.piece, V) ? p.full.dx : p.last.dx;
     Out o{};
     o.c = p.dx ? static_cast<void*>(p.dx) : static_cast<void*>(dX);
     o.ldc = D;
@@ -894,8 +1044,8 @@ hipError_t input_gradient(const Plan& p, const Operand& g, const Operand& w, con
         o.W = whole_w.p;
         o.ldw = whole_w.ld;
     }
-    POSEIDON_TRY((product<E, true, false, STORE>(p.dx_choice, g, w, p.dx_parts, o, T, D, whole_chunks<E>(vp), s)));
-    return last && p.dx ? join_splits(p.dx, p.dx_choice.splits, T * D, dX, s) : hipSuccess;
+    POSEIDON_TRY((product<E, true, false, STORE>(c, g, w, p.dx_parts, o, T, D, whole_chunks<E>(vp), s)));
+    return last && p.dx ? join_splits(p.dx, p.full.dx.splits, T * D, dX, s) : hipSuccess;
 }
 
 // G of the classes v0 .. v0 + vp.
@@ -913,7 +1063,8 @@ hipError_t logit_gradient(const Plan& p, const Operand& x, const Operand& w, con
     o.v0 = v0;
     o.V = V;
     o.target_rest = sizeof(I) == 2 ? p.target_rest : nullptr;
-    return product<E, true, true, GRAD>(p.logits, x, w, p.logits_parts, o, T, vp, whole_chunks<E>(D), s);
+    const Choice& c = vp == std::min(p.piece, V) ? p.full.logits : p.last.logits;
+    return product<E, true, true, GRAD>(c, x, w, p.logits_parts, o, T, vp, whole_chunks<E>(D), s);
 }
 
 template <typename I, typename E>
@@ -931,13 +1082,15 @@ hipError_t backward_typed(const I* X, const I* W, const int64_t* target, const f
             POSEIDON_TRY((logit_gradient<I, E>(p, x, wp, target, lse, dloss, T, V, D, v0, vp, s)));
             POSEIDON_TRY((input_gradient<I, E>(p, g, wp, w, target, T, V, D, v0, vp, dX, s)));
         }
+        const Choice& c = vp == std::min(p.piece, V) ? p.full.dw : p.last.dw;
+        const bool sums = c.splits > 1;
         Out o{};
-        o.c = p.dw ? p.dw : dW + v0 * D;
+        o.c = sums ? p.dw : dW + v0 * D;
         o.ldc = D;
         o.split_stride = vp * D;
-        POSEIDON_TRY((product<E, false, false, STORE>(p.dw_choice, g, x, p.dw_parts, o, vp, D, T, s)));
-        if (p.dw)
-            POSEIDON_TRY(join_splits(p.dw, p.dw_choice.splits, vp * D, dW + v0 * D, s));
+        POSEIDON_TRY((product<E, false, false, STORE>(c, g, x, p.dw_parts, o, vp, D, T, s)));
+        if (sums)
+            POSEIDON_TRY(join_splits(p.dw, c.splits, vp * D, dW + v0 * D, s));
     }
     return hipSuccess;
 }
@@ -962,9 +1115,7 @@ hipError_t factor_typed(const I* X, const I* W, const int64_t* target, const flo
         o.c = U;
         o.ldc = V;
         POSEIDON_TRY((product<E, true, true, LOGITS>(p.logits, x, w, p.logits_parts, o, T, V, whole_chunks<E>(D), s)));
-        loss_kernel<<<static_cast<unsigned>(ceil_div(T, THREADS / 64)), THREADS, 0, s>>>(
-            p.part, p.nparts, p.target_logit, target, T, V, loss, p.lse);
-        POSEIDON_TRY(hipGetLastError());
+        POSEIDON_TRY(join_runs(p, target, T, V, loss, p.lse, s));
         factor_kernel<E, sizeof(I) == 4 && sizeof(E) == 2 ? 3 : 1>
             <<<grid_for(ceil_div(T * (p.ldg / GROUP), THREADS)), THREADS, 0, s>>>(
                 p.lse, target, dloss, T, V, U, static_cast<E*>(p.g), p.ldg, p.target_rest);

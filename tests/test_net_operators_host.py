@@ -139,6 +139,6 @@ def test_binding_checks_p(p):
 def test_binding_asks_for_the_generator():
     with pytest.raises(ValueError, match="rng"):
         api._rng(None, 0.1)
-    assert api._rng(None, 0.0) is None
+    assert api._rng(None, 0.0) is False
     with pytest.raises(TypeError):
         api._rng(torch.zeros(2), 0.1)
