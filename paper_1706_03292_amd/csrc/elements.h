@@ -11,6 +11,7 @@ namespace {
 typedef __bf16 bf8e __attribute__((ext_vector_type(8)));
 typedef __bf16 bf8a __attribute__((ext_vector_type(8), aligned(2)));   // 16 bytes at any element boundary
 typedef float f4a __attribute__((ext_vector_type(4), aligned(4)));
+typedef float f4e __attribute__((ext_vector_type(4)));
 typedef float f8e __attribute__((ext_vector_type(8)));
 
 constexpr int GROUP = 8;   // neighbours that a thread loads together and that share one generator call
@@ -80,6 +81,47 @@ __device__ __forceinline__ void store_some(T* p, int64_t n, const float (&v)[GRO
                 p[i] = static_cast<T>(v[i]);
     }
 }
+
+// A group as it lies in memory, for loads that stay in flight while another
+// group is worked on.
+template <typename T>
+struct Raw;
+template <>
+struct Raw<__bf16> {
+    bf8e v;
+};
+template <>
+struct Raw<float> {
+    f4e a, b;
+};
+
+__device__ __forceinline__ void load_raw(const __bf16* p, int64_t n, Raw<__bf16>& r)
+{
+    if (n >= GROUP) {
+        r.v = *reinterpret_cast<const bf8a*>(p);
+    } else {
+#pragma unroll
+        for (int i = 0; i < GROUP; ++i)
+            r.v[i] = i < n ? p[i] : static_cast<__bf16>(0.f);
+    }
+}
+
+__device__ __forceinline__ void load_raw(const float* p, int64_t n, Raw<float>& r)
+{
+    if (n >= GROUP) {
+        r.a = *reinterpret_cast<const f4a*>(p);
+        r.b = *reinterpret_cast<const f4a*>(p + 4);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            r.a[i] = i < n ? p[i] : 0.f;
+            r.b[i] = 4 + i < n ? p[4 + i] : 0.f;
+        }
+    }
+}
+
+__device__ __forceinline__ float raw_value(const Raw<__bf16>& r, int i) { return static_cast<float>(r.v[i]); }
+__device__ __forceinline__ float raw_value(const Raw<float>& r, int i) { return i < 4 ? r.a[i] : r.b[i - 4]; }
 
 // Philox4x32 (Salmon, Moraes, Dror and Shaw, "Parallel Random Numbers: As Easy
 // as 1, 2, 3", SC 2011) with seven rounds, the fewest that pass the whole of

@@ -66,6 +66,7 @@ __global__ __launch_bounds__(THREADS) void dropout_kernel(const T* __restrict__ 
 // Sums over a team of TPR threads (a power of two; more than 64: the whole
 // workgroup, through LDS).
 // ---------------------------------------------------------------------------
+// (lds: a place per wave)
 template <int TPR>
 __device__ __forceinline__ float team_sum(float v, float* lds)
 {
@@ -255,26 +256,50 @@ __global__ __launch_bounds__(TPR > THREADS ? TPR : THREADS) void norm_backward_k
     __shared__ float lds[32];
     __shared__ float sums[TEAMS > 1 ? 2 * TPR * NG * GROUP : 1];
     const int t = threadIdx.x % TPR, team = threadIdx.x / TPR;
-    const int64_t per_row = (cols + GROUP - 1) / GROUP;
+    const int64_t per_row = (cols + GROUP - 1) / GROUP, step = static_cast<int64_t>(gridDim.x) * TEAMS;
     const float inv = 1.f / static_cast<float>(cols);
     const Rng r = read_rng(d);
     float dg[NG][GROUP] = {}, db[NG][GROUP] = {};
-    // Every team of the workgroup takes part in each step (the sums of teams
-    // above 64 threads meet at barriers); a team past the last row only waits.
-    for (int64_t row = static_cast<int64_t>(blockIdx.x) * TEAMS + team; row < rows;
-         row += static_cast<int64_t>(gridDim.x) * TEAMS) {
+    // The next row's values are on their way while a row is worked on: a team
+    // has one row at a time, and its sums would otherwise wait for each row's
+    // loads in full (16384 x 2048 bf16 with residual and dropout: 100 us so).
+    Raw<T> ry[NG], rh[NG], re[NG];
+    float mean = 0.f, rstd = 0.f;
+    auto fetch = [&](int64_t row) {
         const int64_t base = row * cols;
-        float g[NG][GROUP], n[NG][GROUP], e[NG][GROUP];
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
             const int64_t c = (t + static_cast<int64_t>(i) * TPR) * GROUP;
-            load_some(dy + base + c, cols - c, g[i]);
-            load_some(h + base + c, cols - c, n[i]);
+            load_raw(dy + base + c, cols - c, ry[i]);
+            load_raw(h + base + c, cols - c, rh[i]);
             if (dres)
-                load_some(dres + base + c, cols - c, e[i]);
+                load_raw(dres + base + c, cols - c, re[i]);
         }
-        const float mean = mean_in[row], rstd = rstd_in[row];
+        mean = mean_in[row];
+        rstd = rstd_in[row];
+    };
+    int64_t row = static_cast<int64_t>(blockIdx.x) * TEAMS + team;
+    if (row < rows)
+        fetch(row);
+    // A team above 64 threads is the workgroup: it meets the sums' barriers
+    // together.
+    for (; row < rows; row += step) {
+        const int64_t base = row * cols;
+        float g[NG][GROUP], n[NG][GROUP];
+        Raw<T> e[NG];
+        const float rs = rstd;
         float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+            e[i] = re[i];
+#pragma unroll
+            for (int k = 0; k < GROUP; ++k) {
+                g[i][k] = raw_value(ry[i], k);   // past the row's end: 0, and nothing is stored
+                n[i][k] = (raw_value(rh[i], k) - mean) * rs;
+            }
+        }
+        if (row + step < rows)
+            fetch(row + step);
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
             const int64_t c = (t + static_cast<int64_t>(i) * TPR) * GROUP;
@@ -282,7 +307,6 @@ __global__ __launch_bounds__(TPR > THREADS ? TPR : THREADS) void norm_backward_k
             load_some(gamma + c, cols - c, a);
 #pragma unroll
             for (int k = 0; k < GROUP; ++k) {
-                n[i][k] = (n[i][k] - mean) * rstd;   // past the row's end g is 0, and nothing is stored
                 dg[i][k] = fmaf(g[i][k], n[i][k], dg[i][k]);
                 db[i][k] += g[i][k];
                 g[i][k] *= a[k];
@@ -298,8 +322,8 @@ __global__ __launch_bounds__(TPR > THREADS ? TPR : THREADS) void norm_backward_k
             if (q < per_row) {
 #pragma unroll
                 for (int k = 0; k < GROUP; ++k) {
-                    const float v = rstd * (g[i][k] - s1 - n[i][k] * s2);
-                    g[i][k] = dres ? v + e[i][k] : v;
+                    const float v = rs * (g[i][k] - s1 - n[i][k] * s2);
+                    g[i][k] = dres ? v + raw_value(e[i], k) : v;
                 }
                 store_some(dh + base + c, cols - c, g[i]);
                 if (d.thr) {
@@ -424,24 +448,30 @@ __global__ __launch_bounds__(THREADS) void norm_weights_long(const T* __restrict
     store_some(out + cols + c, cols - c, db);
 }
 
-// dgamma and dbeta from `parts` partial rows: 64 columns a workgroup, each
-// wave adding every fourth partial, then the four in order.
+// dgamma and dbeta from `parts` partial rows: 16 columns a workgroup, 16
+// threads a column, each adding every 16th partial, then theirs in order.
+constexpr int SUM_COLS = 16;
+
 __global__ __launch_bounds__(THREADS) void norm_weights_kernel(const float* __restrict__ partial, int parts,
                                                                int64_t cols, float* __restrict__ dgamma,
                                                                float* __restrict__ dbeta)
 {
-    __shared__ float lds[4][64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * 64 + lane;
+    constexpr int SLICES = THREADS / SUM_COLS;
+    __shared__ float lds[SLICES][SUM_COLS];
+    const int lane = threadIdx.x % SUM_COLS, w = threadIdx.x / SUM_COLS;
+    const int64_t c = static_cast<int64_t>(blockIdx.x) * SUM_COLS + lane;
     float s = 0.f;
     if (c < 2 * cols)
-#pragma unroll 8
-        for (int p = w; p < parts; p += 4)
+#pragma unroll 16
+        for (int p = w; p < parts; p += SLICES)
             s += partial[p * 2 * cols + c];
     lds[w][lane] = s;
     __syncthreads();
     if (w == 0 && c < 2 * cols) {
-        s = (lds[0][lane] + lds[1][lane]) + (lds[2][lane] + lds[3][lane]);
+        s = 0.f;
+#pragma unroll
+        for (int i = 0; i < SLICES; ++i)
+            s += lds[i][lane];
         if (c < cols)
             dgamma[c] = s;
         else
@@ -459,17 +489,20 @@ Drop make_drop(uint32_t thr, const int64_t* rng)
     return Drop{reinterpret_cast<const uint64_t*>(rng), thr, scale};
 }
 
-constexpr int64_t LONGEST = 1024 * 4 * GROUP;   // values of a row that a team holds
+constexpr int64_t LONGEST_FORWARD = 1024 * 4 * GROUP, LONGEST_BACKWARD = 512 * 2 * GROUP;   // values a team holds
 
-// f(integral_constant<TPR>, integral_constant<NG>) for the team that holds a
-// row of `cols` (at most LONGEST) values.
+// f(Int<TPR>, Int<NG>) for the team that holds a row of `cols` values.  The
+// backward pass holds the row's three inputs, the next row's and two sums a
+// column, so its threads take at most two groups (at four, with 290 registers,
+// one wave a SIMD is left: 16384 x 2048 bf16 86 us, with one group of 256
+// threads 68 us).
 template <int V>
 struct Int {
     static constexpr int value = V;
 };
 
 template <typename F>
-hipError_t with_team(int64_t cols, F&& f)
+hipError_t with_forward_team(int64_t cols, F&& f)
 {
     const int64_t groups = (cols + GROUP - 1) / GROUP;
     if (groups <= 16)
@@ -487,18 +520,37 @@ hipError_t with_team(int64_t cols, F&& f)
     return f(Int<1024>(), Int<4>());
 }
 
+template <typename F>
+hipError_t with_backward_team(int64_t cols, F&& f)
+{
+    const int64_t groups = (cols + GROUP - 1) / GROUP;
+    if (groups <= 16)
+        return f(Int<16>(), Int<1>());
+    if (groups <= 64)
+        return f(Int<64>(), Int<1>());
+    if (groups <= 128)
+        return f(Int<64>(), Int<2>());
+    if (groups <= 256)
+        return f(Int<256>(), Int<1>());
+    if (groups <= 512)
+        return f(Int<256>(), Int<2>());
+    return f(Int<512>(), Int<2>());
+}
+
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Workgroups for `work` workgroups' worth, within a launch's limit of 2^32
 // threads: the kernels walk what is over.
 unsigned grid_for(int64_t work) { return static_cast<unsigned>(std::min<int64_t>(work, 1 << 20)); }
 
-// Workgroups of the backward pass: two a CU keep its loads in flight, and
+// Workgroups of the backward pass: a few a CU keep its loads in flight, and
 // each leaves one partial row.
 int backward_groups(int64_t rows, int64_t cols)
 {
-    const int64_t teams = cols > LONGEST ? 1 : cols > 2048 ? 1 : cols > 128 ? 4 : 16;
-    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, teams), 2 * device_cu_count())));
+    const int64_t teams = cols > 1024 ? 1 : cols > 128 ? 4 : 16;
+    const int64_t per_cu = cols > 1024 && cols <= 2048 ? 3 : 2;
+    return static_cast<int>(
+        std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, teams), per_cu * device_cu_count())));
 }
 
 template <typename T>
@@ -517,12 +569,12 @@ template <typename T>
 hipError_t forward_typed(const T* x, const T* res, const float* gamma, const float* beta, int64_t rows, int64_t cols,
                          float eps, const Drop& d, T* h, T* y, float* mean, float* rstd, hipStream_t s)
 {
-    if (cols > LONGEST) {
+    if (cols > LONGEST_FORWARD) {
         norm_forward_long<T><<<grid_for(rows), LONG_THREADS, 0, s>>>(x, res, gamma, beta, rows, cols, eps, d, h, y,
                                                                      mean, rstd);
         return hipGetLastError();
     }
-    return with_team(cols, [&](auto tpr, auto ng) {
+    return with_forward_team(cols, [&](auto tpr, auto ng) {
         constexpr int TPR = decltype(tpr)::value, NG = decltype(ng)::value, NT = TPR > THREADS ? TPR : THREADS;
         norm_forward_kernel<T, TPR, NG><<<grid_for(ceil_div(rows, NT / TPR)), NT, 0, s>>>(
             x, res, gamma, beta, rows, cols, eps, d, h, y, mean, rstd);
@@ -537,7 +589,7 @@ hipError_t backward_typed(const T* dy, const T* h, const float* gamma, const flo
 {
     const int parts = backward_groups(rows, cols);
     hipError_t rc = hipSuccess;
-    if (cols > LONGEST) {
+    if (cols > LONGEST_BACKWARD) {
         if (rows > 0)
             norm_backward_long<T><<<grid_for(rows), LONG_THREADS, 0, s>>>(dy, h, gamma, mean, rstd, dres, rows, cols, d,
                                                                           dx, dh);
@@ -548,7 +600,7 @@ hipError_t backward_typed(const T* dy, const T* h, const float* gamma, const flo
         norm_weights_long<T><<<grid, THREADS, 0, s>>>(dy, h, mean, rstd, rows, cols, partial);
         rc = hipGetLastError();
     } else {
-        rc = with_team(cols, [&](auto tpr, auto ng) {
+        rc = with_backward_team(cols, [&](auto tpr, auto ng) {
             constexpr int TPR = decltype(tpr)::value, NG = decltype(ng)::value, NT = TPR > THREADS ? TPR : THREADS;
             norm_backward_kernel<T, TPR, NG><<<static_cast<unsigned>(parts), NT, 0, s>>>(
                 dy, h, gamma, mean, rstd, dres, rows, cols, d, dx, dh, partial);
@@ -557,8 +609,8 @@ hipError_t backward_typed(const T* dy, const T* h, const float* gamma, const flo
     }
     if (rc != hipSuccess)
         return rc;
-    norm_weights_kernel<<<static_cast<unsigned>(ceil_div(2 * cols, 64)), THREADS, 0, s>>>(partial, parts, cols,
-                                                                                         dgamma, dbeta);
+    norm_weights_kernel<<<static_cast<unsigned>(ceil_div(2 * cols, SUM_COLS)), THREADS, 0, s>>>(partial, parts,
+                                                                                               cols, dgamma, dbeta);
     return hipGetLastError();
 }
 

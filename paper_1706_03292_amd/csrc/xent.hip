@@ -695,28 +695,39 @@ Choice choose(int64_t M, int64_t N, int64_t K, int count, bool may_split)
         const Shape& s = SHAPES[k];
         if (s.step_us[TYPE][0] == 0.0)
             continue;
-        const int64_t tiles = std::max<int64_t>(ceil_div(M, s.bm) * ceil_div(N, s.bn), 1), slots = s.per_cu * cus;
-        const int64_t most = may_split ? std::max<int64_t>(1, std::min<int64_t>(32, steps / 4)) : 1;
-        // Splits worth a look: none, and those that come to whole rounds.
-        for (int round = 0; round <= 4; ++round) {
-            const int z = round == 0 ? 1 : static_cast<int>(std::min(most, round * slots / tiles));
-            if (z < 1 || (round > 0 && z == 1))
-                continue;
-            const double each = static_cast<double>((steps + z - 1) / z * count);
-            // The splits' sums are written (once is counted), read and written, and take a launch.
-            const double joined = z > 1 ? 5.0 + (z + 1) * sums : 0.0;
-            const double us = std::max(tiles_us(s, TYPE, M, N, each, z, OUT), reading) + joined;
-            if (us < best.us)
-                best = Choice{static_cast<ShapeKind>(k), z, us, M, SMALL};
-            const int64_t over = M % s.bm;
-            if (k < SQUARE || over == 0 || over > s.bm / 2 || M < s.bm)
-                continue;
-            const double main = tiles_us(s, TYPE, M - over, N, each, z, OUT);
-            for (int r = over <= 32 ? THIN : SMALL; r <= HALF && main + joined < best.us; ++r) {
-                const double both = main + 2.0 + tiles_us(SHAPES[r], TYPE, over, N, each, z, OUT);
-                if (std::max(both, reading) + joined < best.us)
-                    best = Choice{static_cast<ShapeKind>(k), z, std::max(both, reading) + joined, M - over,
-                                  static_cast<ShapeKind>(r)};
+        const int64_t slots = s.per_cu * cus, across = ceil_div(N, s.bn);
+        const int most = may_split ? static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(32, steps / 4))) : 1;
+        // All rows in this shape, or a ragged rest of them (at most half a
+        // tile's) in a smaller one; k whole, or split into what comes to whole
+        // rounds.
+        const int64_t over = M % s.bm;
+        const bool ragged = k >= SQUARE && over > 0 && over <= s.bm / 2 && M > s.bm;
+        for (int rest = 0; rest <= (ragged ? 1 : 0); ++rest) {
+            const int64_t rows = rest ? M - over : M;
+            const int64_t tiles = std::max<int64_t>(ceil_div(rows, s.bm) * across, 1);
+            for (int round = 0; round <= 4; ++round) {
+                const int z = round == 0 ? 1 : static_cast<int>(std::min<int64_t>(most, round * slots / tiles));
+                if (z < 1 || (round > 0 && z == 1))
+                    continue;
+                const double each = static_cast<double>((steps + z - 1) / z * count);
+                // The splits' sums are written (once is counted), read and written, and take a launch.
+                const double joined = z > 1 ? 5.0 + (z + 1) * sums : 0.0;
+                double us = tiles_us(s, TYPE, rows, N, each, z, OUT);
+                ShapeKind by = SMALL;
+                if (rest) {
+                    double least = 1e30;
+                    for (int r = over <= 32 ? THIN : SMALL; r <= HALF; ++r) {
+                        const double x = tiles_us(SHAPES[r], TYPE, over, N, each, z, OUT);
+                        if (x < least) {
+                            least = x;
+                            by = static_cast<ShapeKind>(r);
+                        }
+                    }
+                    us += 2.0 + least;
+                }
+                us = std::max(us, reading) + joined;
+                if (us < best.us)
+                    best = Choice{static_cast<ShapeKind>(k), z, us, rows, by};
             }
         }
     }
