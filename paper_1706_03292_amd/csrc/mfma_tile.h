@@ -65,8 +65,9 @@ __device__ __forceinline__ void load_to_lds(i4 rs, int v, uint32_t to)
                  : "memory");
 }
 
-// One operand: `rows` x `cols` values of type E from p, ld values apart.
-// k-major: cols = K (a multiple of 16 bytes); r-major: rows = K.  `plane`: the
+// One operand: `rows` rows of values of type E from p (a 4-byte boundary, as
+// every row's start), ld values apart.  k-major: a row holds K of them;
+// r-major: there are K rows.  `plane`: the
 // distance between the bf16 parts of one matrix, for products of parts.
 struct Operand {
     const void* p;
@@ -185,6 +186,22 @@ struct Panel {
         load_to_lds(rs, v, lds_address(stage) + __builtin_amdgcn_readfirstlane((tid >> 6) * 1024) + q * (NT / 64) * 1024);
     }
 
+    // k-major: the step that ends inside a 16-byte chunk has fetched the next
+    // row's first values there.  Clears what is past the k_left values of the
+    // step's rows (whole chunks past them were not fetched and are 0).
+    static __device__ __forceinline__ void clear_past(char* stage, int k_left, int tid)
+    {
+        constexpr int EACH = 16 / SZ;
+        const int c = k_left / EACH, from = k_left % EACH;
+        if (!KMAJOR || from == 0 || c >= CHUNKS)
+            return;
+        for (int r = tid; r < R; r += NT) {
+            E* at = reinterpret_cast<E*>(stage + r * STEP_BYTES + ((c ^ swz_k(r)) << 4));
+            for (int e = from; e < EACH; ++e)
+                at[e] = static_cast<E>(0.f);
+        }
+    }
+
     // The operand fragment of 16 rows, sub-step kk: for bf16 eight k from
     // 32 kk + 8 (lane / 16), for fp32 four from 16 kk + 4 (lane / 16).  Lane l
     // takes row r0 + l % 16 of block j = (row - r0) / 16; SPREAD: of the four
@@ -274,7 +291,8 @@ struct Tile {
     PB pb;
     Parts parts;
     int64_t a_plane, b_plane;
-    int k_left;        // values of k from the next step on (none left: 0 or less)
+    int k_left;        // values of k from the next step to load on (none left: 0 or less)
+    int k_unread;      // and from the stage that is read next
     int part;          // the next product of it
     int wm, wn, lane, tid;
 
@@ -316,6 +334,19 @@ struct Tile {
     template <int S>
     __device__ __forceinline__ h8 b_frag(int j, int kk) const { return PB::frag(b_stage<S>(), wn, j, kk, lane); }
 
+    // Stage S is read next: where K ends inside a chunk of it, what lies past
+    // it is cleared first.  (Products of several parts end on whole chunks.)
+    template <int S>
+    __device__ __forceinline__ void to_read()
+    {
+        if (k_unread > 0 && k_unread < STEP && k_unread % (16 / static_cast<int>(sizeof(E))) != 0) {
+            PA::clear_past(a_stage<S>(), k_unread, tid);
+            PB::clear_past(b_stage<S>(), k_unread, tid);
+            __syncthreads();
+        }
+        k_unread -= STEP;
+    }
+
     template <int S>
     __device__ __forceinline__ void read_ahead(Ahead& f) const
     {
@@ -354,6 +385,7 @@ struct Tile {
                 __builtin_amdgcn_s_waitcnt(wait_imm((STAGES - 2) * LOADS, 0));
                 __builtin_amdgcn_s_barrier();
                 __builtin_amdgcn_sched_barrier(0);
+                to_read<(S + 1) % STAGES>();
                 read_ahead<(S + 1) % STAGES>(f);
                 aim();
 #pragma unroll
@@ -417,7 +449,7 @@ struct Tile {
         parts = p;
         a_plane = a.plane * static_cast<int64_t>(sizeof(E));
         b_plane = b.plane * static_cast<int64_t>(sizeof(E));
-        k_left = static_cast<int>(K);
+        k_left = k_unread = static_cast<int>(K);
         part = 0;
         // Past the last step `load` fetches nothing (every lane outside), which
         // keeps the count of loads in flight the same to the end.
@@ -425,6 +457,7 @@ struct Tile {
         __builtin_amdgcn_s_waitcnt(wait_imm((STAGES - 1) * LOADS, 15));
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
+        to_read<0>();
         Ahead f;
         read_ahead<0>(f);
         for (int left = static_cast<int>((K + STEP - 1) / STEP) * p.count; left > 0; left -= STAGES)

@@ -792,12 +792,12 @@ hipError_t join_splits(const float* part, int64_t splits, int64_t n, O* out, hip
     return hipGetLastError();
 }
 
-// X or W as the caller has it is an operand where its rows lie on 16-byte
-// boundaries; else it is laid out again.
+// X or W as the caller has it is an operand where its rows lie on 4-byte
+// boundaries (fp32 always); else it is laid out again.
 template <typename I>
 bool needs_copy(const void* p, int64_t D)
 {
-    return !aligned16(p) || D * static_cast<int64_t>(sizeof(I)) % 16 != 0;
+    return reinterpret_cast<uintptr_t>(p) % 4 != 0 || D * static_cast<int64_t>(sizeof(I)) % 4 != 0;
 }
 
 template <typename I, typename O, int PARTS>
@@ -963,12 +963,16 @@ hipError_t operands(const Plan& p, const I* X, const I* W, const int64_t* target
     return hipSuccess;
 }
 
-// k-major operands end on 16 bytes.
+// G's rows end on whole chunks (zeros past V).
 template <typename E>
 int64_t whole_chunks(int64_t k)
 {
     return round_up(k, 16 / static_cast<int64_t>(sizeof(E)));
 }
+
+// The depth of the logits' product: rows in parts are padded with zeros, and
+// their products end on whole chunks.
+int64_t k_of(const Plan& p, int64_t D) { return p.logits_parts.count > 1 ? p.ldd : D; }
 
 template <typename E>
 hipError_t row_logits(const Plan& p, const Operand& x, const Operand& w, int64_t T, int64_t V, int64_t D,
@@ -978,7 +982,7 @@ hipError_t row_logits(const Plan& p, const Operand& x, const Operand& w, int64_t
     o.c = p.row_logits;
     o.ldc = V;
     o.split_stride = T * V;
-    return product<E, true, true, STORE>(p.logits, x, w, p.logits_parts, o, T, V, whole_chunks<E>(D), s);
+    return product<E, true, true, STORE>(p.logits, x, w, p.logits_parts, o, T, V, k_of(p, D), s);
 }
 
 template <typename G, bool FACTOR>
@@ -1016,7 +1020,7 @@ hipError_t losses(const Plan& p, const Operand& x, const Operand& w, const int64
     o.nparts = p.nparts;
     o.target_logit = p.target_logit;
     o.target = target;
-    POSEIDON_TRY((product<E, true, true, STATS>(p.logits, x, w, p.logits_parts, o, T, V, whole_chunks<E>(D), s)));
+    POSEIDON_TRY((product<E, true, true, STATS>(p.logits, x, w, p.logits_parts, o, T, V, k_of(p, D), s)));
     return join_runs(p, target, T, V, loss, lse, s);
 }
 
@@ -1075,7 +1079,7 @@ hipError_t logit_gradient(const Plan& p, const Operand& x, const Operand& w, con
     o.V = V;
     o.target_rest = sizeof(I) == 2 ? p.target_rest : nullptr;
     const Choice& c = vp == std::min(p.piece, V) ? p.full.logits : p.last.logits;
-    return product<E, true, true, GRAD>(c, x, w, p.logits_parts, o, T, vp, whole_chunks<E>(D), s);
+    return product<E, true, true, GRAD>(c, x, w, p.logits_parts, o, T, vp, k_of(p, D), s);
 }
 
 template <typename I, typename E>
@@ -1125,7 +1129,7 @@ hipError_t factor_typed(const I* X, const I* W, const int64_t* target, const flo
         o.target = target;
         o.c = U;
         o.ldc = V;
-        POSEIDON_TRY((product<E, true, true, LOGITS>(p.logits, x, w, p.logits_parts, o, T, V, whole_chunks<E>(D), s)));
+        POSEIDON_TRY((product<E, true, true, LOGITS>(p.logits, x, w, p.logits_parts, o, T, V, k_of(p, D), s)));
         POSEIDON_TRY(join_runs(p, target, T, V, loss, p.lse, s));
         factor_kernel<E, sizeof(I) == 4 && sizeof(E) == 2 ? 3 : 1>
             <<<grid_for(ceil_div(T * (p.ldg / GROUP), THREADS)), THREADS, 0, s>>>(

@@ -259,3 +259,30 @@ def test_gradient_against_differences():
                     float((((dX if which == "X" else dW)) * step.double()).sum()))
         rounding = float((bl * dloss.double()).sum()) / eps
         assert abs(slope - float((grad.double() * step.double()).sum())) <= third + 2 * rounding + 1e-6
+
+
+@pytest.mark.parametrize("dtype,D", [(F32, 37), (F32, 64), (BF16, 100), (BF16, 64)], ids=str)
+def test_a_class_masked_by_minus_infinity(dtype, D):
+    """A class whose weights are -inf has logit -inf for positive features and
+    leaves every other class as if it were not there -- also the class before
+    it, whose row ends inside the 16 bytes that hold the masked row's start."""
+    from paper_1706_03292_amd import api
+    log(f"xent masked class {dtype} D={D}")
+    T, V = 9, 150
+    X, W, target, dloss = make(T, V, D, dtype, 7, ignore=0.0)
+    X = X.abs() + torch.finfo(dtype).eps
+    for v in (1, 64, V - 1):
+        W[v] = -float("inf")
+    left = torch.tensor([v for v in range(V) if v not in (1, 64, V - 1)])
+    target = left[target % len(left)]
+    place = torch.searchsorted(left, target)
+    loss, lse, G, dX, dW = O.xent(X, W[left], place, dloss)
+    bl, be, bG, _, _ = O.xent_bounds(X, W[left], place, dloss, lse, G, dX, dW, dtype == BF16)
+    Xd, Wd, td, dd = (v.to(dev()) for v in (X, W, target, dloss))
+    l1, e1 = api.xent_forward(Xd, Wd, td)
+    within(l1, loss, bl, "loss")
+    within(e1, lse, be, "lse")
+    l2, u2, _ = api.xent_factor(Xd, Wd, td, dd)
+    within(l2, loss, bl, "factor loss")
+    within(u2.cpu()[:, left], G, bG, "U")
+    assert (u2.cpu()[:, [1, 64, V - 1]] == 0).all()
