@@ -83,8 +83,24 @@ struct Parts {
     uint32_t sel;
 };
 
-template <typename E, int R, int NT, bool KMAJOR, int KSUB, bool SPREAD>
+// fp32 in memory, multiplied as six bf16 products of its exact three parts
+// (h*h, h*m, m*h, h*l, l*h, m*m: what is dropped is below 2^-23 of a product),
+// the parts made in registers from what the operand reads bring.
+struct Split32 {};
+
+template <typename E>
+struct InMemory {
+    typedef E type;
+};
+template <>
+struct InMemory<Split32> {
+    typedef float type;
+};
+
+template <typename E_, int R, int NT, bool KMAJOR, int KSUB, bool SPREAD>
 struct Panel {
+    typedef typename InMemory<E_>::type E;
+    static constexpr bool SPLIT = !__is_same(E_, E);   // operands are eight fp32 values a lane, k from 8 (lane / 16)
     static constexpr int SZ = sizeof(E);
     static constexpr int STEP_BYTES = KSUB * SUB_BYTES;
     static constexpr int BYTES = R * STEP_BYTES;
@@ -120,7 +136,7 @@ struct Panel {
                 return 0;
         } else {
             if constexpr (PER_ROW % 16 == 0)
-                return ((k >> 2) & 3) << 2;
+                return ((k >> (SPLIT ? 3 : 2)) & 3) << 2;
             else
                 return 0;
         }
@@ -186,6 +202,29 @@ struct Panel {
         load_to_lds(rs, v, lds_address(stage) + __builtin_amdgcn_readfirstlane((tid >> 6) * 1024) + q * (NT / 64) * 1024);
     }
 
+    // SPLIT's operand: row r0 + 16 j + lane % 16, eight k from 8 (lane / 16).
+    static __device__ __forceinline__ f8e frag8(const char* stage, int r0, int j, int lane)
+    {
+        const int g = lane >> 4, i = lane & 15, r = r0 + 16 * j + i;
+        f8e v;
+        if constexpr (KMAJOR) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const acc4 x = *reinterpret_cast<const acc4*>(stage + r * STEP_BYTES + (((2 * g + half) ^ swz_k(r)) << 4));
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    v[4 * half + e] = x[e];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int k = 8 * g + e;
+                v[e] = *reinterpret_cast<const float*>(stage + k * (R * 4) + (((r >> 2) ^ swz_r(k)) << 4) + (r & 3) * 4);
+            }
+        }
+        return v;
+    }
+
     // k-major: the step that ends inside a 16-byte chunk has fetched the next
     // row's first values there.  Clears what is past the k_left values of the
     // step's rows (whole chunks past them were not fetched and are 0).
@@ -239,6 +278,33 @@ struct Panel {
     }
 };
 
+typedef unsigned u4 __attribute__((ext_vector_type(4)));
+typedef __bf16 b2e __attribute__((ext_vector_type(2)));
+typedef float f2e __attribute__((ext_vector_type(2)));
+
+struct Parts3 {
+    h8 h, m, l;
+};
+
+// h and m rounded to nearest, l exact (at most eight bits are left).
+__device__ __forceinline__ Parts3 in_parts3(f8e x)
+{
+    u4 part[3];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        float a = x[2 * q], b = x[2 * q + 1];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const unsigned w = __builtin_bit_cast(unsigned, __builtin_convertvector((f2e){a, b}, b2e));
+            part[p][q] = w;
+            a -= __builtin_bit_cast(float, w << 16);
+            b -= __builtin_bit_cast(float, w & 0xffff0000u);
+        }
+        part[2][q] = __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, b), __builtin_bit_cast(unsigned, a), 0x07060302u);
+    }
+    return Parts3{__builtin_bit_cast(h8, part[0]), __builtin_bit_cast(h8, part[1]), __builtin_bit_cast(h8, part[2])};
+}
+
 template <typename E>
 __device__ __forceinline__ acc4 mfma(h8 a, h8 b, acc4 c)
 {
@@ -271,7 +337,8 @@ template <typename E_, bool AK_, bool BK_, int BM_, int BN_, int WM_, int WN_, i
           bool SPREAD_ = false>
 struct Tile {
     typedef E_ E;
-    static constexpr bool AK = AK_, BKM = BK_;
+    typedef typename InMemory<E_>::type M;   // in memory
+    static constexpr bool AK = AK_, BKM = BK_, SPLIT = !__is_same(E_, M);
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_;
     static constexpr int NWN = BN / WN, WAVES = (BM / WM) * NWN, NT = 64 * WAVES;
     static constexpr int TM = WM / 16, TN = WN / 16, KSUB = KSUB_;
@@ -299,6 +366,19 @@ struct Tile {
     // The operands that the next products need first.
     struct Ahead {
         h8 a[2], b[TN];
+    };
+    struct AheadSplit {
+        Parts3 a, b[TN];   // in parts: the first row block's, and all of B's
+        f8e next;          // as read: the second row block's
+    };
+
+    template <bool, typename = void>
+    struct Choose {
+        typedef Ahead type;
+    };
+    template <typename U>
+    struct Choose<true, U> {
+        typedef AheadSplit type;
     };
 
     __device__ __forceinline__ void aim()
@@ -339,7 +419,7 @@ struct Tile {
     template <int S>
     __device__ __forceinline__ void to_read()
     {
-        if (k_unread > 0 && k_unread < STEP && k_unread % (16 / static_cast<int>(sizeof(E))) != 0) {
+        if (k_unread > 0 && k_unread < STEP && k_unread % (16 / static_cast<int>(sizeof(M))) != 0) {
             PA::clear_past(a_stage<S>(), k_unread, tid);
             PB::clear_past(b_stage<S>(), k_unread, tid);
             __syncthreads();
@@ -405,12 +485,96 @@ struct Tile {
         }
     }
 
+    // The same for fp32 in parts.  A step is one sub-step of 32 k; a group is a
+    // row block's 6 TN products, and while they run the next block is put into
+    // parts (in the last group all that the next stage needs first).
     template <int S>
-    __device__ __forceinline__ void turns(acc4 (&acc)[TM][TN], Ahead& f, int left)
+    __device__ __forceinline__ void turn_split(acc4 (&acc)[TM][TN], AheadSplit& f)
+    {
+        static_assert(!SPLIT || (KSUB == 2 && TM >= 2 && !SPREAD), "steps of 32 fp32 values");
+        f8e raw[TM + 2], next_b[TN];
+        raw[1] = f.next;
+        Parts3 a = f.a;
+#pragma unroll
+        for (int g = 0; g < TM; ++g) {
+            if (g + 2 < TM)
+                raw[g + 2] = PA::frag8(a_stage<S>(), wm, g + 2, lane);
+            if (g == TM - 2) {
+                __builtin_amdgcn_s_waitcnt(wait_imm((STAGES - 2) * LOADS, 0));
+                __builtin_amdgcn_s_barrier();
+                __builtin_amdgcn_sched_barrier(0);
+                constexpr int N = (S + 1) % STAGES;
+                to_read<N>();
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+                    next_b[j] = PB::frag8(b_stage<N>(), wn, j, lane);
+                raw[TM] = PA::frag8(a_stage<N>(), wm, 0, lane);
+                raw[TM + 1] = PA::frag8(a_stage<N>(), wm, 1, lane);
+                aim();
+#pragma unroll
+                for (int q = 0; q < (LOADS + 1) / 2; ++q)
+                    load<S>(q);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (g == TM - 1) {
+#pragma unroll
+                for (int q = (LOADS + 1) / 2; q < LOADS; ++q)
+                    load<S>(q);
+                after_loads();
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            const Parts3 next = in_parts3(raw[g + 1]);
+            products(acc[g], a, f.b);
+            a = next;
+            if (g == TM - 1) {
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+                    f.b[j] = in_parts3(next_b[j]);
+            }
+            // Products and parts in turn: 44 vector instructions put a block
+            // into parts.
+            if (g < TM - 1)
+                interleave<(44 + 6 * TN - 1) / (6 * TN)>();
+            else
+                interleave<(44 * (TN + 1) + 6 * TN - 1) / (6 * TN)>();
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        f.a = a;
+        f.next = raw[TM + 1];
+    }
+
+    template <int VALU>
+    static __device__ __forceinline__ void interleave()
+    {
+#pragma unroll
+        for (int i = 0; i < 6 * TN; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, VALU, 0);
+        }
+    }
+
+    static __device__ __forceinline__ void products(acc4 (&acc)[TN], const Parts3& a, const Parts3 (&b)[TN])
+    {
+#pragma unroll
+        for (int p = 0; p < 6; ++p) {
+            const h8 x = p == 0 || p == 1 || p == 3 ? a.h : p == 4 ? a.l : a.m;
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const h8 y = p == 0 || p == 2 || p == 4 ? b[j].h : p == 3 ? b[j].l : b[j].m;
+                acc[j] = mfma<__bf16>(y, x, acc[j]);
+            }
+        }
+    }
+
+    template <int S, typename F>
+    __device__ __forceinline__ void turns(acc4 (&acc)[TM][TN], F& f, int left)
     {
         if constexpr (S < STAGES) {
             if (left > S) {
-                turn<S>(acc, f);
+                if constexpr (SPLIT)
+                    turn_split<S>(acc, f);
+                else
+                    turn<S>(acc, f);
                 turns<S + 1>(acc, f, left);
             }
         }
@@ -447,8 +611,8 @@ struct Tile {
         pa.init(a, m0, k0, tid);
         pb.init(b, n0, k0, tid);
         parts = p;
-        a_plane = a.plane * static_cast<int64_t>(sizeof(E));
-        b_plane = b.plane * static_cast<int64_t>(sizeof(E));
+        a_plane = a.plane * static_cast<int64_t>(sizeof(M));
+        b_plane = b.plane * static_cast<int64_t>(sizeof(M));
         k_left = k_unread = static_cast<int>(K);
         part = 0;
         // Past the last step `load` fetches nothing (every lane outside), which
@@ -458,8 +622,16 @@ struct Tile {
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
         to_read<0>();
-        Ahead f;
-        read_ahead<0>(f);
+        typename Choose<SPLIT>::type f;
+        if constexpr (SPLIT) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+                f.b[j] = in_parts3(PB::frag8(b_stage<0>(), wn, j, lane));
+            f.a = in_parts3(PA::frag8(a_stage<0>(), wm, 0, lane));
+            f.next = PA::frag8(a_stage<0>(), wm, 1, lane);
+        } else {
+            read_ahead<0>(f);
+        }
         for (int left = static_cast<int>((K + STEP - 1) / STEP) * p.count; left > 0; left -= STAGES)
             turns<0>(acc, f, left);
         // No load may still be writing LDS when the workgroup ends.

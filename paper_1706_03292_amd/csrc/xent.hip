@@ -226,7 +226,7 @@ __device__ __forceinline__ void finish_grad(acc4 (&acc)[T::TM][T::TN], const Out
 #pragma unroll
         for (int j = 0; j < T::TN; j += RUN) {
             const bool in = !EDGE || n0 + first + STRIDE * j < o.ldg;   // ldg: a multiple of eight
-            if constexpr (sizeof(typename T::E) == 4) {
+            if constexpr (sizeof(typename T::M) == 4) {
                 if (in)
                     *reinterpret_cast<acc4*>(static_cast<float*>(o.g) + to + STRIDE * j) = acc[i][j];
             } else {
@@ -263,10 +263,10 @@ __device__ __forceinline__ void finish_store(acc4 (&acc)[T::TM][T::TN], const Ou
             continue;
         const int64_t at = m0 + m;
         float rest = 0.f;
-        const typename T::E* w = nullptr;
+        const typename T::M* w = nullptr;
         if (o.target_rest && z == 0 && counts(o.target[at], o.V)) {
             rest = o.target_rest[at];
-            w = static_cast<const typename T::E*>(o.W) + o.target[at] * o.ldw + n0 + first;
+            w = static_cast<const typename T::M*>(o.W) + o.target[at] * o.ldw + n0 + first;
         }
 #pragma unroll
         for (int j = 0; j < T::TN; ++j) {
@@ -509,8 +509,8 @@ __global__ __launch_bounds__(ROW_THREADS) void row_kernel(float* __restrict__ lo
 }
 
 // Many rows: G from the logits in U and their lse, in place and as the operand
-// of dX (PARTS bf16 parts, or fp32; ldg apart, zeros past V).
-template <typename E, int PARTS>
+// of dX (bf16 or fp32, ldg apart, zeros past V).
+template <typename E>
 __global__ __launch_bounds__(THREADS) void factor_kernel(const float* __restrict__ lse,
                                                          const int64_t* __restrict__ target,
                                                          const float* __restrict__ dloss, int64_t T, int64_t V,
@@ -534,24 +534,16 @@ __global__ __launch_bounds__(THREADS) void factor_kernel(const float* __restrict
             }
         }
         store_some(U + row * V + c, V - c, v);
-#pragma unroll
-        for (int p = 0; p < PARTS; ++p) {
-            store_group(g + p * (T * ldg) + row * ldg + c, v);
-            if (p + 1 < PARTS)
-#pragma unroll
-                for (int i = 0; i < GROUP; ++i)
-                    v[i] -= static_cast<float>(static_cast<__bf16>(v[i]));
-        }
+        store_group(g + row * ldg + c, v);
     }
 }
 
 // A matrix copied with its rows padded to ldo values (zeros), rows without a
-// target (where a target list is given) cleared; or split into its exact bf16
-// parts h + m + l, planes apart (fp32 input only).
-template <typename E, typename O, int PARTS>
+// target (where a target list is given) cleared.
+template <typename E>
 __global__ __launch_bounds__(THREADS) void lay_out_kernel(const E* __restrict__ x, int64_t rows, int64_t cols,
                                                           int64_t ldo, const int64_t* __restrict__ target, int64_t V,
-                                                          O* __restrict__ out, int64_t plane)
+                                                          E* __restrict__ out)
 {
     const int64_t per_row = ldo / GROUP, groups = rows * per_row, step = static_cast<int64_t>(gridDim.x) * THREADS;
     for (int64_t q = static_cast<int64_t>(blockIdx.x) * THREADS + threadIdx.x; q < groups; q += step) {
@@ -562,33 +554,35 @@ __global__ __launch_bounds__(THREADS) void lay_out_kernel(const E* __restrict__ 
 #pragma unroll
             for (int i = 0; i < GROUP; ++i)
                 v[i] = 0.f;
-#pragma unroll
-        for (int p = 0; p < PARTS; ++p) {
-            store_group(out + p * plane + row * ldo + c, v);
-            if (p + 1 < PARTS)
-#pragma unroll
-                for (int i = 0; i < GROUP; ++i)
-                    v[i] -= static_cast<float>(static_cast<__bf16>(v[i]));
-        }
+        store_group(out + row * ldo + c, v);
     }
 }
 
-// The splits' sums in order, rounded once to the result's type.
+// The splits' sums in order, rounded once to the result's type.  A result of
+// few values is bound by the splits' latency: eight splits are loaded together.
 template <typename O>
 __global__ __launch_bounds__(THREADS) void join_splits_kernel(const float* __restrict__ part, int splits,
                                                               int64_t stride, int64_t n, O* __restrict__ out)
 {
-    const int64_t groups = (n + GROUP - 1) / GROUP, step = static_cast<int64_t>(gridDim.x) * THREADS;
+    constexpr int AT_ONCE = 8;
+    const int64_t groups = (n + 3) / 4, step = static_cast<int64_t>(gridDim.x) * THREADS;
     for (int64_t q = static_cast<int64_t>(blockIdx.x) * THREADS + threadIdx.x; q < groups; q += step) {
-        float v[GROUP], x[GROUP];
-        load_some(part + q * GROUP, n - q * GROUP, v);
-        for (int s = 1; s < splits; ++s) {
-            load_some(part + s * stride + q * GROUP, n - q * GROUP, x);
+        const int64_t at = 4 * q;
+        acc4 v = {0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < splits; s += AT_ONCE) {
+            acc4 x[AT_ONCE];
 #pragma unroll
-            for (int i = 0; i < GROUP; ++i)
-                v[i] += x[i];
+            for (int k = 0; k < AT_ONCE; ++k)
+                x[k] = s + k < splits ? get4(part + (s + k) * stride + at, n - at, 0.f) : acc4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k)
+                v += x[k];
         }
-        store_some(out + q * GROUP, n - q * GROUP, v);
+        const int left = static_cast<int>(n - at < 4 ? n - at : 4);
+        if constexpr (sizeof(O) == 2)
+            put4(out + at, __builtin_convertvector(v, b4), left);
+        else
+            put4(out + at, v, left);
     }
 }
 
@@ -614,7 +608,10 @@ struct Arena {
 
 // Tile shapes: rows x columns of a workgroup, of a wave, stages.  All take 128
 // bytes of k a step.  THIN is for 32 rows or fewer; of the others the larger
-// read less per product and the smaller fill the GPU with fewer tiles.
+// read less per product and the smaller fill the GPU with fewer tiles.  fp32 is
+// multiplied by the fp32 matrix instructions up to 64 x 128, in bf16 parts at
+// 128 x 128 (8192 x 8192 x 4096: 134 against 206 TFLOP/s; on 64 x 64 tiles a
+// step waits for its parts, 127 against 114).
 enum ShapeKind { THIN, SMALL, HALF, SQUARE, TALL, LARGE };
 
 template <typename E, bool AK, bool BK>
@@ -642,7 +639,7 @@ constexpr Shape SHAPES[] = {
     {32, 64, 4, 3, {{0.29, 0.46, 0.66}, {0.50, 0.74, 1.02}}, 3.5},
     {64, 64, 2, 3, {{0.30, 0.42, 0.58}, {0.65, 1.09, 1.56}}, 4.0},
     {64, 128, 4, 2, {{0.42, 0.63, 0.}, {1.12, 2.03, 0.}}, 4.5},
-    {128, 128, 2, 2, {{0.78, 1.00, 0.}, {2.17, 3.96, 0.}}, 5.0},
+    {128, 128, 2, 2, {{0.78, 1.00, 0.}, {1.66, 2.78, 0.}}, 5.0},
     {256, 192, 4, 1, {{1.25, 0., 0.}, {0., 0., 0.}}, 6.0},
     {256, 256, 4, 1, {{1.57, 0., 0.}, {0., 0., 0.}}, 6.0},
 };
@@ -757,7 +754,10 @@ hipError_t product_rows(ShapeKind kind, const Operand& a, const Operand& b, cons
     case HALF:
         return launch_product<Half<E, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s);
     case SQUARE:
-        return launch_product<Square<E, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s);
+        if constexpr (sizeof(E) == 4)
+            return launch_product<Square<Split32, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s);
+        else
+            return launch_product<Square<E, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s);
     case TALL:
         if constexpr (sizeof(E) == 2)
             return launch_product<Tall<E, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s);
@@ -781,13 +781,13 @@ hipError_t product(const Choice& c, const Operand& a, const Operand& b, const Pa
 }
 
 // Products of parts, four bits each (A's, then B's): one; three of A with one
-// of B; the six of 3 x 3 that fp32 needs.
-constexpr Parts ONE{1, 0}, THREE_A{3, 0x210}, SIX{6, 0x528140};
+// of B.
+constexpr Parts ONE{1, 0}, THREE_A{3, 0x210};
 
 template <typename O>
 hipError_t join_splits(const float* part, int64_t splits, int64_t n, O* out, hipStream_t s)
 {
-    join_splits_kernel<O><<<grid_for(ceil_div(n, THREADS * GROUP)), THREADS, 0, s>>>(part, static_cast<int>(splits), n,
+    join_splits_kernel<O><<<grid_for(ceil_div(n, THREADS * 4)), THREADS, 0, s>>>(part, static_cast<int>(splits), n,
                                                                                      n, out);
     return hipGetLastError();
 }
@@ -800,23 +800,18 @@ bool needs_copy(const void* p, int64_t D)
     return reinterpret_cast<uintptr_t>(p) % 4 != 0 || D * static_cast<int64_t>(sizeof(I)) % 4 != 0;
 }
 
-template <typename I, typename O, int PARTS>
-hipError_t lay_out(const I* x, int64_t rows, int64_t D, int64_t ldo, const int64_t* target, int64_t V, O* out,
+template <typename E>
+hipError_t lay_out(const E* x, int64_t rows, int64_t D, int64_t ldo, const int64_t* target, int64_t V, E* out,
                    hipStream_t s)
 {
     if (rows > 0)
-        lay_out_kernel<I, O, PARTS><<<grid_for(ceil_div(rows * (ldo / GROUP), THREADS)), THREADS, 0, s>>>(
-            x, rows, D, ldo, target, V, out, rows * ldo);
+        lay_out_kernel<E><<<grid_for(ceil_div(rows * (ldo / GROUP), THREADS)), THREADS, 0, s>>>(x, rows, D, ldo,
+                                                                                             target, V, out);
     return hipGetLastError();
 }
 
-// How a call computes: I, the type of X and W in memory; E, the operands'
-// (bf16, or fp32 multiplied as fp32); fp32 in bf16 parts (I = float, E = bf16)
-// where the products outweigh the splitting.
-//
-// Rows of which the logits of all classes are fewer than this are few: their
-// logits go through memory once (they are small beside W), which lets k be
-// split so that the GPU is full.
+// So many rows are few: the logits of all classes are then small beside W and
+// go through memory once, which lets k be split so that the GPU is full.
 constexpr int64_t FEW_ROWS = 32;
 constexpr int64_t PIECE_BYTES = int64_t(512) << 20;   // of G at a time
 
@@ -834,7 +829,6 @@ struct Plan {
     int64_t ldd = 0;   // row length of what is laid out
     void* x = nullptr;
     void* w = nullptr;
-    Parts logits_parts = ONE, dx_parts = ONE, dw_parts = ONE;
     Choice logits{};      // forward and factor form
     Pieces full, last;    // backward: of the full pieces and the last one
     float* row_logits = nullptr;   // few rows: splits x T x V
@@ -850,36 +844,34 @@ struct Plan {
     int64_t bytes = 0;
 };
 
+// dW = G^T X: G is fp32, or (bf16 X) its three exact bf16 parts.
 template <typename E>
-Pieces pieces(const Plan& p, int64_t T, int64_t rows, int64_t D)
+constexpr Parts DW_PARTS = sizeof(E) == 2 ? THREE_A : ONE;
+
+template <typename E>
+Pieces pieces(int64_t T, int64_t rows, int64_t D)
 {
-    return Pieces{choose<E, GRAD>(T, rows, D, p.logits_parts.count, false),
-                  choose<E, STORE>(T, D, rows, p.dx_parts.count, true),
-                  choose<E, STORE>(rows, D, T, p.dw_parts.count, true)};
+    return Pieces{choose<E, GRAD>(T, rows, D, 1, false), choose<E, STORE>(T, D, rows, 1, true),
+                  choose<E, STORE>(rows, D, T, DW_PARTS<E>.count, true)};
 }
 
-template <typename I, typename E>
+template <typename E>
 Plan make_plan(int op, const void* X, const void* W, int64_t T, int64_t V, int64_t D, char* base)
 {
-    constexpr bool SPLIT = sizeof(I) == 4 && sizeof(E) == 2;   // fp32 in bf16 parts
-    constexpr int64_t SZ = sizeof(E), COPIES = SPLIT ? 3 : 1;
+    constexpr int64_t SZ = sizeof(E);
     Plan p;
     Arena a{base};
     p.ldd = round_up(D, GROUP);
-    p.own_x = SPLIT || op == POSEIDON_XENT_BACKWARD || needs_copy<I>(X, D);
-    p.own_w = SPLIT || needs_copy<I>(W, D);
+    p.own_x = op == POSEIDON_XENT_BACKWARD || needs_copy<E>(X, D);
+    p.own_w = needs_copy<E>(W, D);
     if (p.own_x)
-        p.x = a.take(T * p.ldd * SZ * COPIES);
+        p.x = a.take(T * p.ldd * SZ);
     if (p.own_w)
-        p.w = a.take(V * p.ldd * SZ * COPIES);
-    if (SPLIT)
-        p.logits_parts = p.dx_parts = p.dw_parts = SIX;
-    else if (SZ == 2)
-        p.dw_parts = THREE_A;
+        p.w = a.take(V * p.ldd * SZ);
     p.few = op != POSEIDON_XENT_BACKWARD && T <= FEW_ROWS;
-    p.logits = p.few                         ? choose<E, STORE>(T, V, D, p.logits_parts.count, true)
-               : op == POSEIDON_XENT_FACTOR ? choose<E, LOGITS>(T, V, D, p.logits_parts.count, false)
-                                            : choose<E, STATS>(T, V, D, p.logits_parts.count, false);
+    p.logits = p.few                         ? choose<E, STORE>(T, V, D, 1, true)
+               : op == POSEIDON_XENT_FACTOR ? choose<E, LOGITS>(T, V, D, 1, false)
+                                            : choose<E, STATS>(T, V, D, 1, false);
     if (p.few) {
         p.row_logits = static_cast<float*>(a.take(p.logits.splits * T * V * 4));
     } else if (op != POSEIDON_XENT_BACKWARD) {
@@ -895,9 +887,9 @@ Plan make_plan(int op, const void* X, const void* W, int64_t T, int64_t V, int64
         return p;
     }
     // G: fp32, or in bf16 parts (for a factor's bf16 dX one of them).
-    const int64_t g_value = SZ == 4 ? 4 : op == POSEIDON_XENT_FACTOR && !SPLIT ? 2 : 6;
+    const int64_t g_value = SZ == 4 ? 4 : op == POSEIDON_XENT_FACTOR ? 2 : 6;
     p.piece = round_up(V, GROUP);
-    p.full.dx = choose<E, STORE>(T, D, V, p.dx_parts.count, true);
+    p.full.dx = choose<E, STORE>(T, D, V, 1, true);
     if (op == POSEIDON_XENT_BACKWARD) {
         // Pieces of the vocabulary within the budget: equal ones, or as many
         // classes as make whole rounds of dW's largest tiles and a rest;
@@ -914,7 +906,7 @@ Plan make_plan(int op, const void* X, const void* W, int64_t T, int64_t V, int64
             if (piece < 256 && fewest > 1)
                 continue;
             const int64_t rows = std::min(piece, V), over = V % rows;
-            const Pieces full = pieces<E>(p, T, rows, D), last = over ? pieces<E>(p, T, over, D) : Pieces{};
+            const Pieces full = pieces<E>(T, rows, D), last = over ? pieces<E>(T, over, D) : Pieces{};
             const double us = static_cast<double>(V / rows) * full.us() + last.us();
             if (us < best) {
                 best = us;
@@ -934,7 +926,7 @@ Plan make_plan(int op, const void* X, const void* W, int64_t T, int64_t V, int64
     p.ldg = p.piece;
     p.g = a.take(T * p.ldg * g_value);
     p.target_rest = static_cast<float*>(a.take(T * 4));
-    if (p.full.dx.splits > 1 || (p.piece < V && sizeof(I) == 2))
+    if (p.full.dx.splits > 1 || (p.piece < V && SZ == 2))
         p.dx = static_cast<float*>(a.take(p.full.dx.splits * T * D * 4));
     p.bytes = a.at;
     return p;
@@ -949,17 +941,16 @@ Plan make_plan(int op, const void* X, const void* W, int64_t T, int64_t V, int64
 
 // X and W as operands, laid out where the plan says so (given `target`, X
 // without the rows that have none: whatever they hold must not reach dW).
-template <typename I, typename E>
-hipError_t operands(const Plan& p, const I* X, const I* W, const int64_t* target, int64_t T, int64_t V, int64_t D,
+template <typename E>
+hipError_t operands(const Plan& p, const E* X, const E* W, const int64_t* target, int64_t T, int64_t V, int64_t D,
                     Operand& x, Operand& w, hipStream_t s)
 {
-    constexpr int PARTS = sizeof(I) == 4 && sizeof(E) == 2 ? 3 : 1;
     if (p.own_x)
-        POSEIDON_TRY((lay_out<I, E, PARTS>(X, T, D, p.ldd, target, V, static_cast<E*>(p.x), s)));
+        POSEIDON_TRY(lay_out(X, T, D, p.ldd, target, V, static_cast<E*>(p.x), s));
     if (p.own_w)
-        POSEIDON_TRY((lay_out<I, E, PARTS>(W, V, D, p.ldd, nullptr, V, static_cast<E*>(p.w), s)));
-    x = Operand{p.own_x ? p.x : X, p.own_x ? p.ldd : D, T, T * p.ldd};
-    w = Operand{p.own_w ? p.w : W, p.own_w ? p.ldd : D, V, V * p.ldd};
+        POSEIDON_TRY(lay_out(W, V, D, p.ldd, nullptr, V, static_cast<E*>(p.w), s));
+    x = Operand{p.own_x ? p.x : X, p.own_x ? p.ldd : D, T, 0};
+    w = Operand{p.own_w ? p.w : W, p.own_w ? p.ldd : D, V, 0};
     return hipSuccess;
 }
 
@@ -970,10 +961,6 @@ int64_t whole_chunks(int64_t k)
     return round_up(k, 16 / static_cast<int64_t>(sizeof(E)));
 }
 
-// The depth of the logits' product: rows in parts are padded with zeros, and
-// their products end on whole chunks.
-int64_t k_of(const Plan& p, int64_t D) { return p.logits_parts.count > 1 ? p.ldd : D; }
-
 template <typename E>
 hipError_t row_logits(const Plan& p, const Operand& x, const Operand& w, int64_t T, int64_t V, int64_t D,
                       hipStream_t s)
@@ -982,7 +969,7 @@ hipError_t row_logits(const Plan& p, const Operand& x, const Operand& w, int64_t
     o.c = p.row_logits;
     o.ldc = V;
     o.split_stride = T * V;
-    return product<E, true, true, STORE>(p.logits, x, w, p.logits_parts, o, T, V, k_of(p, D), s);
+    return product<E, true, true, STORE>(p.logits, x, w, ONE, o, T, V, D, s);
 }
 
 template <typename G, bool FACTOR>
@@ -1020,17 +1007,17 @@ hipError_t losses(const Plan& p, const Operand& x, const Operand& w, const int64
     o.nparts = p.nparts;
     o.target_logit = p.target_logit;
     o.target = target;
-    POSEIDON_TRY((product<E, true, true, STATS>(p.logits, x, w, p.logits_parts, o, T, V, k_of(p, D), s)));
+    POSEIDON_TRY((product<E, true, true, STATS>(p.logits, x, w, ONE, o, T, V, D, s)));
     return join_runs(p, target, T, V, loss, lse, s);
 }
 
-template <typename I, typename E>
-hipError_t forward_typed(const I* X, const I* W, const int64_t* target, int64_t T, int64_t V, int64_t D, float* loss,
+template <typename E>
+hipError_t forward_typed(const E* X, const E* W, const int64_t* target, int64_t T, int64_t V, int64_t D, float* loss,
                          float* lse, char* ws, hipStream_t s)
 {
-    const Plan p = make_plan<I, E>(POSEIDON_XENT_FORWARD, X, W, T, V, D, ws);
+    const Plan p = make_plan<E>(POSEIDON_XENT_FORWARD, X, W, T, V, D, ws);
     Operand x, w;
-    POSEIDON_TRY((operands<I, E>(p, X, W, nullptr, T, V, D, x, w, s)));
+    POSEIDON_TRY(operands(p, X, W, nullptr, T, V, D, x, w, s));
     if (!p.few)
         return losses<E>(p, x, w, target, T, V, D, loss, lse, s);
     POSEIDON_TRY(row_logits<E>(p, x, w, T, V, D, s));
@@ -1038,12 +1025,12 @@ hipError_t forward_typed(const I* X, const I* W, const int64_t* target, int64_t 
 }
 
 // dX = G W for one piece of the vocabulary (the first replaces, the others add).
-template <typename I, typename E>
+template <typename E>
 hipError_t input_gradient(const Plan& p, const Operand& g, const Operand& w, const Operand& whole_w,
-                          const int64_t* target, int64_t T, int64_t V, int64_t D, int64_t v0, int64_t vp, I* dX,
+                          const int64_t* target, int64_t T, int64_t V, int64_t D, int64_t v0, int64_t vp, E* dX,
                           hipStream_t s)
 {
-    constexpr bool BF16 = sizeof(I) == 2;
+    constexpr bool BF16 = sizeof(E) == 2;
     const bool first = v0 == 0, last = v0 + vp == V;
     const Choice& c = vp == std::min(p.piece, V) ? p.full.dx : p.last.dx;
     Out o{};
@@ -1059,12 +1046,12 @@ hipError_t input_gradient(const Plan& p, const Operand& g, const Operand& w, con
         o.W = whole_w.p;
         o.ldw = whole_w.ld;
     }
-    POSEIDON_TRY((product<E, true, false, STORE>(c, g, w, p.dx_parts, o, T, D, whole_chunks<E>(vp), s)));
+    POSEIDON_TRY((product<E, true, false, STORE>(c, g, w, ONE, o, T, D, whole_chunks<E>(vp), s)));
     return last && p.dx ? join_splits(p.dx, p.full.dx.splits, T * D, dX, s) : hipSuccess;
 }
 
 // G of the classes v0 .. v0 + vp.
-template <typename I, typename E>
+template <typename E>
 hipError_t logit_gradient(const Plan& p, const Operand& x, const Operand& w, const int64_t* target, const float* lse,
                           const float* dloss, int64_t T, int64_t V, int64_t D, int64_t v0, int64_t vp, hipStream_t s)
 {
@@ -1077,25 +1064,25 @@ hipError_t logit_gradient(const Plan& p, const Operand& x, const Operand& w, con
     o.g_plane = T * p.ldg;
     o.v0 = v0;
     o.V = V;
-    o.target_rest = sizeof(I) == 2 ? p.target_rest : nullptr;
+    o.target_rest = sizeof(E) == 2 ? p.target_rest : nullptr;
     const Choice& c = vp == std::min(p.piece, V) ? p.full.logits : p.last.logits;
-    return product<E, true, true, GRAD>(c, x, w, p.logits_parts, o, T, vp, k_of(p, D), s);
+    return product<E, true, true, GRAD>(c, x, w, ONE, o, T, vp, D, s);
 }
 
-template <typename I, typename E>
-hipError_t backward_typed(const I* X, const I* W, const int64_t* target, const float* lse, const float* dloss,
-                          int64_t T, int64_t V, int64_t D, I* dX, float* dW, char* ws, hipStream_t s)
+template <typename E>
+hipError_t backward_typed(const E* X, const E* W, const int64_t* target, const float* lse, const float* dloss,
+                          int64_t T, int64_t V, int64_t D, E* dX, float* dW, char* ws, hipStream_t s)
 {
-    const Plan p = make_plan<I, E>(POSEIDON_XENT_BACKWARD, X, W, T, V, D, ws);
+    const Plan p = make_plan<E>(POSEIDON_XENT_BACKWARD, X, W, T, V, D, ws);
     Operand x, w;
-    POSEIDON_TRY((operands<I, E>(p, X, W, target, T, V, D, x, w, s)));
+    POSEIDON_TRY(operands(p, X, W, target, T, V, D, x, w, s));
     const Operand g{p.g, p.ldg, T, T * p.ldg};
     for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
         const int64_t vp = std::min(p.piece, V - v0);
-        const Operand wp{static_cast<const E*>(w.p) + v0 * w.ld, w.ld, vp, w.plane};
+        const Operand wp{static_cast<const E*>(w.p) + v0 * w.ld, w.ld, vp, 0};
         if (T > 0) {
-            POSEIDON_TRY((logit_gradient<I, E>(p, x, wp, target, lse, dloss, T, V, D, v0, vp, s)));
-            POSEIDON_TRY((input_gradient<I, E>(p, g, wp, w, target, T, V, D, v0, vp, dX, s)));
+            POSEIDON_TRY((logit_gradient<E>(p, x, wp, target, lse, dloss, T, V, D, v0, vp, s)));
+            POSEIDON_TRY((input_gradient<E>(p, g, wp, w, target, T, V, D, v0, vp, dX, s)));
         }
         const Choice& c = vp == std::min(p.piece, V) ? p.full.dw : p.last.dw;
         const bool sums = c.splits > 1;
@@ -1103,20 +1090,20 @@ hipError_t backward_typed(const I* X, const I* W, const int64_t* target, const f
         o.c = sums ? p.dw : dW + v0 * D;
         o.ldc = D;
         o.split_stride = vp * D;
-        POSEIDON_TRY((product<E, false, false, STORE>(c, g, x, p.dw_parts, o, vp, D, T, s)));
+        POSEIDON_TRY((product<E, false, false, STORE>(c, g, x, DW_PARTS<E>, o, vp, D, T, s)));
         if (sums)
             POSEIDON_TRY(join_splits(p.dw, c.splits, vp * D, dW + v0 * D, s));
     }
     return hipSuccess;
 }
 
-template <typename I, typename E>
-hipError_t factor_typed(const I* X, const I* W, const int64_t* target, const float* dloss, int64_t T, int64_t V,
-                        int64_t D, float* loss, float* U, I* dX, char* ws, hipStream_t s)
+template <typename E>
+hipError_t factor_typed(const E* X, const E* W, const int64_t* target, const float* dloss, int64_t T, int64_t V,
+                        int64_t D, float* loss, float* U, E* dX, char* ws, hipStream_t s)
 {
-    const Plan p = make_plan<I, E>(POSEIDON_XENT_FACTOR, X, W, T, V, D, ws);
+    const Plan p = make_plan<E>(POSEIDON_XENT_FACTOR, X, W, T, V, D, ws);
     Operand x, w;
-    POSEIDON_TRY((operands<I, E>(p, X, W, nullptr, T, V, D, x, w, s)));
+    POSEIDON_TRY(operands(p, X, W, nullptr, T, V, D, x, w, s));
     if (p.few) {
         POSEIDON_TRY(row_logits<E>(p, x, w, T, V, D, s));
         POSEIDON_TRY((rows_done<E, true>(p, target, dloss, T, V, loss, nullptr, U, s)));
@@ -1129,34 +1116,21 @@ hipError_t factor_typed(const I* X, const I* W, const int64_t* target, const flo
         o.target = target;
         o.c = U;
         o.ldc = V;
-        POSEIDON_TRY((product<E, true, true, LOGITS>(p.logits, x, w, p.logits_parts, o, T, V, k_of(p, D), s)));
+        POSEIDON_TRY((product<E, true, true, LOGITS>(p.logits, x, w, ONE, o, T, V, D, s)));
         POSEIDON_TRY(join_runs(p, target, T, V, loss, p.lse, s));
-        factor_kernel<E, sizeof(I) == 4 && sizeof(E) == 2 ? 3 : 1>
-            <<<grid_for(ceil_div(T * (p.ldg / GROUP), THREADS)), THREADS, 0, s>>>(
-                p.lse, target, dloss, T, V, U, static_cast<E*>(p.g), p.ldg, p.target_rest);
+        factor_kernel<E><<<grid_for(ceil_div(T * (p.ldg / GROUP), THREADS)), THREADS, 0, s>>>(
+            p.lse, target, dloss, T, V, U, static_cast<E*>(p.g), p.ldg, p.target_rest);
         POSEIDON_TRY(hipGetLastError());
     }
-    return input_gradient<I, E>(p, Operand{p.g, p.ldg, T, T * p.ldg}, w, w, target, T, V, D, 0, V, dX, s);
-}
-
-// fp32 by six bf16 products at 1250 TFLOP/s (the splitting of X and W, ten
-// bytes a value, at 4 TB/s) or as it is at 125.
-bool in_parts(int op, int64_t T, int64_t V, int64_t D)
-{
-    const double flops = 2.0 * static_cast<double>(T) * static_cast<double>(V) * static_cast<double>(D) *
-                         (op == POSEIDON_XENT_FORWARD ? 1 : op == POSEIDON_XENT_BACKWARD ? 3 : 2);
-    const double bytes = 10.0 * static_cast<double>(T + V) * static_cast<double>(D);
-    return T > FEW_ROWS && flops * (6 / 1.25e15) + bytes / 4e12 < flops / 1.25e14;
+    return input_gradient<E>(p, Operand{p.g, p.ldg, T, T * p.ldg}, w, w, target, T, V, D, 0, V, dX, s);
 }
 
 }  // namespace
 
 int64_t xent_workspace(int32_t op, const void* X, const void* W, int64_t T, int64_t V, int64_t D, int32_t dtype)
 {
-    if (dtype == POSEIDON_BF16)
-        return make_plan<__bf16, __bf16>(op, X, W, T, V, D, nullptr).bytes;
-    return in_parts(op, T, V, D) ? make_plan<float, __bf16>(op, X, W, T, V, D, nullptr).bytes
-                                 : make_plan<float, float>(op, X, W, T, V, D, nullptr).bytes;
+    return dtype == POSEIDON_BF16 ? make_plan<__bf16>(op, X, W, T, V, D, nullptr).bytes
+                                  : make_plan<float>(op, X, W, T, V, D, nullptr).bytes;
 }
 
 hipError_t launch_xent_forward(const void* X, const void* W, const int64_t* target, int64_t T, int64_t V, int64_t D,
@@ -1164,10 +1138,9 @@ hipError_t launch_xent_forward(const void* X, const void* W, const int64_t* targ
 {
     char* w = static_cast<char*>(ws);
     if (dtype == POSEIDON_BF16)
-        return forward_typed<__bf16, __bf16>(static_cast<const __bf16*>(X), static_cast<const __bf16*>(W), target, T,
+        return forward_typed(static_cast<const __bf16*>(X), static_cast<const __bf16*>(W), target, T,
                                              V, D, loss, lse, w, stream);
-    auto* f = in_parts(POSEIDON_XENT_FORWARD, T, V, D) ? forward_typed<float, __bf16> : forward_typed<float, float>;
-    return f(static_cast<const float*>(X), static_cast<const float*>(W), target, T, V, D, loss, lse, w, stream);
+    return forward_typed(static_cast<const float*>(X), static_cast<const float*>(W), target, T, V, D, loss, lse, w, stream);
 }
 
 hipError_t launch_xent_backward(const void* X, const void* W, const int64_t* target, const float* lse,
@@ -1176,10 +1149,9 @@ hipError_t launch_xent_backward(const void* X, const void* W, const int64_t* tar
 {
     char* w = static_cast<char*>(ws);
     if (dtype == POSEIDON_BF16)
-        return backward_typed<__bf16, __bf16>(static_cast<const __bf16*>(X), static_cast<const __bf16*>(W), target,
+        return backward_typed(static_cast<const __bf16*>(X), static_cast<const __bf16*>(W), target,
                                               lse, dloss, T, V, D, static_cast<__bf16*>(dX), dW, w, stream);
-    auto* f = in_parts(POSEIDON_XENT_BACKWARD, T, V, D) ? backward_typed<float, __bf16> : backward_typed<float, float>;
-    return f(static_cast<const float*>(X), static_cast<const float*>(W), target, lse, dloss, T, V, D,
+    return backward_typed(static_cast<const float*>(X), static_cast<const float*>(W), target, lse, dloss, T, V, D,
              static_cast<float*>(dX), dW, w, stream);
 }
 
@@ -1189,10 +1161,9 @@ hipError_t launch_xent_factor(const void* X, const void* W, const int64_t* targe
 {
     char* w = static_cast<char*>(ws);
     if (dtype == POSEIDON_BF16)
-        return factor_typed<__bf16, __bf16>(static_cast<const __bf16*>(X), static_cast<const __bf16*>(W), target,
+        return factor_typed(static_cast<const __bf16*>(X), static_cast<const __bf16*>(W), target,
                                             dloss, T, V, D, loss, U, static_cast<__bf16*>(dX), w, stream);
-    auto* f = in_parts(POSEIDON_XENT_FACTOR, T, V, D) ? factor_typed<float, __bf16> : factor_typed<float, float>;
-    return f(static_cast<const float*>(X), static_cast<const float*>(W), target, dloss, T, V, D, loss, U,
+    return factor_typed(static_cast<const float*>(X), static_cast<const float*>(W), target, dloss, T, V, D, loss, U,
              static_cast<float*>(dX), w, stream);
 }
 
