@@ -129,6 +129,14 @@ __device__ __forceinline__ void finish_stats(acc4 (&acc)[T::TM][T::TN], const Ou
                                              int64_t block, int rows, int cols, int wm, int wn, int lane)
 {
     const int first = wn + 4 * (lane >> 4);   // the lane's columns: first + 16 j + r
+    // What the rows need from memory is asked for at once: a wait per row
+    // block was most of an epilogue's time.
+    int64_t target[T::TM];
+#pragma unroll
+    for (int i = 0; i < T::TM; ++i) {
+        const int m = wm + 16 * i + (lane & 15);
+        target[i] = m < rows ? o.target[m0 + m] : -1;
+    }
 #pragma unroll
     for (int i = 0; i < T::TM; ++i) {
         const int m = wm + 16 * i + (lane & 15);
@@ -160,7 +168,7 @@ __device__ __forceinline__ void finish_stats(acc4 (&acc)[T::TM][T::TN], const Ou
             // from / log2 e: join() and the last logarithm put it back.
             if (lane < 16)
                 o.part[at * o.nparts + block] = Run{top == -INFINITY ? -INFINITY : from, sum};
-            const int64_t t = o.target[at] - n0 - first;
+            const int64_t t = target[i] - n0 - first;
             if (t >= 0 && t < T::WN) {
 #pragma unroll
                 for (int j = 0; j < T::TN; ++j)
@@ -189,14 +197,24 @@ __device__ __forceinline__ void finish_grad(acc4 (&acc)[T::TM][T::TN], const Out
     // The lane's columns: first + STRIDE j + r.
     constexpr int STRIDE = T::SPREAD ? 4 : 16;
     const int first = wn + (T::SPREAD ? 16 : 4) * (lane >> 4);
+    int64_t target[T::TM];
+    float lses[T::TM], dlosses[T::TM];
+#pragma unroll
+    for (int i = 0; i < T::TM; ++i) {
+        const int m = wm + 16 * i + (lane & 15);
+        const int64_t at = m0 + (m < rows ? m : 0);
+        target[i] = o.target[at];
+        lses[i] = o.lse[at];
+        dlosses[i] = o.dloss[at];
+    }
 #pragma unroll
     for (int i = 0; i < T::TM; ++i) {
         const int m = wm + 16 * i + (lane & 15);
         if (m >= rows)
             continue;
-        const int64_t at = m0 + m, t = o.target[at];
+        const int64_t at = m0 + m, t = target[i];
         const bool has = counts(t, o.V);
-        const float lse = has ? o.lse[at] : 0.f, d = has ? o.dloss[at] : 0.f;
+        const float lse = has ? lses[i] : 0.f, d = has ? dlosses[i] : 0.f;
         const float from = lse * LOG2E;
         const float rest = fmaf(lse, LOG2E, -from) + lse * LOG2E_REST;
         const float scale = has ? fmaf(d, -rest * LN2, d) : 0.f;
@@ -256,6 +274,18 @@ __device__ __forceinline__ void finish_store(acc4 (&acc)[T::TM][T::TN], const Ou
                                              int cols, int wm, int wn, int lane, int z)
 {
     const int first = wn + 4 * (lane >> 4);
+    int64_t target[T::TM];
+    float rests[T::TM];
+    const bool mend = o.target_rest && z == 0;
+    if (mend) {
+#pragma unroll
+        for (int i = 0; i < T::TM; ++i) {
+            const int m = wm + 16 * i + (lane & 15);
+            const int64_t at = m0 + (m < rows ? m : 0);
+            target[i] = o.target[at];
+            rests[i] = o.target_rest[at];
+        }
+    }
 #pragma unroll
     for (int i = 0; i < T::TM; ++i) {
         const int m = wm + 16 * i + (lane & 15);
@@ -264,9 +294,9 @@ __device__ __forceinline__ void finish_store(acc4 (&acc)[T::TM][T::TN], const Ou
         const int64_t at = m0 + m;
         float rest = 0.f;
         const typename T::M* w = nullptr;
-        if (o.target_rest && z == 0 && counts(o.target[at], o.V)) {
-            rest = o.target_rest[at];
-            w = static_cast<const typename T::M*>(o.W) + o.target[at] * o.ldw + n0 + first;
+        if (mend && counts(target[i], o.V)) {
+            rest = rests[i];
+            w = static_cast<const typename T::M*>(o.W) + target[i] * o.ldw + n0 + first;
         }
 #pragma unroll
         for (int j = 0; j < T::TN; ++j) {
@@ -923,7 +953,9 @@ Plan make_plan(int op, const void* X, const void* W, int64_t T, int64_t V, int64
         if (dw_sums > 0)
             p.dw = static_cast<float*>(a.take(dw_sums * D * 4));
     }
-    p.ldg = p.piece;
+    // Rows of a multiple of 4 KB would put the 16 rows of a store on one memory
+    // channel (G of 4096 x 16384, in parts: 222 us, with 512 bytes more 200).
+    p.ldg = p.piece + (p.piece * (SZ == 4 ? 4 : 2) % 4096 == 0 ? 512 / SZ : 0);
     p.g = a.take(T * p.ldg * g_value);
     p.target_rest = static_cast<float*>(a.take(T * 4));
     if (p.full.dx.splits > 1 || (p.piece < V && SZ == 2))
