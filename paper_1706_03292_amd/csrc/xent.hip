@@ -50,11 +50,11 @@ __device__ __forceinline__ bool counts(int64_t target, int64_t V) { return targe
 // What a tile does with its sums.  acc[i][j][r] of lane l is row
 // m0 + 16 i + l % 16, column n0 + 16 j + 4 (l / 16) + r.
 // ---------------------------------------------------------------------------
-enum Use { STATS, LOGITS, GRAD, STORE };
+enum Use { STATS, GRAD, STORE };
 
 struct Out {
-    // STATS, LOGITS: per row and column block the running maximum and sum, and
-    // the target's logit; LOGITS also the logits (`c`, ldc apart).
+    // STATS: per row and column block the running maximum and sum, and the
+    // target's logit.
     Run* part;
     int64_t nparts;
     float* target_logit;
@@ -121,10 +121,10 @@ __device__ __forceinline__ f2 rest_of_pair(float a, float b, unsigned p)
     return f2{a - __builtin_bit_cast(float, p << 16), b - __builtin_bit_cast(float, p & 0xffff0000u)};
 }
 
-// STATS, LOGITS.  A row's maximum and the sum of exponentials below it over
+// STATS.  A row's maximum and the sum of exponentials below it over
 // the wave's columns: in a lane first, then across the four lanes that share
 // the row.
-template <typename T, bool EDGE, bool KEEP>
+template <typename T, bool EDGE>
 __device__ __forceinline__ void finish_stats(acc4 (&acc)[T::TM][T::TN], const Out& o, int64_t m0, int64_t n0,
                                              int64_t block, int rows, int cols, int wm, int wn, int lane)
 {
@@ -177,12 +177,6 @@ __device__ __forceinline__ void finish_stats(acc4 (&acc)[T::TM][T::TN], const Ou
                         if (t == 16 * j + r && (!EDGE || first + 16 * j + r < cols))
                             o.target_logit[at] = acc[i][j][r];
             }
-            if constexpr (KEEP)
-#pragma unroll
-                for (int j = 0; j < T::TN; ++j)
-                    if (!EDGE || first + 16 * j < cols)
-                        put4(static_cast<float*>(o.c) + at * o.ldc + n0 + first + 16 * j, acc[i][j],
-                             EDGE ? cols - first - 16 * j : 4);
         }
     }
 }
@@ -217,13 +211,14 @@ __device__ __forceinline__ void finish_grad(acc4 (&acc)[T::TM][T::TN], const Out
         const float lse = has ? lses[i] : 0.f, d = has ? dlosses[i] : 0.f;
         const float from = lse * LOG2E;
         const float rest = fmaf(lse, LOG2E, -from) + lse * LOG2E_REST;
-        const float scale = has ? fmaf(d, -rest * LN2, d) : 0.f;
+        const float scale = fmaf(d, -rest * LN2, d);
 #pragma unroll
         for (int j = 0; j < T::TN; ++j)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const float g = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], LOG2E, -from)) * scale;
-                acc[i][j][r] = EDGE && first + STRIDE * j + r >= cols ? 0.f : g;   // past V: zeros
+                // Rows without a target and, up to the row's end, past V: zeros.
+                acc[i][j][r] = has && (!EDGE || first + STRIDE * j + r < cols) ? g : 0.f;
             }
         const int64_t tl = t - o.v0 - n0 - first;
         if (has && tl >= 0 && tl < T::WN) {
@@ -336,12 +331,12 @@ __device__ __forceinline__ void finish(acc4 (&acc)[T::TM][T::TN], const Out& o, 
     const int rows = static_cast<int>(M - m0 < T::BM ? M - m0 : T::BM);
     const int cols = static_cast<int>(N - n0 < T::BN ? N - n0 : T::BN);
     const bool edge = cols < T::BN;
-    if constexpr (USE == STATS || USE == LOGITS) {
+    if constexpr (USE == STATS) {
         const int64_t block = tile_n * T::NWN + w % T::NWN;
         if (edge)
-            finish_stats<T, true, USE == LOGITS>(acc, o, m0, n0, block, rows, cols, wm, wn, lane);
+            finish_stats<T, true>(acc, o, m0, n0, block, rows, cols, wm, wn, lane);
         else
-            finish_stats<T, false, USE == LOGITS>(acc, o, m0, n0, block, rows, cols, wm, wn, lane);
+            finish_stats<T, false>(acc, o, m0, n0, block, rows, cols, wm, wn, lane);
     } else if constexpr (USE == GRAD) {
         if (edge)
             finish_grad<T, true>(acc, o, m0, n0, rows, cols, wm, wn, lane);
@@ -355,14 +350,48 @@ __device__ __forceinline__ void finish(acc4 (&acc)[T::TM][T::TN], const Out& o, 
     }
 }
 
-// Rows m_first to M in tiles over k split gridDim.y ways (k_split values each, a multiple of
-// the step).
+// A matrix copied with its rows padded to ldo values (zeros), rows without a
+// target (where a target list is given) cleared.
+struct RowCopy {
+    const void* x;
+    int64_t rows, cols, ldo;
+    const int64_t* target;
+    int64_t V;
+    void* out;
+};
+
+template <typename E>
+__device__ __forceinline__ void copy_rows(const RowCopy& o, int64_t first, int64_t step)
+{
+    const int64_t per_row = o.ldo / GROUP, groups = o.rows * per_row;
+    for (int64_t q = first; q < groups; q += step) {
+        const int64_t row = q / per_row, c = (q - row * per_row) * GROUP;
+        float v[GROUP];
+        load_some(static_cast<const E*>(o.x) + row * o.cols + c, o.cols - c, v);
+        if (o.target && !counts(o.target[row], o.V))
+#pragma unroll
+            for (int i = 0; i < GROUP; ++i)
+                v[i] = 0.f;
+        store_group(static_cast<E*>(o.out) + row * o.ldo + c, v);
+    }
+}
+
+// Rows m_first to M in tiles over k split gridDim.y ways (k_split values each, a
+// multiple of the step).  GRAD: workgroups past the tiles make the copy of X
+// that dW's product reads, which would otherwise be a launch of its own.
 template <typename T, Use USE>
 __global__ __launch_bounds__(T::NT, 2) void product_kernel(Operand a, Operand b, Parts parts, Out o,
                                                            int64_t m_first, int64_t M, int64_t N, int64_t K,
                                                            int64_t k_split, int64_t tiles_m, int64_t tiles_n,
-                                                           int group)
+                                                           int group, RowCopy copy)
 {
+    if constexpr (USE == GRAD) {
+        const int64_t over = static_cast<int64_t>(blockIdx.x) - tiles_m * tiles_n;
+        if (over >= 0) {
+            copy_rows<typename T::M>(copy, over * T::NT + threadIdx.x, (gridDim.x - tiles_m * tiles_n) * T::NT);
+            return;
+        }
+    }
     int64_t tm, tn;
     tile_of(blockIdx.x, tiles_m, tiles_n, group, tm, tn);
     const int64_t k0 = blockIdx.y * k_split;
@@ -411,181 +440,222 @@ __global__ __launch_bounds__(THREADS) void loss_kernel(const Run* __restrict__ p
     }
 }
 
-// One workgroup a row, where the rows are few: the row's logits are the sums of
-// the product's splits of k; their loss, lse and (given U) G, as U and as the
-// operand of dX (bf16 or fp32, ldg apart, zeros past V).  A thread holds EACH
-// groups of four neighbours; rows longer than 32768 go through memory: the
-// sums replace the first split's and are read again.  What bounds it is one
-// CU's reading of its row: all loads of a split are in flight together.
-constexpr int ROW_THREADS = 1024;
+// The factor form, and the forward pass where the rows are few: the logits are
+// the sums of the product's splits of k, and pass through memory (in the factor
+// form G replaces them in U).  Rows of up to ROW_MOST values are a workgroup's:
+// a thread holds EACH groups of four neighbours, and all loads of a split are
+// in flight together.  Longer rows go in chunks, so that a few of them fill the
+// GPU too: one kernel leaves every chunk's run, another joins a row's runs and
+// turns each chunk into G.
+constexpr int64_t ROW_MOST = 16384;
+constexpr int CHUNK_EACH = 4, CHUNK = THREADS * 4 * CHUNK_EACH;
 
-// n values at p, past them -inf (logits) or 0.
-__device__ __forceinline__ acc4 get4(const float* p, int64_t n, float past)
+// n values at p, past them `past`.
+__device__ __forceinline__ acc4 get4(const float* p, int n, float past)
 {
-    if (n >= 4)
-        return *reinterpret_cast<const f4a*>(p);
-    acc4 v;
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-        v[r] = r < n ? p[r] : past;
+    acc4 v = {past, past, past, past};
+    if (n >= 4) {
+        v = *reinterpret_cast<const f4a*>(p);
+    } else if (n > 0) {
+        v[0] = p[0];
+        if (n > 1)
+            v[1] = p[1];
+        if (n > 2)
+            v[2] = p[2];
+    }
     return v;
 }
 
-template <typename G, int EACH, bool FACTOR>
-__global__ __launch_bounds__(ROW_THREADS) void row_kernel(float* __restrict__ logits, int splits, int64_t stride,
-                                                          const int64_t* __restrict__ target,
-                                                          const float* __restrict__ dloss, int64_t V,
-                                                          float* __restrict__ loss, float* __restrict__ lse_out,
-                                                          float* __restrict__ U, G* __restrict__ g, int64_t ldg,
-                                                          float* __restrict__ target_rest)
+// EACH groups of a row's (or chunk's) n logits from s on, the splits' sums, past
+// n -inf; and the run of what the thread holds.
+template <int NT, int EACH>
+__device__ __forceinline__ Run held_logits(const float* s, int n, int splits, int64_t stride, acc4 (&held)[EACH])
 {
-    constexpr bool HELD = EACH > 0;
-    __shared__ Run runs[ROW_THREADS / 64];
-    const int64_t row = blockIdx.x;
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    float* s = logits + row * V;
-    const int64_t t = target[row];
-    const bool has = counts(t, V);
-    const float d = FACTOR && has ? dloss[row] : 0.f;
-    acc4 held[HELD ? EACH : 1];
-    Run r{-INFINITY, 0.f};
-    auto place = [&](int e) { return 4 * (threadIdx.x + static_cast<int64_t>(e) * ROW_THREADS); };
-    auto add = [&](acc4& x) {
-        float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) * LOG2E;
-        const float from = top == -INFINITY ? 0.f : top;
-        float sum = 0.f;
+    const int at = 4 * static_cast<int>(threadIdx.x);
+#pragma unroll
+    for (int e = 0; e < EACH; ++e)
+        held[e] = get4(s + at + 4 * NT * e, n - at - 4 * NT * e, -INFINITY);
+    for (int z = 1; z < splits; ++z) {
+        acc4 x[EACH];
+#pragma unroll
+        for (int e = 0; e < EACH; ++e)
+            x[e] = get4(s + z * stride + at + 4 * NT * e, n - at - 4 * NT * e, 0.f);
+#pragma unroll
+        for (int e = 0; e < EACH; ++e)
+            held[e] += x[e];
+    }
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            sum += __builtin_amdgcn_exp2f(fmaf(x[i], LOG2E, -from));   // past V: 0
-        r = join(r, Run{top, sum});
-    };
-    if constexpr (HELD) {
+            top = fmaxf(top, held[e][i]);
+    top *= LOG2E;
+    const float from = top == -INFINITY ? 0.f : top;
 #pragma unroll
-        for (int e = 0; e < EACH; ++e)
-            held[e] = get4(s + place(e), V - place(e), -INFINITY);
-#pragma unroll 2
-        for (int z = 1; z < splits; ++z) {
-            acc4 x[EACH];
+    for (int e = 0; e < EACH; ++e)
 #pragma unroll
-            for (int e = 0; e < EACH; ++e)
-                x[e] = get4(s + z * stride + place(e), V - place(e), 0.f);
-#pragma unroll
-            for (int e = 0; e < EACH; ++e)
-                held[e] += x[e];
-        }
-#pragma unroll
-        for (int e = 0; e < EACH; ++e)
-            add(held[e]);
-    } else {
-        for (int64_t v = place(0); v < V; v += 4 * ROW_THREADS) {
-            acc4 x = get4(s + v, V - v, -INFINITY);
-            for (int z = 1; z < splits; ++z)
-                x += get4(s + z * stride + v, V - v, 0.f);
-            put4(s + v, x, static_cast<int>(V - v < 4 ? V - v : 4));
-            add(x);
-        }
-    }
+        for (int i = 0; i < 4; ++i)
+            sum += __builtin_amdgcn_exp2f(fmaf(held[e][i], LOG2E, -from));   // past n: 0
+    return Run{top, sum};
+}
+
+template <int NT>
+__device__ __forceinline__ Run group_join(Run r)
+{
+    __shared__ Run runs[NT / 64];
     r = wave_join(r);
-    if (lane == 0)
-        runs[w] = r;
+    __syncthreads();   // the row before has read its runs
+    if ((threadIdx.x & 63) == 0)
+        runs[threadIdx.x >> 6] = r;
     __syncthreads();
-    r = lane < ROW_THREADS / 64 ? runs[lane] : Run{-INFINITY, 0.f};
-    r = wave_join(r);
-    const float lse = lse_of(r);
-    if (threadIdx.x == 0) {
-        if (lse_out)
-            lse_out[row] = lse;
-        if (!has)
-            loss[row] = 0.f;
+    return wave_join((threadIdx.x & 63) < NT / 64 ? runs[threadIdx.x & 63] : Run{-INFINITY, 0.f});
+}
+
+// What turns a row's logits into G (as finish_grad does).
+struct RowGrad {
+    bool has;
+    float from, scale, dloss;
+    __device__ __forceinline__ RowGrad(bool has_, float lse, float d)
+    {
+        has = has_;
+        dloss = d;
+        from = has ? lse * LOG2E : 0.f;
+        const float rest = fmaf(lse, LOG2E, -from) + lse * LOG2E_REST;
+        scale = has ? fmaf(d, -rest * LN2, d) : 0.f;
     }
-    const float from = has ? lse * LOG2E : 0.f;
-    const float rest = fmaf(lse, LOG2E, -from) + lse * LOG2E_REST;
-    const float scale = has ? fmaf(d, -rest * LN2, d) : 0.f;
-    auto done = [&](int64_t v, acc4 x) {
-        const bool hit = has && t >= v && t < v + 4;
-        if (hit) {
+};
+
+// Four of a row's values from column v on: G to U and to the operand of dX (bf16
+// or fp32; `g` up to ldg values, zeros past V).
+template <typename G>
+__device__ __forceinline__ void put_grad(const RowGrad& q, acc4 x, int v, int V, int ldg, int64_t target, float* U,
+                                         G* g, float* target_rest)
+{
+    const int64_t hit = q.has ? target - v : -1;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (t == v + i)
-                    loss[row] = lse - x[i];
+    for (int i = 0; i < 4; ++i) {
+        x[i] = q.has && v + i < V ? __builtin_amdgcn_exp2f(fmaf(x[i], LOG2E, -q.from)) * q.scale : 0.f;
+        if (hit == i) {
+            x[i] -= q.dloss;
+            *target_rest = x[i] - static_cast<float>(static_cast<G>(x[i]));
         }
-        if constexpr (FACTOR) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[i] = has && v + i < V ? __builtin_amdgcn_exp2f(fmaf(x[i], LOG2E, -from)) * scale : 0.f;
-                if (hit && t == v + i) {
-                    x[i] -= d;
-                    target_rest[row] = x[i] - static_cast<float>(static_cast<G>(x[i]));
-                }
-            }
-            if (v < V)
-                put4(U + row * V + v, x, static_cast<int>(V - v < 4 ? V - v : 4));
-            if (v < ldg) {   // ldg: a multiple of eight
-                if constexpr (sizeof(G) == 2)
-                    *reinterpret_cast<b4*>(g + row * ldg + v) = __builtin_convertvector(x, b4);
-                else
-                    *reinterpret_cast<acc4*>(g + row * ldg + v) = x;
-            }
-        }
-    };
-    if constexpr (HELD) {
-#pragma unroll
-        for (int e = 0; e < EACH; ++e)
-            done(place(e), held[e]);
-    } else {
-        for (int64_t v = place(0); v < V || (FACTOR && v < ldg); v += 4 * ROW_THREADS)
-            done(v, v < V ? get4(s + v, V - v, -INFINITY) : acc4{0.f, 0.f, 0.f, 0.f});
+    }
+    if (v < V)
+        put4(U + v, x, V - v);
+    if (v < ldg) {   // ldg: a multiple of eight
+        if constexpr (sizeof(G) == 2)
+            *reinterpret_cast<b4*>(g + v) = __builtin_convertvector(x, b4);
+        else
+            *reinterpret_cast<acc4*>(g + v) = x;
     }
 }
 
-// Many rows: G from the logits in U and their lse, in place and as the operand
-// of dX (bf16 or fp32, ldg apart, zeros past V).
-template <typename E>
-__global__ __launch_bounds__(THREADS) void factor_kernel(const float* __restrict__ lse,
-                                                         const int64_t* __restrict__ target,
-                                                         const float* __restrict__ dloss, int64_t T, int64_t V,
-                                                         float* __restrict__ U, E* __restrict__ g, int64_t ldg,
-                                                         float* __restrict__ target_rest)
+template <typename G, int NT, int EACH, bool FACTOR>
+__global__ __launch_bounds__(NT) void row_kernel(const float* logits, int splits, int64_t T, int64_t stride,
+                                                 const int64_t* __restrict__ target, const float* __restrict__ dloss,
+                                                 int V, float* __restrict__ loss, float* __restrict__ lse_out,
+                                                 float* U, G* __restrict__ g, int ldg, float* __restrict__ target_rest)
 {
-    const int64_t per_row = ldg / GROUP, step = static_cast<int64_t>(gridDim.x) * THREADS;
-    for (int64_t q = static_cast<int64_t>(blockIdx.x) * THREADS + threadIdx.x; q < T * per_row; q += step) {
-        const int64_t row = q / per_row, c = (q - row * per_row) * GROUP, t = target[row];
+    const int at = 4 * static_cast<int>(threadIdx.x);
+    for (int64_t row = blockIdx.x; row < T; row += gridDim.x) {
+        acc4 held[EACH];
+        const int64_t t = target[row];
         const bool has = counts(t, V);
-        const float l = has ? lse[row] : 0.f, d = has ? dloss[row] : 0.f, from = l * LOG2E;
-        const float rest = fmaf(l, LOG2E, -from) + l * LOG2E_REST, scale = has ? fmaf(d, -rest * LN2, d) : 0.f;
-        float v[GROUP];
-        load_some(U + row * V + c, V - c, v);
-#pragma unroll
-        for (int i = 0; i < GROUP; ++i) {
-            v[i] = has && c + i < V ? __builtin_amdgcn_exp2f(fmaf(v[i], LOG2E, -from)) * scale : 0.f;
-            if (has && c + i == t) {
-                v[i] -= d;
-                target_rest[row] = v[i] - static_cast<float>(static_cast<E>(v[i]));
-            }
+        const float d = FACTOR && has ? dloss[row] : 0.f;
+        const float lse = lse_of(group_join<NT>(held_logits<NT, EACH>(logits + row * V, V, splits, stride, held)));
+        if (threadIdx.x == 0) {
+            if (!FACTOR)
+                lse_out[row] = lse;
+            if (!has)
+                loss[row] = 0.f;
         }
-        store_some(U + row * V + c, V - c, v);
-        store_group(g + row * ldg + c, v);
+        const RowGrad q(has, lse, d);
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const int v = at + 4 * NT * e;
+            if (has && t >= v && t < v + 4) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (t == v + i)
+                        loss[row] = lse - held[e][i];
+            }
+            if constexpr (FACTOR)
+                put_grad(q, held[e], v, V, ldg, t, U + row * V, g + row * ldg, target_rest + row);
+        }
     }
 }
 
-// A matrix copied with its rows padded to ldo values (zeros), rows without a
-// target (where a target list is given) cleared.
-template <typename E>
-__global__ __launch_bounds__(THREADS) void lay_out_kernel(const E* __restrict__ x, int64_t rows, int64_t cols,
-                                                          int64_t ldo, const int64_t* __restrict__ target, int64_t V,
-                                                          E* __restrict__ out)
+// A chunk's run; in the factor form of several splits also their sums, to U.
+template <bool FACTOR>
+__global__ __launch_bounds__(THREADS) void chunk_kernel(const float* logits, int splits, int64_t T, int64_t stride,
+                                                        int chunks, const int64_t* __restrict__ target, int V,
+                                                        Run* __restrict__ part, float* __restrict__ target_logit,
+                                                        float* U)
 {
-    const int64_t per_row = ldo / GROUP, groups = rows * per_row, step = static_cast<int64_t>(gridDim.x) * THREADS;
-    for (int64_t q = static_cast<int64_t>(blockIdx.x) * THREADS + threadIdx.x; q < groups; q += step) {
-        const int64_t row = q / per_row, c = (q - row * per_row) * GROUP;
-        float v[GROUP];
-        load_some(x + row * cols + c, cols - c, v);
-        if (target && !counts(target[row], V))
+    const int at = 4 * static_cast<int>(threadIdx.x);
+    for (int64_t b = blockIdx.x; b < T * chunks; b += gridDim.x) {
+        const int64_t row = b / chunks, from = (b - row * chunks) * CHUNK;
+        const int n = static_cast<int>(V - from < CHUNK ? V - from : CHUNK);
+        acc4 held[CHUNK_EACH];
+        const Run r = group_join<THREADS>(
+            held_logits<THREADS, CHUNK_EACH>(logits + row * V + from, n, splits, stride, held));
+        if (threadIdx.x == 0)
+            part[b] = r;
+        const int64_t t = target[row] - from;
 #pragma unroll
-            for (int i = 0; i < GROUP; ++i)
-                v[i] = 0.f;
-        store_group(out + row * ldo + c, v);
+        for (int e = 0; e < CHUNK_EACH; ++e) {
+            const int v = at + 4 * THREADS * e;
+            if (t >= v && t < v + 4 && t < n) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (t == v + i)
+                        target_logit[row] = held[e][i];
+            }
+            if (FACTOR && splits > 1 && v < n)
+                put4(U + row * V + from + v, held[e], n - v);
+        }
     }
+}
+
+template <typename G>
+__global__ __launch_bounds__(THREADS) void chunk_grad_kernel(const Run* __restrict__ part, int64_t T, int chunks,
+                                                             const float* __restrict__ target_logit,
+                                                             const int64_t* __restrict__ target,
+                                                             const float* __restrict__ dloss, int V,
+                                                             float* __restrict__ loss, float* __restrict__ U,
+                                                             G* __restrict__ g, int ldg,
+                                                             float* __restrict__ target_rest)
+{
+    const int at = 4 * static_cast<int>(threadIdx.x);
+    for (int64_t b = blockIdx.x; b < T * chunks; b += gridDim.x) {
+        const int64_t row = b / chunks;
+        const int from = static_cast<int>(b - row * chunks) * CHUNK;
+        acc4 x[CHUNK_EACH];
+#pragma unroll
+        for (int e = 0; e < CHUNK_EACH; ++e)
+            x[e] = get4(U + row * V + from + at + 4 * THREADS * e, V - from - at - 4 * THREADS * e, 0.f);
+        Run r{-INFINITY, 0.f};
+        for (int p = threadIdx.x & 63; p < chunks; p += 64)
+            r = join(r, part[row * chunks + p]);
+        const float lse = lse_of(wave_join(r));
+        const int64_t t = target[row];
+        const bool has = counts(t, V);
+        if (from == 0 && threadIdx.x == 0)
+            loss[row] = has ? lse - target_logit[row] : 0.f;
+        const RowGrad q(has, lse, has ? dloss[row] : 0.f);
+        // The last chunk also clears what is between V and the operand's row end.
+#pragma unroll
+        for (int e = 0; e < CHUNK_EACH; ++e)
+            put_grad(q, x[e], from + at + 4 * THREADS * e, V, ldg, t, U + row * V, g + row * ldg, target_rest + row);
+    }
+}
+
+template <typename E>
+__global__ __launch_bounds__(THREADS) void lay_out_kernel(RowCopy c)
+{
+    copy_rows<E>(c, static_cast<int64_t>(blockIdx.x) * THREADS + threadIdx.x,
+                 static_cast<int64_t>(gridDim.x) * THREADS);
 }
 
 // The splits' sums in order, rounded once to the result's type.  A result of
@@ -598,17 +668,17 @@ __global__ __launch_bounds__(THREADS) void join_splits_kernel(const float* __res
     const int64_t groups = (n + 3) / 4, step = static_cast<int64_t>(gridDim.x) * THREADS;
     for (int64_t q = static_cast<int64_t>(blockIdx.x) * THREADS + threadIdx.x; q < groups; q += step) {
         const int64_t at = 4 * q;
+        const int left = static_cast<int>(n - at < 4 ? n - at : 4);
         acc4 v = {0.f, 0.f, 0.f, 0.f};
         for (int s = 0; s < splits; s += AT_ONCE) {
             acc4 x[AT_ONCE];
 #pragma unroll
             for (int k = 0; k < AT_ONCE; ++k)
-                x[k] = s + k < splits ? get4(part + (s + k) * stride + at, n - at, 0.f) : acc4{0.f, 0.f, 0.f, 0.f};
+                x[k] = s + k < splits ? get4(part + (s + k) * stride + at, left, 0.f) : acc4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int k = 0; k < AT_ONCE; ++k)
                 v += x[k];
         }
-        const int left = static_cast<int>(n - at < 4 ? n - at : 4);
         if constexpr (sizeof(O) == 2)
             put4(out + at, __builtin_convertvector(v, b4), left);
         else
@@ -763,38 +833,41 @@ Choice choose(int64_t M, int64_t N, int64_t K, int count, bool may_split)
 
 template <typename T, Use USE>
 hipError_t launch_product(const Operand& a, const Operand& b, const Parts& p, const Out& o, int64_t m_first,
-                          int64_t M, int64_t N, int64_t K, int64_t splits, hipStream_t s)
+                          int64_t M, int64_t N, int64_t K, int64_t splits, hipStream_t s, const RowCopy& copy = {})
 {
     const int64_t tm = ceil_div(M - m_first, T::BM), tn = ceil_div(N, T::BN);
     const int64_t k_split = round_up(ceil_div(std::max<int64_t>(K, 1), splits), T::STEP);
-    product_kernel<T, USE><<<dim3(static_cast<unsigned>(tm * tn), static_cast<unsigned>(splits)), T::NT, 0, s>>>(
-        a, b, p, o, m_first, M, N, K, k_split, tm, tn, 1024 / T::BM);
+    const int64_t copies = USE == GRAD && copy.out
+                               ? std::min<int64_t>(ceil_div(copy.rows * (copy.ldo / GROUP), T::NT), 2 * device_cu_count())
+                               : 0;
+    product_kernel<T, USE><<<dim3(static_cast<unsigned>(tm * tn + copies), static_cast<unsigned>(splits)), T::NT, 0,
+                             s>>>(a, b, p, o, m_first, M, N, K, k_split, tm, tn, 1024 / T::BM, copy);
     return hipGetLastError();
 }
 
 template <typename E, bool AK, bool BK, Use USE>
 hipError_t product_rows(ShapeKind kind, const Operand& a, const Operand& b, const Parts& p, const Out& o,
-                        int64_t m_first, int64_t M, int64_t N, int64_t K, int64_t splits, hipStream_t s)
+                        int64_t m_first, int64_t M, int64_t N, int64_t K, int64_t splits, hipStream_t s, const RowCopy& copy)
 {
     switch (kind) {
     case THIN:
-        return launch_product<Thin<E, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s);
+        return launch_product<Thin<E, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s, copy);
     case SMALL:
-        return launch_product<Small<E, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s);
+        return launch_product<Small<E, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s, copy);
     case HALF:
-        return launch_product<Half<E, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s);
+        return launch_product<Half<E, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s, copy);
     case SQUARE:
         if constexpr (sizeof(E) == 4)
-            return launch_product<Square<Split32, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s);
+            return launch_product<Square<Split32, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s, copy);
         else
-            return launch_product<Square<E, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s);
+            return launch_product<Square<E, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s, copy);
     case TALL:
         if constexpr (sizeof(E) == 2)
-            return launch_product<Tall<E, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s);
+            return launch_product<Tall<E, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s, copy);
         break;
     case LARGE:
         if constexpr (sizeof(E) == 2)
-            return launch_product<Large<E, AK, BK, USE == GRAD>, USE>(a, b, p, o, m_first, M, N, K, splits, s);
+            return launch_product<Large<E, AK, BK, USE == GRAD>, USE>(a, b, p, o, m_first, M, N, K, splits, s, copy);
         break;
     }
     return hipErrorInvalidValue;
@@ -802,12 +875,12 @@ hipError_t product_rows(ShapeKind kind, const Operand& a, const Operand& b, cons
 
 template <typename E, bool AK, bool BK, Use USE>
 hipError_t product(const Choice& c, const Operand& a, const Operand& b, const Parts& p, const Out& o, int64_t M,
-                   int64_t N, int64_t K, hipStream_t s)
+                   int64_t N, int64_t K, hipStream_t s, const RowCopy& copy = {})
 {
-    const hipError_t rc = product_rows<E, AK, BK, USE>(c.kind, a, b, p, o, 0, c.rows, N, K, c.splits, s);
+    const hipError_t rc = product_rows<E, AK, BK, USE>(c.kind, a, b, p, o, 0, c.rows, N, K, c.splits, s, copy);
     if (rc != hipSuccess || c.rows == M)
         return rc;
-    return product_rows<E, AK, BK, USE>(c.rest, a, b, p, o, c.rows, M, N, K, c.splits, s);
+    return product_rows<E, AK, BK, USE>(c.rest, a, b, p, o, c.rows, M, N, K, c.splits, s, RowCopy{});
 }
 
 // Products of parts, four bits each (A's, then B's): one; three of A with one
@@ -831,17 +904,16 @@ bool needs_copy(const void* p, int64_t D)
 }
 
 template <typename E>
-hipError_t lay_out(const E* x, int64_t rows, int64_t D, int64_t ldo, const int64_t* target, int64_t V, E* out,
-                   hipStream_t s)
+hipError_t lay_out(const RowCopy& c, hipStream_t s)
 {
-    if (rows > 0)
-        lay_out_kernel<E><<<grid_for(ceil_div(rows * (ldo / GROUP), THREADS)), THREADS, 0, s>>>(x, rows, D, ldo,
-                                                                                             target, V, out);
+    if (c.rows > 0)
+        lay_out_kernel<E><<<grid_for(ceil_div(c.rows * (c.ldo / GROUP), THREADS)), THREADS, 0, s>>>(c);
     return hipGetLastError();
 }
 
-// So many rows are few: the logits of all classes are then small beside W and
-// go through memory once, which lets k be split so that the GPU is full.
+// So many rows are few: the logits of all classes are then small beside W, and
+// the forward pass too takes them through memory, which lets k be split so that
+// the GPU is full.
 constexpr int64_t FEW_ROWS = 32;
 constexpr int64_t PIECE_BYTES = int64_t(512) << 20;   // of G at a time
 
@@ -855,17 +927,17 @@ struct Pieces {
 };
 
 struct Plan {
-    bool few = false, own_x = false, own_w = false;
+    bool by_row = false, own_x = false, own_w = false;
     int64_t ldd = 0;   // row length of what is laid out
     void* x = nullptr;
+    void* clean_x = nullptr;   // backward: X without the rows that have no target
     void* w = nullptr;
     Choice logits{};      // forward and factor form
     Pieces full, last;    // backward: of the full pieces and the last one
-    float* row_logits = nullptr;   // few rows: splits x T x V
-    Run* part = nullptr;           // many: a run per row and column block
+    float* row_logits = nullptr;   // by row: splits x T x V
+    Run* part = nullptr;           // else: a run per row and column block
     int64_t nparts = 0;
     float* target_logit = nullptr;
-    float* lse = nullptr;
     void* g = nullptr;
     int64_t piece = 0, ldg = 0;
     float* target_rest = nullptr;
@@ -892,25 +964,29 @@ Plan make_plan(int op, const void* X, const void* W, int64_t T, int64_t V, int64
     Plan p;
     Arena a{base};
     p.ldd = round_up(D, GROUP);
-    p.own_x = op == POSEIDON_XENT_BACKWARD || needs_copy<E>(X, D);
+    p.own_x = needs_copy<E>(X, D);
     p.own_w = needs_copy<E>(W, D);
     if (p.own_x)
         p.x = a.take(T * p.ldd * SZ);
+    if (op == POSEIDON_XENT_BACKWARD)
+        p.clean_x = a.take(T * p.ldd * SZ);
     if (p.own_w)
         p.w = a.take(V * p.ldd * SZ);
-    p.few = op != POSEIDON_XENT_BACKWARD && T <= FEW_ROWS;
-    p.logits = p.few                         ? choose<E, STORE>(T, V, D, 1, true)
-               : op == POSEIDON_XENT_FACTOR ? choose<E, LOGITS>(T, V, D, 1, false)
-                                            : choose<E, STATS>(T, V, D, 1, false);
-    if (p.few) {
-        p.row_logits = static_cast<float*>(a.take(p.logits.splits * T * V * 4));
+    p.by_row = op == POSEIDON_XENT_FACTOR || (op == POSEIDON_XENT_FORWARD && T <= FEW_ROWS);
+    p.logits = p.by_row ? choose<E, STORE>(T, V, D, 1, true) : choose<E, STATS>(T, V, D, 1, false);
+    if (p.by_row) {
+        if (op == POSEIDON_XENT_FORWARD || p.logits.splits > 1)
+            p.row_logits = static_cast<float*>(a.take(p.logits.splits * T * V * 4));
+        if (V > ROW_MOST) {
+            p.part = static_cast<Run*>(a.take(T * ceil_div(V + GROUP, CHUNK) * static_cast<int64_t>(sizeof(Run))));
+            p.target_logit = static_cast<float*>(a.take(T * 4));
+        }
     } else if (op != POSEIDON_XENT_BACKWARD) {
         p.nparts = column_blocks(p.logits.kind, V);
         if (p.logits.rows < T)
             p.nparts = std::max(p.nparts, column_blocks(p.logits.rest, V));
         p.part = static_cast<Run*>(a.take(T * p.nparts * static_cast<int64_t>(sizeof(Run))));
         p.target_logit = static_cast<float*>(a.take(T * 4));
-        p.lse = static_cast<float*>(a.take(T * 4));
     }
     if (op == POSEIDON_XENT_FORWARD) {
         p.bytes = a.at;
@@ -971,16 +1047,15 @@ Plan make_plan(int op, const void* X, const void* W, int64_t T, int64_t V, int64
             return rc_;              \
     } while (0)
 
-// X and W as operands, laid out where the plan says so (given `target`, X
-// without the rows that have none: whatever they hold must not reach dW).
+// X and W as operands, laid out where their rows' places ask for it.
 template <typename E>
-hipError_t operands(const Plan& p, const E* X, const E* W, const int64_t* target, int64_t T, int64_t V, int64_t D,
-                    Operand& x, Operand& w, hipStream_t s)
+hipError_t operands(const Plan& p, const E* X, const E* W, int64_t T, int64_t V, int64_t D, Operand& x, Operand& w,
+                    hipStream_t s)
 {
     if (p.own_x)
-        POSEIDON_TRY(lay_out(X, T, D, p.ldd, target, V, static_cast<E*>(p.x), s));
+        POSEIDON_TRY(lay_out<E>(RowCopy{X, T, D, p.ldd, nullptr, V, p.x}, s));
     if (p.own_w)
-        POSEIDON_TRY(lay_out(W, V, D, p.ldd, nullptr, V, static_cast<E*>(p.w), s));
+        POSEIDON_TRY(lay_out<E>(RowCopy{W, V, D, p.ldd, nullptr, V, p.w}, s));
     x = Operand{p.own_x ? p.x : X, p.own_x ? p.ldd : D, T, 0};
     w = Operand{p.own_w ? p.w : W, p.own_w ? p.ldd : D, V, 0};
     return hipSuccess;
@@ -994,39 +1069,58 @@ int64_t whole_chunks(int64_t k)
 }
 
 template <typename E>
-hipError_t row_logits(const Plan& p, const Operand& x, const Operand& w, int64_t T, int64_t V, int64_t D,
+hipError_t row_logits(const Plan& p, const Operand& x, const Operand& w, int64_t T, int64_t V, int64_t D, float* U,
                       hipStream_t s)
 {
     Out o{};
-    o.c = p.row_logits;
+    o.c = p.row_logits ? p.row_logits : U;
     o.ldc = V;
     o.split_stride = T * V;
     return product<E, true, true, STORE>(p.logits, x, w, ONE, o, T, V, D, s);
 }
 
+hipError_t join_runs(const Plan& p, int64_t stride, int64_t main_rows, int64_t main_count, int64_t rest_count,
+                     const int64_t* target, int64_t T, int64_t V, float* loss, float* lse, hipStream_t s)
+{
+    loss_kernel<<<static_cast<unsigned>(ceil_div(T, THREADS / 64)), THREADS, 0, s>>>(
+        p.part, stride, main_rows, main_count, rest_count, p.target_logit, target, T, V, loss, lse);
+    return hipGetLastError();
+}
+
+// Losses (and lse, or G) from the logits in memory.
 template <typename G, bool FACTOR>
 hipError_t rows_done(const Plan& p, const int64_t* target, const float* dloss, int64_t T, int64_t V, float* loss,
                      float* lse, float* U, hipStream_t s)
 {
-    const int64_t each = ceil_div(round_up(V, GROUP), 4 * ROW_THREADS);
-    auto* k = each <= 1   ? row_kernel<G, 1, FACTOR>
-              : each <= 2 ? row_kernel<G, 2, FACTOR>
-              : each <= 4 ? row_kernel<G, 4, FACTOR>
-              : each <= 8 ? row_kernel<G, 8, FACTOR>
-                          : row_kernel<G, 0, FACTOR>;
-    k<<<static_cast<unsigned>(T), ROW_THREADS, 0, s>>>(p.row_logits, static_cast<int>(p.logits.splits), T * V, target,
-                                                       dloss, V, loss, lse, U, static_cast<G*>(p.g), p.ldg,
-                                                       p.target_rest);
-    return hipGetLastError();
-}
-
-hipError_t join_runs(const Plan& p, const int64_t* target, int64_t T, int64_t V, float* loss, float* lse,
-                     hipStream_t s)
-{
-    loss_kernel<<<static_cast<unsigned>(ceil_div(T, THREADS / 64)), THREADS, 0, s>>>(
-        p.part, p.nparts, p.logits.rows, column_blocks(p.logits.kind, V), column_blocks(p.logits.rest, V),
-        p.target_logit, target, T, V, loss, lse);
-    return hipGetLastError();
+    const float* logits = p.row_logits ? p.row_logits : U;
+    const int splits = static_cast<int>(p.logits.splits), v = static_cast<int>(V), ldg = static_cast<int>(p.ldg);
+    G* g = static_cast<G*>(p.g);
+    if (V <= ROW_MOST) {
+        auto run = [&](auto* k, int threads) {
+            k<<<grid_for(T), threads, 0, s>>>(logits, splits, T, T * V, target, dloss, v, loss, lse, U, g, ldg,
+                                              p.target_rest);
+        };
+        // Groups of eight end the operand's rows, so a row's last group counts whole.
+        const int64_t values = round_up(V, GROUP);
+        if (values <= 1024)
+            run(row_kernel<G, 256, 1, FACTOR>, 256);
+        else if (values <= 4096)
+            run(row_kernel<G, 256, 4, FACTOR>, 256);
+        else
+            run(row_kernel<G, 1024, 4, FACTOR>, 1024);
+        return hipGetLastError();
+    }
+    const int chunks = static_cast<int>(ceil_div(round_up(V, GROUP), CHUNK));
+    chunk_kernel<FACTOR><<<grid_for(T * chunks), THREADS, 0, s>>>(logits, splits, T, T * V, chunks, target, v, p.part,
+                                                                  p.target_logit, U);
+    POSEIDON_TRY(hipGetLastError());
+    if constexpr (FACTOR) {
+        chunk_grad_kernel<G><<<grid_for(T * chunks), THREADS, 0, s>>>(p.part, T, chunks, p.target_logit, target, dloss,
+                                                                     v, loss, U, g, ldg, p.target_rest);
+        return hipGetLastError();
+    } else {
+        return join_runs(p, chunks, T, chunks, chunks, target, T, V, loss, lse, s);
+    }
 }
 
 // Losses and lse without keeping logits.
@@ -1040,7 +1134,8 @@ hipError_t losses(const Plan& p, const Operand& x, const Operand& w, const int64
     o.target_logit = p.target_logit;
     o.target = target;
     POSEIDON_TRY((product<E, true, true, STATS>(p.logits, x, w, ONE, o, T, V, D, s)));
-    return join_runs(p, target, T, V, loss, lse, s);
+    return join_runs(p, p.nparts, p.logits.rows, column_blocks(p.logits.kind, V), column_blocks(p.logits.rest, V),
+                     target, T, V, loss, lse, s);
 }
 
 template <typename E>
@@ -1049,10 +1144,10 @@ hipError_t forward_typed(const E* X, const E* W, const int64_t* target, int64_t 
 {
     const Plan p = make_plan<E>(POSEIDON_XENT_FORWARD, X, W, T, V, D, ws);
     Operand x, w;
-    POSEIDON_TRY(operands(p, X, W, nullptr, T, V, D, x, w, s));
-    if (!p.few)
+    POSEIDON_TRY(operands(p, X, W, T, V, D, x, w, s));
+    if (!p.by_row)
         return losses<E>(p, x, w, target, T, V, D, loss, lse, s);
-    POSEIDON_TRY(row_logits<E>(p, x, w, T, V, D, s));
+    POSEIDON_TRY(row_logits<E>(p, x, w, T, V, D, nullptr, s));
     return rows_done<E, false>(p, target, nullptr, T, V, loss, lse, nullptr, s);
 }
 
@@ -1085,7 +1180,8 @@ hipError_t input_gradient(const Plan& p, const Operand& g, const Operand& w, con
 // G of the classes v0 .. v0 + vp.
 template <typename E>
 hipError_t logit_gradient(const Plan& p, const Operand& x, const Operand& w, const int64_t* target, const float* lse,
-                          const float* dloss, int64_t T, int64_t V, int64_t D, int64_t v0, int64_t vp, hipStream_t s)
+                          const float* dloss, int64_t T, int64_t V, int64_t D, int64_t v0, int64_t vp,
+                          const RowCopy& copy, hipStream_t s)
 {
     Out o{};
     o.target = target;
@@ -1098,7 +1194,7 @@ hipError_t logit_gradient(const Plan& p, const Operand& x, const Operand& w, con
     o.V = V;
     o.target_rest = sizeof(E) == 2 ? p.target_rest : nullptr;
     const Choice& c = vp == std::min(p.piece, V) ? p.full.logits : p.last.logits;
-    return product<E, true, true, GRAD>(c, x, w, ONE, o, T, vp, D, s);
+    return product<E, true, true, GRAD>(c, x, w, ONE, o, T, vp, D, s, copy);
 }
 
 template <typename E>
@@ -1107,13 +1203,17 @@ hipError_t backward_typed(const E* X, const E* W, const int64_t* target, const f
 {
     const Plan p = make_plan<E>(POSEIDON_XENT_BACKWARD, X, W, T, V, D, ws);
     Operand x, w;
-    POSEIDON_TRY(operands(p, X, W, target, T, V, D, x, w, s));
+    POSEIDON_TRY(operands(p, X, W, T, V, D, x, w, s));
     const Operand g{p.g, p.ldg, T, T * p.ldg};
+    // dW multiplies G's zero rows too: whatever X holds where a row has no
+    // target must not reach it.
+    const RowCopy clean{X, T, D, p.ldd, target, V, p.clean_x};
+    const Operand cx{p.clean_x, p.ldd, T, 0};
     for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
         const int64_t vp = std::min(p.piece, V - v0);
         const Operand wp{static_cast<const E*>(w.p) + v0 * w.ld, w.ld, vp, 0};
         if (T > 0) {
-            POSEIDON_TRY((logit_gradient<E>(p, x, wp, target, lse, dloss, T, V, D, v0, vp, s)));
+            POSEIDON_TRY(logit_gradient<E>(p, x, wp, target, lse, dloss, T, V, D, v0, vp, v0 == 0 ? clean : RowCopy{}, s));
             POSEIDON_TRY((input_gradient<E>(p, g, wp, w, target, T, V, D, v0, vp, dX, s)));
         }
         const Choice& c = vp == std::min(p.piece, V) ? p.full.dw : p.last.dw;
@@ -1122,7 +1222,7 @@ hipError_t backward_typed(const E* X, const E* W, const int64_t* target, const f
         o.c = sums ? p.dw : dW + v0 * D;
         o.ldc = D;
         o.split_stride = vp * D;
-        POSEIDON_TRY((product<E, false, false, STORE>(c, g, x, DW_PARTS<E>, o, vp, D, T, s)));
+        POSEIDON_TRY((product<E, false, false, STORE>(c, g, cx, DW_PARTS<E>, o, vp, D, T, s)));
         if (sums)
             POSEIDON_TRY(join_splits(p.dw, c.splits, vp * D, dW + v0 * D, s));
     }
@@ -1135,25 +1235,9 @@ hipError_t factor_typed(const E* X, const E* W, const int64_t* target, const flo
 {
     const Plan p = make_plan<E>(POSEIDON_XENT_FACTOR, X, W, T, V, D, ws);
     Operand x, w;
-    POSEIDON_TRY(operands(p, X, W, nullptr, T, V, D, x, w, s));
-    if (p.few) {
-        POSEIDON_TRY(row_logits<E>(p, x, w, T, V, D, s));
-        POSEIDON_TRY((rows_done<E, true>(p, target, dloss, T, V, loss, nullptr, U, s)));
-    } else {
-        // The payload is G whole: the logits go to it, and G replaces them.
-        Out o{};
-        o.part = p.part;
-        o.nparts = p.nparts;
-        o.target_logit = p.target_logit;
-        o.target = target;
-        o.c = U;
-        o.ldc = V;
-        POSEIDON_TRY((product<E, true, true, LOGITS>(p.logits, x, w, ONE, o, T, V, D, s)));
-        POSEIDON_TRY(join_runs(p, target, T, V, loss, p.lse, s));
-        factor_kernel<E><<<grid_for(ceil_div(T * (p.ldg / GROUP), THREADS)), THREADS, 0, s>>>(
-            p.lse, target, dloss, T, V, U, static_cast<E*>(p.g), p.ldg, p.target_rest);
-        POSEIDON_TRY(hipGetLastError());
-    }
+    POSEIDON_TRY(operands(p, X, W, T, V, D, x, w, s));
+    POSEIDON_TRY(row_logits<E>(p, x, w, T, V, D, U, s));
+    POSEIDON_TRY((rows_done<E, true>(p, target, dloss, T, V, loss, nullptr, U, s)));
     return input_gradient<E>(p, Operand{p.g, p.ldg, T, T * p.ldg}, w, w, target, T, V, D, 0, V, dX, s);
 }
 
