@@ -246,11 +246,19 @@ __global__ __launch_bounds__(LONG_THREADS) void norm_forward_long(
 //   dh = rstd * (g - avg(g) - n * avg(g * n)) + dres,   dx = dropout(dh),
 //   dgamma = sum over rows of dy * n,                   dbeta = sum over rows of dy.
 // ---------------------------------------------------------------------------
+// Where a workgroup's sums over its rows go, `stride` values apart: partial
+// rows, or (one workgroup) the results themselves.
+struct WeightSums {
+    float* dgamma;
+    float* dbeta;
+    int64_t stride;
+};
+
 template <typename T, int TPR, int NG>
 __global__ __launch_bounds__(TPR > THREADS ? TPR : THREADS) void norm_backward_kernel(
     const T* __restrict__ dy, const T* __restrict__ h, const float* __restrict__ gamma,
     const float* __restrict__ mean_in, const float* __restrict__ rstd_in, const T* __restrict__ dres, int64_t rows,
-    int64_t cols, Drop d, T* __restrict__ dx, T* __restrict__ dh, float* __restrict__ partial)
+    int64_t cols, Drop d, T* __restrict__ dx, T* __restrict__ dh, WeightSums out)
 {
     constexpr int NT = TPR > THREADS ? TPR : THREADS, TEAMS = NT / TPR;
     __shared__ float lds[32];
@@ -357,13 +365,13 @@ __global__ __launch_bounds__(TPR > THREADS ? TPR : THREADS) void norm_backward_k
         if (team != TEAMS - 1)
             return;
     }
-    float* out = partial + static_cast<int64_t>(blockIdx.x) * 2 * cols;
+    const int64_t part = static_cast<int64_t>(blockIdx.x) * out.stride;
 #pragma unroll
     for (int i = 0; i < NG; ++i) {
         const int64_t c = (t + static_cast<int64_t>(i) * TPR) * GROUP;
         if (c < cols) {
-            store_some(out + c, cols - c, dg[i]);
-            store_some(out + cols + c, cols - c, db[i]);
+            store_some(out.dgamma + part + c, cols - c, dg[i]);
+            store_some(out.dbeta + part + c, cols - c, db[i]);
         }
     }
 }
@@ -427,7 +435,7 @@ template <typename T>
 __global__ __launch_bounds__(THREADS) void norm_weights_long(const T* __restrict__ dy, const T* __restrict__ h,
                                                              const float* __restrict__ mean_in,
                                                              const float* __restrict__ rstd_in, int64_t rows,
-                                                             int64_t cols, float* __restrict__ partial)
+                                                             int64_t cols, WeightSums out)
 {
     const int64_t c = (static_cast<int64_t>(blockIdx.x) * THREADS + threadIdx.x) * GROUP;
     if (c >= cols)
@@ -443,9 +451,9 @@ __global__ __launch_bounds__(THREADS) void norm_weights_long(const T* __restrict
             db[k] += g[k];
         }
     }
-    float* out = partial + static_cast<int64_t>(blockIdx.y) * 2 * cols;
-    store_some(out + c, cols - c, dg);
-    store_some(out + cols + c, cols - c, db);
+    const int64_t part = static_cast<int64_t>(blockIdx.y) * out.stride;
+    store_some(out.dgamma + part + c, cols - c, dg);
+    store_some(out.dbeta + part + c, cols - c, db);
 }
 
 // dgamma and dbeta from `parts` partial rows: 16 columns a workgroup, 16
@@ -544,13 +552,16 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 unsigned grid_for(int64_t work) { return static_cast<unsigned>(std::min<int64_t>(work, 1 << 20)); }
 
 // Workgroups of the backward pass: a few a CU keep its loads in flight, and
-// each leaves one partial row.
+// each leaves one partial row.  One walks up to four rows a team by itself: its
+// sums are the result, and the launch that adds partial rows is spared (a
+// sixteen-row call is bound by its launches).
 int backward_groups(int64_t rows, int64_t cols)
 {
     const int64_t teams = cols > 1024 ? 1 : cols > 128 ? 4 : 16;
+    if (rows <= 4 * teams)
+        return 1;
     const int64_t per_cu = cols > 1024 && cols <= 2048 ? 3 : 2;
-    return static_cast<int>(
-        std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, teams), per_cu * device_cu_count())));
+    return static_cast<int>(std::min<int64_t>(ceil_div(rows, teams), per_cu * device_cu_count()));
 }
 
 template <typename T>
@@ -588,6 +599,7 @@ hipError_t backward_typed(const T* dy, const T* h, const float* gamma, const flo
                           float* dbeta, float* partial, hipStream_t s)
 {
     const int parts = backward_groups(rows, cols);
+    const WeightSums sums = parts > 1 ? WeightSums{partial, partial + cols, 2 * cols} : WeightSums{dgamma, dbeta, 0};
     hipError_t rc = hipSuccess;
     if (cols > LONGEST_BACKWARD) {
         if (rows > 0)
@@ -597,17 +609,17 @@ hipError_t backward_typed(const T* dy, const T* h, const float* gamma, const flo
         if (rc != hipSuccess)
             return rc;
         const dim3 grid(static_cast<unsigned>(ceil_div(cols, THREADS * GROUP)), static_cast<unsigned>(parts));
-        norm_weights_long<T><<<grid, THREADS, 0, s>>>(dy, h, mean, rstd, rows, cols, partial);
+        norm_weights_long<T><<<grid, THREADS, 0, s>>>(dy, h, mean, rstd, rows, cols, sums);
         rc = hipGetLastError();
     } else {
         rc = with_backward_team(cols, [&](auto tpr, auto ng) {
             constexpr int TPR = decltype(tpr)::value, NG = decltype(ng)::value, NT = TPR > THREADS ? TPR : THREADS;
             norm_backward_kernel<T, TPR, NG><<<static_cast<unsigned>(parts), NT, 0, s>>>(
-                dy, h, gamma, mean, rstd, dres, rows, cols, d, dx, dh, partial);
+                dy, h, gamma, mean, rstd, dres, rows, cols, d, dx, dh, sums);
             return hipGetLastError();
         });
     }
-    if (rc != hipSuccess)
+    if (rc != hipSuccess || parts == 1)
         return rc;
     norm_weights_kernel<<<static_cast<unsigned>(ceil_div(2 * cols, SUM_COLS)), THREADS, 0, s>>>(partial, parts,
                                                                                                cols, dgamma, dbeta);
