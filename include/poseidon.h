@@ -697,17 +697,21 @@ int poseidon_norm_backward(const void* dy, const void* h, const float* gamma, co
  * dloss_t is the gradient of the whole loss with respect to loss_t (1 / rows
  * for a mean).
  *
- * poseidon_xent_forward and poseidon_xent_backward keep no logits: the
- * backward pass makes them again, a piece of the vocabulary at a time, from
- * the lse that the forward pass left.  dW is the dense payload of the
- * parameter server (it may lie in a shard), replaced, exact to fp32 whatever
- * the type; with T = 0 it is 0.  poseidon_xent_factor is for a layer that is
- * synchronised by sufficient factors: it leaves the layer's factor U = G
- * (T x V fp32; the layer's V factor is X), the losses and dX in one call.
- * fp32 inputs are multiplied as fp32; bf16 inputs on the bf16 matrix cores,
- * with G rounded to bf16 for a bf16 dX and in three exact parts for dW.
- * Returns POSEIDON_OK, POSEIDON_ERR_INVALID_ARG (negative T; V or D < 1; T, V
- * above 2^24, T*V above 2^37, D above 2^20; an unknown dtype; NULL arrays with
+ * poseidon_xent_forward and poseidon_xent_backward keep no logits (but for up
+ * to 32 rows, in the workspace): the backward pass makes them again, a piece of
+ * the vocabulary at a time, from the lse that the forward pass left.  dW is the
+ * dense payload of the parameter server (it may lie in a shard), replaced,
+ * exact to fp32 whatever the type; with T = 0 it is 0.  poseidon_xent_factor is
+ * for a layer that is synchronised by sufficient factors: it leaves the layer's
+ * factor U = G (T x V fp32; the layer's V factor is X), the losses and dX in one
+ * call.
+ * fp32 inputs are multiplied to fp32's accuracy, by fp32 products or (larger
+ * ones) by six products of exact bf16 parts as poseidon_sf_apply's; the latter
+ * make NaN of infinite operands and of finite ones above 3.39e38.  bf16 inputs
+ * are multiplied on the bf16 matrix cores, with G rounded to bf16 for a bf16 dX
+ * (its entry at the target exactly) and in three exact parts for dW.
+ * Returns POSEIDON_OK, POSEIDON_ERR_INVALID_ARG (negative T; V or D < 1; T
+ * above 2^24, V above 2^21, D above 2^20, T*V above 2^37; an unknown dtype; NULL arrays with
  * work; outputs overlapping each other, the workspace or an input; a workspace
  * too small or off its boundary) or POSEIDON_ERR_HIP.
  */

@@ -56,12 +56,15 @@ __device__ __forceinline__ uint32_t lds_address(const char* p)
 
 // 16 bytes per lane from rs + v to LDS, lane after lane from `to`.  Written as
 // an instruction, not as the builtin: the compiler makes every transposing LDS
-// read after the builtin wait for all loads in flight, whichever stage they
-// go to (dW of a 4097 x 50001 x 1024 product: see the tile shapes below).  It has no
-// result register; whoever reads the stage waits for it (Tile::turn).
+// read after the builtin wait for all loads in flight, whichever stage they go
+// to.  It has no result register; whoever reads the stage waits for it
+// (Tile::turn).  The wait states are those of a vector load whose scalar
+// operands (M0 among them) were written just before, by a vector instruction
+// even: the compiler does not look for that inside.  (M0 is reserved: the compiler
+// sets it itself right before each use of its own, of which these kernels have none.)
 __device__ __forceinline__ void load_to_lds(i4 rs, int v, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(v), "s"(rs)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(v), "s"(rs)
                  : "memory");
 }
 

@@ -51,11 +51,14 @@ struct Ranges {
 int status(hipError_t rc) { return rc == hipSuccess ? POSEIDON_OK : POSEIDON_ERR_HIP; }
 
 constexpr int64_t MOST_COLS = int64_t(1) << 28;
-constexpr int64_t MOST_ROWS = int64_t(1) << 24, MOST_LOGITS = int64_t(1) << 37, MOST_FEATURES = int64_t(1) << 20;
+// A tile's 256 rows of W, X or G lie within the 2 GB that one buffer resource
+// addresses.
+constexpr int64_t MOST_ROWS = int64_t(1) << 24, MOST_CLASSES = int64_t(1) << 21, MOST_FEATURES = int64_t(1) << 20;
+constexpr int64_t MOST_LOGITS = int64_t(1) << 37;
 
 bool xent_sizes_ok(int64_t T, int64_t V, int64_t D, int32_t dtype)
 {
-    return size_of(dtype) && T >= 0 && T <= MOST_ROWS && V >= 1 && V <= MOST_ROWS && D >= 1 && D <= MOST_FEATURES &&
+    return size_of(dtype) && T >= 0 && T <= MOST_ROWS && V >= 1 && V <= MOST_CLASSES && D >= 1 && D <= MOST_FEATURES &&
            T * V <= MOST_LOGITS;
 }
 

@@ -21,7 +21,7 @@
 namespace poseidon {
 namespace {
 
-constexpr float LOG2E = 1.44269504f, LOG2E_REST = 1.92596299e-8f, LN2 = 0.693147181f;
+constexpr float LOG2E = 1.44269504f, LN2 = 0.693147181f;
 
 // A running maximum, in units of log2 e, and the sum of powers of two below it.
 struct Run {
@@ -182,8 +182,8 @@ __device__ __forceinline__ void finish_stats(acc4 (&acc)[T::TM][T::TN], const Ou
 }
 
 // GRAD.  p = 2^(s log2 e - lse log2 e): the product of lse is rounded once a
-// row, and what that (and log2 e's own rounding) leaves goes into the row's
-// factor, so that a probability is as exact as its logit.
+// row, and what that leaves goes into the row's factor, so that a probability is
+// as exact as its logit.  (The rounding of log2 e itself concerns only s - lse.)
 template <typename T, bool EDGE>
 __device__ __forceinline__ void finish_grad(acc4 (&acc)[T::TM][T::TN], const Out& o, int64_t m0, int64_t n0, int rows,
                                             int cols, int wm, int wn, int lane)
@@ -210,7 +210,7 @@ __device__ __forceinline__ void finish_grad(acc4 (&acc)[T::TM][T::TN], const Out
         const bool has = counts(t, o.V);
         const float lse = has ? lses[i] : 0.f, d = has ? dlosses[i] : 0.f;
         const float from = lse * LOG2E;
-        const float rest = fmaf(lse, LOG2E, -from) + lse * LOG2E_REST;
+        const float rest = fmaf(lse, LOG2E, -from);
         const float scale = fmaf(d, -rest * LN2, d);
 #pragma unroll
         for (int j = 0; j < T::TN; ++j)
@@ -521,7 +521,7 @@ struct RowGrad {
         has = has_;
         dloss = d;
         from = has ? lse * LOG2E : 0.f;
-        const float rest = fmaf(lse, LOG2E, -from) + lse * LOG2E_REST;
+        const float rest = fmaf(lse, LOG2E, -from);
         scale = has ? fmaf(d, -rest * LN2, d) : 0.f;
     }
 };
