@@ -9,8 +9,8 @@
 // products logits = X W^T, dX = G W and dW = G^T X read X, W and G as they are
 // and nothing is transposed in memory.
 //
-// A step takes 64 or 128 bytes of k per row (32 or 64 bf16 values, half as many
-// fp32) from each operand straight into LDS (gfx950's 16-byte LDS-direct buffer loads; what is
+// A step takes 128 bytes of k per row (64 bf16 or 32 fp32 values) from each
+// operand straight into LDS (gfx950's 16-byte LDS-direct buffer loads; what is
 // outside the operand reads 0 by the buffer's range check), up to STAGES
 // steps ahead.  Each stage is an LDS object of its own, so that reading one does not
 // wait for the loads in flight into another.
@@ -45,7 +45,7 @@ constexpr int XCDS = 8;              // MI355X: eight dies, each with an L2 of i
 constexpr int RSRC_RAW = 0x00020000; // buffer resource word 3: raw 32-bit accesses
 constexpr int64_t RSRC_MOST = 0x7fff0000;
 constexpr int OUTSIDE = 0x7ffffff0;  // an offset no resource here contains
-constexpr int SUB_BYTES = 64;        // k per row and sub-step: one operand fragment of 16 rows is 1 KB
+constexpr int STEP_BYTES = 128;      // k per row and step: two sub-steps (fragments of 16 rows and 64 bytes)
 
 typedef int i4 __attribute__((ext_vector_type(4)));
 
@@ -100,12 +100,11 @@ struct InMemory<Split32> {
     typedef float type;
 };
 
-template <typename E_, int R, int NT, bool KMAJOR, int KSUB, bool SPREAD>
+template <typename E_, int R, int NT, bool KMAJOR, bool SPREAD>
 struct Panel {
     typedef typename InMemory<E_>::type E;
     static constexpr bool SPLIT = !__is_same(E_, E);   // operands are eight fp32 values a lane, k from 8 (lane / 16)
     static constexpr int SZ = sizeof(E);
-    static constexpr int STEP_BYTES = KSUB * SUB_BYTES;
     static constexpr int BYTES = R * STEP_BYTES;
     static constexpr int LOADS = BYTES / 16 / NT;
     static constexpr int BK = STEP_BYTES / SZ;
@@ -120,11 +119,7 @@ struct Panel {
     // lie in different banks.
     static __device__ __forceinline__ int swz_k(int r)
     {
-        if constexpr (CHUNKS == 8)
-            return SPREAD ? ((r & 3) ^ ((r >> 5) & 1)) | (((r >> 4) & 1) << 2) : (r & 7) ^ ((r >> 3) & 1);
-        else
-            return SPREAD ? (((r >> 4) & 1) << 1) | (((r >> 1) ^ (r >> 5)) & 1)
-                          : (((r >> 2) & 1) << 1) | (((r >> 1) ^ (r >> 3)) & 1);
+        return SPREAD ? ((r & 3) ^ ((r >> 5) & 1)) | (((r >> 4) & 1) << 2) : (r & 7) ^ ((r >> 3) & 1);
     }
 
     // r-major: which chunk of a k row sits in slot s is s ^ swz_r(k).
@@ -132,14 +127,14 @@ struct Panel {
     {
         if constexpr (SZ == 2) {
             if constexpr (PER_ROW % 16 == 0)   // rows of a multiple of 256 bytes: eight pairs
-                return (((k & 3) | (((k >> 3) & 1) << 2)) << 1);
+                return (((k & 3) | (((k >> 4) & 1) << 2)) << 1);
             else if constexpr (PER_ROW % 8 == 0)   // of 128: the row's parity is half of the bank, four pairs
-                return ((((k >> 1) & 1) | (((k >> 3) & 1) << 1)) << 1);
+                return ((((k >> 1) & 1) | (((k >> 4) & 1) << 1)) << 1);
             else
                 return 0;
         } else {
             if constexpr (PER_ROW % 16 == 0)
-                return ((k >> (SPLIT ? 3 : 2)) & 3) << 2;
+                return ((k >> 3) & 3) << 2;
             else
                 return 0;
         }
@@ -244,8 +239,11 @@ struct Panel {
         }
     }
 
-    // The operand fragment of 16 rows, sub-step kk: for bf16 eight k from
-    // 32 kk + 8 (lane / 16), for fp32 four from 16 kk + 4 (lane / 16).  Lane l
+    // The operand fragment of 16 rows, sub-step kk: lane l has the k of the 16
+    // bytes 2 (l / 16) + kk of the step's 128 (every operand alike: which k meet
+    // in an instruction is free).  Read so, no two lanes of a k-major read that
+    // are served together want one bank; with bytes 4 kk + l / 16 some do (22%
+    // of the cycles of an 8192 x 32768 x 2048 product).  Lane l
     // takes row r0 + l % 16 of block j = (row - r0) / 16; SPREAD: of the four
     // blocks from r0 on, rows 16 (i / 4) + 4 j + i % 4, i = l % 16.
     static __device__ __forceinline__ h8 frag(const char* stage, int r0, int j, int kk, int lane)
@@ -253,12 +251,12 @@ struct Panel {
         const int g = lane >> 4, i = lane & 15;
         if constexpr (KMAJOR) {
             const int r = SPREAD ? r0 + 16 * (i >> 2) + 4 * j + (i & 3) : r0 + 16 * j + i;
-            return *reinterpret_cast<const h8*>(stage + r * STEP_BYTES + (((4 * kk + g) ^ swz_k(r)) << 4));
+            return *reinterpret_cast<const h8*>(stage + r * STEP_BYTES + (((2 * g + kk) ^ swz_k(r)) << 4));
         } else if constexpr (SZ == 2) {
             h8 v;
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                const int k = 32 * kk + 8 * g + 4 * half + (i >> 2);
+                const int k = 8 * (2 * g + kk) + 4 * half + (i >> 2);
                 const int byte = (r0 + 16 * j) * 2 + (i & 3) * 8;
                 const char* at = stage + k * (R * 2) + (((byte >> 4) ^ swz_r(k)) << 4) + (byte & 15);
                 const h4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_h4*)at);
@@ -271,7 +269,7 @@ struct Panel {
             acc4 v;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int k = 16 * kk + 4 * g + e;
+                const int k = 4 * (2 * g + kk) + e;
                 const int byte = (r0 + 16 * j + i) * 4;
                 v[e] = *reinterpret_cast<const float*>(stage + k * (R * 4) + (((byte >> 4) ^ swz_r(k)) << 4) +
                                                        (byte & 15));
@@ -336,19 +334,18 @@ struct Stage {
 // s_waitcnt's operand: at most so many vector loads and LDS operations left.
 constexpr int wait_imm(int vm, int lgkm) { return 0x0070 | (lgkm << 8) | (vm & 15) | ((vm >> 4) << 14); }
 
-template <typename E_, bool AK_, bool BK_, int BM_, int BN_, int WM_, int WN_, int STAGES_, int KSUB_,
-          bool SPREAD_ = false>
+template <typename E_, bool AK_, bool BK_, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool SPREAD_ = false>
 struct Tile {
     typedef E_ E;
     typedef typename InMemory<E_>::type M;   // in memory
     static constexpr bool AK = AK_, BKM = BK_, SPLIT = !__is_same(E_, M);
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_;
     static constexpr int NWN = BN / WN, WAVES = (BM / WM) * NWN, NT = 64 * WAVES;
-    static constexpr int TM = WM / 16, TN = WN / 16, KSUB = KSUB_;
+    static constexpr int TM = WM / 16, TN = WN / 16;
     static constexpr bool SPREAD = SPREAD_;   // a lane's sums are 16 neighbours of a row, not four of each block
     static_assert(!SPREAD || (TN == 4 && BKM), "four blocks of k-major rows");
-    using PA = Panel<E, BM, NT, AK, KSUB, false>;
-    using PB = Panel<E, BN, NT, BKM, KSUB, SPREAD>;
+    using PA = Panel<E, BM, NT, AK, false>;
+    using PB = Panel<E, BN, NT, BKM, SPREAD>;
     static constexpr int LOADS = PA::LOADS + PB::LOADS;
     static constexpr int STEP = PA::BK;
 
@@ -448,9 +445,9 @@ struct Tile {
     template <int S>
     __device__ __forceinline__ void turn(acc4 (&acc)[TM][TN], Ahead& f)
     {
-        constexpr int G = KSUB * TM, FIRST_B = TM - 2 - TN > 0 ? TM - 2 - TN : 0;
-        static_assert(G > 2 && TN <= TM, "groups to read in");
-        h8 a[G], b[KSUB][TN];
+        constexpr int G = 2 * TM, FIRST_B = TM - 2 - TN > 0 ? TM - 2 - TN : 0;
+        static_assert(TM >= 2 && TN <= TM, "groups to read in");
+        h8 a[G], b[2][TN];
 #pragma unroll
         for (int j = 0; j < TN; ++j)
             b[0][j] = f.b[j];
@@ -460,8 +457,8 @@ struct Tile {
         for (int g = 0; g < G; ++g) {
             if (g + 2 < G)
                 a[g + 2] = a_frag<S>(g + 2);
-            if (KSUB > 1 && g >= FIRST_B && g - FIRST_B < TN)
-                b[KSUB - 1][g - FIRST_B] = b_frag<S>(g - FIRST_B, 1);
+            if (g >= FIRST_B && g - FIRST_B < TN)
+                b[1][g - FIRST_B] = b_frag<S>(g - FIRST_B, 1);
             if (g == G - 2) {
                 // All of this wave's reads of the stage are done, and its own
                 // loads of the next stage; then the other waves'.
@@ -494,7 +491,7 @@ struct Tile {
     template <int S>
     __device__ __forceinline__ void turn_split(acc4 (&acc)[TM][TN], AheadSplit& f)
     {
-        static_assert(!SPLIT || (KSUB == 2 && TM >= 2 && !SPREAD), "steps of 32 fp32 values");
+        static_assert(!SPLIT || (TM >= 2 && !SPREAD), "row blocks to read in");
         f8e raw[TM + 2], next_b[TN];
         raw[1] = f.next;
         Parts3 a = f.a;

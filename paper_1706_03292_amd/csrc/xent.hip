@@ -715,17 +715,17 @@ struct Arena {
 enum ShapeKind { THIN, SMALL, HALF, SQUARE, TALL, LARGE };
 
 template <typename E, bool AK, bool BK>
-using Thin = Tile<E, AK, BK, 32, 64, 32, 16, 4, 2>;
+using Thin = Tile<E, AK, BK, 32, 64, 32, 16, 4>;
 template <typename E, bool AK, bool BK>
-using Small = Tile<E, AK, BK, 64, 64, 32, 32, 3, 2>;
+using Small = Tile<E, AK, BK, 64, 64, 32, 32, 3>;
 template <typename E, bool AK, bool BK>
-using Half = Tile<E, AK, BK, 64, 128, 64, 32, 3, 2>;
+using Half = Tile<E, AK, BK, 64, 128, 64, 32, 3>;
 template <typename E, bool AK, bool BK>
-using Square = Tile<E, AK, BK, 128, 128, 64, 64, 2, 2>;
+using Square = Tile<E, AK, BK, 128, 128, 64, 64, 2>;
 template <typename E, bool AK, bool BK>
-using Tall = Tile<E, AK, BK, 256, 192, 128, 48, 2, 2>;
+using Tall = Tile<E, AK, BK, 256, 192, 128, 48, 2>;
 template <typename E, bool AK, bool BK, bool SPREAD = false>
-using Large = Tile<E, AK, BK, 256, 256, 128, 64, 2, 2, SPREAD>;
+using Large = Tile<E, AK, BK, 256, 256, 128, 64, 2, SPREAD>;
 
 // What a shape costs, as measured (products over K = 4096, 512 and 64 on 256, 512
 // and 768 tiles): microseconds of a step with one, two, three workgroups on a
