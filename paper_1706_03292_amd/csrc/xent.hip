@@ -4,16 +4,18 @@
 //     s = X W^T,  lse_t = log sum_v exp s_tv,  loss_t = lse_t - s_t,target
 //     G = (exp(s - lse) - onehot(target)) * dloss,  dX = G W,  dW = G^T X.
 //
-// The logits never leave the matrix cores' registers in the forward and the
-// backward pass: the forward tile's epilogue reduces its columns to a running
-// maximum and sum per row, and a second kernel joins them; the backward pass
-// makes the logits again, a piece of the vocabulary at a time, turns them into
-// G in the epilogue and multiplies the piece with W and X while it is in the
-// last-level cache.  The factor form, for layers that are synchronised by
-// sufficient factors, writes G whole, because there G is the payload.
+// For many rows the logits never leave the matrix cores' registers: the forward
+// tile's epilogue reduces its columns to a running maximum and sum per row, and a
+// second kernel joins them; the backward pass makes the logits again, a piece of
+// the vocabulary at a time, turns them into G in the epilogue and multiplies the
+// piece with W and X.  The factor form, for layers that are synchronised by
+// sufficient factors, writes G whole, because there G is the payload; up to 32
+// rows take the forward pass too through memory.
 //
-// Bound: 2TVD operations a product on the matrix cores for many rows, reading
-// W once for few.
+// Bound: 2TVD operations a product on the matrix cores for many rows (8192 x
+// 32768 x 2048 bf16: 0.90 ms, 1.2 PFLOP/s; backward 4097 x 50001 x 1024 2.2 ms,
+// 512 x 21841 x 4096 fp32 1.56 ms), reading W for few (32 x 21841 x 4096 fp32: 85
+// us, of which the product 75 at 4.7 TB/s; factors in bf16 95 us, W read twice).
 #include <math.h>
 
 #include "mfma_tile.h"
