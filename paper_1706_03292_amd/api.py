@@ -591,21 +591,17 @@ def _typed(name: str, t: torch.Tensor) -> tuple[int, int]:
     return _DTYPES[t.dtype], device
 
 
-def _drops(p: float) -> bool:
-    """Whether p, rounded to 2^-16, drops anything."""
-    return p * 65536 + 0.5 >= 1.0
-
-
 def _rng(rng, p: float, device: int = 0) -> bool:
     """Checks p and the generator's state; whether p drops anything (it needs
     the generator then)."""
     if not 0.0 <= p <= 1.0:
         raise ValueError(f"p must lie in 0..1, got {p}")
+    drops = p * 65536 + 0.5 >= 1.0   # p rounded to 2^-16
     if rng is not None:
         _dev("rng", rng, torch.int64, device, (2,))
-    elif _drops(p):
+    elif drops:
         raise ValueError("dropout needs rng: two int64 values (seed, offset) on the device")
-    return _drops(p)
+    return drops
 
 
 def _work_on(stream, device):
@@ -620,10 +616,11 @@ def _work_on(stream, device):
 
 
 def _rows_cols(x: torch.Tensor) -> tuple[int, int]:
-    if x.dim() < 1:
+    shape = x.shape
+    if not shape:
         raise ValueError("x must have at least one dimension")
-    cols = x.shape[-1]
-    return (x.numel() // cols if cols else 0), cols
+    cols = shape[-1]
+    return (shape[0] if len(shape) == 2 else x.numel() // cols if cols else 0), cols
 
 
 def dropout(x: torch.Tensor, p: float, rng: torch.Tensor | None, residual: torch.Tensor | None = None,
@@ -642,7 +639,8 @@ def dropout(x: torch.Tensor, p: float, rng: torch.Tensor | None, residual: torch
     with _work_on(stream, x.device):
         if y is None:
             y = torch.empty_like(x)
-        _uses(stream, x, residual, rng, y)
+        if stream is not None:
+            _uses(stream, x, residual, rng, y)
         _check("poseidon_dropout", L.lib().poseidon_dropout(
             x.data_ptr(), _ptr(residual), rows, cols, dt, p, _ptr(rng), y.data_ptr(),
             _stream_handle(stream, x.device)))
@@ -671,7 +669,8 @@ def norm_forward(x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor, eps: 
         h = torch.empty_like(x) if drops or residual is not None else x
         mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
         rstd = torch.empty_like(mean)
-        _uses(stream, x, gamma, beta, residual, rng, y)
+        if stream is not None:
+            _uses(stream, x, gamma, beta, residual, rng, y)
         _check("poseidon_norm_forward", L.lib().poseidon_norm_forward(
             x.data_ptr(), _ptr(residual), gamma.data_ptr(), beta.data_ptr(), rows, cols, dt, eps, p, _ptr(rng),
             None if h is x else h.data_ptr(), y.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
@@ -710,7 +709,8 @@ def norm_backward(dy: torch.Tensor, h: torch.Tensor, gamma: torch.Tensor, mean: 
         dh = torch.empty_like(dy)
         dx = torch.empty_like(dy) if drops else dh
         ws = torch.empty(size.value, dtype=torch.uint8, device=dy.device)
-        _uses(stream, dy, h, gamma, mean, rstd, dresidual, rng, dgamma, dbeta)
+        if stream is not None:
+            _uses(stream, dy, h, gamma, mean, rstd, dresidual, rng, dgamma, dbeta)
         _check("poseidon_norm_backward", lib.poseidon_norm_backward(
             dy.data_ptr(), h.data_ptr(), gamma.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _ptr(dresidual), rows,
             cols, dt, p, _ptr(rng), None if dx is dh else dx.data_ptr(), dh.data_ptr(), dgamma.data_ptr(),
@@ -756,7 +756,8 @@ def xent_forward(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, stream=
         ws, size = _xent_workspace(L.XENT_FORWARD, X, W, T, V, D, dt)
         loss = torch.empty(T, dtype=torch.float32, device=X.device)
         lse = torch.empty_like(loss)
-        _uses(stream, X, W, target)
+        if stream is not None:
+            _uses(stream, X, W, target)
         _check("poseidon_xent_forward", L.lib().poseidon_xent_forward(
             X.data_ptr(), W.data_ptr(), target.data_ptr(), T, V, D, dt, loss.data_ptr(), lse.data_ptr(),
             ws.data_ptr(), size, _stream_handle(stream, X.device)))
@@ -778,7 +779,8 @@ def xent_backward(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, lse: t
         if dW is None:
             dW = torch.empty((V, D), dtype=torch.float32, device=X.device)
         dX = torch.empty_like(X)
-        _uses(stream, X, W, target, lse, dloss, dW)
+        if stream is not None:
+            _uses(stream, X, W, target, lse, dloss, dW)
         _check("poseidon_xent_backward", L.lib().poseidon_xent_backward(
             X.data_ptr(), W.data_ptr(), target.data_ptr(), lse.data_ptr(), dloss.data_ptr(), T, V, D, dt,
             dX.data_ptr(), dW.data_ptr(), ws.data_ptr(), size, _stream_handle(stream, X.device)))
@@ -801,7 +803,8 @@ def xent_factor(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, dloss: t
             U = torch.empty((T, V), dtype=torch.float32, device=X.device)
         dX = torch.empty_like(X)
         loss = torch.empty(T, dtype=torch.float32, device=X.device)
-        _uses(stream, X, W, target, dloss, U)
+        if stream is not None:
+            _uses(stream, X, W, target, dloss, U)
         _check("poseidon_xent_factor", L.lib().poseidon_xent_factor(
             X.data_ptr(), W.data_ptr(), target.data_ptr(), dloss.data_ptr(), T, V, D, dt, loss.data_ptr(),
             U.data_ptr(), dX.data_ptr(), ws.data_ptr(), size, _stream_handle(stream, X.device)))
