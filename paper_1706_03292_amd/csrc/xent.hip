@@ -58,7 +58,7 @@ struct Out {
     // STATS: per row and column block the running maximum and sum, and the
     // target's logit.
     Run* part;
-    int64_t nparts;
+    int64_t nparts, block_first;
     float* target_logit;
     const int64_t* target;
     // GRAD: the piece's G from lse and dloss, in three bf16 parts (planes apart)
@@ -334,7 +334,7 @@ __device__ __forceinline__ void finish(acc4 (&acc)[T::TM][T::TN], const Out& o, 
     const int cols = static_cast<int>(N - n0 < T::BN ? N - n0 : T::BN);
     const bool edge = cols < T::BN;
     if constexpr (USE == STATS) {
-        const int64_t block = tile_n * T::NWN + w % T::NWN;
+        const int64_t block = o.block_first + tile_n * T::NWN + w % T::NWN;
         if (edge)
             finish_stats<T, true>(acc, o, m0, n0, block, rows, cols, wm, wn, lane);
         else
@@ -378,13 +378,13 @@ __device__ __forceinline__ void copy_rows(const RowCopy& o, int64_t first, int64
     }
 }
 
-// Rows m_first to M in tiles over k split gridDim.y ways (k_split values each, a
-// multiple of the step).  GRAD: workgroups past the tiles make the copy of X
+// Rows m_first to M and columns n_first to N in tiles, over k split gridDim.y ways
+// (k_split values each, a multiple of the step).  GRAD: workgroups past the tiles make the copy of X
 // that dW's product reads, which would otherwise be a launch of its own.
 template <typename T, Use USE>
 __global__ __launch_bounds__(T::NT, 2) void product_kernel(Operand a, Operand b, Parts parts, Out o,
-                                                           int64_t m_first, int64_t M, int64_t N, int64_t K,
-                                                           int64_t k_split, int64_t tiles_m, int64_t tiles_n,
+                                                           int64_t m_first, int64_t n_first, int64_t M, int64_t N,
+                                                           int64_t K, int64_t k_split, int64_t tiles_m, int64_t tiles_n,
                                                            int group, RowCopy copy)
 {
     if constexpr (USE == GRAD) {
@@ -397,7 +397,7 @@ __global__ __launch_bounds__(T::NT, 2) void product_kernel(Operand a, Operand b,
     int64_t tm, tn;
     tile_of(blockIdx.x, tiles_m, tiles_n, group, tm, tn);
     const int64_t k0 = blockIdx.y * k_split;
-    const int64_t m0 = m_first + tm * T::BM, n0 = tn * T::BN;
+    const int64_t m0 = m_first + tm * T::BM, n0 = n_first + tn * T::BN;
     T tile;
     acc4 acc[T::TM][T::TN];
     tile.run(acc, a, b, parts, m0, n0, k0, K - k0 < k_split ? K - k0 : k_split);
@@ -751,14 +751,14 @@ constexpr Shape SHAPES[] = {
 template <typename E, Use USE>
 constexpr double OUT_BYTES = USE == STATS ? 0.5 : USE == GRAD && sizeof(E) == 2 ? 8.0 : 4.0;
 
-// How a product of M rows is computed: the first `rows` of them in tiles of
-// `kind`, a rest that would leave most of a tile empty in tiles of `rest`; k
-// split `splits` ways, whose sums a kernel of their own adds.
+// How an M x N product is computed: the first `rows` x `cols` of it in tiles of
+// `kind`; rows past them, or columns (never both), in tiles of `rest`; k split
+// `splits` ways, whose sums a kernel of their own adds.
 struct Choice {
     ShapeKind kind;
     int64_t splits;
     double us;
-    int64_t rows;
+    int64_t rows, cols;
     ShapeKind rest;
 };
 
@@ -778,6 +778,23 @@ inline double tiles_us(const Shape& s, int type, int64_t M, int64_t N, double st
     return us;
 }
 
+// The smaller shape that finishes first (its estimate in `us`).
+inline ShapeKind rest_shape(int type, int64_t M, int64_t N, double steps, int z, double out_bytes, double& us)
+{
+    ShapeKind by = SMALL;
+    us = 1e30;
+    for (int k = M <= 32 ? THIN : SMALL; k <= LARGE; ++k) {
+        if (SHAPES[k].step_us[type][0] == 0.0)
+            continue;
+        const double x = tiles_us(SHAPES[k], type, M, N, steps, z, out_bytes);
+        if (x < us) {
+            us = x;
+            by = static_cast<ShapeKind>(k);
+        }
+    }
+    return by;
+}
+
 // The choice that finishes M x N values over K of k first, by these estimates;
 // never less than reading both operands takes.
 template <typename E, Use USE>
@@ -785,48 +802,58 @@ Choice choose(int64_t M, int64_t N, int64_t K, int count, bool may_split)
 {
     constexpr int TYPE = sizeof(E) / 4;
     constexpr double OUT = OUT_BYTES<E, USE>;
+    if (M == 0 || N == 0)   // nothing is launched
+        return Choice{SMALL, 1, 0.0, M, N, SMALL};
     const int64_t steps = ceil_div(std::max<int64_t>(K, 1), 128 / static_cast<int64_t>(sizeof(E)));
     const int64_t cus = device_cu_count();
     const double reading = static_cast<double>((M + N) * K) * sizeof(E) / 4.8e6;
     const double sums = 4.0 * static_cast<double>(M * N) / 4e6;   // written or read once, at 4 TB/s
-    Choice best{SMALL, 1, 1e30, M, SMALL};
+    Choice best{SMALL, 1, 1e30, M, N, SMALL};
     for (int k = M <= 32 ? THIN : SMALL; k <= LARGE; ++k) {
         const Shape& s = SHAPES[k];
         if (s.step_us[TYPE][0] == 0.0)
             continue;
-        const int64_t slots = s.per_cu * cus, across = ceil_div(N, s.bn);
+        const int64_t slots = s.per_cu * cus, down = ceil_div(M, s.bm), across = ceil_div(N, s.bn);
         const int most = may_split ? static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(32, steps / 4))) : 1;
-        // All rows in this shape, or a ragged rest of them (at most half a
-        // tile's) in a smaller one; k whole, or split into what comes to whole
-        // rounds.
         const int64_t over = M % s.bm;
-        const bool ragged = k >= SQUARE && over > 0 && over <= s.bm / 2 && M > s.bm;
-        for (int rest = 0; rest <= (ragged ? 1 : 0); ++rest) {
-            const int64_t rows = rest ? M - over : M;
-            const int64_t tiles = std::max<int64_t>(ceil_div(rows, s.bm) * across, 1);
+        // All of it in this shape; or (large shapes) without a ragged rest of
+        // rows, at most half a tile's; or without the columns past the last full
+        // round of workgroups.  k whole, or split into what comes to whole rounds.
+        for (int form = 0; form < (k >= SQUARE ? 3 : 1); ++form) {
+            if (form == 1 && (over == 0 || over > s.bm / 2 || M < s.bm))
+                continue;
+            const int64_t rows = form == 1 ? M - over : M;
+            const int64_t tiles = form == 1 ? (down - 1) * across : down * across;
             for (int round = 0; round <= 4; ++round) {
                 const int z = round == 0 ? 1 : static_cast<int>(std::min<int64_t>(most, round * slots / tiles));
                 if (z < 1 || (round > 0 && z == 1))
                     continue;
+                int64_t cols = N;
+                if (form == 2) {
+                    const int64_t full = tiles * z / slots * slots / z / down;   // columns of tiles in full rounds
+                    if (full < 1 || full >= across)
+                        continue;
+                    cols = full * s.bn;
+                }
                 const double each = static_cast<double>((steps + z - 1) / z * count);
                 // The splits' sums are written (once is counted), read and written, and take a launch.
                 const double joined = z > 1 ? 5.0 + (z + 1) * sums : 0.0;
-                double us = tiles_us(s, TYPE, rows, N, each, z, OUT);
+                double us = tiles_us(s, TYPE, rows, cols, each, z, OUT);
                 ShapeKind by = SMALL;
-                if (rest) {
-                    double least = 1e30;
-                    for (int r = over <= 32 ? THIN : SMALL; r <= HALF; ++r) {
-                        const double x = tiles_us(SHAPES[r], TYPE, over, N, each, z, OUT);
-                        if (x < least) {
-                            least = x;
-                            by = static_cast<ShapeKind>(r);
-                        }
-                    }
-                    us += 2.0 + least;
+                if (form > 0 && us + joined < best.us) {
+                    // A launch of its own: 4 us, and its workgroups no longer
+                    // start as the first ones of the last round end (a round's
+                    // sixth: 512 x 21841 x 4096 fp32 531 us whole, 588 so).
+                    double rest;
+                    by = form == 1 ? rest_shape(TYPE, over, N, each, z, OUT, rest)
+                                   : rest_shape(TYPE, M, N - cols, each, z, OUT, rest);
+                    us += 4.0 + rest;
+                    if (form == 2)
+                        us += each * s.step_us[TYPE][s.per_cu - 1] / 6;
                 }
                 us = std::max(us, reading) + joined;
                 if (us < best.us)
-                    best = Choice{static_cast<ShapeKind>(k), z, us, rows, by};
+                    best = Choice{static_cast<ShapeKind>(k), z, us, rows, cols, by};
             }
         }
     }
@@ -835,54 +862,65 @@ Choice choose(int64_t M, int64_t N, int64_t K, int count, bool may_split)
 
 template <typename T, Use USE>
 hipError_t launch_product(const Operand& a, const Operand& b, const Parts& p, const Out& o, int64_t m_first,
-                          int64_t M, int64_t N, int64_t K, int64_t splits, hipStream_t s, const RowCopy& copy = {})
+                          int64_t n_first, int64_t M, int64_t N, int64_t K, int64_t splits, hipStream_t s,
+                          const RowCopy& copy)
 {
-    const int64_t tm = ceil_div(M - m_first, T::BM), tn = ceil_div(N, T::BN);
+    const int64_t tm = ceil_div(M - m_first, T::BM), tn = ceil_div(N - n_first, T::BN);
     const int64_t k_split = round_up(ceil_div(std::max<int64_t>(K, 1), splits), T::STEP);
     const int64_t copies = USE == GRAD && copy.out
                                ? std::min<int64_t>(ceil_div(copy.rows * (copy.ldo / GROUP), T::NT), 2 * device_cu_count())
                                : 0;
     product_kernel<T, USE><<<dim3(static_cast<unsigned>(tm * tn + copies), static_cast<unsigned>(splits)), T::NT, 0,
-                             s>>>(a, b, p, o, m_first, M, N, K, k_split, tm, tn, 1024 / T::BM, copy);
+                             s>>>(a, b, p, o, m_first, n_first, M, N, K, k_split, tm, tn, 1024 / T::BM, copy);
     return hipGetLastError();
 }
 
 template <typename E, bool AK, bool BK, Use USE>
-hipError_t product_rows(ShapeKind kind, const Operand& a, const Operand& b, const Parts& p, const Out& o,
-                        int64_t m_first, int64_t M, int64_t N, int64_t K, int64_t splits, hipStream_t s, const RowCopy& copy)
+hipError_t product_part(ShapeKind kind, const Operand& a, const Operand& b, const Parts& p, const Out& o,
+                        int64_t m_first, int64_t n_first, int64_t M, int64_t N, int64_t K, int64_t splits,
+                        hipStream_t s, const RowCopy& copy)
 {
+    auto go = [&](auto* launch) { return launch(a, b, p, o, m_first, n_first, M, N, K, splits, s, copy); };
     switch (kind) {
     case THIN:
-        return launch_product<Thin<E, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s, copy);
+        return go(launch_product<Thin<E, AK, BK>, USE>);
     case SMALL:
-        return launch_product<Small<E, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s, copy);
+        return go(launch_product<Small<E, AK, BK>, USE>);
     case HALF:
-        return launch_product<Half<E, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s, copy);
+        return go(launch_product<Half<E, AK, BK>, USE>);
     case SQUARE:
         if constexpr (sizeof(E) == 4)
-            return launch_product<Square<Split32, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s, copy);
+            return go(launch_product<Square<Split32, AK, BK>, USE>);
         else
-            return launch_product<Square<E, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s, copy);
+            return go(launch_product<Square<E, AK, BK>, USE>);
     case TALL:
         if constexpr (sizeof(E) == 2)
-            return launch_product<Tall<E, AK, BK>, USE>(a, b, p, o, m_first, M, N, K, splits, s, copy);
+            return go(launch_product<Tall<E, AK, BK>, USE>);
         break;
     case LARGE:
         if constexpr (sizeof(E) == 2)
-            return launch_product<Large<E, AK, BK, USE == GRAD>, USE>(a, b, p, o, m_first, M, N, K, splits, s, copy);
+            return go(launch_product<Large<E, AK, BK, USE == GRAD>, USE>);
         break;
     }
     return hipErrorInvalidValue;
 }
 
+// Runs that a row of N columns leaves, one a wave.
+int64_t column_blocks(ShapeKind kind, int64_t N) { return ceil_div(N, SHAPES[kind].bn) * SHAPES[kind].waves_n; }
+
 template <typename E, bool AK, bool BK, Use USE>
 hipError_t product(const Choice& c, const Operand& a, const Operand& b, const Parts& p, const Out& o, int64_t M,
                    int64_t N, int64_t K, hipStream_t s, const RowCopy& copy = {})
 {
-    const hipError_t rc = product_rows<E, AK, BK, USE>(c.kind, a, b, p, o, 0, c.rows, N, K, c.splits, s, copy);
-    if (rc != hipSuccess || c.rows == M)
+    const hipError_t rc =
+        product_part<E, AK, BK, USE>(c.kind, a, b, p, o, 0, 0, c.rows, c.cols, K, c.splits, s, copy);
+    if (rc != hipSuccess || (c.rows == M && c.cols == N))
         return rc;
-    return product_rows<E, AK, BK, USE>(c.rest, a, b, p, o, c.rows, M, N, K, c.splits, s, RowCopy{});
+    if (c.rows < M)
+        return product_part<E, AK, BK, USE>(c.rest, a, b, p, o, c.rows, 0, M, N, K, c.splits, s, RowCopy{});
+    Out right = o;
+    right.block_first = column_blocks(c.kind, c.cols);
+    return product_part<E, AK, BK, USE>(c.rest, a, b, p, right, 0, c.cols, M, N, K, c.splits, s, RowCopy{});
 }
 
 // Products of parts, four bits each (A's, then B's): one; three of A with one
@@ -919,9 +957,6 @@ hipError_t lay_out(const RowCopy& c, hipStream_t s)
 constexpr int64_t FEW_ROWS = 32;
 constexpr int64_t PIECE_BYTES = int64_t(512) << 20;   // of G at a time
 
-// Runs that a row of N columns leaves, one a wave.
-int64_t column_blocks(ShapeKind kind, int64_t N) { return ceil_div(N, SHAPES[kind].bn) * SHAPES[kind].waves_n; }
-
 // How the three products of one piece are computed.
 struct Pieces {
     Choice logits{}, dx{}, dw{};
@@ -938,7 +973,7 @@ struct Plan {
     Pieces full, last;    // backward: of the full pieces and the last one
     float* row_logits = nullptr;   // by row: splits x T x V
     Run* part = nullptr;           // else: a run per row and column block
-    int64_t nparts = 0;
+    int64_t nparts = 0, main_runs = 0, rest_runs = 0;   // of a row; of the main rows; of the others
     float* target_logit = nullptr;
     void* g = nullptr;
     int64_t piece = 0, ldg = 0;
@@ -984,9 +1019,11 @@ Plan make_plan(int op, const void* X, const void* W, int64_t T, int64_t V, int64
             p.target_logit = static_cast<float*>(a.take(T * 4));
         }
     } else if (op != POSEIDON_XENT_BACKWARD) {
-        p.nparts = column_blocks(p.logits.kind, V);
-        if (p.logits.rows < T)
-            p.nparts = std::max(p.nparts, column_blocks(p.logits.rest, V));
+        p.main_runs = column_blocks(p.logits.kind, p.logits.cols);
+        if (p.logits.cols < V)
+            p.main_runs += column_blocks(p.logits.rest, V - p.logits.cols);
+        p.rest_runs = p.logits.rows < T ? column_blocks(p.logits.rest, V) : 0;
+        p.nparts = std::max(p.main_runs, p.rest_runs);
         p.part = static_cast<Run*>(a.take(T * p.nparts * static_cast<int64_t>(sizeof(Run))));
         p.target_logit = static_cast<float*>(a.take(T * 4));
     }
@@ -1136,8 +1173,7 @@ hipError_t losses(const Plan& p, const Operand& x, const Operand& w, const int64
     o.target_logit = p.target_logit;
     o.target = target;
     POSEIDON_TRY((product<E, true, true, STATS>(p.logits, x, w, ONE, o, T, V, D, s)));
-    return join_runs(p, p.nparts, p.logits.rows, column_blocks(p.logits.kind, V), column_blocks(p.logits.rest, V),
-                     target, T, V, loss, lse, s);
+    return join_runs(p, p.nparts, p.logits.rows, p.main_runs, p.rest_runs, target, T, V, loss, lse, s);
 }
 
 template <typename E>
