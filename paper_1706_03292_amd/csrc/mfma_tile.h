@@ -91,7 +91,7 @@ struct Parts {
 };
 
 // fp32 in memory, multiplied as six bf16 products of its exact three parts
-// (h*h, h*m, m*h, h*l, l*h, m*m: what is dropped is below 2^-23 of a product),
+// (h*h, h*m, m*h, h*l, l*h, m*m: what is dropped is below 2^-21 of a product),
 // the parts made in registers from what the operand reads bring.
 struct Split32 {};
 
@@ -291,7 +291,14 @@ struct Parts3 {
     h8 h, m, l;
 };
 
-// h and m rounded to nearest, l exact (at most eight bits are left).
+// The upper halves of a and b, a's in the low half.
+__device__ __forceinline__ unsigned upper_halves(float a, float b)
+{
+    return __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, b), __builtin_bit_cast(unsigned, a), 0x07060302u);
+}
+
+// h the upper half as it is (rounded, the type's largest values would become
+// infinite), m rounded to nearest, l exact (at most eight bits are left).
 __device__ __forceinline__ Parts3 in_parts3(f8e x)
 {
     u4 part[3];
@@ -300,12 +307,13 @@ __device__ __forceinline__ Parts3 in_parts3(f8e x)
         float a = x[2 * q], b = x[2 * q + 1];
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
-            const unsigned w = __builtin_bit_cast(unsigned, __builtin_convertvector((f2e){a, b}, b2e));
+            const unsigned w = p == 0 ? upper_halves(a, b)
+                                      : __builtin_bit_cast(unsigned, __builtin_convertvector((f2e){a, b}, b2e));
             part[p][q] = w;
             a -= __builtin_bit_cast(float, w << 16);
             b -= __builtin_bit_cast(float, w & 0xffff0000u);
         }
-        part[2][q] = __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, b), __builtin_bit_cast(unsigned, a), 0x07060302u);
+        part[2][q] = upper_halves(a, b);
     }
     return Parts3{__builtin_bit_cast(h8, part[0]), __builtin_bit_cast(h8, part[1]), __builtin_bit_cast(h8, part[2])};
 }

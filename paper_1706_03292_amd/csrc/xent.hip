@@ -23,9 +23,12 @@
 namespace poseidon {
 namespace {
 
-constexpr float LOG2E = 1.44269504f, LN2 = 0.693147181f;
+// exp(a - b).  The difference comes first: a product of a logit and log2 e would
+// overflow where the logit is near the type's lowest value (a class that is to
+// count for nothing), and its rounding error would grow with the logit.
+__device__ __forceinline__ float exp_diff(float a, float b) { return __builtin_amdgcn_exp2f((a - b) * 1.44269504f); }
 
-// A running maximum, in units of log2 e, and the sum of powers of two below it.
+// A running maximum and the sum of exponentials below it.
 struct Run {
     float m, s;
 };
@@ -34,17 +37,12 @@ __device__ __forceinline__ Run join(Run a, Run b)
 {
     const float m = fmaxf(a.m, b.m);
     // A side without a finite maximum (no column, or all -inf) adds nothing.
-    const float ea = a.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(a.m - m);
-    const float eb = b.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(b.m - m);
+    const float ea = a.m == -INFINITY ? 0.f : exp_diff(a.m, m);
+    const float eb = b.m == -INFINITY ? 0.f : exp_diff(b.m, m);
     return Run{m, fmaf(a.s, ea, b.s * eb)};
 }
 
-__device__ __forceinline__ float lse_of(Run r)
-{
-    // m ln 2 to fp32's accuracy: ln 2 in two parts.
-    return r.m == -INFINITY && r.s == 0.f ? -INFINITY
-                                          : fmaf(r.m, 0.693147182f, fmaf(r.m, -1.90465421e-9f, logf(r.s)));
-}
+__device__ __forceinline__ float lse_of(Run r) { return r.m + logf(r.s); }
 
 __device__ __forceinline__ bool counts(int64_t target, int64_t V) { return target >= 0 && target < V; }
 
@@ -154,22 +152,19 @@ __device__ __forceinline__ void finish_stats(acc4 (&acc)[T::TM][T::TN], const Ou
         // A NaN logit is no maximum, but makes the sum NaN.
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
-        const float from = top == -INFINITY ? 0.f : top * LOG2E;
+        const float from = top == -INFINITY ? 0.f : top;
         float sum = 0.f;
 #pragma unroll
         for (int j = 0; j < T::TN; ++j)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
                 if (!EDGE || first + 16 * j + r < cols)
-                    sum += __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], LOG2E, -from));
+                    sum += exp_diff(acc[i][j][r], from);
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
         if (row) {
-            // The sum is of 2^(s log2 e - from); `from` is the maximum's
-            // multiple as rounded, so the maximum that belongs to the sum is
-            // from / log2 e: join() and the last logarithm put it back.
             if (lane < 16)
-                o.part[at * o.nparts + block] = Run{top == -INFINITY ? -INFINITY : from, sum};
+                o.part[at * o.nparts + block] = Run{top, sum};
             const int64_t t = target[i] - n0 - first;
             if (t >= 0 && t < T::WN) {
 #pragma unroll
@@ -183,9 +178,7 @@ __device__ __forceinline__ void finish_stats(acc4 (&acc)[T::TM][T::TN], const Ou
     }
 }
 
-// GRAD.  p = 2^(s log2 e - lse log2 e): the product of lse is rounded once a
-// row, and what that leaves goes into the row's factor, so that a probability is
-// as exact as its logit.  (The rounding of log2 e itself concerns only s - lse.)
+// GRAD.
 template <typename T, bool EDGE>
 __device__ __forceinline__ void finish_grad(acc4 (&acc)[T::TM][T::TN], const Out& o, int64_t m0, int64_t n0, int rows,
                                             int cols, int wm, int wn, int lane)
@@ -211,14 +204,11 @@ __device__ __forceinline__ void finish_grad(acc4 (&acc)[T::TM][T::TN], const Out
         const int64_t at = m0 + m, t = target[i];
         const bool has = counts(t, o.V);
         const float lse = has ? lses[i] : 0.f, d = has ? dlosses[i] : 0.f;
-        const float from = lse * LOG2E;
-        const float rest = fmaf(lse, LOG2E, -from);
-        const float scale = fmaf(d, -rest * LN2, d);
 #pragma unroll
         for (int j = 0; j < T::TN; ++j)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const float g = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], LOG2E, -from)) * scale;
+                const float g = exp_diff(acc[i][j][r], lse) * d;
                 // Rows without a target and, up to the row's end, past V: zeros.
                 acc[i][j][r] = has && (!EDGE || first + STRIDE * j + r < cols) ? g : 0.f;
             }
@@ -492,13 +482,12 @@ __device__ __forceinline__ Run held_logits(const float* s, int n, int splits, in
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             top = fmaxf(top, held[e][i]);
-    top *= LOG2E;
     const float from = top == -INFINITY ? 0.f : top;
 #pragma unroll
     for (int e = 0; e < EACH; ++e)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            sum += __builtin_amdgcn_exp2f(fmaf(held[e][i], LOG2E, -from));   // past n: 0
+            sum += exp_diff(held[e][i], from);   // past n: 0
     return Run{top, sum};
 }
 
@@ -517,15 +506,7 @@ __device__ __forceinline__ Run group_join(Run r)
 // What turns a row's logits into G (as finish_grad does).
 struct RowGrad {
     bool has;
-    float from, scale, dloss;
-    __device__ __forceinline__ RowGrad(bool has_, float lse, float d)
-    {
-        has = has_;
-        dloss = d;
-        from = has ? lse * LOG2E : 0.f;
-        const float rest = fmaf(lse, LOG2E, -from);
-        scale = has ? fmaf(d, -rest * LN2, d) : 0.f;
-    }
+    float lse, dloss;
 };
 
 // Four of a row's values from column v on: G to U and to the operand of dX (bf16
@@ -537,7 +518,7 @@ __device__ __forceinline__ void put_grad(const RowGrad& q, acc4 x, int v, int V,
     const int64_t hit = q.has ? target - v : -1;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        x[i] = q.has && v + i < V ? __builtin_amdgcn_exp2f(fmaf(x[i], LOG2E, -q.from)) * q.scale : 0.f;
+        x[i] = q.has && v + i < V ? exp_diff(x[i], q.lse) * q.dloss : 0.f;
         if (hit == i) {
             x[i] -= q.dloss;
             *target_rest = x[i] - static_cast<float>(static_cast<G>(x[i]));
@@ -572,7 +553,7 @@ __global__ __launch_bounds__(NT) void row_kernel(const float* logits, int splits
             if (!has)
                 loss[row] = 0.f;
         }
-        const RowGrad q(has, lse, d);
+        const RowGrad q{has, lse, d};
 #pragma unroll
         for (int e = 0; e < EACH; ++e) {
             const int v = at + 4 * NT * e;
@@ -645,7 +626,7 @@ __global__ __launch_bounds__(THREADS) void chunk_grad_kernel(const Run* __restri
         const bool has = counts(t, V);
         if (from == 0 && threadIdx.x == 0)
             loss[row] = has ? lse - target_logit[row] : 0.f;
-        const RowGrad q(has, lse, has ? dloss[row] : 0.f);
+        const RowGrad q{has, lse, has ? dloss[row] : 0.f};
         // The last chunk also clears what is between V and the operand's row end.
 #pragma unroll
         for (int e = 0; e < CHUNK_EACH; ++e)

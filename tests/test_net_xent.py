@@ -17,7 +17,7 @@ F32, BF16 = torch.float32, torch.bfloat16
 # classes and the reverse.
 SIZES = [(1, 1, 1), (1, 1000, 64), (2, 7, 3), (31, 63, 65), (32, 64, 32), (33, 65, 129), (64, 128, 64), (128, 128, 8),
          (129, 257, 72), (200, 1000, 100), (257, 300, 256), (300, 2000, 513), (1000, 40, 16), (5, 21841, 40),
-         (700, 513, 1030)]
+         (700, 513, 1030), (1174, 10709, 640), (2308, 6801, 320)]
 
 
 def make(T, V, D, dtype, seed, ignore=0.2):
@@ -131,6 +131,37 @@ def test_large_logits(dtype):
     _, u2, x2 = api.xent_factor(Xd, Wd, td, dd)
     for got, want, b, what in ((l1, loss, bl, "loss"), (e1, lse, be, "lse"), (x1, dX, bX, "dX"), (w1, dW, bW, "dW"),
                                (u2, G, bG, "U"), (x2, dX, bX, "factor dX")):
+        within(got, want, b, what)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T,V,D", [(32, 1000, 64), (300, 2100, 200), (1300, 5000, 264), (5, 21841, 40)])
+def test_classes_at_the_lowest_value(T, V, D, dtype):
+    """Classes kept out by a weight of the type's lowest value at a feature that
+    is 1 (a padded vocabulary): whole tiles of them and odd ones, results as
+    without them."""
+    from paper_1706_03292_amd import api
+    log(f"xent lowest {T}x{V}x{D} {dtype}")
+    X, W, target, dloss = make(T, V, D, dtype, 21)
+    out = (torch.arange(V) // 256 % 2 == 1) | (torch.arange(V) % 7 == 3) | (torch.arange(V) >= V - 90)
+    X[:, 0], W[:, 0] = 1, 0
+    W[out] = 0
+    W[out, 0] = torch.finfo(dtype).min
+    kept = torch.nonzero(~out)[:, 0]
+    none = (target < 0) | (target >= V)
+    place = torch.randint(0, len(kept), (T,), generator=torch.Generator().manual_seed(22))
+    target = torch.where(none, target, kept[place])
+    small = torch.where(none, torch.full_like(place, -1), place)
+    loss, lse, G, dX, dW = O.xent(X, W[kept], small, dloss)
+    bl, be, bG, bX, bW = O.xent_bounds(X, W[kept], small, dloss, lse, G, dX, dW, dtype == BF16)
+    Xd, Wd, td, dd = (v.to(dev()) for v in (X, W, target, dloss))
+    l1, e1 = api.xent_forward(Xd, Wd, td)
+    x1, w1 = api.xent_backward(Xd, Wd, td, e1, dd)
+    l2, u2, x2 = api.xent_factor(Xd, Wd, td, dd)
+    assert (w1.cpu()[out] == 0).all() and (u2.cpu()[:, out] == 0).all()
+    for got, want, b, what in ((l1, loss, bl, "loss"), (e1, lse, be, "lse"), (x1, dX, bX, "dX"),
+                               (w1.cpu()[kept], dW, bW, "dW"), (l2, loss, bl, "factor loss"),
+                               (u2.cpu()[:, kept], G, bG, "U"), (x2, dX, bX, "factor dX")):
         within(got, want, b, what)
 
 
