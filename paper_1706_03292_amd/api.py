@@ -11,6 +11,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import functools
+import math
 
 import torch
 
@@ -620,7 +621,7 @@ def _rows_cols(x: torch.Tensor) -> tuple[int, int]:
     if not shape:
         raise ValueError("x must have at least one dimension")
     cols = shape[-1]
-    return (shape[0] if len(shape) == 2 else x.numel() // cols if cols else 0), cols
+    return (shape[0] if len(shape) == 2 else x.numel() // cols if cols else math.prod(shape[:-1])), cols
 
 
 def dropout(x: torch.Tensor, p: float, rng: torch.Tensor | None, residual: torch.Tensor | None = None,

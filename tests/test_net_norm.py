@@ -183,6 +183,17 @@ def test_no_rows(dtype):
     assert (dgamma == 0).all() and (dbeta == 0).all()
 
 
+@pytest.mark.parametrize("shape", [(4, 0), (2, 3, 0)])
+def test_no_columns(shape):
+    """A row of no values has no mean; dropout of nothing is nothing."""
+    from paper_1706_03292_amd import api
+    log(f"norm no columns {shape}")
+    x, none = torch.empty(shape, device=dev()), torch.empty(0, device=dev())
+    with pytest.raises(api.PoseidonError):
+        api.norm_forward(x, none, none)
+    assert api.dropout(x, 0.5, state()).shape == shape
+
+
 @DTYPES
 @pytest.mark.parametrize("cols", [96, 1000, 4096])
 def test_any_boundary_and_leading_shape(cols, dtype):
