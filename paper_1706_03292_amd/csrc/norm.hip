@@ -2,7 +2,7 @@
 // and dropout alone (include/poseidon.h gives the formulas).  All of it is a
 // few operations per value, bound by memory: what counts is that every input
 // is read once, every output written once, and that enough loads are in
-// flight.  With residual and dropout, bf16: forward 16384 x 4096 113 us (4.8 TB/s;
+// flight.  With residual and dropout, bf16: forward 16384 x 4096 112 us (4.8 TB/s;
 // a device copy reaches 5.2), backward 16384 x 2048 73 us (4.6 TB/s), dropout
 // alone 8191 x 4096 38 us (5.3 TB/s).
 //

@@ -13,8 +13,8 @@
 // rows take the forward pass too through memory.
 //
 // Bound: 2TVD operations a product on the matrix cores for many rows (8192 x
-// 32768 x 2048 bf16: 0.90 ms, 1.2 PFLOP/s; backward 4097 x 50001 x 1024 2.2 ms,
-// 512 x 21841 x 4096 fp32 1.56 ms), reading W for few (32 x 21841 x 4096 fp32: 85
+// 32768 x 2048 bf16: 0.89 ms, 1.2 PFLOP/s; backward 4097 x 50001 x 1024 2.2 ms,
+// 512 x 21841 x 4096 fp32 1.54 ms), reading W for few (32 x 21841 x 4096 fp32: 85
 // us, of which the product 75 at 4.7 TB/s; factors in bf16 95 us, W read twice).
 #include <math.h>
 
