@@ -708,8 +708,8 @@ int poseidon_norm_backward(const void* dy, const void* h, const float* gamma, co
  * fp32 inputs are multiplied to fp32's accuracy, by fp32 products or (larger
  * ones) by six products of exact bf16 parts as poseidon_sf_apply's; the latter
  * make NaN of infinite operands and of finite ones above 3.39e38.  bf16 inputs
- * are multiplied on the bf16 matrix cores, with G rounded to bf16 for a bf16 dX
- * (its entry at the target exactly) and in three exact parts for dW.
+ * are multiplied on the bf16 matrix cores, with G in two bf16 parts (2^-16 of
+ * each entry is left out) for a bf16 dX and in three exact parts for dW.
  * Returns POSEIDON_OK, POSEIDON_ERR_INVALID_ARG (negative T; V or D < 1; T
  * above 2^24, V above 2^21, D above 2^20, T*V above 2^37; an unknown dtype; NULL arrays with
  * work; outputs overlapping each other, the workspace or an input; a workspace

@@ -13,9 +13,9 @@
 // rows take the forward pass too through memory.
 //
 // Bound: 2TVD operations a product on the matrix cores for many rows (8192 x
-// 32768 x 2048 bf16: 0.89 ms, 1.2 PFLOP/s; backward 4097 x 50001 x 1024 2.2 ms,
+// 32768 x 2048 bf16: 0.89 ms, 1.2 PFLOP/s; backward 4097 x 50001 x 1024 2.6 ms,
 // 512 x 21841 x 4096 fp32 1.54 ms), reading W for few (32 x 21841 x 4096 fp32: 85
-// us, of which the product 75 at 4.7 TB/s; factors in bf16 95 us, W read twice).
+// us, of which the product 75 at 4.7 TB/s; factors in bf16 101 us, W read twice).
 #include <math.h>
 
 #include "mfma_tile.h"
@@ -66,13 +66,6 @@ struct Out {
     void* g;
     int64_t ldg, g_plane;
     int64_t v0, V;
-    // GRAD writes, and STORE of a bf16 dX reads, what rounding G to bf16 left of
-    // each row's entry at its target: that entry is near -dloss where all others
-    // are small, and its rounding error, the same in all of the row's dX, would
-    // be most of the error.  STORE adds it times the target's row of W.
-    float* target_rest;
-    const void* W;
-    int64_t ldw;
     // STORE: C (ldc apart), fp32 or bf16, added to what is there or not; with
     // several splits of k, split z's sums go to c + z * split_stride.
     void* c;
@@ -218,11 +211,8 @@ __device__ __forceinline__ void finish_grad(acc4 (&acc)[T::TM][T::TN], const Out
             for (int j = 0; j < T::TN; ++j)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    if (tl == STRIDE * j + r) {
+                    if (tl == STRIDE * j + r)
                         acc[i][j][r] -= d;
-                        if (o.target_rest)
-                            o.target_rest[at] = acc[i][j][r] - static_cast<float>(static_cast<__bf16>(acc[i][j][r]));
-                    }
         }
         const int64_t to = at * o.ldg + n0 + first;
         // Runs of values that lie together (SPREAD: eight, else four).
@@ -261,42 +251,18 @@ __device__ __forceinline__ void finish_store(acc4 (&acc)[T::TM][T::TN], const Ou
                                              int cols, int wm, int wn, int lane, int z)
 {
     const int first = wn + 4 * (lane >> 4);
-    int64_t target[T::TM];
-    float rests[T::TM];
-    const bool mend = o.target_rest && z == 0;
-    if (mend) {
-#pragma unroll
-        for (int i = 0; i < T::TM; ++i) {
-            const int m = wm + 16 * i + (lane & 15);
-            const int64_t at = m0 + (m < rows ? m : 0);
-            target[i] = o.target[at];
-            rests[i] = o.target_rest[at];
-        }
-    }
 #pragma unroll
     for (int i = 0; i < T::TM; ++i) {
         const int m = wm + 16 * i + (lane & 15);
         if (m >= rows)
             continue;
         const int64_t at = m0 + m;
-        float rest = 0.f;
-        const typename T::M* w = nullptr;
-        if (mend && counts(target[i], o.V)) {
-            rest = rests[i];
-            w = static_cast<const typename T::M*>(o.W) + target[i] * o.ldw + n0 + first;
-        }
 #pragma unroll
         for (int j = 0; j < T::TN; ++j) {
             const int left = EDGE ? cols - first - 16 * j : 4;
             if (left <= 0)
                 continue;
             acc4 v = acc[i][j];
-            if (w) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (r < left)
-                        v[r] = fmaf(rest, static_cast<float>(w[16 * j + r]), v[r]);
-            }
             const int64_t to = at * o.ldc + n0 + first + 16 * j;
             if (o.bf16) {
                 put4(static_cast<__bf16*>(o.c) + to, __builtin_convertvector(v, b4), left);
@@ -509,27 +475,27 @@ struct RowGrad {
     float lse, dloss;
 };
 
-// Four of a row's values from column v on: G to U and to the operand of dX (bf16
-// or fp32; `g` up to ldg values, zeros past V).
+// Four of a row's values from column v on: G to U and to the operand of dX (fp32,
+// or bf16 in two parts `plane` apart; `g` up to ldg values, zeros past V).
 template <typename G>
-__device__ __forceinline__ void put_grad(const RowGrad& q, acc4 x, int v, int V, int ldg, int64_t target, float* U,
-                                         G* g, float* target_rest)
+__device__ __forceinline__ void put_grad(const RowGrad& q, acc4 x, int v, int V, int ldg, int64_t plane,
+                                         int64_t target, float* U, G* g)
 {
     const int64_t hit = q.has ? target - v : -1;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         x[i] = q.has && v + i < V ? exp_diff(x[i], q.lse) * q.dloss : 0.f;
-        if (hit == i) {
+        if (hit == i)
             x[i] -= q.dloss;
-            *target_rest = x[i] - static_cast<float>(static_cast<G>(x[i]));
-        }
     }
     if (v < V)
         put4(U + v, x, V - v);
     if (v < ldg) {   // ldg: a multiple of eight
-        if constexpr (sizeof(G) == 2)
-            *reinterpret_cast<b4*>(g + v) = __builtin_convertvector(x, b4);
-        else
+        if constexpr (sizeof(G) == 2) {
+            const b4 h = __builtin_convertvector(x, b4);
+            *reinterpret_cast<b4*>(g + v) = h;
+            *reinterpret_cast<b4*>(g + plane + v) = __builtin_convertvector(x - __builtin_convertvector(h, acc4), b4);
+        } else
             *reinterpret_cast<acc4*>(g + v) = x;
     }
 }
@@ -538,7 +504,7 @@ template <typename G, int NT, int EACH, bool FACTOR>
 __global__ __launch_bounds__(NT) void row_kernel(const float* logits, int splits, int64_t T, int64_t stride,
                                                  const int64_t* __restrict__ target, const float* __restrict__ dloss,
                                                  int V, float* __restrict__ loss, float* __restrict__ lse_out,
-                                                 float* U, G* __restrict__ g, int ldg, float* __restrict__ target_rest)
+                                                 float* U, G* __restrict__ g, int ldg, int64_t plane)
 {
     const int at = 4 * static_cast<int>(threadIdx.x);
     for (int64_t row = blockIdx.x; row < T; row += gridDim.x) {
@@ -564,7 +530,7 @@ __global__ __launch_bounds__(NT) void row_kernel(const float* logits, int splits
                         loss[row] = lse - held[e][i];
             }
             if constexpr (FACTOR)
-                put_grad(q, held[e], v, V, ldg, t, U + row * V, g + row * ldg, target_rest + row);
+                put_grad(q, held[e], v, V, ldg, plane, t, U + row * V, g + row * ldg);
         }
     }
 }
@@ -607,8 +573,7 @@ __global__ __launch_bounds__(THREADS) void chunk_grad_kernel(const Run* __restri
                                                              const int64_t* __restrict__ target,
                                                              const float* __restrict__ dloss, int V,
                                                              float* __restrict__ loss, float* __restrict__ U,
-                                                             G* __restrict__ g, int ldg,
-                                                             float* __restrict__ target_rest)
+                                                             G* __restrict__ g, int ldg, int64_t plane)
 {
     const int at = 4 * static_cast<int>(threadIdx.x);
     for (int64_t b = blockIdx.x; b < T * chunks; b += gridDim.x) {
@@ -630,7 +595,7 @@ __global__ __launch_bounds__(THREADS) void chunk_grad_kernel(const Run* __restri
         // The last chunk also clears what is between V and the operand's row end.
 #pragma unroll
         for (int e = 0; e < CHUNK_EACH; ++e)
-            put_grad(q, x[e], from + at + 4 * THREADS * e, V, ldg, t, U + row * V, g + row * ldg, target_rest + row);
+            put_grad(q, x[e], from + at + 4 * THREADS * e, V, ldg, plane, t, U + row * V, g + row * ldg);
     }
 }
 
@@ -904,9 +869,9 @@ hipError_t product(const Choice& c, const Operand& a, const Operand& b, const Pa
     return product_part<E, AK, BK, USE>(c.rest, a, b, p, right, 0, c.cols, M, N, K, c.splits, s, RowCopy{});
 }
 
-// Products of parts, four bits each (A's, then B's): one; three of A with one
-// of B.
-constexpr Parts ONE{1, 0}, THREE_A{3, 0x210};
+// Products of parts, four bits each (A's, then B's): one; two, three of A with
+// one of B.
+constexpr Parts ONE{1, 0}, TWO_A{2, 0x10}, THREE_A{3, 0x210};
 
 template <typename O>
 hipError_t join_splits(const float* part, int64_t splits, int64_t n, O* out, hipStream_t s)
@@ -958,7 +923,6 @@ struct Plan {
     float* target_logit = nullptr;
     void* g = nullptr;
     int64_t piece = 0, ldg = 0;
-    float* target_rest = nullptr;
     float* dx = nullptr;
     float* dw = nullptr;
     int64_t bytes = 0;
@@ -967,11 +931,20 @@ struct Plan {
 // dW = G^T X: G is fp32, or (bf16 X) its three exact bf16 parts.
 template <typename E>
 constexpr Parts DW_PARTS = sizeof(E) == 2 ? THREE_A : ONE;
+// dX = G W: of a bf16 G the first two parts, which leave out 2^-16 of each entry.
+// One part (2^-8, the target's entry exact) hides below dX's own rounding where
+// W's rows average to 0, but a row of G sums to 0, so what W's rows share cancels
+// in exact arithmetic and what rounding left of it does not: with a shared
+// component of 30 times their spread dX was off by 3.6 to 5.8 times its rounding.
+// The second part costs a product (backward 4097 x 50001 x 1024 2.20 -> 2.57 ms,
+// factors 32 x 21841 x 4096 95 -> 101 us).
+template <typename E>
+constexpr Parts DX_PARTS = sizeof(E) == 2 ? TWO_A : ONE;
 
 template <typename E>
 Pieces pieces(int64_t T, int64_t rows, int64_t D)
 {
-    return Pieces{choose<E, GRAD>(T, rows, D, 1, false), choose<E, STORE>(T, D, rows, 1, true),
+    return Pieces{choose<E, GRAD>(T, rows, D, 1, false), choose<E, STORE>(T, D, rows, DX_PARTS<E>.count, true),
                   choose<E, STORE>(rows, D, T, DW_PARTS<E>.count, true)};
 }
 
@@ -1012,10 +985,10 @@ Plan make_plan(int op, const void* X, const void* W, int64_t T, int64_t V, int64
         p.bytes = a.at;
         return p;
     }
-    // G: fp32, or in bf16 parts (for a factor's bf16 dX one of them).
-    const int64_t g_value = SZ == 4 ? 4 : op == POSEIDON_XENT_FACTOR ? 2 : 6;
+    // G: fp32, or in bf16 parts (for a factor's bf16 dX two of them).
+    const int64_t g_value = SZ == 4 || op == POSEIDON_XENT_FACTOR ? 4 : 6;
     p.piece = round_up(V, GROUP);
-    p.full.dx = choose<E, STORE>(T, D, V, 1, true);
+    p.full.dx = choose<E, STORE>(T, D, V, DX_PARTS<E>.count, true);
     if (op == POSEIDON_XENT_BACKWARD) {
         // Pieces of the vocabulary within the budget: equal ones, or as many
         // classes as make whole rounds of dW's largest tiles and a rest;
@@ -1053,7 +1026,6 @@ Plan make_plan(int op, const void* X, const void* W, int64_t T, int64_t V, int64
     // channel (G of 4096 x 16384, in parts: 222 us, with 512 bytes more 200).
     p.ldg = p.piece + (p.piece * (SZ == 4 ? 4 : 2) % 4096 == 0 ? 512 / SZ : 0);
     p.g = a.take(T * p.ldg * g_value);
-    p.target_rest = static_cast<float*>(a.take(T * 4));
     if (p.full.dx.splits > 1 || (p.piece < V && SZ == 2))
         p.dx = static_cast<float*>(a.take(p.full.dx.splits * T * D * 4));
     p.bytes = a.at;
@@ -1118,7 +1090,7 @@ hipError_t rows_done(const Plan& p, const int64_t* target, const float* dloss, i
     if (V <= ROW_MOST) {
         auto run = [&](auto* k, int threads) {
             k<<<grid_for(T), threads, 0, s>>>(logits, splits, T, T * V, target, dloss, v, loss, lse, U, g, ldg,
-                                              p.target_rest);
+                                              T * p.ldg);
         };
         // Groups of eight end the operand's rows, so a row's last group counts whole.
         const int64_t values = round_up(V, GROUP);
@@ -1136,7 +1108,7 @@ hipError_t rows_done(const Plan& p, const int64_t* target, const float* dloss, i
     POSEIDON_TRY(hipGetLastError());
     if constexpr (FACTOR) {
         chunk_grad_kernel<G><<<grid_for(T * chunks), THREADS, 0, s>>>(p.part, T, chunks, p.target_logit, target, dloss,
-                                                                     v, loss, U, g, ldg, p.target_rest);
+                                                                     v, loss, U, g, ldg, T * p.ldg);
         return hipGetLastError();
     } else {
         return join_runs(p, chunks, T, chunks, chunks, target, T, V, loss, lse, s);
@@ -1172,9 +1144,8 @@ hipError_t forward_typed(const E* X, const E* W, const int64_t* target, int64_t 
 
 // dX = G W for one piece of the vocabulary (the first replaces, the others add).
 template <typename E>
-hipError_t input_gradient(const Plan& p, const Operand& g, const Operand& w, const Operand& whole_w,
-                          const int64_t* target, int64_t T, int64_t V, int64_t D, int64_t v0, int64_t vp, E* dX,
-                          hipStream_t s)
+hipError_t input_gradient(const Plan& p, const Operand& g, const Operand& w, int64_t T, int64_t V, int64_t D,
+                          int64_t v0, int64_t vp, E* dX, hipStream_t s)
 {
     constexpr bool BF16 = sizeof(E) == 2;
     const bool first = v0 == 0, last = v0 + vp == V;
@@ -1185,14 +1156,7 @@ hipError_t input_gradient(const Plan& p, const Operand& g, const Operand& w, con
     o.split_stride = T * D;
     o.bf16 = BF16 && !p.dx;
     o.add = !first;
-    if (BF16 && last) {   // every piece has left its targets' rest by now
-        o.target_rest = p.target_rest;
-        o.target = target;
-        o.V = V;
-        o.W = whole_w.p;
-        o.ldw = whole_w.ld;
-    }
-    POSEIDON_TRY((product<E, true, false, STORE>(c, g, w, ONE, o, T, D, whole_chunks<E>(vp), s)));
+    POSEIDON_TRY((product<E, true, false, STORE>(c, g, w, DX_PARTS<E>, o, T, D, whole_chunks<E>(vp), s)));
     return last && p.dx ? join_splits(p.dx, p.full.dx.splits, T * D, dX, s) : hipSuccess;
 }
 
@@ -1211,7 +1175,6 @@ hipError_t logit_gradient(const Plan& p, const Operand& x, const Operand& w, con
     o.g_plane = T * p.ldg;
     o.v0 = v0;
     o.V = V;
-    o.target_rest = sizeof(E) == 2 ? p.target_rest : nullptr;
     const Choice& c = vp == std::min(p.piece, V) ? p.full.logits : p.last.logits;
     return product<E, true, true, GRAD>(c, x, w, ONE, o, T, vp, D, s, copy);
 }
@@ -1233,7 +1196,7 @@ hipError_t backward_typed(const E* X, const E* W, const int64_t* target, const f
         const Operand wp{static_cast<const E*>(w.p) + v0 * w.ld, w.ld, vp, 0};
         if (T > 0) {
             POSEIDON_TRY(logit_gradient<E>(p, x, wp, target, lse, dloss, T, V, D, v0, vp, v0 == 0 ? clean : RowCopy{}, s));
-            POSEIDON_TRY((input_gradient<E>(p, g, wp, w, target, T, V, D, v0, vp, dX, s)));
+            POSEIDON_TRY((input_gradient<E>(p, g, wp, T, V, D, v0, vp, dX, s)));
         }
         const Choice& c = vp == std::min(p.piece, V) ? p.full.dw : p.last.dw;
         const bool sums = c.splits > 1;
@@ -1257,7 +1220,7 @@ hipError_t factor_typed(const E* X, const E* W, const int64_t* target, const flo
     POSEIDON_TRY(operands(p, X, W, T, V, D, x, w, s));
     POSEIDON_TRY(row_logits<E>(p, x, w, T, V, D, U, s));
     POSEIDON_TRY((rows_done<E, true>(p, target, dloss, T, V, loss, nullptr, U, s)));
-    return input_gradient<E>(p, Operand{p.g, p.ldg, T, T * p.ldg}, w, w, target, T, V, D, 0, V, dX, s);
+    return input_gradient<E>(p, Operand{p.g, p.ldg, T, T * p.ldg}, w, T, V, D, 0, V, dX, s);
 }
 
 }  // namespace
