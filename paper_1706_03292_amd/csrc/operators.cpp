@@ -136,9 +136,11 @@ extern "C" int poseidon_norm_backward(const void* dy, const void* h, const float
                                       float* dbeta, void* workspace, int64_t workspace_bytes, hipStream_t stream)
 {
     const int64_t size = size_of(dtype);
-    const int32_t thr = threshold(p);
+    int32_t thr = threshold(p);
     if (!size || !sizes_ok(rows, cols) || cols > MOST_COLS || thr < 0)
         return POSEIDON_ERR_INVALID_ARG;
+    if (rows == 0)
+        thr = 0;   // a launch still clears dgamma and dbeta: without rows nothing is dropped, and no rng is read
     if (cols < 1)
         return rows == 0 ? POSEIDON_OK : POSEIDON_ERR_INVALID_ARG;
     if (!dgamma || !dbeta || (rows > 0 && (!dy || !h || !gamma || !mean || !rstd || !dh || (thr && (!rng || !dx)))))

@@ -279,3 +279,25 @@ def test_repeated_on_another_stream_and_in_a_graph(dtype):
         for a, b in zip(held, both()):
             assert torch.equal(a, b)
         torch.cuda.synchronize()
+
+
+@DTYPES
+@pytest.mark.parametrize("cols", [40, 2000, 9000])
+def test_norm_backward_of_no_rows_needs_no_generator(cols, dtype):
+    """A C call without rows may leave every array of rows and the generator
+    NULL, with dropout too: dgamma and dbeta are 0."""
+    import ctypes
+
+    from paper_1706_03292_amd import _lib as L
+    log(f"norm_backward no rows, no generator {cols} {dtype}")
+    lib, size = L.lib(), ctypes.c_int64()
+    assert lib.poseidon_norm_workspace(0, cols, ctypes.byref(size)) == L.OK
+    dgamma, dbeta = torch.full((2, cols), 3.0, device=dev())
+    ws = torch.empty(max(size.value, 16), dtype=torch.uint8, device=dev())
+    code = L.F32 if dtype == F32 else L.BF16
+    for p in (0.0, 0.5, 1.0):
+        assert lib.poseidon_norm_backward(None, None, None, None, None, None, 0, cols, code, p, None, None, None,
+                                          dgamma.data_ptr(), dbeta.data_ptr(), ws.data_ptr(), size.value,
+                                          torch.cuda.current_stream().cuda_stream) == L.OK
+        assert (dgamma == 0).all() and (dbeta == 0).all()
+        dgamma.fill_(3.0), dbeta.fill_(3.0)
