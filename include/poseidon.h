@@ -706,8 +706,9 @@ int poseidon_norm_backward(const void* dy, const void* h, const float* gamma, co
  * factor U = G (T x V fp32; the layer's V factor is X), the losses and dX in one
  * call.
  * fp32 inputs are multiplied to fp32's accuracy, by fp32 products or (larger
- * ones) by six products of exact bf16 parts as poseidon_sf_apply's; the latter
- * make NaN of infinite operands and of finite ones above 3.39e38.  bf16 inputs
+ * ones) by six products of exact bf16 parts as poseidon_sf_apply's; a tile of
+ * the latter with a sum that is not finite is made again by fp32 products, so
+ * that infinite operands mean the same at every size.  bf16 inputs
  * are multiplied on the bf16 matrix cores, with G in two bf16 parts (2^-16 of
  * each entry is left out) for a bf16 dX and in three exact parts for dW.
  * Returns POSEIDON_OK, POSEIDON_ERR_INVALID_ARG (negative T; V or D < 1; T

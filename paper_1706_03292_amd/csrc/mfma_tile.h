@@ -92,7 +92,9 @@ struct Parts {
 
 // fp32 in memory, multiplied as six bf16 products of its exact three parts
 // (h*h, h*m, m*h, h*l, l*h, m*m: what is dropped is below 2^-21 of a product),
-// the parts made in registers from what the operand reads bring.
+// the parts made in registers from what the operand reads bring.  An infinity
+// has no such parts (its m is NaN, and so are the sums it meets): a tile with a
+// sum that is not finite is made again by the fp32 products (Tile::InFp32).
 struct Split32 {};
 
 template <typename E>
@@ -356,6 +358,8 @@ struct Tile {
     static constexpr int TM = WM / 16, TN = WN / 16;
     static constexpr bool SPREAD = SPREAD_;   // a lane's sums are 16 neighbours of a row, not four of each block
     static_assert(!SPREAD || (TN == 4 && BKM), "four blocks of k-major rows");
+    // The same tile by the fp32 matrix instructions, in the same LDS.
+    using InFp32 = Tile<M, AK, BKM, BM, BN, WM, WN, STAGES, SPREAD>;
     using PA = Panel<E, BM, NT, AK, false>;
     using PB = Panel<E, BN, NT, BKM, SPREAD>;
     static constexpr int LOADS = PA::LOADS + PB::LOADS;
@@ -650,6 +654,35 @@ struct Tile {
         __builtin_amdgcn_s_waitcnt(wait_imm(0, 0));
     }
 };
+
+// Whether a sum of the wave's that lies within the tile's rows and cols is not
+// finite (past them are other rows' values).
+template <typename T>
+__device__ __forceinline__ bool any_not_finite(const acc4 (&acc)[T::TM][T::TN], int rows, int cols)
+{
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int m = (w / T::NWN) * T::WM + (lane & 15), n = (w % T::NWN) * T::WN + 4 * (lane >> 4);
+    float zero = 0.f;   // 0 times what is finite
+    if (rows == T::BM && cols == T::BN) {
+#pragma unroll
+        for (int i = 0; i < T::TM; ++i)
+#pragma unroll
+            for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    zero = fmaf(acc[i][j][r], 0.f, zero);
+    } else {
+#pragma unroll
+        for (int i = 0; i < T::TM; ++i)
+#pragma unroll
+            for (int j = 0; j < T::TN; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (m + 16 * i < rows && n + 16 * j + r < cols)
+                        zero = fmaf(acc[i][j][r], 0.f, zero);
+    }
+    return zero != 0.f;   // NaN
+}
 
 // Workgroup number -> tile: consecutive workgroups go to the eight dies in
 // turn, so each die gets a contiguous run of tiles, walked `group` tile rows at

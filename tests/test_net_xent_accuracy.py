@@ -3,15 +3,27 @@ worst-case bound over a whole sum would not see it."""
 import pytest
 import torch
 
-from _helpers import dev, log
+import _net_oracle as O
+from _helpers import dev, kernels, log
+from test_net_xent import make, within
 
 pytestmark = pytest.mark.gpu
 
 F32, BF16 = torch.float32, torch.bfloat16
 
 
+# fp32 sizes whose logits are products of bf16 parts, with a rest of rows in a
+# launch of fp32 products and without.
+SPLIT_SIZES = [(2308, 6801, 320), (1300, 5000, 264)]
+
+
 def rms(x):
     return float(x.double().square().mean().sqrt())
+
+
+def in_parts(call):
+    """How many of a call's launches multiply fp32 in bf16 parts."""
+    return sum("product_kernel<Tile<Split32" in n.replace("poseidon::", "") for n in kernels(call))
 
 
 @pytest.mark.parametrize("T,V,D", [(24, 900, 136), (24, 20000, 64), (300, 2100, 200), (700, 4100, 513)])
@@ -42,3 +54,72 @@ def test_bf16_input_gradient_of_classes_that_share_a_component(T, V, D):
     for got, what in ((x2, "factor dX"), (x1, "dX")):
         err = rms(got.double() - want)
         assert err <= 1.05 * rounding, f"{what}: {err / rounding:.2f} times the rounding of dX"
+
+
+@pytest.mark.parametrize("T,V,D", SPLIT_SIZES)
+def test_classes_masked_by_minus_infinity_where_fp32_is_multiplied_in_parts(T, V, D):
+    """An infinite weight has no finite bf16 parts: classes masked by one still
+    leave every other class as if they were not there, whichever tile a size
+    takes.  (dX is not checked: 0 times infinity is its value.)"""
+    from paper_1706_03292_amd import api
+    log(f"xent masked classes {T}x{V}x{D} f32")
+    X, W, target, dloss = make(T, V, D, F32, 7)
+    X = X.abs() + torch.finfo(F32).eps
+    out = (torch.arange(V) % 997 == 1) | (torch.arange(V) >= V - 70)
+    W[out] = -float("inf")
+    kept = torch.nonzero(~out)[:, 0]
+    none = (target < 0) | (target >= V)
+    place = torch.randint(0, len(kept), (T,), generator=torch.Generator().manual_seed(22))
+    target = torch.where(none, target, kept[place])
+    small = torch.where(none, torch.full_like(place, -1), place)
+    loss, lse, G, dX, dW = O.xent(X, W[kept], small, dloss)
+    bl, be, bG, _, bW = O.xent_bounds(X, W[kept], small, dloss, lse, G, dX, dW, False)
+    Xd, Wd, td, dd = (v.to(dev()) for v in (X, W, target, dloss))
+    assert in_parts(lambda: api.xent_forward(Xd, Wd, td)) >= 1
+    l1, e1 = api.xent_forward(Xd, Wd, td)
+    within(l1, loss, bl, "loss")
+    within(e1, lse, be, "lse")
+    _, w1 = api.xent_backward(Xd, Wd, td, e1, dd)
+    assert (w1.cpu()[out] == 0).all()
+    within(w1.cpu()[kept], dW, bW, "dW")
+    l2, u2, _ = api.xent_factor(Xd, Wd, td, dd)
+    within(l2, loss, bl, "factor loss")
+    within(u2.cpu()[:, kept], G, bG, "U")
+    assert (u2.cpu()[:, out] == 0).all()
+
+
+@pytest.mark.parametrize("T,V,D", SPLIT_SIZES)
+def test_bad_rows_where_fp32_is_multiplied_in_parts(T, V, D):
+    """NaN, infinities and the type's ends in rows without a target leave the
+    tile's other rows as they are, and in rows with one too."""
+    from paper_1706_03292_amd import api
+    log(f"xent bad rows {T}x{V}x{D} f32")
+    X, W, target, dloss = make(T, V, D, F32, 9)
+    none = (target < 0) | (target >= V)
+    bad = X.clone()
+    at = torch.nonzero(none)[:, 0]
+    bad[at[0::4]] = float("nan")
+    bad[at[1::4], ::2] = float("inf")
+    bad[at[2::4], 1::3] = -float("inf")
+    bad[at[3::4], ::5] = torch.finfo(F32).max
+    loss, lse, G, dX, dW = O.xent(X, W, target, dloss)
+    bl, be, bG, bX, bW = O.xent_bounds(X, W, target, dloss, lse, G, dX, dW, False)
+    Xd, Wd, td, dd = (v.to(dev()) for v in (bad, W, target, dloss))
+    l1, e1 = api.xent_forward(Xd, Wd, td)
+    within(l1, loss, bl, "loss")
+    within(e1.cpu()[~none], lse[~none], be[~none], "lse")
+    x1, w1 = api.xent_backward(Xd, Wd, td, e1, dd)
+    within(x1, dX, bX, "dX")
+    within(w1, dW, bW, "dW")
+    l2, u2, x2 = api.xent_factor(Xd, Wd, td, dd)
+    within(l2, loss, bl, "factor loss")
+    within(u2, G, bG, "U")
+    within(x2, dX, bX, "factor dX")
+    seen = (int(at[0]) + 1) % T       # a row with a target, made NaN: its own loss is NaN, no other row's
+    while bool(none[seen]):
+        seen = (seen + 1) % T
+    bad[seen] = float("nan")
+    l3, _ = api.xent_forward(bad.to(dev()), Wd, td)
+    others = torch.arange(T) != seen
+    assert torch.isnan(l3[seen])
+    within(l3.cpu()[others], loss[others], bl[others], "loss beside a NaN row")
