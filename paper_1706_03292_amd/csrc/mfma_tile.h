@@ -91,10 +91,11 @@ struct Parts {
 };
 
 // fp32 in memory, multiplied as six bf16 products of its exact three parts
-// (h*h, h*m, m*h, h*l, l*h, m*m: what is dropped is below 2^-21 of a product),
-// the parts made in registers from what the operand reads bring.  An infinity
-// has no such parts (its m is NaN, and so are the sums it meets): a tile with a
-// sum that is not finite is made again by the fp32 products (Tile::InFp32).
+// (h*h, h*m, m*h, h*l, l*h, m*m: what is dropped is below 2^-23 of a product),
+// the parts made in registers from what the operand reads bring.  An infinity,
+// and a value above 3.39e38, whose h is one, have no such parts (a later one is NaN,
+// and so are the sums it meets): a tile with a sum that is not finite is made
+// again by the fp32 products (Tile::InFp32).
 struct Split32 {};
 
 template <typename E>
@@ -293,14 +294,16 @@ struct Parts3 {
     h8 h, m, l;
 };
 
-// The upper halves of a and b, a's in the low half.
+// The upper halves of a and b, a's in the low half: they are bf16 values, exact
+// where no more than eight bits are left.
 __device__ __forceinline__ unsigned upper_halves(float a, float b)
 {
     return __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, b), __builtin_bit_cast(unsigned, a), 0x07060302u);
 }
 
-// h the upper half as it is (rounded, the type's largest values would become
-// infinite), m rounded to nearest, l exact (at most eight bits are left).
+// h and m rounded to nearest, l exact (at most eight bits are left).  Cut off
+// instead, h would leave m and l twice as large, and what the six products drop
+// four times.
 __device__ __forceinline__ Parts3 in_parts3(f8e x)
 {
     u4 part[3];
@@ -309,8 +312,7 @@ __device__ __forceinline__ Parts3 in_parts3(f8e x)
         float a = x[2 * q], b = x[2 * q + 1];
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
-            const unsigned w = p == 0 ? upper_halves(a, b)
-                                      : __builtin_bit_cast(unsigned, __builtin_convertvector((f2e){a, b}, b2e));
+            const unsigned w = __builtin_bit_cast(unsigned, __builtin_convertvector((f2e){a, b}, b2e));
             part[p][q] = w;
             a -= __builtin_bit_cast(float, w << 16);
             b -= __builtin_bit_cast(float, w & 0xffff0000u);

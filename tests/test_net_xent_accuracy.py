@@ -123,3 +123,85 @@ def test_bad_rows_where_fp32_is_multiplied_in_parts(T, V, D):
     others = torch.arange(T) != seen
     assert torch.isnan(l3[seen])
     within(l3.cpu()[others], loss[others], bl[others], "loss beside a NaN row")
+
+
+def any_mantissa(n, g):
+    """fp32 values of either sign, any mantissa and a few orders."""
+    v = (1 + torch.rand(n, generator=g, dtype=torch.float64)) * 2.0 ** torch.randint(-3, 4, (n,), generator=g)
+    return (v * (2 * torch.randint(0, 2, (n,), generator=g) - 1)).float()
+
+
+def below_a_step(n, g):
+    """fp32 values a little less than one bf16 step above 1.  To nearest, their
+    first part is that step and two parts hold them; cut off, it is 1, the second
+    part is as large as it can be, and so is nearly the third."""
+    third = 2.0 ** -16 * (0.5 + 0.5 * torch.rand(n, generator=g, dtype=torch.float64))
+    return (1 + 2.0 ** -7 - 2.0 ** -15 + third).float()
+
+
+@pytest.mark.parametrize("values,worst,mean", [(any_mantissa, 12.0, None), (below_a_step, None, 2.0)],
+                         ids=["any", "below_a_step"])
+def test_single_fp32_products_in_parts(values, worst, mean):
+    """Each result is one product, the other terms 0, of operands that the call
+    leaves as they are: with logits 0 and lse 0, G is dloss (its column at the
+    target 0), and a row whose one large logit is above all others has it as its
+    lse.  In units of 2^-24 of the product: what the six products of parts drop is
+    below 1 (2 * 2^-8 * 2^-17), their five sums round by at most 1 each, to
+    nearest, or 2, and lse once more: 12.  Without any of the six it is 60 or more.
+    Where two parts hold a value nothing is dropped and three sums round, each by
+    half a unit on average: 2.  With the first part cut off, the dropped products
+    come to 3 there."""
+    from paper_1706_03292_amd import api
+    log(f"xent single products {values.__name__}")
+    T, V, D = SPLIT_SIZES[0]
+    g = torch.Generator().manual_seed(5)
+    one_class, one_row = torch.randperm(V - 1, generator=g)[:D], torch.randperm(T, generator=g)[:D]
+    feature = torch.arange(D)
+    w, d, x = values(D, g), values(T, g), values(D, g)
+    target, lse = torch.full((T,), V - 1, device=dev()), torch.zeros(T, device=dev())
+    dloss = d.to(dev())
+
+    def check(got, want, what):
+        units = ((got.double().cpu() - want) / want).abs() * 2 ** 24
+        assert worst is None or float(units.max()) <= worst, f"{what}: {float(units.max()):.1f} units"
+        assert mean is None or float(units.mean()) <= mean, f"{what}: {float(units.mean()):.2f} units on average"
+
+    # dX[t, k] = dloss_t * W[class of k, k]
+    X, W = torch.zeros(T, D, device=dev()), torch.zeros(V, D)
+    W[one_class, feature] = w
+    W = W.to(dev())
+    assert in_parts(lambda: api.xent_backward(X, W, target, lse, dloss)) == 3
+    check(api.xent_backward(X, W, target, lse, dloss)[0], d.double()[:, None] * w.double(), "dX")
+    # dW[v, k] = dloss of k's row * X[that row, k]
+    X, W = torch.zeros(T, D), torch.zeros(V, D, device=dev())
+    X[one_row, feature] = x
+    X = X.to(dev())
+    assert in_parts(lambda: api.xent_backward(X, W, target, lse, dloss)) == 3
+    dW = api.xent_backward(X, W, target, lse, dloss)[1]
+    check(dW[:-1], (d[one_row].double() * x.double()).expand(V - 1, D), "dW")
+    # lse_t = X[t, k] * W[class of k, k] for the row's one feature k
+    X, W, k = torch.zeros(T, D), torch.zeros(V, D), torch.randint(0, D, (T,), generator=g)
+    W[one_class, feature] = w.abs()
+    X[torch.arange(T), k] = 128 * d.abs()
+    want = 128 * d.double().abs() * w.double().abs()[k]
+    large = want > 60                          # the other classes' e^-60 is nothing beside 1
+    assert int(large.sum()) > T // 2
+    check(api.xent_forward(X.to(dev()), W.to(dev()), target)[1][large.to(dev())], want[large], "lse")
+
+
+def test_single_bf16_products_of_the_weight_gradient():
+    """dW of bf16 inputs from G in three exact parts: each result is one product
+    of an fp32 dloss and a bf16 X (as above).  Two sums round, each by at most a
+    unit of 2^-24, to nearest, or 2: 4.  Two parts of G leave up to 128."""
+    from paper_1706_03292_amd import api
+    log("xent single bf16 products")
+    T, V, D = SPLIT_SIZES[0]
+    g = torch.Generator().manual_seed(6)
+    d, x, one_row = any_mantissa(T, g), any_mantissa(D, g).to(BF16), torch.randperm(T, generator=g)[:D]
+    X = torch.zeros(T, D, dtype=BF16)
+    X[one_row, torch.arange(D)] = x
+    target, lse = torch.full((T,), V - 1, device=dev()), torch.zeros(T, device=dev())
+    _, dW = api.xent_backward(X.to(dev()), torch.zeros(V, D, dtype=BF16, device=dev()), target, lse, d.to(dev()))
+    want = (d[one_row].double() * x.double()).expand(V - 1, D)
+    units = ((dW[:-1].double().cpu() - want) / want).abs() * 2 ** 24
+    assert float(units.max()) <= 4.0, f"{float(units.max()):.1f} units"
