@@ -67,7 +67,8 @@ extern "C" {
 #define POSEIDON_WFBP_SERIAL   3   /* the caller's stream waits for every ready event, then the plain
                                       iteration on it: the serial order (default) */
 
-/* Arithmetic of the SF reconstruction's contraction (poseidon_sf_set_arithmetic). */
+/* Arithmetic of the SF reconstruction's contraction and of the classifier loss's
+   fp32 products (poseidon_sf_set_arithmetic). */
 #define POSEIDON_SF_BF16X6 0   /* split-bf16 products, fp32 accumulation (default) */
 #define POSEIDON_SF_FP32   1   /* fp32 matrix-core products, fp32 accumulation */
 
@@ -119,16 +120,17 @@ int poseidon_sf_apply_momentum(float* W, float* buf, const float* U, const float
 
 /*
  * Chooses how every SF reconstruction enqueued after the call, from any
- * thread, forms its products (the sums, the update and the layouts are the
- * same): POSEIDON_SF_BF16X6 (the default) splits each fp32 operand x exactly
+ * thread, forms its products, and every classifier loss (poseidon_xent_*) its
+ * fp32 ones (the sums, the update, the layouts and workspaces are the same):
+ * POSEIDON_SF_BF16X6 (the default) splits each fp32 operand x exactly
  * into bf16 parts h + m + l (h and m rounded to nearest, l the remainder,
  * which has at most 8 significant bits) and accumulates the six products
  * h*h, h*m, m*h, h*l, l*h and m*m in fp32 on the bf16 matrix cores (the six-
  * product split of Henry, Tang and Heinecke, ARITH 2019); POSEIDON_SF_FP32
  * accumulates the fp32 matrix-core products.  The two agree to fp32
  * rounding on finite operands below 3.39e38 in magnitude (the largest bf16);
- * an infinite or larger operand makes the outputs it reaches NaN with the
- * split products (inf or NaN with the fp32 ones).  The choice is process-wide
+ * an infinite or larger operand makes the reconstructed values it reaches NaN
+ * with the split products (inf or NaN with the fp32 ones).  The choice is process-wide
  * and does not change which scheme Alg. 1 picks.  Returns POSEIDON_OK or
  * POSEIDON_ERR_INVALID_ARG (an unknown value; the setting is unchanged).
  */
@@ -706,9 +708,10 @@ int poseidon_norm_backward(const void* dy, const void* h, const float* gamma, co
  * factor U = G (T x V fp32; the layer's V factor is X), the losses and dX in one
  * call.
  * fp32 inputs are multiplied to fp32's accuracy, by fp32 products or (larger
- * ones) by six products of exact bf16 parts as poseidon_sf_apply's; a tile of
- * the latter with a sum that is not finite is made again by fp32 products, so
- * that infinite operands mean the same at every size.  bf16 inputs
+ * ones, unless poseidon_sf_set_arithmetic chose POSEIDON_SF_FP32) by six products
+ * of exact bf16 parts as poseidon_sf_apply's; a tile of the latter with a sum
+ * that is not finite is made again by fp32 products, so that infinite operands
+ * mean the same at every size.  bf16 inputs
  * are multiplied on the bf16 matrix cores, with G in two bf16 parts (2^-16 of
  * each entry is left out) for a bf16 dX and in three exact parts for dW.
  * Returns POSEIDON_OK, POSEIDON_ERR_INVALID_ARG (negative T; V or D < 1; T

@@ -153,7 +153,8 @@ def sf_apply_momentum(W: torch.Tensor, buf: torch.Tensor, U: torch.Tensor, V: to
 
 
 def sf_set_arithmetic(arithmetic: int) -> None:
-    """How later SF reconstructions form their products, process-wide
+    """How later SF reconstructions, and classifier losses of fp32 inputs, form
+    their products, process-wide
     (poseidon_sf_set_arithmetic): SF_BF16X6 (the default: six products of
     exact bf16 parts, fp32 accumulation) or SF_FP32 (fp32 products)."""
     _check("poseidon_sf_set_arithmetic", L.lib().poseidon_sf_set_arithmetic(int(arithmetic)))

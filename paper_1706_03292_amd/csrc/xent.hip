@@ -846,10 +846,12 @@ hipError_t product_part(ShapeKind kind, const Operand& a, const Operand& b, cons
     case HALF:
         return go(launch_product<Half<E, AK, BK>, USE>);
     case SQUARE:
+        // (The choice of shapes, and with it the workspace, is the split's in
+        // either arithmetic: the setting may change between query and call.)
         if constexpr (sizeof(E) == 4)
-            return go(launch_product<Square<Split32, AK, BK>, USE>);
-        else
-            return go(launch_product<Square<E, AK, BK>, USE>);
+            if (sf_arithmetic() != POSEIDON_SF_FP32)
+                return go(launch_product<Square<Split32, AK, BK>, USE>);
+        return go(launch_product<Square<E, AK, BK>, USE>);
     case TALL:
         if constexpr (sizeof(E) == 2)
             return go(launch_product<Tall<E, AK, BK>, USE>);

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import _net_oracle as O
-from _helpers import dev, kernels, log
+from _helpers import dev, kernels, log, sf_arithmetic
 from test_net_xent import make, within
 
 pytestmark = pytest.mark.gpu
@@ -205,3 +205,32 @@ def test_single_bf16_products_of_the_weight_gradient():
     want = (d[one_row].double() * x.double()).expand(V - 1, D)
     units = ((dW[:-1].double().cpu() - want) / want).abs() * 2 ** 24
     assert float(units.max()) <= 4.0, f"{float(units.max()):.1f} units"
+
+
+@pytest.mark.parametrize("T,V,D", SPLIT_SIZES)
+def test_fp32_products_where_the_process_asks_for_them(T, V, D):
+    """poseidon_sf_set_arithmetic reaches the loss's fp32 products, on workspaces
+    of the same size, and setting it back gives the former bits."""
+    from paper_1706_03292_amd import api
+    log(f"xent arithmetic {T}x{V}x{D}")
+    X, W, target, dloss = make(T, V, D, F32, 13)
+    loss, lse, G, dX, dW = O.xent(X, W, target, dloss)
+    bounds = O.xent_bounds(X, W, target, dloss, lse, G, dX, dW, False)
+    Xd, Wd, td, dd = (v.to(dev()) for v in (X, W, target, dloss))
+
+    def everything():
+        l1, e1 = api.xent_forward(Xd, Wd, td)
+        x1, w1 = api.xent_backward(Xd, Wd, td, e1, dd)
+        return (l1, e1, x1, w1) + tuple(api.xent_factor(Xd, Wd, td, dd))
+
+    before = everything()
+    with sf_arithmetic(api.SF_FP32):
+        assert in_parts(everything) == 0
+        l1, e1, x1, w1, l2, u2, x2 = everything()
+    assert in_parts(everything) >= 3
+    for got, want, b, what in ((l1, loss, bounds[0], "loss"), (e1, lse, bounds[1], "lse"), (u2, G, bounds[2], "U"),
+                               (x1, dX, bounds[3], "dX"), (w1, dW, bounds[4], "dW"), (l2, loss, bounds[0], "factor loss"),
+                               (x2, dX, bounds[3], "factor dX")):
+        within(got, want, b, what)
+    for a, b in zip(before, everything()):
+        assert torch.equal(a, b)
