@@ -458,7 +458,7 @@ __global__ __launch_bounds__(THREADS) void norm_weights_long(const T* __restrict
     store_some(out.dbeta + part + c, cols - c, db);
 }
 
-// dgamma and dbeta from `parts` partial rows: 16 columns a workgroup, 16
+// dgamma and dbeta from `parts` partial rows: 16 columns a workgroup and turn, 16
 // threads a column, each adding every 16th partial, then theirs in order.
 constexpr int SUM_COLS = 16;
 
@@ -469,23 +469,28 @@ __global__ __launch_bounds__(THREADS) void norm_weights_kernel(const float* __re
     constexpr int SLICES = THREADS / SUM_COLS;
     __shared__ float lds[SLICES][SUM_COLS];
     const int lane = threadIdx.x % SUM_COLS, w = threadIdx.x / SUM_COLS;
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * SUM_COLS + lane;
-    float s = 0.f;
-    if (c < 2 * cols)
+    // (The whole workgroup takes each turn: it meets the barriers together.)
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * SUM_COLS; first < 2 * cols;
+         first += static_cast<int64_t>(gridDim.x) * SUM_COLS) {
+        const int64_t c = first + lane;
+        float s = 0.f;
+        if (c < 2 * cols)
 #pragma unroll 16
-        for (int p = w; p < parts; p += SLICES)
-            s += partial[p * 2 * cols + c];
-    lds[w][lane] = s;
-    __syncthreads();
-    if (w == 0 && c < 2 * cols) {
-        s = 0.f;
+            for (int p = w; p < parts; p += SLICES)
+                s += partial[p * 2 * cols + c];
+        lds[w][lane] = s;
+        __syncthreads();
+        if (w == 0 && c < 2 * cols) {
+            s = 0.f;
 #pragma unroll
-        for (int i = 0; i < SLICES; ++i)
-            s += lds[i][lane];
-        if (c < cols)
-            dgamma[c] = s;
-        else
-            dbeta[c - cols] = s;
+            for (int i = 0; i < SLICES; ++i)
+                s += lds[i][lane];
+            if (c < cols)
+                dgamma[c] = s;
+            else
+                dbeta[c - cols] = s;
+        }
+        __syncthreads();
     }
 }
 
@@ -623,8 +628,8 @@ hipError_t backward_typed(const T* dy, const T* h, const float* gamma, const flo
     }
     if (rc != hipSuccess || parts == 1)
         return rc;
-    norm_weights_kernel<<<static_cast<unsigned>(ceil_div(2 * cols, SUM_COLS)), THREADS, 0, s>>>(partial, parts,
-                                                                                               cols, dgamma, dbeta);
+    norm_weights_kernel<<<grid_for(ceil_div(2 * cols, SUM_COLS)), THREADS, 0, s>>>(partial, parts, cols, dgamma,
+                                                                                   dbeta);
     return hipGetLastError();
 }
 

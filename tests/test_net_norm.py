@@ -301,3 +301,28 @@ def test_norm_backward_of_no_rows_needs_no_generator(cols, dtype):
                                           torch.cuda.current_stream().cuda_stream) == L.OK
         assert (dgamma == 0).all() and (dbeta == 0).all()
         dgamma.fill_(3.0), dbeta.fill_(3.0)
+
+
+@pytest.mark.parametrize("rows,cols", [(6, 2 ** 23 + 5), (5, 2 ** 27)])
+def test_norm_backward_of_the_longest_rows(rows, cols):
+    """More columns than one launch of the partial sums' workgroups covers (2^23),
+    and as many as would ask for 2^32 threads: dgamma and dbeta are sums of a few
+    products of bf16 values, each fp32."""
+    from paper_1706_03292_amd import api
+    log(f"norm_backward long {rows}x{cols}")
+    g = torch.Generator(device=dev()).manual_seed(cols)
+    dy = torch.randn(rows, cols, generator=g, device=dev(), dtype=BF16)
+    h = torch.randn(rows, cols, generator=g, device=dev(), dtype=BF16)
+    gamma = torch.ones(cols, device=dev())
+    mean, rstd = torch.linspace(-0.1, 0.2, rows, device=dev()), torch.linspace(0.5, 1.5, rows, device=dev())
+    _, _, dgamma, dbeta = api.norm_backward(dy, h, gamma, mean, rstd)
+    for at in range(0, cols, 1 << 23):
+        c = slice(at, at + (1 << 23))
+        d = dy[:, c].double()
+        n = (h[:, c].double() - mean.double()[:, None]) * rstd.double()[:, None]
+        # rows sums, and two roundings of n in each
+        over = (dgamma[c].double() - (d * n).sum(0)).abs() - (rows + 4) * O.U32 * (
+            d.abs() * (h[:, c].double().abs() + mean.double().abs()[:, None]) * rstd.double()[:, None]).sum(0)
+        assert float(over.max()) <= 0, f"dgamma from {at}"
+        over = (dbeta[c].double() - d.sum(0)).abs() - rows * O.U32 * d.abs().sum(0)
+        assert float(over.max()) <= 0, f"dbeta from {at}"
