@@ -706,7 +706,8 @@ int poseidon_norm_backward(const void* dy, const void* h, const float* gamma, co
  * exact to fp32 whatever the type; with T = 0 it is 0.  poseidon_xent_factor is
  * for a layer that is synchronised by sufficient factors: it leaves the layer's
  * factor U = G (T x V fp32; the layer's V factor is X), the losses and dX in one
- * call.
+ * call.  U is 0 in a row without a target, but the rebuild multiplies it with that
+ * row of the V factor: the caller clears there what is infinite or NaN in X.
  * fp32 inputs are multiplied to fp32's accuracy, by fp32 products or (larger
  * ones, unless poseidon_sf_set_arithmetic chose POSEIDON_SF_FP32) by six products
  * of exact bf16 parts as poseidon_sf_apply's; a tile of the latter with a sum

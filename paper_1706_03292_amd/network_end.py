@@ -69,8 +69,12 @@ class NetworkEnd:
     def step(self, x: torch.Tensor, residual: torch.Tensor, target: torch.Tensor):
         """One iteration: every worker's rows (P*B of them, worker after
         worker), then the synchronisation.  Rows without a target (outside the
-        classes) count for nothing.  Returns (mean loss, dx, dresidual)."""
+        classes) count for nothing, whatever they hold.  Returns (mean loss, dx,
+        dresidual)."""
         valid = (target >= 0) & (target < self.W.shape[0])
+        # Their gradients are 0, but the normalisation's sums and the rebuild from
+        # factors multiply those with the rows' values.
+        x, residual = (torch.where(valid[:, None], v, torch.zeros_like(v)) for v in (x, residual))
         dloss = valid.float() / valid.sum().clamp(min=1)
         W = self.W if self.dtype == torch.float32 else self.W.to(self.dtype)
         out = []

@@ -66,3 +66,26 @@ def test_training_lowers_the_loss(dtype):
         losses.append(float(end.step(x, torch.zeros_like(x), target)[0]))
     assert sum(losses[-5:]) < 0.5 * sum(losses[:5]), losses
     end.close()
+
+
+@pytest.mark.parametrize("classes,features,B,P", [(300, 40, 8, 3), (40, 16, 64, 2)], ids=["factors", "shards"])
+def test_rows_without_a_target_count_for_nothing(classes, features, B, P):
+    """A step whose padding rows hold NaN and infinities gives the bits of one
+    whose padding rows hold zeros."""
+    from paper_1706_03292_amd.network_end import NetworkEnd
+    log(f"network end padding {classes}x{features} B={B} P={P}")
+    g = torch.Generator().manual_seed(4)
+    x, res = torch.randn(P * B, features, generator=g), torch.randn(P * B, features, generator=g)
+    target = torch.randint(0, classes, (P * B,), generator=g)
+    target[::5], target[3] = -1, classes
+    none = (target < 0) | (target >= classes)
+    left = []
+    for fill in (0.0, float("nan"), float("inf")):
+        a, b = (torch.where(none[:, None], torch.full_like(v, fill), v).to(dev()) for v in (x, res))
+        end = NetworkEnd(classes, features, B, P, 0.25, momentum=0.9, p=0.25, seed=3)
+        loss, dx, dres = end.step(a, b, target.to(dev()))
+        left.append((loss, dx, dres, end.W.clone(), end.gamma.clone(), end.beta.clone()))
+        end.close()
+    for now in left[1:]:
+        for a, b in zip(left[0], now):
+            assert torch.isfinite(b).all() and torch.equal(a, b)
