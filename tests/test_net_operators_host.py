@@ -142,3 +142,45 @@ def test_binding_asks_for_the_generator():
     assert api._rng(None, 0.0) is False
     with pytest.raises(TypeError):
         api._rng(torch.zeros(2), 0.1)
+
+
+def test_xent_limits_each_on_its_own():
+    """Rows, classes, features and logits at their limits and one past them, the
+    others small."""
+    lib, n = L.lib(), ctypes.c_int64()
+
+    def size(T, V, D, dtype=L.BF16, op=L.XENT_FORWARD):
+        return lib.poseidon_xent_workspace(op, A, B, T, V, D, dtype, ctypes.byref(n))
+
+    for op in (L.XENT_FORWARD, L.XENT_BACKWARD, L.XENT_FACTOR):
+        for dtype in (L.F32, L.BF16):
+            assert size(2 ** 24, 2, 1, dtype, op) == L.OK and size(2 ** 24 + 1, 2, 1, dtype, op) == BAD
+            assert size(2, 2 ** 21, 1, dtype, op) == L.OK and size(2, 2 ** 21 + 1, 1, dtype, op) == BAD
+            assert size(2, 2, 2 ** 20, dtype, op) == L.OK and size(2, 2, 2 ** 20 + 1, dtype, op) == BAD
+            assert size(2 ** 17, 2 ** 20, 1, dtype, op) == L.OK and size(2 ** 17 + 1, 2 ** 20, 1, dtype, op) == BAD
+
+
+@pytest.mark.parametrize("W,D,copied", [(0x1000, 66, False), (0x1004, 66, False), (0x1002, 66, True), (0x1004, 64, False),
+                                        (0x1000, 65, True), (0x1004, 65, True)])
+def test_a_weight_on_rows_of_4_bytes_is_not_copied(W, D, copied):
+    """bf16 rows that all start on 4-byte boundaries are read as they are, on
+    16-byte boundaries or not; others are laid out again in the workspace.  fp32
+    rows always are on them."""
+    lib, n = L.lib(), ctypes.c_int64()
+    V = 1000
+    for op in (L.XENT_FORWARD, L.XENT_BACKWARD, L.XENT_FACTOR):
+        got = []
+        for at in (0x1000 if D % 2 == 0 else None, W):
+            if at is None:
+                got.append(None)
+                continue
+            assert lib.poseidon_xent_workspace(op, A, ctypes.c_void_p(at), 8, V, D, L.BF16, ctypes.byref(n)) == L.OK
+            got.append(n.value)
+        if copied:
+            assert got[1] >= V * D * 2 + (got[0] or 0)
+        else:
+            assert got[1] == got[0]
+        assert lib.poseidon_xent_workspace(op, A, ctypes.c_void_p(0x1000), 8, V, D, L.F32, ctypes.byref(n)) == L.OK
+        aligned = n.value
+        assert lib.poseidon_xent_workspace(op, A, ctypes.c_void_p(0x1004), 8, V, D, L.F32, ctypes.byref(n)) == L.OK
+        assert n.value == aligned
