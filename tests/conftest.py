@@ -15,3 +15,10 @@ def pytest_configure(config):
 @pytest.fixture(scope="session")
 def golden_dir():
     return os.path.join(ROOT, "tests", "golden")
+
+
+def pytest_collection_modifyitems(items):
+    """test_gpu_wfbp.py first, however the files are named or given: its overlap
+    tests need a hardware queue for each of three streams, and which of the
+    process's four queues a stream gets depends on the streams made before it."""
+    items.sort(key=lambda item: item.path.name != "test_gpu_wfbp.py")
