@@ -567,6 +567,12 @@ int backward_groups(int64_t rows, int64_t cols)
     const int64_t teams = cols > 1024 ? 1 : cols > 128 ? 4 : 16;
     if (rows <= 4 * teams)
         return 1;
+    // Three a CU for the team of 256 threads with one group each, which needs the
+    // fewest registers, two elsewhere.  16384 rows with residual and dropout, us
+    // with two and three, bf16 then fp32: x 1032 74, 57 and 107, 90; x 1536 62, 52
+    // and 97, 105; x 2048 78, 71 and 127, 136; outside that range x 1000 39, 36
+    // and 71, 82; x 1024 34, 35 and 69, 78; x 2056 120, 99 and 158, 197; x 4096
+    // 133, 142 and 260, 261; x 8192 274, 286 and 508, 527.
     const int64_t per_cu = cols > 1024 && cols <= 2048 ? 3 : 2;
     return static_cast<int>(std::min<int64_t>(ceil_div(rows, teams), per_cu * device_cu_count()));
 }
