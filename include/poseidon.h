@@ -741,8 +741,134 @@ int poseidon_xent_factor(const void* X, const void* W, const int64_t* target, co
                          int64_t T, int64_t V, int64_t D, int32_t dtype, float* loss, float* U, void* dX,
                          void* workspace, int64_t workspace_bytes, hipStream_t stream);
 
+/*
+ * AdamW (Loshchilov and Hutter, ICLR 2019) over all of a network's tensors at
+ * once, from the workers' dense gradient shards -- the parameter server's update
+ * where the network is not trained by SGD.  Per value, with t the step number
+ * counted from 1 and s the gradients' scale:
+ *
+ *     g   = s * sum_{p<P} G_p
+ *     m  <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2
+ *     W  <- W - lr (decay W + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps))
+ *     copy <- W rounded to bf16                         (where a copy is asked for)
+ *
+ * The sum over the workers is formed in 64 bits.  The moments m and v are fp32
+ * or, for a tensor with an exponents array, 8 bits a value:
+ *
+ * A block of 128 consecutive values of a tensor (the last one shorter) shares
+ * one exponent byte for m and one for v, exponents[2 b] and exponents[2 b + 1]:
+ * the exponent E, biased by 127 as in fp32, of the block's largest magnitude, at
+ * least 16 for m and 32 for v.  A code k > 0 stands for the number whose fp32
+ * bits are ((E + 1) << 23) - ((top - k) << 20): eight codes to a power of two,
+ * top the code of 2^(E + 1 - 127); 0 stands for 0.  m has top 127 and its sign in
+ * bit 7; v has top 255.  So all-zero arrays are zero moments.  A moment is
+ * computed in 64 bits, from the values that the codes stand for, and rounded
+ * between its two neighbouring codes by 16 random bits r: upwards when its share
+ * of the way from the lower one is at least 1 - r / 65536, so that the rounding
+ * is right on average (v changes by a thousandth a step at beta2 = 0.999, a code
+ * is a tenth: rounded to nearest it would stand still).  The step itself uses the
+ * moments before that rounding.  m becomes 0 below its codes; v, which divides,
+ * stays at code 1 there; values below 2^-126 are 0.  A block with an infinite or
+ * NaN moment gets the exponent byte 255 and all of its moments read as NaN.
+ *
+ * The random bits are poseidon_dropout's: rng holds the key and the counter's
+ * high 64 bits, its low 64 bits are the group of eight values, numbered through
+ * the optimizer's tensors in their order with 16 groups to a block of 128 (fp32
+ * tensors counted too); value i of a group takes bits 16 i .. 16 i + 15 for m,
+ * and the same with its two bytes exchanged for v.  The caller gives each step
+ * another rng[1].  rng == NULL rounds to the nearest code (r = 32768).
+ */
+typedef struct poseidon_adamw_tensor {
+    float*      W;             /* n values, updated in place */
+    const void* shards;        /* P rows of n gradient values, `stride` values apart */
+    void*       m;             /* n moments: fp32, or bytes with `exponents` */
+    void*       v;
+    uint8_t*    exponents;     /* 2 ceil(n / 128) bytes, or NULL for fp32 moments */
+    void*       copy;          /* n bf16 values, written by a step, or NULL */
+    float*      sum;           /* n values, written by poseidon_adamw_clip, or NULL */
+    int64_t     n;
+    int64_t     stride;        /* values between two workers' rows: at least n where P > 1 */
+    int32_t     P;
+    float       weight_decay;
+} poseidon_adamw_tensor;
+
+/* What a step goes by.  clock (two values in device memory: lr and t; a t below
+ * 1 counts as 1) takes the place of lr and step where it is given, so that a
+ * captured graph's replays can each have their own.  scale (one value in device
+ * memory, NULL for 1) is poseidon_adamw_clip's result[1] as a rule; where it is
+ * infinite or NaN the step is left out: everything keeps its value. */
+typedef struct poseidon_adamw_rule {
+    double         lr;
+    double         beta1;
+    double         beta2;
+    double         eps;
+    int64_t        step;       /* t */
+    const double*  clock;
+    const float*   scale;
+    const int64_t* rng;        /* two values in device memory, or NULL */
+    int32_t        from_sums;  /* 1: the gradients are the tensors' sums, as poseidon_adamw_clip left them */
+    int32_t        reserved;   /* must be 0 */
+} poseidon_adamw_rule;
+
+/* An optimizer: the list of tensors, checked once.  It keeps their pointers for
+ * its lifetime (the caller keeps the memory valid), allocates no device memory,
+ * and is not changed by its calls, which several threads may make at once. */
+typedef struct poseidon_adamw poseidon_adamw;
+
+/*
+ * Create an optimizer of `count` tensors whose shards are of `dtype`
+ * (POSEIDON_F32 or POSEIDON_BF16).  Tensors with n = 0 are skipped.  Arrays lie
+ * on any boundary of their own type.  Returns POSEIDON_OK,
+ * POSEIDON_ERR_INVALID_ARG (count < 0, an unknown dtype, n negative or above
+ * 2^34, P outside 1..1024, stride < n with P > 1, P * stride above 2^56, a
+ * NULL W, shards, m or v with n > 0, a negative or non-finite weight_decay, a
+ * written array overlapping any other, NULL out) or POSEIDON_ERR_HIP (out of
+ * host memory).
+ */
+int poseidon_adamw_create(const poseidon_adamw_tensor* tensors, int32_t count, int32_t dtype, poseidon_adamw** out);
+
+/* Destroy an optimizer (work that it enqueued need not have run).  NULL is a no-op. */
+int poseidon_adamw_destroy(poseidon_adamw* optimizer);
+
+/*
+ * One step of every tensor.  Returns POSEIDON_OK, POSEIDON_ERR_INVALID_ARG (NULL
+ * arguments; reserved not 0; without clock a non-finite lr or step < 1; beta1 or
+ * beta2 outside 0 .. 1 (1 excluded); eps not above 0 or not finite; from_sums
+ * other than 0 and 1, or 1 where a tensor with values has no sum; clock, scale or
+ * rng lying in a written array) or POSEIDON_ERR_HIP.
+ */
+int poseidon_adamw_step(const poseidon_adamw* optimizer, const poseidon_adamw_rule* rule, hipStream_t stream);
+
+/*
+ * The moments as fp32, whatever they are held in: n values each to m[t] and v[t]
+ * of tensor t (NULL: not wanted).  Returns POSEIDON_OK, POSEIDON_ERR_INVALID_ARG
+ * (NULL arguments with tensors; outputs overlapping each other or an array of the
+ * optimizer) or POSEIDON_ERR_HIP.
+ */
+int poseidon_adamw_values(const poseidon_adamw* optimizer, float* const* m, float* const* v, hipStream_t stream);
+
+/* Bytes of workspace for poseidon_adamw_clip.  Host-only. */
+int poseidon_adamw_workspace(const poseidon_adamw* optimizer, int64_t* bytes);
+
+/*
+ * The norm of the whole gradient, over every value of every tensor, and the scale
+ * that clips a step to max_norm:
+ *
+ *     result[0] = sqrt(sum (sum_{p<P} G_p)^2),   result[1] = min(1, max_norm / norm)
+ *
+ * (1 for norm 0, NaN for an infinite or NaN norm: poseidon_adamw_step then leaves
+ * the step out).  All sums are formed in 64 bits.  A tensor with a `sum` array
+ * gets sum_{p<P} G_p there, rounded to fp32, so that the step need not read the
+ * workers' shards again (from_sums).  Returns POSEIDON_OK,
+ * POSEIDON_ERR_INVALID_ARG (NULL arguments; max_norm not above 0 or NaN; result
+ * or workspace overlapping each other or an array of the optimizer; a workspace
+ * too small or off its boundary) or POSEIDON_ERR_HIP.
+ */
+int poseidon_adamw_clip(const poseidon_adamw* optimizer, double max_norm, float* result, void* workspace,
+                        int64_t workspace_bytes, hipStream_t stream);
+
 /* Library version, for the binding's load check: returns POSEIDON_ABI_VERSION. */
-#define POSEIDON_ABI_VERSION 4
+#define POSEIDON_ABI_VERSION 5
 int poseidon_abi_version(void);
 
 #ifdef __cplusplus

@@ -9,7 +9,7 @@ import os
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libposeidon.so")
-ABI_VERSION = 4
+ABI_VERSION = 5
 
 OK = 0
 ERR_INVALID_ARG = -1
@@ -44,7 +44,8 @@ EXPORTS = ("poseidon_sf_apply", "poseidon_sf_apply_momentum", "poseidon_sf_apply
            "poseidon_kv_message_size", "poseidon_kv_pack", "poseidon_sf_set_arithmetic",
            "poseidon_sf_arithmetic", "poseidon_dropout", "poseidon_norm_forward", "poseidon_norm_workspace",
            "poseidon_norm_backward", "poseidon_xent_workspace", "poseidon_xent_forward", "poseidon_xent_backward",
-           "poseidon_xent_factor")
+           "poseidon_xent_factor", "poseidon_adamw_create", "poseidon_adamw_destroy", "poseidon_adamw_step",
+           "poseidon_adamw_values", "poseidon_adamw_workspace", "poseidon_adamw_clip")
 
 
 class PoseidonTensor(ctypes.Structure):
@@ -82,6 +83,22 @@ class PoseidonKvPair(ctypes.Structure):
 class PoseidonKvTensor(ctypes.Structure):
     """Mirror of ``poseidon_kv_tensor`` in include/poseidon.h."""
     _fields_ = [("W", ctypes.c_void_p), ("buf", ctypes.c_void_p), ("n", ctypes.c_int64)]
+
+
+class PoseidonAdamwTensor(ctypes.Structure):
+    """Mirror of ``poseidon_adamw_tensor`` in include/poseidon.h."""
+    _fields_ = [("W", ctypes.c_void_p), ("shards", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("exponents", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("sum", ctypes.c_void_p),
+                ("n", ctypes.c_int64), ("stride", ctypes.c_int64), ("P", ctypes.c_int32),
+                ("weight_decay", ctypes.c_float)]
+
+
+class PoseidonAdamwRule(ctypes.Structure):
+    """Mirror of ``poseidon_adamw_rule`` in include/poseidon.h."""
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("step", ctypes.c_int64), ("clock", ctypes.c_void_p),
+                ("scale", ctypes.c_void_p), ("rng", ctypes.c_void_p), ("from_sums", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
 
 
 _lib = None
@@ -139,6 +156,12 @@ def lib() -> ctypes.CDLL:
     L.poseidon_xent_forward.argtypes = [vp] * 3 + [i64] * 3 + [i32] + [vp] * 3 + [i64, vp]
     L.poseidon_xent_backward.argtypes = [vp] * 5 + [i64] * 3 + [i32] + [vp] * 3 + [i64, vp]
     L.poseidon_xent_factor.argtypes = [vp] * 4 + [i64] * 3 + [i32] + [vp] * 4 + [i64, vp]
+    L.poseidon_adamw_create.argtypes = [ctypes.POINTER(PoseidonAdamwTensor), i32, i32, ctypes.POINTER(vp)]
+    L.poseidon_adamw_destroy.argtypes = [vp]
+    L.poseidon_adamw_step.argtypes = [vp, ctypes.POINTER(PoseidonAdamwRule), vp]
+    L.poseidon_adamw_values.argtypes = [vp, ctypes.POINTER(vp), ctypes.POINTER(vp), vp]
+    L.poseidon_adamw_workspace.argtypes = [vp, ctypes.POINTER(i64)]
+    L.poseidon_adamw_clip.argtypes = [vp, f64, vp, vp, i64, vp]
     for name in EXPORTS:
         getattr(L, name).restype = ctypes.c_int
     if L.poseidon_abi_version() != ABI_VERSION:

@@ -811,3 +811,173 @@ def xent_factor(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, dloss: t
             X.data_ptr(), W.data_ptr(), target.data_ptr(), dloss.data_ptr(), T, V, D, dt, loss.data_ptr(),
             U.data_ptr(), dX.data_ptr(), ws.data_ptr(), size, _stream_handle(stream, X.device)))
     return loss, U, dX
+
+
+# --------------------------------------------------------------------------
+# AdamW
+# --------------------------------------------------------------------------
+
+ADAMW_BLOCK = 128   # values of an 8-bit moment that share an exponent byte
+
+
+class AdamW:
+    """AdamW over a list of tensors, from one dense gradient shard per worker
+    (poseidon_adamw_*).
+
+    Each entry is a dict with ``W`` (fp32), ``shards`` (P rows of W.numel()
+    values, as ``(P, n)`` or ``(P, *W.shape)``; the rows may lie apart, e.g. as
+    slices of one flat buffer per worker) and the moments ``m`` and ``v``: fp32 of
+    W's size, or uint8 of W's size together with ``exponents``, uint8 of
+    2 * ceil(n / 128).  All-zero arrays are zero moments (``moments`` makes them).
+    Optional: ``weight_decay`` (0), ``copy`` (bf16 of W's size, receives the new
+    weights), ``sum`` (fp32 of W's size, receives the summed gradient in
+    ``clip``).  The shards of all entries have one type, fp32 or bf16.  The
+    descriptor list is built and checked once."""
+
+    def __init__(self, tensors: list, betas=(0.9, 0.999), eps: float = 1e-8):
+        self.betas, self.eps = (float(betas[0]), float(betas[1])), float(eps)
+        self._h = ctypes.c_void_p()
+        self._keep = []
+        arr = (L.PoseidonAdamwTensor * max(1, len(tensors)))()
+        dtype, dev = torch.float32, None
+        for i, t in enumerate(tensors):
+            W, G = t["W"], t["shards"]
+            _dev_f32("W", W)
+            if dev is None:
+                if not isinstance(G, torch.Tensor) or G.dtype not in _DTYPES:
+                    raise TypeError(f"tensor {i}: shards must be a float32 or bfloat16 tensor")
+                dtype, dev = G.dtype, W.get_device()
+            n = W.numel()
+            _dev("W", W, torch.float32, dev, W.shape)
+            P, stride = _rows_of(i, G, W, dtype, dev)
+            coded = t.get("exponents") is not None
+            for name in ("m", "v"):
+                _sized(i, name, t[name], torch.uint8 if coded else torch.float32, dev, n)
+            for name, kind, size in (("exponents", torch.uint8, 2 * (-(-n // ADAMW_BLOCK))),
+                                     ("copy", torch.bfloat16, n), ("sum", torch.float32, n)):
+                if t.get(name) is not None:
+                    _sized(i, name, t[name], kind, dev, size)
+            arr[i] = L.PoseidonAdamwTensor(W.data_ptr(), G.data_ptr(), t["m"].data_ptr(), t["v"].data_ptr(),
+                                           _ptr(t.get("exponents")), _ptr(t.get("copy")), _ptr(t.get("sum")), n,
+                                           stride, P, float(t.get("weight_decay", 0.0)))
+            self._keep.append((W, G, t["m"], t["v"], t.get("exponents"), t.get("copy"), t.get("sum")))
+        self.device = torch.device("cuda", torch.cuda.current_device() if dev is None else dev)
+        _check("poseidon_adamw_create", L.lib().poseidon_adamw_create(arr, len(tensors), _DTYPES[dtype],
+                                                                      ctypes.byref(self._h)))
+        size = ctypes.c_int64()
+        _check("poseidon_adamw_workspace", L.lib().poseidon_adamw_workspace(self._h, ctypes.byref(size)))
+        self._ws_bytes = size.value
+        self._rule = L.PoseidonAdamwRule(0.0, *self.betas, self.eps, 1, None, None, None, 0, 0)
+        self._kept_uses = _KeptUses([x for keep in self._keep for x in keep])
+
+    @staticmethod
+    def moments(W: torch.Tensor, bits: int = 32) -> dict:
+        """Zero moments for a parameter: the entries ``m``, ``v`` and, for 8
+        bits, ``exponents``."""
+        if bits == 32:
+            return {"m": torch.zeros_like(W), "v": torch.zeros_like(W)}
+        if bits != 8:
+            raise ValueError(f"bits must be 8 or 32, got {bits}")
+        n = W.numel()
+        return {name: torch.zeros(size, dtype=torch.uint8, device=W.device)
+                for name, size in (("m", n), ("v", n), ("exponents", 2 * (-(-n // ADAMW_BLOCK))))}
+
+    def step(self, lr: float | None = None, step: int | None = None, clock: torch.Tensor | None = None,
+             scale: torch.Tensor | None = None, rng: torch.Tensor | None = None, from_sums: bool = False,
+             stream=None) -> None:
+        """One step of every tensor, in place (poseidon_adamw_step).  ``lr`` and
+        ``step`` (counted from 1), or ``clock``, the two as float64 values on the
+        device for steps that are replayed from a graph; ``scale``, one float32 on
+        the device, multiplies the gradients (clip's result[1:2]; not finite: the
+        step is left out); ``rng`` holds (seed, offset) as two int64 values on the
+        device for the rounding of 8-bit moments, with another offset for every
+        step (None: to nearest); ``from_sums`` takes the gradients from the sums
+        that clip left."""
+        rule = L.PoseidonAdamwRule.from_buffer_copy(self._rule)
+        dev = self.device.index
+        if clock is not None:
+            _dev("clock", clock, torch.float64, dev, (2,))
+            rule.clock = clock.data_ptr()
+        elif lr is None or step is None:
+            raise ValueError("a step needs lr and step, or clock")
+        else:
+            rule.lr, rule.step = float(lr), int(step)
+        if scale is not None:
+            _dev("scale", scale, torch.float32, dev, (1,))
+            rule.scale = scale.data_ptr()
+        if rng is not None:
+            _dev("rng", rng, torch.int64, dev, (2,))
+            rule.rng = rng.data_ptr()
+        rule.from_sums = int(bool(from_sums))
+        if stream is not None:
+            self._kept_uses(stream)
+            _uses(stream, clock, scale, rng)
+        with _on(self.device):
+            _check("poseidon_adamw_step", L.lib().poseidon_adamw_step(
+                self._h, ctypes.byref(rule), _stream_handle(stream, self.device)))
+
+    def clip(self, max_norm: float, stream=None) -> torch.Tensor:
+        """The norm of the whole gradient and the scale that clips it to
+        ``max_norm`` (poseidon_adamw_clip), as two float32 values on the device:
+        ``result[1:2]`` is step's ``scale``.  Entries with ``sum`` get the summed
+        gradient there."""
+        with _work_on(stream, self.device):
+            result = torch.empty(2, dtype=torch.float32, device=self.device)
+            ws = torch.empty(self._ws_bytes, dtype=torch.uint8, device=self.device)
+            if stream is not None:
+                self._kept_uses(stream)
+            _check("poseidon_adamw_clip", L.lib().poseidon_adamw_clip(
+                self._h, max_norm, result.data_ptr(), ws.data_ptr(), self._ws_bytes,
+                _stream_handle(stream, self.device)))
+        return result
+
+    def values(self, out: list | None = None, stream=None) -> list:
+        """The moments as fp32 tensors, one pair (m, v) per entry
+        (poseidon_adamw_values), written to ``out`` where it is given (a list of
+        such pairs; None in the place of one that is not wanted)."""
+        dev = self.device.index
+        with _work_on(stream, self.device):
+            if out is None:
+                out = [(torch.empty_like(k[0]), torch.empty_like(k[0])) for k in self._keep]
+            if len(out) != len(self._keep):
+                raise ValueError(f"out needs one pair for each of the {len(self._keep)} tensors")
+            for i, (pair, k) in enumerate(zip(out, self._keep)):
+                for name, x in zip(("m", "v"), pair):
+                    if x is not None:
+                        _sized(i, name, x, torch.float32, dev, k[0].numel())
+            ptrs = [(ctypes.c_void_p * max(1, len(out)))(*[_ptr(pair[j]) for pair in out]) for j in (0, 1)]
+            if stream is not None:
+                self._kept_uses(stream)
+                _uses(stream, *[x for pair in out for x in pair])
+            _check("poseidon_adamw_values", L.lib().poseidon_adamw_values(
+                self._h, *ptrs, _stream_handle(stream, self.device)))
+        return out
+
+    def close(self):
+        if self._h:
+            L.lib().poseidon_adamw_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def _sized(i: int, name: str, t: torch.Tensor, dtype: torch.dtype, device: int, n: int) -> None:
+    """Checks a contiguous tensor of n values of the given type on the device."""
+    _dev(f"tensor {i}: {name}", t, dtype, device, t.shape if isinstance(t, torch.Tensor) else ())
+    if t.numel() != n:
+        raise ValueError(f"tensor {i}: {name} must have {n} values, got {t.numel()}")
+
+
+def _rows_of(i: int, G: torch.Tensor, W: torch.Tensor, dtype: torch.dtype, device: int) -> tuple[int, int]:
+    """(P, stride) of one tensor's shards: P rows, each without gaps."""
+    if not isinstance(G, torch.Tensor):
+        raise TypeError(f"tensor {i}: shards must be a torch.Tensor")
+    P = G.shape[0] if G.dim() else 0
+    if P < 1 or G.shape[1:] not in (W.shape, (W.numel(),)):
+        raise ValueError(f"tensor {i}: shards must be P x {W.numel()} or P x {tuple(W.shape)}, got {tuple(G.shape)}")
+    _dev(f"tensor {i}: shards", G[0], dtype, device, G.shape[1:])
+    return P, G.stride(0)
