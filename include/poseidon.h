@@ -742,6 +742,56 @@ int poseidon_xent_factor(const void* X, const void* W, const int64_t* target, co
                          void* workspace, int64_t workspace_bytes, hipStream_t stream);
 
 /*
+ * Group norm with an activation, channels last: x is N samples of L positions
+ * (a feature map's height times width) of C channels, row-major, in `groups`
+ * groups of D = C / groups neighbouring channels.  Per sample and group, over
+ * its L D values:
+ *
+ *     mean = avg(x),  rstd = 1 / sqrt(avg((x - mean)^2) + eps)
+ *     z = (x - mean) * rstd * gamma + beta,  y = act(z)
+ *
+ * x and y are of `dtype`; gamma and beta have C values, mean and rstd N * groups.
+ * act: z itself, max(z, 0), or z / (1 + e^-z).
+ */
+#define POSEIDON_ACT_NONE 0
+#define POSEIDON_ACT_RELU 1
+#define POSEIDON_ACT_SILU 2
+
+#define POSEIDON_GROUP_NORM_FORWARD  0
+#define POSEIDON_GROUP_NORM_BACKWARD 1
+
+/* Bytes of workspace for the call `op` at these sizes.  Host-only. */
+int poseidon_group_norm_workspace(int32_t op, int64_t N, int64_t L, int64_t C, int64_t groups, int32_t dtype,
+                                  int64_t* bytes);
+
+/*
+ * Returns POSEIDON_OK, POSEIDON_ERR_INVALID_ARG (negative N; L, C or groups < 1;
+ * groups not dividing C; N above 2^24, C above 2^16, N L C above 2^40; an unknown
+ * dtype or act; a negative or NaN eps; NULL arrays with work; outputs overlapping
+ * each other, the workspace or an input; a workspace too small or off its
+ * boundary) or POSEIDON_ERR_HIP.
+ */
+int poseidon_group_norm_forward(const void* x, const float* gamma, const float* beta, int64_t N, int64_t L, int64_t C,
+                                int64_t groups, int32_t dtype, float eps, int32_t act, void* y, float* mean,
+                                float* rstd, void* workspace, int64_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Its backward pass, from mean and rstd as the forward pass left them; with
+ * n = (x - mean) * rstd, dz = dy * act'(n * gamma + beta) and g = dz * gamma:
+ *
+ *     dx = rstd * (g - avg(g) - n * avg(g * n))       (averages over sample and group)
+ *     dgamma = sum over samples and positions of dz * n,   dbeta = the same of dz
+ *
+ * max(z, 0) passes the gradient where z > 0, z taken as n * gamma + beta exactly
+ * from these inputs.  dgamma and dbeta (C values, replaced) may lie in a gradient
+ * shard; with N = 0 they are 0.  Returns as poseidon_group_norm_forward.
+ */
+int poseidon_group_norm_backward(const void* dy, const void* x, const float* gamma, const float* beta,
+                                 const float* mean, const float* rstd, int64_t N, int64_t L, int64_t C,
+                                 int64_t groups, int32_t dtype, int32_t act, void* dx, float* dgamma, float* dbeta,
+                                 void* workspace, int64_t workspace_bytes, hipStream_t stream);
+
+/*
  * AdamW (Loshchilov and Hutter, ICLR 2019) over all of a network's tensors at
  * once, from the workers' dense gradient shards -- the parameter server's update
  * where the network is not trained by SGD.  Per value, with t the step number

@@ -31,6 +31,11 @@ BF16 = 1
 XENT_FORWARD = 0
 XENT_BACKWARD = 1
 XENT_FACTOR = 2
+ACT_NONE = 0
+ACT_RELU = 1
+ACT_SILU = 2
+GROUP_NORM_FORWARD = 0
+GROUP_NORM_BACKWARD = 1
 
 EXPORTS = ("poseidon_sf_apply", "poseidon_sf_apply_momentum", "poseidon_sf_apply_batch",
            "poseidon_ps_apply", "poseidon_ps_apply_batch",
@@ -45,7 +50,8 @@ EXPORTS = ("poseidon_sf_apply", "poseidon_sf_apply_momentum", "poseidon_sf_apply
            "poseidon_sf_arithmetic", "poseidon_dropout", "poseidon_norm_forward", "poseidon_norm_workspace",
            "poseidon_norm_backward", "poseidon_xent_workspace", "poseidon_xent_forward", "poseidon_xent_backward",
            "poseidon_xent_factor", "poseidon_adamw_create", "poseidon_adamw_destroy", "poseidon_adamw_step",
-           "poseidon_adamw_values", "poseidon_adamw_workspace", "poseidon_adamw_clip")
+           "poseidon_adamw_values", "poseidon_adamw_workspace", "poseidon_adamw_clip",
+           "poseidon_group_norm_workspace", "poseidon_group_norm_forward", "poseidon_group_norm_backward")
 
 
 class PoseidonTensor(ctypes.Structure):
@@ -156,6 +162,9 @@ def lib() -> ctypes.CDLL:
     L.poseidon_xent_forward.argtypes = [vp] * 3 + [i64] * 3 + [i32] + [vp] * 3 + [i64, vp]
     L.poseidon_xent_backward.argtypes = [vp] * 5 + [i64] * 3 + [i32] + [vp] * 3 + [i64, vp]
     L.poseidon_xent_factor.argtypes = [vp] * 4 + [i64] * 3 + [i32] + [vp] * 4 + [i64, vp]
+    L.poseidon_group_norm_workspace.argtypes = [i32, i64, i64, i64, i64, i32, ctypes.POINTER(i64)]
+    L.poseidon_group_norm_forward.argtypes = [vp] * 3 + [i64] * 4 + [i32, f32, i32] + [vp] * 4 + [i64, vp]
+    L.poseidon_group_norm_backward.argtypes = [vp] * 6 + [i64] * 4 + [i32, i32] + [vp] * 4 + [i64, vp]
     L.poseidon_adamw_create.argtypes = [ctypes.POINTER(PoseidonAdamwTensor), i32, i32, ctypes.POINTER(vp)]
     L.poseidon_adamw_destroy.argtypes = [vp]
     L.poseidon_adamw_step.argtypes = [vp, ctypes.POINTER(PoseidonAdamwRule), vp]

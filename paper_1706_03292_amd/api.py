@@ -814,6 +814,102 @@ def xent_factor(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor, dloss: t
 
 
 # --------------------------------------------------------------------------
+# Group norm
+# --------------------------------------------------------------------------
+
+_ACTS = {None: L.ACT_NONE, "none": L.ACT_NONE, "relu": L.ACT_RELU, "silu": L.ACT_SILU}
+
+
+def _act(act) -> int:
+    if act not in _ACTS:
+        raise ValueError(f"act must be 'none', 'relu' or 'silu', got {act!r}")
+    return _ACTS[act]
+
+
+def _map_sizes(name: str, x: torch.Tensor) -> tuple[int, int, int]:
+    """(N, L, C) of a channels-last feature map (N, ..., C)."""
+    shape = x.shape
+    if len(shape) < 2:
+        raise ValueError(f"{name} must be (N, ..., C), got {tuple(shape)}")
+    return shape[0], math.prod(shape[1:-1]), shape[-1]
+
+
+@functools.lru_cache(maxsize=4096)
+def _group_norm_size(op, N, L_, C, groups, dt) -> int:
+    size = ctypes.c_int64()
+    _check("poseidon_group_norm_workspace", L.lib().poseidon_group_norm_workspace(op, N, L_, C, groups, dt,
+                                                                                  ctypes.byref(size)))
+    return size.value
+
+
+def group_norm_forward(x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor, groups: int, eps: float = 1e-5,
+                       act: str | None = None, y: torch.Tensor | None = None, stream=None):
+    """y = act((x - mean) * rstd * gamma + beta), normalised over each sample's
+    positions and each group's channels (poseidon_group_norm_forward).  x is
+    (N, ..., C), channels last and without gaps (of an (N, C, H, W) tensor in
+    torch's channels_last layout: x.permute(0, 2, 3, 1)); ``act`` is None, 'relu'
+    or 'silu'.  Returns (y, mean, rstd), the latter two (N, groups) fp32."""
+    dt, dev = _typed("x", x)
+    N, L_, C = _map_sizes("x", x)
+    code = _act(act)
+    _dev("gamma", gamma, torch.float32, dev, (C,))
+    _dev("beta", beta, torch.float32, dev, (C,))
+    if y is not None:
+        _dev("y", y, x.dtype, dev, x.shape)
+    size = _group_norm_size(L.GROUP_NORM_FORWARD, N, L_, C, groups, dt)
+    with _work_on(stream, x.device):
+        if y is None:
+            y = torch.empty_like(x)
+        mean = torch.empty((N, groups), dtype=torch.float32, device=x.device)
+        rstd = torch.empty_like(mean)
+        ws = torch.empty(size, dtype=torch.uint8, device=x.device)
+        if stream is not None:
+            _uses(stream, x, gamma, beta, y)
+        _check("poseidon_group_norm_forward", L.lib().poseidon_group_norm_forward(
+            x.data_ptr(), gamma.data_ptr(), beta.data_ptr(), N, L_, C, groups, dt, eps, code, y.data_ptr(),
+            mean.data_ptr(), rstd.data_ptr(), ws.data_ptr(), size, _stream_handle(stream, x.device)))
+    return y, mean, rstd
+
+
+def group_norm_backward(dy: torch.Tensor, x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor,
+                        mean: torch.Tensor, rstd: torch.Tensor, act: str | None = None,
+                        dgamma: torch.Tensor | None = None, dbeta: torch.Tensor | None = None, stream=None):
+    """The backward pass of group_norm_forward (poseidon_group_norm_backward),
+    from its mean and rstd: returns (dx, dgamma, dbeta).  dgamma and dbeta may be
+    given, e.g. as this worker's gradient shards."""
+    dt, dev = _typed("dy", dy)
+    N, L_, C = _map_sizes("dy", dy)
+    code = _act(act)
+    _dev("x", x, dy.dtype, dev, dy.shape)
+    if not isinstance(mean, torch.Tensor) or mean.dim() != 2:
+        raise ValueError("mean must be (N, groups)")
+    groups = mean.shape[1]
+    _dev("gamma", gamma, torch.float32, dev, (C,))
+    _dev("beta", beta, torch.float32, dev, (C,))
+    _dev("mean", mean, torch.float32, dev, (N, groups))
+    _dev("rstd", rstd, torch.float32, dev, (N, groups))
+    if dgamma is not None:
+        _dev("dgamma", dgamma, torch.float32, dev, (C,))
+    if dbeta is not None:
+        _dev("dbeta", dbeta, torch.float32, dev, (C,))
+    size = _group_norm_size(L.GROUP_NORM_BACKWARD, N, L_, C, groups, dt)
+    with _work_on(stream, dy.device):
+        if dgamma is None:
+            dgamma = torch.empty_like(gamma)
+        if dbeta is None:
+            dbeta = torch.empty_like(gamma)
+        dx = torch.empty_like(dy)
+        ws = torch.empty(size, dtype=torch.uint8, device=dy.device)
+        if stream is not None:
+            _uses(stream, dy, x, gamma, beta, mean, rstd, dgamma, dbeta)
+        _check("poseidon_group_norm_backward", L.lib().poseidon_group_norm_backward(
+            dy.data_ptr(), x.data_ptr(), gamma.data_ptr(), beta.data_ptr(), mean.data_ptr(), rstd.data_ptr(), N, L_, C,
+            groups, dt, code, dx.data_ptr(), dgamma.data_ptr(), dbeta.data_ptr(), ws.data_ptr(), size,
+            _stream_handle(stream, dy.device)))
+    return dx, dgamma, dbeta
+
+
+# --------------------------------------------------------------------------
 # AdamW
 # --------------------------------------------------------------------------
 

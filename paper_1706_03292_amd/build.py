@@ -20,7 +20,8 @@ BUILD_DIR = os.path.join(ROOT, "_build")
 ARCH = "gfx950"
 
 SOURCES = ["sf_apply.hip", "ps_apply.hip", "entry.cpp", "sync.cpp", "hybcomm.cpp", "kvstore.cpp",
-           "norm.hip", "xent.hip", "operators.cpp", "adamw.hip", "optimizer.cpp"]
+           "norm.hip", "xent.hip", "operators.cpp", "adamw.hip", "optimizer.cpp",
+           "group_norm.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-ffp-contract=off",

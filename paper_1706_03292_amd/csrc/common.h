@@ -162,6 +162,14 @@ hipError_t launch_xent_backward(const void* X, const void* W, const int64_t* tar
 hipError_t launch_xent_factor(const void* X, const void* W, const int64_t* target, const float* dloss, int64_t T,
                               int64_t V, int64_t D, int32_t dtype, float* loss, float* U, void* dX, void* ws,
                               hipStream_t stream);
+int64_t group_norm_workspace(int32_t op, int64_t N, int64_t L, int64_t C, int64_t groups, int32_t dtype);
+hipError_t launch_group_norm_forward(const void* x, const float* gamma, const float* beta, int64_t N, int64_t L,
+                                     int64_t C, int64_t groups, int32_t dtype, float eps, int32_t act, void* y,
+                                     float* mean, float* rstd, void* ws, hipStream_t stream);
+hipError_t launch_group_norm_backward(const void* dy, const void* x, const float* gamma, const float* beta,
+                                      const float* mean, const float* rstd, int64_t N, int64_t L, int64_t C,
+                                      int64_t groups, int32_t dtype, int32_t act, void* dx, float* dgamma,
+                                      float* dbeta, void* ws, hipStream_t stream);
 
 // Argument checks of the public entry points (no device work).
 int check_sf_args(const float* W, const float* U, const float* V,

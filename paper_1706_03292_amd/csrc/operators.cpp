@@ -1,5 +1,6 @@
 // The C entry points of the operators at a network's end (include/poseidon.h):
-// the argument checks, then the launchers of norm.hip and xent.hip.  Host code
+// the argument checks, then the launchers of norm.hip, xent.hip and
+// group_norm.hip.  Host code
 // only; every check runs before anything is enqueued.
 #include <math.h>
 
@@ -61,6 +62,16 @@ bool xent_sizes_ok(int64_t T, int64_t V, int64_t D, int32_t dtype)
     return size_of(dtype) && T >= 0 && T <= MOST_ROWS && V >= 1 && V <= MOST_CLASSES && D >= 1 && D <= MOST_FEATURES &&
            T * V <= MOST_LOGITS;
 }
+
+constexpr int64_t MOST_SAMPLES = int64_t(1) << 24, MOST_CHANNELS = int64_t(1) << 16, MOST_MAP = int64_t(1) << 40;
+
+bool group_norm_sizes_ok(int64_t N, int64_t L, int64_t C, int64_t groups, int32_t dtype)
+{
+    return size_of(dtype) && N >= 0 && N <= MOST_SAMPLES && C >= 1 && C <= MOST_CHANNELS && groups >= 1 &&
+           C % groups == 0 && L >= 1 && L <= MOST_MAP / C / std::max<int64_t>(N, 1);
+}
+
+bool act_ok(int32_t act) { return act >= POSEIDON_ACT_NONE && act <= POSEIDON_ACT_SILU; }
 
 bool workspace_ok(const void* ws, int64_t bytes, int64_t needed)
 {
@@ -246,4 +257,71 @@ extern "C" int poseidon_xent_factor(const void* X, const void* W, const int64_t*
     if (r.collide())
         return POSEIDON_ERR_INVALID_ARG;
     return status(launch_xent_factor(X, W, target, dloss, T, V, D, dtype, loss, U, dX, workspace, stream));
+}
+
+extern "C" int poseidon_group_norm_workspace(int32_t op, int64_t N, int64_t L, int64_t C, int64_t groups,
+                                             int32_t dtype, int64_t* bytes)
+{
+    if (!bytes || (op != POSEIDON_GROUP_NORM_FORWARD && op != POSEIDON_GROUP_NORM_BACKWARD) ||
+        !group_norm_sizes_ok(N, L, C, groups, dtype))
+        return POSEIDON_ERR_INVALID_ARG;
+    *bytes = group_norm_workspace(op, N, L, C, groups, dtype);
+    return POSEIDON_OK;
+}
+
+extern "C" int poseidon_group_norm_forward(const void* x, const float* gamma, const float* beta, int64_t N, int64_t L,
+                                           int64_t C, int64_t groups, int32_t dtype, float eps, int32_t act, void* y,
+                                           float* mean, float* rstd, void* workspace, int64_t workspace_bytes,
+                                           hipStream_t stream)
+{
+    if (!group_norm_sizes_ok(N, L, C, groups, dtype) || !act_ok(act) || !(eps >= 0.f))
+        return POSEIDON_ERR_INVALID_ARG;
+    if (N == 0)
+        return POSEIDON_OK;
+    const int64_t map = N * L * C * size_of(dtype);
+    const int64_t needed = group_norm_workspace(POSEIDON_GROUP_NORM_FORWARD, N, L, C, groups, dtype);
+    if (!x || !gamma || !beta || !y || !mean || !rstd || !workspace_ok(workspace, workspace_bytes, needed))
+        return POSEIDON_ERR_INVALID_ARG;
+    Ranges r;
+    r.in(x, map);
+    r.in(gamma, C * 4);
+    r.in(beta, C * 4);
+    r.out(y, map);
+    r.out(mean, N * groups * 4);
+    r.out(rstd, N * groups * 4);
+    r.out(workspace, needed);
+    if (r.collide())
+        return POSEIDON_ERR_INVALID_ARG;
+    return status(launch_group_norm_forward(x, gamma, beta, N, L, C, groups, dtype, eps, act, y, mean, rstd,
+                                            workspace, stream));
+}
+
+extern "C" int poseidon_group_norm_backward(const void* dy, const void* x, const float* gamma, const float* beta,
+                                            const float* mean, const float* rstd, int64_t N, int64_t L, int64_t C,
+                                            int64_t groups, int32_t dtype, int32_t act, void* dx, float* dgamma,
+                                            float* dbeta, void* workspace, int64_t workspace_bytes,
+                                            hipStream_t stream)
+{
+    if (!group_norm_sizes_ok(N, L, C, groups, dtype) || !act_ok(act))
+        return POSEIDON_ERR_INVALID_ARG;
+    const int64_t map = N * L * C * size_of(dtype);
+    const int64_t needed = group_norm_workspace(POSEIDON_GROUP_NORM_BACKWARD, N, L, C, groups, dtype);
+    if (!dgamma || !dbeta || (N > 0 && (!dy || !x || !gamma || !beta || !mean || !rstd || !dx)) ||
+        !workspace_ok(workspace, workspace_bytes, needed))
+        return POSEIDON_ERR_INVALID_ARG;
+    Ranges r;
+    r.in(dy, map);
+    r.in(x, map);
+    r.in(gamma, C * 4);
+    r.in(beta, C * 4);
+    r.in(mean, N * groups * 4);
+    r.in(rstd, N * groups * 4);
+    r.out(dx, map);
+    r.out(dgamma, C * 4);
+    r.out(dbeta, C * 4);
+    r.out(workspace, needed);
+    if (r.collide())
+        return POSEIDON_ERR_INVALID_ARG;
+    return status(launch_group_norm_backward(dy, x, gamma, beta, mean, rstd, N, L, C, groups, dtype, act, dx, dgamma,
+                                             dbeta, workspace, stream));
 }
