@@ -860,14 +860,14 @@ def group_norm_forward(x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor,
     with _work_on(stream, x.device):
         if y is None:
             y = torch.empty_like(x)
-        mean = torch.empty((N, groups), dtype=torch.float32, device=x.device)
+        mean = gamma.new_empty((N, groups))
         rstd = torch.empty_like(mean)
-        ws = torch.empty(size, dtype=torch.uint8, device=x.device)
+        ws = torch.empty(size, dtype=torch.uint8, device=x.device) if size else None
         if stream is not None:
             _uses(stream, x, gamma, beta, y)
         _check("poseidon_group_norm_forward", L.lib().poseidon_group_norm_forward(
             x.data_ptr(), gamma.data_ptr(), beta.data_ptr(), N, L_, C, groups, dt, eps, code, y.data_ptr(),
-            mean.data_ptr(), rstd.data_ptr(), ws.data_ptr(), size, _stream_handle(stream, x.device)))
+            mean.data_ptr(), rstd.data_ptr(), _ptr(ws), size, _stream_handle(stream, x.device)))
     return y, mean, rstd
 
 
@@ -899,12 +899,12 @@ def group_norm_backward(dy: torch.Tensor, x: torch.Tensor, gamma: torch.Tensor, 
         if dbeta is None:
             dbeta = torch.empty_like(gamma)
         dx = torch.empty_like(dy)
-        ws = torch.empty(size, dtype=torch.uint8, device=dy.device)
+        ws = torch.empty(size, dtype=torch.uint8, device=dy.device) if size else None
         if stream is not None:
             _uses(stream, dy, x, gamma, beta, mean, rstd, dgamma, dbeta)
         _check("poseidon_group_norm_backward", L.lib().poseidon_group_norm_backward(
             dy.data_ptr(), x.data_ptr(), gamma.data_ptr(), beta.data_ptr(), mean.data_ptr(), rstd.data_ptr(), N, L_, C,
-            groups, dt, code, dx.data_ptr(), dgamma.data_ptr(), dbeta.data_ptr(), ws.data_ptr(), size,
+            groups, dt, code, dx.data_ptr(), dgamma.data_ptr(), dbeta.data_ptr(), _ptr(ws), size,
             _stream_handle(stream, dy.device)))
     return dx, dgamma, dbeta
 

@@ -2,204 +2,157 @@
 // (include/poseidon.h gives the formulas).  A few operations per value, bound by
 // memory: x (and dy) read, y (dx) written once each is what it cannot do without.
 //
-// A sample is L rows of C channels.  A workgroup takes a chunk of a sample's rows
-// and up to 256 groups of eight neighbouring channels; a thread keeps its eight
-// channels and walks the rows.  Three launches: sums of each chunk and channel,
-// each group's statistics from them (and the weights' gradients), the result.
+// A sample is L rows of C channels.  Threads stand in teams of a row each, a thread
+// at eight neighbouring channels (a column), and walk the rows.  Maps whose groups
+// fit a workgroup's registers are read once (held_*_kernel).  Others take three
+// launches: sums of each chunk of rows and channel; each group's statistics from
+// them; the result, from a second read.
 //
-// Sums over a thread's rows (at most 64) are fp32, of differences from the first
-// of its values, so that a mean far from 0 costs no accuracy; what joins threads,
-// chunks and channels are means and sums of squares about them, in 64 bits.
-// Nothing depends on timing.
+// A row that does not divide into eights has its last column end with it: that
+// thread's first `skip` channels belong to the column before, count for no sum and
+// are stored twice, alike.  So every access is of eight values (fewer channels than
+// eight in all are read one by one).
+//
+// Sums over a thread's rows are fp32, of differences from a value of the group or
+// from its mean, so that a mean far from 0 costs no accuracy; what joins chunks and
+// channels is in 64 bits.  Every order is fixed: nothing depends on timing.
 #include "elements.h"
 
 namespace poseidon {
 namespace {
 
-constexpr int COLS = 256;        // groups of eight channels that a workgroup holds
-constexpr int MOST_THREADS = 256;
-constexpr int MOST_ROWS = 64;    // of a thread
 constexpr int SUM_THREADS = 256;
 
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+__host__ __device__ __forceinline__ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// How the rows and channels are cut: columns of eight channels, teams of threads
-// that hold one row each, rows a chunk.
-struct Cut {
-    int64_t N, L, C, groups, D;   // D channels a group
-    int64_t rows;                 // of a chunk
-    int32_t chunks, cols, sides;  // chunks of a sample; columns and workgroups across
-    int32_t teams, threads;
-};
-
-Cut make_cut(int64_t N, int64_t L, int64_t C, int64_t groups)
-{
-    Cut c{N, L, C, groups, C / groups, 0, 0, 0, 0, 0, 0};
-    const int64_t all = ceil_div(C, GROUP);
-    c.sides = static_cast<int32_t>(ceil_div(all, COLS));
-    c.cols = static_cast<int32_t>(ceil_div(all, c.sides));
-    c.teams = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(MOST_THREADS / c.cols, L)));
-    c.threads = static_cast<int32_t>(ceil_div(static_cast<int64_t>(c.cols) * c.teams, 64) * 64);
-    // Eight workgroups a CU, where each thread then has at least four rows.
-    const int64_t wanted = std::max<int64_t>(1, ceil_div(8 * 256, std::max<int64_t>(1, N * c.sides)));
-    const int64_t per_thread = std::min<int64_t>(MOST_ROWS, std::max<int64_t>(4, ceil_div(L, wanted * c.teams)));
-    c.rows = std::min<int64_t>(L, per_thread * c.teams);
-    c.chunks = static_cast<int32_t>(ceil_div(L, std::max<int64_t>(1, c.rows)));
-    return c;
-}
-
-// The place of a workgroup: sample, chunk and side, walked in one dimension.
-struct Place {
-    int64_t n, chunk, first_row, end_row;
-    int64_t channel;     // of this thread; past the last: at least C
-    int team;
-    bool active;
-};
-
-__device__ __forceinline__ Place place_of(const Cut& c, int64_t b)
-{
-    Place p;
-    const int64_t side = b % c.sides;
-    b /= c.sides;
-    p.chunk = b % c.chunks;
-    p.n = b / c.chunks;
-    p.first_row = p.chunk * c.rows;
-    p.end_row = p.first_row + c.rows < c.L ? p.first_row + c.rows : c.L;
-    const int t = threadIdx.x;
-    p.team = t / c.cols;
-    p.channel = (side * c.cols + t % c.cols) * GROUP;
-    p.active = p.team < c.teams && p.channel < c.C;
-    return p;
-}
-
-// A pair of sums for each chunk and channel.
+// A pair of sums.
 struct Pair {
     float a, b;
 };
 
-__device__ __forceinline__ Pair* pair_at(Pair* partial, const Cut& c, int64_t n, int64_t chunk, int64_t channel)
+// The map, and how it is cut: workgroups of `teams` rows of `cols` columns, `sides`
+// of them across a row; `chunks` of `rows` rows down a sample.
+struct Map {
+    int64_t N, L, C, groups, rows, chunks, work;   // work: workgroups
+    int32_t D, cols, sides, teams, threads;        // D: channels a group
+    int32_t piece;     // channels of one group that lie together in every thread's eight
+    int32_t shift;     // its logarithm
+    int32_t fold;      // cols is a power of two up to 64: a wave's teams are joined by shuffles
+    int32_t span;      // groups of a workgroup (held)
+    int32_t lanes;     // that add up one group (held): a power of two up to 64
+    float inv_D;
+};
+
+// channel / D, for channels below 2^16: the quotient's distance from the next
+// integer is at least 1 / (2 D), its error below 2^-22 of it.
+__device__ __forceinline__ int group_of(const Map& h, int channel)
 {
-    return partial + (n * c.chunks + chunk) * c.C + channel;
+    return static_cast<int>((static_cast<float>(channel) + 0.5f) * h.inv_D);
 }
 
-// The eight values of a group's array at this thread's channels.
-__device__ __forceinline__ void per_channel(const float* of_groups, const Cut& c, int64_t n, int64_t channel,
-                                            float (&v)[GROUP])
+// Where a thread stands.
+struct Spot {
+    int64_t n, first_row, end_row;   // of its sample; rows of its chunk
+    int64_t base;                    // of its first row's first value
+    int channel, first;              // its first channel, its workgroup's first channel
+    int col, team, skip;
+    bool active;
+};
+
+__device__ __forceinline__ Spot spot_of(const Map& h, int64_t b)
+{
+    Spot s;
+    const int side = static_cast<int>(b % h.sides);
+    b /= h.sides;
+    s.n = b / h.chunks;
+    s.first_row = (b - s.n * h.chunks) * h.rows;
+    s.end_row = s.first_row + h.rows < h.L ? s.first_row + h.rows : h.L;
+    s.col = static_cast<int>(threadIdx.x) % h.cols;
+    s.team = static_cast<int>(threadIdx.x) / h.cols;
+    const int C = static_cast<int>(h.C), at = (side * h.cols + s.col) * GROUP;
+    s.first = side * h.cols * GROUP;
+    s.active = s.team < h.teams && at < C;
+    s.channel = at + GROUP <= C || C < GROUP ? at : C - GROUP;
+    s.skip = at - s.channel;
+    s.base = (s.n * h.L + s.first_row + s.team) * h.C + s.channel;
+    return s;
+}
+
+// Eight values of a row, or all of a row of fewer.
+template <typename T>
+__device__ __forceinline__ void load_row(const Map& h, const T* p, Raw<T>& r)
+{
+    if (h.C >= GROUP)
+        load_raw(p, GROUP, r);
+    else
+        load_raw(p, h.C, r);
+}
+
+template <typename T>
+__device__ __forceinline__ void store_row(const Map& h, T* p, const float (&v)[GROUP])
+{
+    if (h.C >= GROUP)
+        store_group(p, v);
+    else
+        store_some(p, h.C, v);
+}
+
+template <typename T>
+__device__ __forceinline__ void values_of(const Raw<T>& r, float (&v)[GROUP])
 {
 #pragma unroll
     for (int i = 0; i < GROUP; ++i)
-        v[i] = channel + i < c.C ? of_groups[n * c.groups + (channel + i) / c.D] : 0.f;
+        v[i] = raw_value(r, i);
 }
 
-// ---------------------------------------------------------------------------
-// Forward: mean and sum of squares about it of each chunk and channel.
-// ---------------------------------------------------------------------------
+// The same for a result that is not read again here, past the caches: what the second
+// read of a large map finds there stays (32 x 224 x 224 x 64 bf16, forward 137 us with
+// plain stores, 117 so).
+__device__ __forceinline__ void stream_group(float* p, const float (&v)[GROUP])
+{
+    f4a a, b;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        a[i] = v[i];
+        b[i] = v[4 + i];
+    }
+    __builtin_nontemporal_store(a, reinterpret_cast<f4a*>(p));
+    __builtin_nontemporal_store(b, reinterpret_cast<f4a*>(p + 4));
+}
+
+__device__ __forceinline__ void stream_group(__bf16* p, const float (&v)[GROUP])
+{
+    f8e a;
+#pragma unroll
+    for (int i = 0; i < GROUP; ++i)
+        a[i] = v[i];
+    __builtin_nontemporal_store(__builtin_convertvector(a, bf8e), reinterpret_cast<bf8a*>(p));
+}
+
 template <typename T>
-__global__ __launch_bounds__(MOST_THREADS) void chunk_stats_kernel(const T* __restrict__ x, Cut c, int64_t work,
-                                                                   Pair* __restrict__ partial)
+__device__ __forceinline__ void stream_row(const Map& h, T* p, const float (&v)[GROUP])
 {
-    __shared__ Pair lds[MOST_THREADS * GROUP];
-    for (int64_t b = blockIdx.x; b < work; b += gridDim.x) {
-        const Place p = place_of(c, b);
-        const int64_t left = c.C - p.channel;
-        const int64_t first = p.first_row + p.team;
-        if (p.active && first < p.end_row) {
-            const T* at = x + (p.n * c.L + first) * c.C + p.channel;
-            float pivot[GROUP], s1[GROUP] = {}, s2[GROUP] = {}, v[GROUP];
-            load_some(at, left, pivot);
-            for (int64_t r = first + c.teams; r < p.end_row; r += c.teams) {
-                at += c.teams * c.C;
-                load_some(at, left, v);
-#pragma unroll
-                for (int i = 0; i < GROUP; ++i) {
-                    const float d = v[i] - pivot[i];
-                    s1[i] += d;
-                    s2[i] = fmaf(d, d, s2[i]);
-                }
-            }
-            const float inv = 1.f / static_cast<float>((p.end_row - first + c.teams - 1) / c.teams);
-#pragma unroll
-            for (int i = 0; i < GROUP; ++i) {
-                const float m = s1[i] * inv;
-                lds[threadIdx.x * GROUP + i] = Pair{pivot[i] + m, fmaxf(fmaf(-m, s1[i], s2[i]), 0.f)};
-            }
-        }
-        __syncthreads();
-        // The teams of each channel, in order.
-        const int64_t rows = p.end_row - p.first_row;
-        const int teams = static_cast<int>(rows < c.teams ? rows : c.teams);
-        for (int k = threadIdx.x; k < c.cols * GROUP; k += blockDim.x) {
-            const int64_t channel = p.channel - (threadIdx.x % c.cols) * GROUP + k;
-            if (channel >= c.C)
-                continue;
-            float mean = 0.f, m2 = 0.f, sum = 0.f;
-            for (int w = 0; w < teams; ++w) {
-                const float count = static_cast<float>((rows - w + c.teams - 1) / c.teams);
-                sum = fmaf(count, lds[w * c.cols * GROUP + k].a - lds[k].a, sum);
-            }
-            mean = lds[k].a + sum / static_cast<float>(rows);
-            for (int w = 0; w < teams; ++w) {
-                const float count = static_cast<float>((rows - w + c.teams - 1) / c.teams);
-                const Pair q = lds[w * c.cols * GROUP + k];
-                m2 += fmaf(count * (q.a - mean), q.a - mean, q.b);
-            }
-            *pair_at(partial, c, p.n, p.chunk, channel) = Pair{mean, m2};
-        }
-        __syncthreads();
-    }
+    if (h.C >= GROUP)
+        stream_group(p, v);
+    else
+        store_some(p, h.C, v);
 }
 
-__device__ __forceinline__ double workgroup_sum(double v, double* lds)
+// A weight array's values at a thread's channels.
+__device__ __forceinline__ void load_weights(const Map& h, const Spot& s, const float* p, float (&v)[GROUP])
 {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1)
-        v += __shfl_xor(v, d);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0)
-        lds[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = 0.0;
-    for (unsigned i = 0; i < blockDim.x / 64; ++i)
-        v += lds[i];
-    return v;
+    load_some(p + s.channel, s.active ? h.C - s.channel : 0, v);
 }
 
-// Each group's mean and rstd, one workgroup a group.
-__global__ __launch_bounds__(SUM_THREADS) void group_stats_kernel(const Pair* __restrict__ partial, Cut c, float eps,
-                                                                  float* __restrict__ mean_out,
-                                                                  float* __restrict__ rstd_out)
+// ---------------------------------------------------------------------------
+// The activation and its slope.
+// ---------------------------------------------------------------------------
+// 1 / (1 + e^-z), the exponential and the reciprocal by the instructions that are
+// right to 1 ulp: z's product with log2 e adds |z| 2^-23 to the exponential's error.
+__device__ __forceinline__ float sigmoid(float z)
 {
-    __shared__ double lds[SUM_THREADS / 64];
-    const int64_t pairs = c.chunks * c.D;
-    const double count = static_cast<double>(c.L) * static_cast<double>(c.D);
-    for (int64_t q = blockIdx.x; q < c.N * c.groups; q += gridDim.x) {
-        const int64_t n = q / c.groups, first = (q - n * c.groups) * c.D;
-        auto at = [&](int64_t i, double& rows) {
-            const int64_t chunk = i / c.D;
-            rows = static_cast<double>(chunk + 1 < c.chunks ? c.rows : c.L - chunk * c.rows);
-            return partial[(n * c.chunks + chunk) * c.C + first + (i - chunk * c.D)];
-        };
-        double s = 0.0, rows;
-        for (int64_t i = threadIdx.x; i < pairs; i += SUM_THREADS) {
-            const Pair p = at(i, rows);
-            s += rows * p.a;
-        }
-        const double mean = workgroup_sum(s, lds) / count;
-        s = 0.0;
-        for (int64_t i = threadIdx.x; i < pairs; i += SUM_THREADS) {
-            const Pair p = at(i, rows);
-            s += p.b + rows * (p.a - mean) * (p.a - mean);
-        }
-        s = workgroup_sum(s, lds);
-        if (threadIdx.x == 0) {
-            mean_out[q] = static_cast<float>(mean);
-            rstd_out[q] = static_cast<float>(1.0 / sqrt(s / count + eps));
-        }
-    }
+    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504f));
 }
-
-// 1 / (1 + e^-z)
-__device__ __forceinline__ float sigmoid(float z) { return 1.f / (1.f + __expf(-z)); }
 
 template <int ACT>
 __device__ __forceinline__ float activated(float z)
@@ -211,209 +164,970 @@ __device__ __forceinline__ float activated(float z)
     return z;
 }
 
-template <typename T, int ACT>
-__global__ __launch_bounds__(MOST_THREADS) void forward_kernel(const T* __restrict__ x, const float* __restrict__ gamma,
-                                                               const float* __restrict__ beta, Cut c, int64_t work,
-                                                               const float* __restrict__ mean_in,
-                                                               const float* __restrict__ rstd_in, T* __restrict__ y)
+// What a backward pass reads of its inputs besides x and dy.
+struct Inputs {
+    const float* gamma;
+    const float* beta;
+    const float* mean;
+    const float* rstd;
+};
+
+// A thread's channels in the backward pass: d = x - mean, z = d scale + shift.
+struct Lines {
+    float mean[GROUP], scale[GROUP], shift[GROUP];
+};
+
+__device__ __forceinline__ void load_lines(const Map& h, const Spot& s, const Inputs& in, Lines& l, float (&rstd)[GROUP])
 {
-    for (int64_t b = blockIdx.x; b < work; b += gridDim.x) {
-        const Place p = place_of(c, b);
-        if (!p.active)
-            continue;
-        const int64_t left = c.C - p.channel;
-        float mean[GROUP], scale[GROUP], shift[GROUP], v[GROUP];
-        per_channel(mean_in, c, p.n, p.channel, mean);
-        per_channel(rstd_in, c, p.n, p.channel, scale);
-        load_some(gamma + p.channel, left, v);
-        load_some(beta + p.channel, left, shift);
+    load_weights(h, s, in.gamma, l.scale);
+    load_weights(h, s, in.beta, l.shift);
+    if (!s.active)
+        return;
+    const float* mean = in.mean + s.n * h.groups;
+    const float* r = in.rstd + s.n * h.groups;
 #pragma unroll
-        for (int i = 0; i < GROUP; ++i)
-            scale[i] *= v[i];
-        for (int64_t r = p.first_row + p.team; r < p.end_row; r += c.teams) {
-            const int64_t at = (p.n * c.L + r) * c.C + p.channel;
-            load_some(x + at, left, v);
-#pragma unroll
-            for (int i = 0; i < GROUP; ++i)
-                v[i] = activated<ACT>(fmaf(v[i] - mean[i], scale[i], shift[i]));
-            store_some(y + at, left, v);
-        }
+    for (int i = 0; i < GROUP; ++i) {
+        const int c = s.channel + i < h.C ? s.channel + i : static_cast<int>(h.C) - 1, g = group_of(h, c);
+        l.mean[i] = mean[g];
+        rstd[i] = r[g];
+        l.scale[i] *= rstd[i];
     }
 }
 
-// ---------------------------------------------------------------------------
-// Backward: dz = dy act'(z), with n = (x - mean) rstd and z = n gamma + beta.
-// ---------------------------------------------------------------------------
-// The gradient that reaches z.  ReLU: z next to 0 -- within 2^-20 of its terms,
-// which fp32 gets right to 2^-22 -- is made again in 64 bits, so that which side
-// it falls on does not depend on how it is rounded.
+// dz = dy act'(z) of a thread's channels, v: x, d: x - mean.
+//
+// ReLU: z is within 4 u (|d scale| + |shift|) of its value, u = 2^-24.  Its sign can
+// be wrong only where |z| is below that, where |d scale| is |shift| but for as much:
+// z below 2^-19 |shift| is made again in 64 bits, so that the side it falls on does
+// not depend on how it was rounded.
 template <int ACT>
-__device__ __forceinline__ float gradient(float dy, float x, float mean, float rstd, float n, float gamma, float beta)
+__device__ __forceinline__ void slopes(const Map& h, const Spot& s, const Inputs& in, const Lines& l,
+                                       const float (&v)[GROUP], const float (&d)[GROUP], float (&dz)[GROUP])
 {
     if (ACT == POSEIDON_ACT_NONE)
-        return dy;
-    const float z = fmaf(n, gamma, beta);
+        return;
     if (ACT == POSEIDON_ACT_SILU) {
-        const float q = sigmoid(z);
-        return dy * q * fmaf(z, 1.f - q, 1.f);
-    }
-    bool on = z > 0.f;
-    if (fabsf(z) <= 0x1p-20f * (fabsf(n * gamma) + fabsf(beta)))
-        on = (static_cast<double>(x) - mean) * rstd * gamma + beta > 0.0;
-    return on ? dy : 0.f;
-}
-
-// Sums over each chunk's rows: dz and dz n of each channel.
-template <typename T, int ACT>
-__global__ __launch_bounds__(MOST_THREADS) void chunk_sums_kernel(
-    const T* __restrict__ dy, const T* __restrict__ x, const float* __restrict__ gamma, const float* __restrict__ beta,
-    Cut c, int64_t work, const float* __restrict__ mean_in, const float* __restrict__ rstd_in,
-    Pair* __restrict__ partial)
-{
-    __shared__ Pair lds[MOST_THREADS * GROUP];
-    for (int64_t b = blockIdx.x; b < work; b += gridDim.x) {
-        const Place p = place_of(c, b);
-        const int64_t left = c.C - p.channel;
-        float s1[GROUP] = {}, s2[GROUP] = {};
-        if (p.active) {
-            float mean[GROUP], rstd[GROUP], w[GROUP], shift[GROUP], v[GROUP], d[GROUP];
-            per_channel(mean_in, c, p.n, p.channel, mean);
-            per_channel(rstd_in, c, p.n, p.channel, rstd);
-            load_some(gamma + p.channel, left, w);
-            load_some(beta + p.channel, left, shift);
-            for (int64_t r = p.first_row + p.team; r < p.end_row; r += c.teams) {
-                const int64_t at = (p.n * c.L + r) * c.C + p.channel;
-                load_some(x + at, left, v);
-                load_some(dy + at, left, d);
-#pragma unroll
-                for (int i = 0; i < GROUP; ++i) {
-                    const float n = (v[i] - mean[i]) * rstd[i];
-                    const float dz = gradient<ACT>(d[i], v[i], mean[i], rstd[i], n, w[i], shift[i]);
-                    s1[i] += dz;
-                    s2[i] = fmaf(dz, n, s2[i]);
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < GROUP; ++i)
-                lds[threadIdx.x * GROUP + i] = Pair{s1[i], s2[i]};
-        }
-        __syncthreads();
-        for (int k = threadIdx.x; k < c.cols * GROUP; k += blockDim.x) {
-            const int64_t channel = p.channel - (threadIdx.x % c.cols) * GROUP + k;
-            if (channel >= c.C)
-                continue;
-            Pair s{0.f, 0.f};
-            for (int w = 0; w < c.teams; ++w) {
-                s.a += lds[w * c.cols * GROUP + k].a;
-                s.b += lds[w * c.cols * GROUP + k].b;
-            }
-            *pair_at(partial, c, p.n, p.chunk, channel) = s;
-        }
-        __syncthreads();
-    }
-}
-
-// Each group's averages of g = gamma dz and of g n (the first N groups of work),
-// then dgamma and dbeta, SUM_COLS channels a workgroup.
-constexpr int SUM_COLS = 16;
-
-__global__ __launch_bounds__(SUM_THREADS) void join_sums_kernel(const Pair* __restrict__ partial, Cut c,
-                                                                const float* __restrict__ gamma,
-                                                                Pair* __restrict__ averages,
-                                                                float* __restrict__ dgamma, float* __restrict__ dbeta)
-{
-    __shared__ double lds[SUM_THREADS * 2];
-    const int64_t of_groups = c.N * c.groups, work = of_groups + (c.C + SUM_COLS - 1) / SUM_COLS;
-    const int64_t pairs = c.chunks * c.D;
-    const double count = static_cast<double>(c.L) * static_cast<double>(c.D);
-    for (int64_t q = blockIdx.x; q < work; q += gridDim.x) {
-        if (q < of_groups) {
-            const int64_t n = q / c.groups, first = (q - n * c.groups) * c.D;
-            double s1 = 0.0, s2 = 0.0;
-            for (int64_t i = threadIdx.x; i < pairs; i += SUM_THREADS) {
-                const int64_t chunk = i / c.D, channel = first + (i - chunk * c.D);
-                const Pair p = partial[(n * c.chunks + chunk) * c.C + channel];
-                s1 += static_cast<double>(gamma[channel]) * p.a;
-                s2 += static_cast<double>(gamma[channel]) * p.b;
-            }
-            s1 = workgroup_sum(s1, lds);
-            s2 = workgroup_sum(s2, lds);
-            if (threadIdx.x == 0)
-                averages[q] = Pair{static_cast<float>(s1 / count), static_cast<float>(s2 / count)};
-            continue;
-        }
-        constexpr int SLICES = SUM_THREADS / SUM_COLS;
-        const int lane = threadIdx.x % SUM_COLS, w = threadIdx.x / SUM_COLS;
-        const int64_t channel = (q - of_groups) * SUM_COLS + lane;
-        double s1 = 0.0, s2 = 0.0;
-        if (channel < c.C)
-            for (int64_t i = w; i < c.N * c.chunks; i += SLICES) {
-                const Pair p = partial[i * c.C + channel];
-                s1 += p.a;
-                s2 += p.b;
-            }
-        __syncthreads();
-        lds[threadIdx.x * 2] = s1;
-        lds[threadIdx.x * 2 + 1] = s2;
-        __syncthreads();
-        if (w == 0 && channel < c.C) {
-            s1 = s2 = 0.0;
-            for (int i = 0; i < SLICES; ++i) {
-                s1 += lds[(i * SUM_COLS + lane) * 2];
-                s2 += lds[(i * SUM_COLS + lane) * 2 + 1];
-            }
-            dbeta[channel] = static_cast<float>(s1);
-            dgamma[channel] = static_cast<float>(s2);
-        }
-    }
-}
-
-template <typename T, int ACT>
-__global__ __launch_bounds__(MOST_THREADS) void backward_kernel(
-    const T* __restrict__ dy, const T* __restrict__ x, const float* __restrict__ gamma, const float* __restrict__ beta,
-    Cut c, int64_t work, const float* __restrict__ mean_in, const float* __restrict__ rstd_in,
-    const Pair* __restrict__ averages, T* __restrict__ dx)
-{
-    for (int64_t b = blockIdx.x; b < work; b += gridDim.x) {
-        const Place p = place_of(c, b);
-        if (!p.active)
-            continue;
-        const int64_t left = c.C - p.channel;
-        float mean[GROUP], rstd[GROUP], w[GROUP], shift[GROUP], a1[GROUP], a2[GROUP], v[GROUP], d[GROUP];
-        per_channel(mean_in, c, p.n, p.channel, mean);
-        per_channel(rstd_in, c, p.n, p.channel, rstd);
-        load_some(gamma + p.channel, left, w);
-        load_some(beta + p.channel, left, shift);
 #pragma unroll
         for (int i = 0; i < GROUP; ++i) {
-            const Pair q = p.channel + i < c.C ? averages[p.n * c.groups + (p.channel + i) / c.D] : Pair{0.f, 0.f};
-            a1[i] = q.a;
-            a2[i] = q.b;
+            const float z = fmaf(d[i], l.scale[i], l.shift[i]), q = sigmoid(z);
+            dz[i] = dz[i] * q * fmaf(z, 1.f - q, 1.f);
         }
-        for (int64_t r = p.first_row + p.team; r < p.end_row; r += c.teams) {
-            const int64_t at = (p.n * c.L + r) * c.C + p.channel;
-            load_some(x + at, left, v);
-            load_some(dy + at, left, d);
+        return;
+    }
+    uint32_t on = 0, near = 0;
+#pragma unroll
+    for (int i = 0; i < GROUP; ++i) {
+        const float z = fmaf(d[i], l.scale[i], l.shift[i]);
+        on |= (z > 0.f ? 1u : 0u) << i;
+        near |= (fabsf(z) <= fabsf(l.shift[i]) * 0x1p-19f ? 1u : 0u) << i;
+    }
+    for (; near; near &= near - 1) {   // (one after another: rare, and few registers)
+        const int i = __builtin_ctz(near);
+        float x = v[0];
+#pragma unroll
+        for (int k = 1; k < GROUP; ++k)
+            x = i == k ? v[k] : x;
+        const int c = s.channel + i < h.C ? s.channel + i : static_cast<int>(h.C) - 1;
+        const int64_t g = s.n * h.groups + group_of(h, c);
+        const double z = (static_cast<double>(x) - in.mean[g]) * in.rstd[g] * in.gamma[c] + in.beta[c];
+        on = (on & ~(1u << i)) | (z > 0.0 ? 1u : 0u) << i;
+    }
+#pragma unroll
+    for (int i = 0; i < GROUP; ++i)
+        dz[i] = on >> i & 1 ? dz[i] : 0.f;
+}
+
+// ---------------------------------------------------------------------------
+// Maps held in registers: one workgroup takes whole groups of one sample, reads
+// them once, and has all their values when it knows their statistics.  Thread
+// (team, col) holds rows team, team + teams, ...: up to K of them.
+// ---------------------------------------------------------------------------
+constexpr int XCDS = 8;
+
+// Neighbouring workgroups run on different dies, each with a cache of its own: the
+// workgroups of one sample, which share memory lines, are given to one die.
+__device__ __forceinline__ int64_t on_one_die(int64_t work)
+{
+    const int64_t each = gridDim.x / XCDS;
+    const int64_t b = static_cast<int64_t>(blockIdx.x % XCDS) * each + blockIdx.x / XCDS;
+    return b < work ? b : -1;
+}
+
+template <typename T, int K>
+__device__ __forceinline__ void hold(const T* x, const Map& h, const Spot& s, Raw<T> (&r)[K])
+{
+    const int64_t step = h.teams * h.C;
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        r[j] = Raw<T>{};
+        if (s.active && s.team + j * h.teams < h.L)
+            load_row(h, x + s.base + j * step, r[j]);
+    }
+}
+
+// Keeps the compiler from carrying what it unpacked in one pass over the held
+// values to the next, which would take twice the registers of bf16 values.
+__device__ __forceinline__ void unpack_again(Raw<__bf16>& r)
+{
+    typedef unsigned u4 __attribute__((ext_vector_type(4)));
+    u4 w = __builtin_bit_cast(u4, r);
+    asm volatile("" : "+v"(w));
+    r = __builtin_bit_cast(Raw<__bf16>, w);
+}
+__device__ __forceinline__ void unpack_again(Raw<float>&) {}
+
+// V sums a channel (v: of this thread's rows; 0 in its skipped channels) joined over
+// the workgroup's groups: out[g * V + i], in LDS.
+template <int NT, int V>
+__device__ __forceinline__ void join_groups(float (&v)[V][GROUP], const Map& h, const Spot& s, float* parts, float* out)
+{
+    const int pieces = GROUP / h.piece, skip = s.skip / h.piece;   // (piece divides 8 and the row's rest: whole pieces)
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        if (h.piece >= 2) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                v[i][k] = v[i][2 * k] + v[i][2 * k + 1];
+        }
+        if (h.piece >= 4) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                v[i][k] = v[i][2 * k] + v[i][2 * k + 1];
+        }
+        if (h.piece >= 8)
+            v[i][0] += v[i][1];
+    }
+    const int each = h.D / h.piece, rows = h.fold ? NT / 64 : h.teams;   // pieces of a group and row
+    int row = s.team;
+    bool writes = s.active;
+    if (h.fold) {
+        for (int m = h.cols; m < 64; m <<= 1)
+#pragma unroll
+            for (int k = 0; k < GROUP; ++k)
+                if (k < pieces)
+#pragma unroll
+                    for (int i = 0; i < V; ++i)
+                        v[i][k] += __shfl_xor(v[i][k], m);
+        row = threadIdx.x >> 6;
+        writes = s.active && (threadIdx.x & 63) < h.cols;
+    }
+    __syncthreads();   // what an earlier sum left has been read
+    if (writes) {
+#pragma unroll
+        for (int k = 0; k < GROUP; ++k)
+            if (k >= skip && k < pieces) {
+                const int c = s.channel - s.first + k * h.piece, g = group_of(h, c);
+                if (g < h.span) {   // (past the last channel: none)
+                    const int at = (g * rows + row) * each + ((c - g * h.D) >> h.shift);
+#pragma unroll
+                    for (int i = 0; i < V; ++i)
+                        parts[at * V + i] = v[i][k];
+                }
+            }
+    }
+    __syncthreads();
+    for (int g = static_cast<int>(threadIdx.x) / h.lanes; g < h.span; g += NT / h.lanes) {
+        float a[V] = {};
+        const float* of = parts + g * rows * each * V;
+#pragma unroll 4
+        for (int q = threadIdx.x & (h.lanes - 1); q < rows * each; q += h.lanes)
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                a[i] += of[q * V + i];
+        for (int m = 1; m < h.lanes; m <<= 1)
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                a[i] += __shfl_xor(a[i], m);
+        if ((threadIdx.x & (h.lanes - 1)) == 0)
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                out[g * V + i] = a[i];
+    }
+    __syncthreads();
+}
+
+// The mean is a first sum, corrected by the sum of the differences from it, which
+// also gives the spread.
+template <typename T, int ACT, int NT, int K>
+__global__ __launch_bounds__(NT) void held_forward_kernel(const T* __restrict__ x, const float* __restrict__ gamma,
+                                                          const float* __restrict__ beta, Map h, float eps,
+                                                          T* __restrict__ y, float* __restrict__ mean_out,
+                                                          float* __restrict__ rstd_out)
+{
+    extern __shared__ float lds[];
+    const int64_t b = on_one_die(h.work);
+    if (b < 0)
+        return;
+    const Spot s = spot_of(h, b);
+    float* const sums = lds;                  // of the groups
+    float* const parts = lds + 2 * h.span;
+    Raw<T> r[K];
+    hold(x, h, s, r);
+    const float inv = 1.f / (static_cast<float>(h.L) * static_cast<float>(h.D));
+    const int local = s.channel - s.first, most = h.span - 1;
+    float mean[GROUP], a[1][GROUP] = {};
+#pragma unroll
+    for (int j = 0; j < K; ++j)
+#pragma unroll
+        for (int i = 0; i < GROUP; ++i)
+            a[0][i] += raw_value(r[j], i);
+#pragma unroll
+    for (int i = 0; i < GROUP; ++i)
+        a[0][i] = i < s.skip ? 0.f : a[0][i];
+    join_groups<NT, 1>(a, h, s, parts, sums);
+#pragma unroll
+    for (int i = 0; i < GROUP; ++i) {
+        const int g = group_of(h, local + i);
+        mean[i] = sums[g < most ? g : most] * inv;   // (past the last channel: nothing is stored)
+    }
+    float c[2][GROUP] = {};
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        unpack_again(r[j]);
+        if (s.active && s.team + j * h.teams < h.L) {
 #pragma unroll
             for (int i = 0; i < GROUP; ++i) {
-                const float n = (v[i] - mean[i]) * rstd[i];
-                const float dz = gradient<ACT>(d[i], v[i], mean[i], rstd[i], n, w[i], shift[i]);
-                v[i] = rstd[i] * (fmaf(w[i], dz, -a1[i]) - n * a2[i]);
+                const float d = raw_value(r[j], i) - mean[i];
+                c[0][i] += d;
+                c[1][i] = fmaf(d, d, c[1][i]);
             }
-            store_some(dx + at, left, v);
         }
+    }
+#pragma unroll
+    for (int i = 0; i < GROUP; ++i) {
+        const bool own = i >= s.skip && s.channel + i < h.C;
+        c[0][i] = own ? c[0][i] : 0.f;
+        c[1][i] = own ? c[1][i] : 0.f;
+    }
+    float scale[GROUP], shift[GROUP];
+    load_weights(h, s, gamma, scale);
+    load_weights(h, s, beta, shift);
+    join_groups<NT, 2>(c, h, s, parts, sums);
+#pragma unroll
+    for (int i = 0; i < GROUP; ++i) {
+        int g = group_of(h, local + i);
+        g = g < most ? g : most;
+        const float off = sums[2 * g] * inv, var = sums[2 * g + 1] * inv - off * off;
+        const float rstd = 1.f / sqrtf((var < 0.f ? 0.f : var) + eps);   // (NaN stays)
+        mean[i] += off;
+        if (s.active && s.team == 0 && s.channel + i < h.C && i >= s.skip && (local + i) - g * h.D == 0) {
+            const int64_t at = s.n * h.groups + s.first / h.D + g;
+            mean_out[at] = mean[i];
+            rstd_out[at] = rstd;
+        }
+        scale[i] *= rstd;
+    }
+    if (!s.active)
+        return;
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        if (s.team + j * h.teams >= h.L)
+            break;
+        unpack_again(r[j]);
+        float v[GROUP];
+#pragma unroll
+        for (int i = 0; i < GROUP; ++i)
+            v[i] = activated<ACT>(fmaf(raw_value(r[j], i) - mean[i], scale[i], shift[i]));
+        store_row(h, y + s.base + j * (h.teams * h.C), v);
+    }
+}
+
+// totals: dz and dz (x - mean) rstd of each sample and channel (or, of one sample,
+// dbeta and dgamma themselves).
+template <typename T, int ACT, int NT, int K>
+__global__ __launch_bounds__(NT) void held_backward_kernel(const T* __restrict__ dy, const T* __restrict__ x, Inputs in,
+                                                           Map h, T* __restrict__ dx, Pair* __restrict__ totals,
+                                                           float* __restrict__ dgamma, float* __restrict__ dbeta)
+{
+    extern __shared__ float lds[];
+    const int64_t b = on_one_die(h.work);
+    if (b < 0)
+        return;
+    const Spot s = spot_of(h, b);
+    const int channels = h.cols * GROUP, local = s.channel - s.first;
+    float* const sums = lds;                                         // of the groups
+    Pair* const parts = reinterpret_cast<Pair*>(lds + 2 * h.span);   // of the channels
+    Raw<T> rx[K], rd[K];
+    hold(x, h, s, rx);
+    hold(dy, h, s, rd);
+    Lines l;
+    float rstd[GROUP] = {};
+    load_lines(h, s, in, l, rstd);
+    float c[2][GROUP] = {};
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        if (s.active && s.team + j * h.teams < h.L) {
+            float v[GROUP], d[GROUP], dz[GROUP];
+            values_of(rx[j], v);
+            values_of(rd[j], dz);
+#pragma unroll
+            for (int i = 0; i < GROUP; ++i)
+                d[i] = v[i] - l.mean[i];
+            slopes<ACT>(h, s, in, l, v, d, dz);
+#pragma unroll
+            for (int i = 0; i < GROUP; ++i) {
+                c[0][i] += dz[i];
+                c[1][i] = fmaf(dz[i], d[i], c[1][i]);
+            }
+        }
+    }
+    // Each channel's sums over the workgroup's rows ...
+    int row = s.team;
+    bool writes = s.active;
+    if (h.fold) {
+        for (int m = h.cols; m < 64; m <<= 1)
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int i = 0; i < GROUP; ++i)
+                    c[k][i] += __shfl_xor(c[k][i], m);
+        row = threadIdx.x >> 6;
+        writes = s.active && (threadIdx.x & 63) < h.cols;
+    }
+    if (writes) {
+#pragma unroll
+        for (int i = 0; i < GROUP; ++i)
+            if (i >= s.skip)
+                parts[row * channels + local + i] = Pair{c[0][i], c[1][i] * rstd[i]};
+    }
+    __syncthreads();
+    const int rows = h.fold ? NT / 64 : h.teams;
+    for (int k = threadIdx.x; k < channels; k += NT) {
+        if (s.first + k >= h.C)
+            continue;
+        Pair t{0.f, 0.f};
+        for (int q = 0; q < rows; ++q) {
+            t.a += parts[q * channels + k].a;
+            t.b += parts[q * channels + k].b;
+        }
+        if (h.N == 1) {
+            dbeta[s.first + k] = t.a;
+            dgamma[s.first + k] = t.b;
+        } else {
+            totals[s.n * h.C + s.first + k] = t;
+        }
+        parts[k] = t;     // (only this thread reads column k)
+    }
+    __syncthreads();
+    // ... and each group's averages of g = gamma dz and of g n.
+    const double count = static_cast<double>(h.L) * static_cast<double>(h.D);
+    for (int g = static_cast<int>(threadIdx.x) / h.lanes; g < h.span; g += NT / h.lanes) {
+        double a1 = 0.0, a2 = 0.0;
+        for (int q = threadIdx.x & (h.lanes - 1); q < h.D; q += h.lanes) {
+            const double w = in.gamma[s.first + g * h.D + q];
+            a1 += w * parts[g * h.D + q].a;
+            a2 += w * parts[g * h.D + q].b;
+        }
+        for (int m = 1; m < h.lanes; m <<= 1) {
+            a1 += __shfl_xor(a1, m);
+            a2 += __shfl_xor(a2, m);
+        }
+        if ((threadIdx.x & (h.lanes - 1)) == 0) {
+            sums[2 * g] = static_cast<float>(a1 / count);
+            sums[2 * g + 1] = static_cast<float>(a2 / count);
+        }
+    }
+    __syncthreads();
+    if (!s.active)
+        return;
+    // dx = rstd (gamma dz - a1 - d rstd a2)
+    float k1[GROUP], k2[GROUP];
+#pragma unroll
+    for (int i = 0; i < GROUP; ++i) {
+        int g = group_of(h, local + i);
+        g = g < h.span ? g : h.span - 1;
+        k1[i] = -rstd[i] * sums[2 * g];
+        k2[i] = -rstd[i] * rstd[i] * sums[2 * g + 1];
+    }
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        if (s.team + j * h.teams >= h.L)
+            break;
+        unpack_again(rx[j]);
+        unpack_again(rd[j]);
+        float v[GROUP], d[GROUP], dz[GROUP];
+        values_of(rx[j], v);
+        values_of(rd[j], dz);
+#pragma unroll
+        for (int i = 0; i < GROUP; ++i)
+            d[i] = v[i] - l.mean[i];
+        slopes<ACT>(h, s, in, l, v, d, dz);
+#pragma unroll
+        for (int i = 0; i < GROUP; ++i)
+            v[i] = fmaf(l.scale[i], dz[i], fmaf(d[i], k2[i], k1[i]));
+        store_row(h, dx + s.base + j * (h.teams * h.C), v);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Three launches, forward: mean and sum of squares about it of each chunk and
+// channel; each group's mean and rstd; the result.
+// ---------------------------------------------------------------------------
+constexpr int MOST_THREADS = 256;
+constexpr int MOST_ROWS = 64;    // of a thread
+constexpr int AT_ONCE = 4;       // rows in flight
+
+// f(row's values) for the rows of this thread, from its `from`-th, AT_ONCE loaded
+// together.
+template <int M, typename T, typename F>
+__device__ __forceinline__ void walk(const Map& h, const Spot& s, const T* const (&x)[M], int from, F&& f)
+{
+    const int64_t step = h.teams * h.C;
+    int64_t at = s.base + from * step;
+    for (int64_t row = s.first_row + s.team + static_cast<int64_t>(from) * h.teams; row < s.end_row;
+         row += AT_ONCE * h.teams, at += AT_ONCE * step) {
+        Raw<T> r[AT_ONCE][M];
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j)
+            if (row + j * h.teams < s.end_row)
+#pragma unroll
+                for (int m = 0; m < M; ++m)
+                    load_row(h, x[m] + at + j * step, r[j][m]);
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j)
+            if (row + j * h.teams < s.end_row)
+                f(r[j], at + j * step);
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(MOST_THREADS) void chunk_stats_kernel(const T* __restrict__ x, Map h,
+                                                                   Pair* __restrict__ partial)
+{
+    __shared__ Pair lds[MOST_THREADS * GROUP];
+    __shared__ float counts[MOST_THREADS];
+    for (int64_t b = blockIdx.x; b < h.work; b += gridDim.x) {
+        const Spot s = spot_of(h, b);
+        const int local = s.channel - s.first, channels = h.cols * GROUP;
+        float mean[GROUP] = {}, m2[GROUP] = {}, count = 0.f;
+        if (s.active && s.first_row + s.team < s.end_row) {
+            // differences from the thread's own first value
+            Raw<T> first;
+            load_row(h, x + s.base, first);
+            float s1[GROUP] = {};
+            walk<1, T>(h, s, {x}, 1, [&](const Raw<T> (&r)[1], int64_t) {
+#pragma unroll
+                for (int i = 0; i < GROUP; ++i) {
+                    const float d = raw_value(r[0], i) - raw_value(first, i);
+                    s1[i] += d;
+                    m2[i] = fmaf(d, d, m2[i]);
+                }
+            });
+            count = static_cast<float>((s.end_row - s.first_row - s.team + h.teams - 1) / h.teams);
+            const float inv = 1.f / count;
+#pragma unroll
+            for (int i = 0; i < GROUP; ++i) {
+                const float m = s1[i] * inv, q = fmaf(-m, s1[i], m2[i]);
+                mean[i] = raw_value(first, i) + m;
+                m2[i] = q < 0.f ? 0.f : q;   // (NaN stays)
+            }
+        }
+        int row = s.team;
+        bool writes = s.active;
+        if (h.fold) {
+            // two teams: their means' distance d moves the mean by d times the other's
+            // share, and adds d^2 times the smaller count's harmonic part
+            for (int m = h.cols; m < 64; m <<= 1) {
+                const float other = __shfl_xor(count, m), both = count + other;
+                const float share = both > 0.f ? other / both : 0.f;
+#pragma unroll
+                for (int i = 0; i < GROUP; ++i) {
+                    const float o = __shfl_xor(mean[i], m), q = __shfl_xor(m2[i], m);
+                    const float d = o - mean[i];
+                    if (other > 0.f) {
+                        m2[i] = count > 0.f ? fmaf(d * d, count * share, m2[i] + q) : q;
+                        mean[i] = count > 0.f ? fmaf(d, share, mean[i]) : o;
+                    }
+                }
+                count = both;
+            }
+            row = threadIdx.x >> 6;
+            writes = s.active && (threadIdx.x & 63) < h.cols;
+        }
+        if (writes) {
+#pragma unroll
+            for (int i = 0; i < GROUP; ++i)
+                if (i >= s.skip)
+                    lds[row * channels + local + i] = Pair{mean[i], m2[i]};
+            if (s.col == 0)
+                counts[row] = count;
+        }
+        __syncthreads();
+        // The rows of each channel, in order: the first is never empty.
+        const int rows = h.fold ? (h.threads + 63) / 64 : h.teams;
+        const float all = static_cast<float>(s.end_row - s.first_row);
+        for (int k = threadIdx.x; k < channels; k += h.threads) {
+            if (s.first + k >= h.C)
+                continue;
+            const float from = lds[k].a;
+            float sum = 0.f, q = 0.f;
+            for (int w = 1; w < rows; ++w)
+                if (counts[w] > 0.f)
+                    sum = fmaf(counts[w], lds[w * channels + k].a - from, sum);
+            const float m = from + sum / all;
+            for (int w = 0; w < rows; ++w)
+                if (counts[w] > 0.f) {
+                    const Pair p = lds[w * channels + k];
+                    q += fmaf(counts[w] * (p.a - m), p.a - m, p.b);
+                }
+            partial[(s.n * h.chunks + s.first_row / h.rows) * h.C + s.first + k] = Pair{m, q};
+        }
+        __syncthreads();
+    }
+}
+
+// A sum over TEAM threads: a wave, or the workgroup.
+template <int TEAM>
+__device__ __forceinline__ double team_sum(double v, double* lds)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1)
+        v += __shfl_xor(v, d);
+    if constexpr (TEAM > 64) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0)
+            lds[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = 0.0;
+#pragma unroll
+        for (int i = 0; i < TEAM / 64; ++i)
+            v += lds[i];
+    }
+    return v;
+}
+
+// TEAM threads a group, of at most TEAM * HELD pairs, which they hold; more pairs
+// (HELD = 0) are read twice.
+template <int TEAM, int HELD>
+__global__ __launch_bounds__(SUM_THREADS) void group_stats_kernel(const Pair* __restrict__ partial, Map h, float eps,
+                                                                  float* __restrict__ mean_out,
+                                                                  float* __restrict__ rstd_out)
+{
+    __shared__ double lds[SUM_THREADS / 64];
+    constexpr int TEAMS = SUM_THREADS / TEAM;
+    const int t = threadIdx.x % TEAM;
+    const int64_t pairs = h.chunks * h.D;
+    const double count = static_cast<double>(h.L) * static_cast<double>(h.D);
+    const int64_t chunk_step = TEAM / h.D;
+    const int rest = TEAM - static_cast<int>(chunk_step) * h.D;
+    for (int64_t q = static_cast<int64_t>(blockIdx.x) * TEAMS + threadIdx.x / TEAM; q < h.N * h.groups;
+         q += static_cast<int64_t>(gridDim.x) * TEAMS) {
+        const int64_t n = q / h.groups;
+        const Pair* at = partial + n * h.chunks * h.C + (q - n * h.groups) * h.D;
+        int64_t chunk = t / h.D;
+        int c = t - static_cast<int>(chunk) * h.D;   // pair i: of chunk i / D, channel i % D
+        auto next = [&](double& rows) {
+            const Pair* p = at + chunk * h.C + c;
+            rows = static_cast<double>(chunk + 1 < h.chunks ? h.rows : h.L - chunk * h.rows);
+            chunk += chunk_step;
+            c += rest;
+            if (c >= h.D) {
+                c -= h.D;
+                ++chunk;
+            }
+            return p;
+        };
+        double s = 0.0, mean;
+        if constexpr (HELD > 0) {
+            Pair p[HELD];
+            double rows[HELD];
+#pragma unroll
+            for (int k = 0; k < HELD; ++k) {
+                const Pair* from = next(rows[k]);
+                const bool in = t + k * TEAM < pairs;
+                rows[k] = in ? rows[k] : 0.0;
+                p[k] = in ? *from : Pair{0.f, 0.f};
+            }
+#pragma unroll
+            for (int k = 0; k < HELD; ++k)
+                s += rows[k] * p[k].a;
+            mean = team_sum<TEAM>(s, lds) / count;
+            s = 0.0;
+#pragma unroll
+            for (int k = 0; k < HELD; ++k)
+                s += rows[k] > 0.0 ? p[k].b + rows[k] * (p[k].a - mean) * (p[k].a - mean) : 0.0;
+        } else {
+            double rows;
+            for (int64_t i = t; i < pairs; i += TEAM) {
+                const Pair p = *next(rows);
+                s += rows * p.a;
+            }
+            mean = team_sum<TEAM>(s, lds) / count;
+            s = 0.0;
+            chunk = t / h.D;
+            c = t - static_cast<int>(chunk) * h.D;
+            for (int64_t i = t; i < pairs; i += TEAM) {
+                const Pair p = *next(rows);
+                s += p.b + rows * (p.a - mean) * (p.a - mean);
+            }
+        }
+        s = team_sum<TEAM>(s, lds);
+        if (t == 0) {
+            mean_out[q] = static_cast<float>(mean);
+            rstd_out[q] = static_cast<float>(1.0 / sqrt(s / count + eps));
+        }
+    }
+}
+
+template <typename T, int ACT>
+__global__ __launch_bounds__(MOST_THREADS) void forward_kernel(const T* __restrict__ x, Inputs in, Map h,
+                                                               T* __restrict__ y)
+{
+    for (int64_t b = blockIdx.x; b < h.work; b += gridDim.x) {
+        const Spot s = spot_of(h, h.work - 1 - b);   // last read, first read again
+        if (!s.active)
+            continue;
+        Lines l;
+        float rstd[GROUP];
+        load_lines(h, s, in, l, rstd);
+        walk<1, T>(h, s, {x}, 0, [&](const Raw<T> (&r)[1], int64_t at) {
+            float v[GROUP];
+#pragma unroll
+            for (int i = 0; i < GROUP; ++i)
+                v[i] = activated<ACT>(fmaf(raw_value(r[0], i) - l.mean[i], l.scale[i], l.shift[i]));
+            stream_row(h, y + at, v);
+        });
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Three launches, backward: sums of dz and dz n of each chunk and channel; of each
+// sample and channel, and each group's averages; the result, and dgamma and dbeta.
+// ---------------------------------------------------------------------------
+template <typename T, int ACT>
+__global__ __launch_bounds__(MOST_THREADS) void chunk_sums_kernel(const T* __restrict__ dy, const T* __restrict__ x,
+                                                                  Inputs in, Map h, Pair* __restrict__ partial)
+{
+    __shared__ Pair lds[MOST_THREADS * GROUP];
+    for (int64_t b = blockIdx.x; b < h.work; b += gridDim.x) {
+        const Spot s = spot_of(h, b);
+        const int local = s.channel - s.first, channels = h.cols * GROUP;
+        float c[2][GROUP] = {}, rstd[GROUP] = {};
+        if (s.active) {
+            Lines l;
+            load_lines(h, s, in, l, rstd);
+            walk<2, T>(h, s, {x, dy}, 0, [&](const Raw<T> (&r)[2], int64_t) {
+                float v[GROUP], d[GROUP], dz[GROUP];
+                values_of(r[0], v);
+                values_of(r[1], dz);
+#pragma unroll
+                for (int i = 0; i < GROUP; ++i)
+                    d[i] = v[i] - l.mean[i];
+                slopes<ACT>(h, s, in, l, v, d, dz);
+#pragma unroll
+                for (int i = 0; i < GROUP; ++i) {
+                    c[0][i] += dz[i];
+                    c[1][i] = fmaf(dz[i], d[i], c[1][i]);
+                }
+            });
+        }
+        int row = s.team;
+        bool writes = s.active;
+        if (h.fold) {
+            for (int m = h.cols; m < 64; m <<= 1)
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int i = 0; i < GROUP; ++i)
+                        c[k][i] += __shfl_xor(c[k][i], m);
+            row = threadIdx.x >> 6;
+            writes = s.active && (threadIdx.x & 63) < h.cols;
+        }
+        if (writes) {
+#pragma unroll
+            for (int i = 0; i < GROUP; ++i)
+                if (i >= s.skip)
+                    lds[row * channels + local + i] = Pair{c[0][i], c[1][i] * rstd[i]};
+        }
+        __syncthreads();
+        const int rows = h.fold ? (h.threads + 63) / 64 : h.teams;
+        for (int k = threadIdx.x; k < channels; k += h.threads) {
+            if (s.first + k >= h.C)
+                continue;
+            Pair t{0.f, 0.f};
+            for (int w = 0; w < rows; ++w) {
+                t.a += lds[w * channels + k].a;
+                t.b += lds[w * channels + k].b;
+            }
+            partial[(s.n * h.chunks + s.first_row / h.rows) * h.C + s.first + k] = t;
+        }
+        __syncthreads();
+    }
+}
+
+// One workgroup a group of one sample: its channels' sums over the chunks, a channel
+// a lane of `lanes`, and its averages.
+__global__ __launch_bounds__(SUM_THREADS) void join_sums_kernel(const Pair* __restrict__ partial, Map h,
+                                                                const float* __restrict__ gamma,
+                                                                Pair* __restrict__ totals, Pair* __restrict__ averages)
+{
+    __shared__ double lds[SUM_THREADS * 2];
+    int lanes = 1;
+    while (lanes < 64 && lanes < h.D)
+        lanes *= 2;
+    const int slices = SUM_THREADS / lanes, lane = threadIdx.x & (lanes - 1), slice = threadIdx.x / lanes;
+    const double count = static_cast<double>(h.L) * static_cast<double>(h.D);
+    for (int64_t q = blockIdx.x; q < h.N * h.groups; q += gridDim.x) {
+        const int64_t n = q / h.groups, first = (q - n * h.groups) * h.D;
+        double a1 = 0.0, a2 = 0.0;
+        for (int64_t c = lane; c - lane < h.D; c += lanes) {
+            double s1 = 0.0, s2 = 0.0;
+            if (c < h.D)
+                for (int64_t k = slice; k < h.chunks; k += slices) {
+                    const Pair p = partial[(n * h.chunks + k) * h.C + first + c];
+                    s1 += p.a;
+                    s2 += p.b;
+                }
+            lds[threadIdx.x * 2] = s1;
+            lds[threadIdx.x * 2 + 1] = s2;
+            __syncthreads();
+            if (slice == 0 && c < h.D) {
+                for (int k = 1; k < slices; ++k) {
+                    s1 += lds[(k * lanes + lane) * 2];
+                    s2 += lds[(k * lanes + lane) * 2 + 1];
+                }
+                totals[n * h.C + first + c] = Pair{static_cast<float>(s1), static_cast<float>(s2)};
+                a1 += gamma[first + c] * s1;
+                a2 += gamma[first + c] * s2;
+            }
+            __syncthreads();
+        }
+        if (slice == 0) {   // within one wave
+            for (int m = 1; m < lanes; m <<= 1) {
+                a1 += __shfl_xor(a1, m);
+                a2 += __shfl_xor(a2, m);
+            }
+            if (lane == 0)
+                averages[q] = Pair{static_cast<float>(a1 / count), static_cast<float>(a2 / count)};
+        }
+    }
+}
+
+// dgamma and dbeta from the samples' totals, SUM_COLS channels a workgroup.
+constexpr int SUM_COLS = 16;
+
+__device__ __forceinline__ void sum_samples(const Pair* __restrict__ totals, int64_t N, int64_t C, int64_t first,
+                                            double* lds, float* __restrict__ dgamma, float* __restrict__ dbeta)
+{
+    constexpr int SLICES = SUM_THREADS / SUM_COLS;
+    const int lane = threadIdx.x % SUM_COLS, w = threadIdx.x / SUM_COLS;
+    const int64_t channel = first + lane;
+    double s1 = 0.0, s2 = 0.0;
+    if (w < SLICES && channel < C)
+#pragma unroll 4
+        for (int64_t i = w; i < N; i += SLICES) {
+            const Pair p = totals[i * C + channel];
+            s1 += p.a;
+            s2 += p.b;
+        }
+    __syncthreads();
+    if (w < SLICES) {
+        lds[threadIdx.x * 2] = s1;
+        lds[threadIdx.x * 2 + 1] = s2;
+    }
+    __syncthreads();
+    if (w == 0 && channel < C) {
+        for (int i = 1; i < SLICES; ++i) {
+            s1 += lds[(i * SUM_COLS + lane) * 2];
+            s2 += lds[(i * SUM_COLS + lane) * 2 + 1];
+        }
+        dbeta[channel] = static_cast<float>(s1);
+        dgamma[channel] = static_cast<float>(s2);
+    }
+}
+
+__global__ __launch_bounds__(SUM_THREADS) void weights_kernel(const Pair* __restrict__ totals, int64_t N, int64_t C,
+                                                              float* __restrict__ dgamma, float* __restrict__ dbeta)
+{
+    __shared__ double lds[SUM_THREADS * 2];
+    sum_samples(totals, N, C, static_cast<int64_t>(blockIdx.x) * SUM_COLS, lds, dgamma, dbeta);
+}
+
+template <typename T, int ACT>
+__global__ __launch_bounds__(MOST_THREADS) void backward_kernel(const T* __restrict__ dy, const T* __restrict__ x,
+                                                                Inputs in, Map h, const Pair* __restrict__ averages,
+                                                                T* __restrict__ dx)
+{
+    for (int64_t b = blockIdx.x; b < h.work; b += gridDim.x) {
+        const Spot s = spot_of(h, h.work - 1 - b);   // last read, first read again
+        if (!s.active)
+            continue;
+        Lines l;
+        float rstd[GROUP], k1[GROUP], k2[GROUP];
+        load_lines(h, s, in, l, rstd);
+#pragma unroll
+        for (int i = 0; i < GROUP; ++i) {
+            const int c = s.channel + i < h.C ? s.channel + i : static_cast<int>(h.C) - 1;
+            const Pair a = averages[s.n * h.groups + group_of(h, c)];
+            k1[i] = -rstd[i] * a.a;
+            k2[i] = -rstd[i] * rstd[i] * a.b;
+        }
+        walk<2, T>(h, s, {x, dy}, 0, [&](const Raw<T> (&r)[2], int64_t at) {
+            float v[GROUP], d[GROUP], dz[GROUP];
+            values_of(r[0], v);
+            values_of(r[1], dz);
+#pragma unroll
+            for (int i = 0; i < GROUP; ++i)
+                d[i] = v[i] - l.mean[i];
+            slopes<ACT>(h, s, in, l, v, d, dz);
+#pragma unroll
+            for (int i = 0; i < GROUP; ++i)
+                v[i] = fmaf(l.scale[i], dz[i], fmaf(d[i], k2[i], k1[i]));
+            stream_row(h, dx + at, v);
+        });
     }
 }
 
 // ---------------------------------------------------------------------------
 // Launches.
 // ---------------------------------------------------------------------------
-int64_t workgroups(const Cut& c) { return c.N * c.chunks * c.sides; }
+int32_t gcd(int64_t a, int64_t b) { return static_cast<int32_t>(b ? gcd(b, a % b) : a); }
+
+Map map_of(int64_t N, int64_t L, int64_t C, int64_t groups, int64_t cols, int64_t threads)
+{
+    Map h{};
+    h.N = N;
+    h.L = L;
+    h.C = C;
+    h.groups = groups;
+    h.D = static_cast<int32_t>(C / groups);
+    h.inv_D = 1.f / static_cast<float>(h.D);
+    h.cols = static_cast<int32_t>(cols);
+    h.sides = static_cast<int32_t>(ceil_div(ceil_div(C, GROUP), cols));
+    h.teams = static_cast<int32_t>(threads / cols);
+    h.threads = static_cast<int32_t>(threads);
+    h.piece = gcd(h.D, GROUP);
+    h.shift = h.piece == 8 ? 3 : h.piece >> 1;   // 1, 2, 4
+    h.fold = cols <= 64 && (cols & (cols - 1)) == 0;
+    h.rows = L;
+    h.chunks = 1;
+    h.work = N * h.sides;
+    return h;
+}
+
+// The cut of the three launches: eight workgroups a CU, where each thread then has
+// at least four rows and at most MOST_ROWS.
+Map cut(int64_t N, int64_t L, int64_t C, int64_t groups)
+{
+    const int64_t all = ceil_div(C, GROUP), sides = ceil_div(all, MOST_THREADS), cols = ceil_div(all, sides);
+    int64_t teams = std::max<int64_t>(1, std::min<int64_t>(MOST_THREADS / cols, L));
+    if (cols <= 64 && (cols & (cols - 1)) == 0)   // whole waves, which are joined by shuffles
+        teams = ceil_div(teams * cols, 64) * 64 / cols;
+    Map h = map_of(N, L, C, groups, cols, ceil_div(cols * teams, 64) * 64);
+    h.teams = static_cast<int32_t>(teams);
+    const int64_t wanted = std::max<int64_t>(1, ceil_div(8 * 256, std::max<int64_t>(1, N * h.sides)));
+    const int64_t each = std::min<int64_t>(MOST_ROWS, std::max<int64_t>(4, ceil_div(L, wanted * teams)));
+    h.rows = std::min<int64_t>(L, each * teams);
+    h.chunks = ceil_div(L, h.rows);
+    h.work = N * h.chunks * h.sides;
+    return h;
+}
+
+// Threads and held rows of a workgroup.
+template <int NT_, int K_>
+struct Shape {
+    static constexpr int NT = NT_, K = K_;
+};
+
+constexpr int SHAPES = 6;
+constexpr int SHAPE_NT[SHAPES] = {256, 256, 256, 512, 512, 512};
+constexpr int SHAPE_K[SHAPES] = {2, 4, 8, 8, 16, 32};
+
+// Held values (`maps`: x, or x and dy) take at most half of a CU's registers, and 128
+// of a thread's.
+constexpr int64_t MOST_HELD = 512 * 128 * 4;
+constexpr bool shape_fits(int K, int value_bytes, int maps) { return K * maps * value_bytes * GROUP / 4 <= 128; }
+
+template <typename F>
+hipError_t with_shape(int shape, F&& f)
+{
+    switch (shape) {
+    case 0: return f(Shape<SHAPE_NT[0], SHAPE_K[0]>());
+    case 1: return f(Shape<SHAPE_NT[1], SHAPE_K[1]>());
+    case 2: return f(Shape<SHAPE_NT[2], SHAPE_K[2]>());
+    case 3: return f(Shape<SHAPE_NT[3], SHAPE_K[3]>());
+    case 4: return f(Shape<SHAPE_NT[4], SHAPE_K[4]>());
+    default: return f(Shape<SHAPE_NT[5], SHAPE_K[5]>());
+    }
+}
+
+struct Choice {
+    int shape = -1;   // -1: three launches
+    Map h{};
+    int64_t lds = 0;
+};
+
+constexpr int64_t MOST_LDS = 65536;
+
+// The workgroup of `shape` with `cols` columns, where a sample's groups fit it.
+Choice held_as(int op, int64_t N, int64_t L, int64_t C, int64_t groups, int shape, int64_t cols)
+{
+    Choice q;
+    const int NT = SHAPE_NT[shape];
+    if (cols > NT || ceil_div(L, NT / cols) > SHAPE_K[shape])
+        return q;
+    Map& h = q.h;
+    h = map_of(N, L, C, groups, cols, NT);
+    h.span = static_cast<int32_t>(h.sides == 1 ? groups : cols * GROUP / h.D);
+    h.lanes = 1;
+    while (h.lanes < 64 && 2 * h.lanes * h.span <= NT)
+        h.lanes *= 2;
+    const int64_t rows = h.fold ? NT / 64 : h.teams;
+    q.lds = 8 * (h.span + rows * h.cols * GROUP / (op == POSEIDON_GROUP_NORM_FORWARD ? h.piece : 1));
+    if (q.lds <= MOST_LDS && h.work <= (int64_t(1) << 22) - XCDS)
+        q.shape = shape;
+    return q;
+}
+
+// Of the workgroups of whole groups that hold their share of a sample: the widest
+// (rows of up to 512 bytes) that still give every CU one, else the narrowest; of the
+// shapes for it, the first that fits.  What is left to three launches, us held and in
+// three: rows below 64 bytes, which share memory lines with other workgroups, in more
+// than one round of workgroups (backward, bf16, 32 x 3136 x 256 in rows of 16 bytes
+// 93, 60); workgroups that fill a CU's registers, which load and store in turn, but
+// for one round of them over half of the chip or more (forward, 4 x 12544 x 128 on 64
+// CUs 36, 21, 32 x 3136 x 256 on 256 30, 38; backward, 2 x 1024 x 320 on 16 CUs 20,
+// 15, 16 x 3136 x 256 on 256 28, 37); those that fill half of them on fewer than 64
+// CUs (forward, 40 x 900 x 57 on 40 CUs 21, 16).
+Choice choose(int op, int64_t N, int64_t L, int64_t C, int64_t groups, int32_t dtype)
+{
+    const int64_t all = ceil_div(C, GROUP), D = C / groups, bytes = dtype == POSEIDON_BF16 ? 2 : 4;
+    const int64_t unit = C % GROUP ? all : D / gcd(D, GROUP);   // columns of whole groups
+    const int maps = op == POSEIDON_GROUP_NORM_FORWARD ? 1 : 2;
+    Choice best;
+    for (int64_t cols = unit; cols <= all && cols <= 512; cols += unit) {
+        if (all % cols)
+            continue;
+        const int64_t work = N * (all / cols), wide = cols * GROUP * bytes;
+        if (best.shape >= 0 && (work < 256 || wide > 512))
+            break;
+        if (wide < 64 && cols < all && work > 256)
+            continue;
+        for (int shape = 0; shape < SHAPES; ++shape) {
+            const int64_t held = SHAPE_NT[shape] * SHAPE_K[shape] * GROUP * bytes * maps;   // bytes
+            if (held > MOST_HELD || (held > MOST_HELD / 2 && (work < 128 || work > 256)) ||
+                (held > MOST_HELD / 4 && work < 64))
+                continue;
+            const Choice q = held_as(op, N, L, C, groups, shape, cols);
+            if (q.shape >= 0) {
+                best = q;
+                break;
+            }
+        }
+    }
+    return best;
+}
+
+unsigned held_grid(const Map& h) { return static_cast<unsigned>(ceil_div(h.work, XCDS) * XCDS); }
 
 // Within a launch's limit of 2^32 threads: the kernels walk what is over.
 unsigned grid_for(int64_t work) { return static_cast<unsigned>(std::min<int64_t>(work, 1 << 20)); }
 
-int64_t partial_bytes(const Cut& c) { return c.N * c.chunks * c.C * static_cast<int64_t>(sizeof(Pair)); }
+template <typename T>
+constexpr int32_t type_of()
+{
+    return sizeof(T) == 2 ? POSEIDON_BF16 : POSEIDON_F32;
+}
 
 template <typename F>
 void with_act(int32_t act, F&& f)
@@ -426,75 +1140,114 @@ void with_act(int32_t act, F&& f)
 }
 
 template <typename T>
-hipError_t forward_typed(const Cut& c, const T* x, const float* gamma, const float* beta, float eps, int32_t act, T* y,
-                         float* mean, float* rstd, void* ws, hipStream_t s)
+hipError_t forward_typed(int64_t N, int64_t L, int64_t C, int64_t groups, const T* x, const float* gamma,
+                         const float* beta, float eps, int32_t act, T* y, float* mean, float* rstd, void* ws,
+                         hipStream_t s)
 {
-    const int64_t work = workgroups(c);
+    const Choice q = choose(POSEIDON_GROUP_NORM_FORWARD, N, L, C, groups, type_of<T>());
+    if (q.shape >= 0)
+        return with_shape(q.shape, [&](auto shape) {
+            with_act(act, [&](auto a) {
+                constexpr int NT = decltype(shape)::NT, K = decltype(shape)::K;
+                if constexpr (shape_fits(K, sizeof(T), 1))
+                    held_forward_kernel<T, decltype(a)::value, NT, K><<<held_grid(q.h), NT, q.lds, s>>>(
+                        x, gamma, beta, q.h, eps, y, mean, rstd);
+            });
+            return hipGetLastError();
+        });
+    const Map h = cut(N, L, C, groups);
     Pair* partial = static_cast<Pair*>(ws);
-    chunk_stats_kernel<T><<<grid_for(work), c.threads, 0, s>>>(x, c, work, partial);
+    chunk_stats_kernel<T><<<grid_for(h.work), h.threads, 0, s>>>(x, h, partial);
     hipError_t rc = hipGetLastError();
     if (rc != hipSuccess)
         return rc;
-    group_stats_kernel<<<grid_for(c.N * c.groups), SUM_THREADS, 0, s>>>(partial, c, eps, mean, rstd);
+    const int64_t pairs = h.chunks * h.D, all = N * groups;
+    auto stats = [&](auto* kernel, int team) {
+        kernel<<<grid_for(ceil_div(all, SUM_THREADS / team)), SUM_THREADS, 0, s>>>(partial, h, eps, mean, rstd);
+    };
+    if (pairs <= 64 * 2)
+        stats(group_stats_kernel<64, 2>, 64);
+    else if (pairs <= 64 * 8)
+        stats(group_stats_kernel<64, 8>, 64);
+    else if (pairs <= SUM_THREADS * 8)
+        stats(group_stats_kernel<SUM_THREADS, 8>, SUM_THREADS);
+    else
+        stats(group_stats_kernel<SUM_THREADS, 0>, SUM_THREADS);
     rc = hipGetLastError();
     if (rc != hipSuccess)
         return rc;
     with_act(act, [&](auto a) {
-        forward_kernel<T, decltype(a)::value><<<grid_for(work), c.threads, 0, s>>>(x, gamma, beta, c, work, mean, rstd,
-                                                                                   y);
+        forward_kernel<T, decltype(a)::value><<<grid_for(h.work), h.threads, 0, s>>>(x, Inputs{gamma, beta, mean, rstd},
+                                                                                     h, y);
     });
     return hipGetLastError();
 }
 
 template <typename T>
-hipError_t backward_typed(const Cut& c, const T* dy, const T* x, const float* gamma, const float* beta,
-                          const float* mean, const float* rstd, int32_t act, T* dx, float* dgamma, float* dbeta,
-                          void* ws, hipStream_t s)
+hipError_t backward_typed(int64_t N, int64_t L, int64_t C, int64_t groups, const T* dy, const T* x, const Inputs& in,
+                          int32_t act, T* dx, float* dgamma, float* dbeta, void* ws, hipStream_t s)
 {
-    const int64_t work = workgroups(c);
-    Pair* partial = static_cast<Pair*>(ws);
-    Pair* averages = partial + c.N * c.chunks * c.C;
+    Pair* const totals = static_cast<Pair*>(ws);
+    const Choice q = choose(POSEIDON_GROUP_NORM_BACKWARD, N, L, C, groups, type_of<T>());
     hipError_t rc = hipSuccess;
-    if (work > 0) {
+    if (N > 0 && q.shape >= 0) {
+        rc = with_shape(q.shape, [&](auto shape) {
+            with_act(act, [&](auto a) {
+                constexpr int NT = decltype(shape)::NT, K = decltype(shape)::K;
+                if constexpr (shape_fits(K, sizeof(T), 2))
+                    held_backward_kernel<T, decltype(a)::value, NT, K><<<held_grid(q.h), NT, q.lds, s>>>(
+                        dy, x, in, q.h, dx, totals, dgamma, dbeta);
+            });
+            return hipGetLastError();
+        });
+        if (rc != hipSuccess || N == 1)
+            return rc;
+    } else if (N > 0) {
+        const Map h = cut(N, L, C, groups);
+        Pair* const averages = totals + N * C;
+        Pair* const partial = averages + N * groups;
         with_act(act, [&](auto a) {
-            chunk_sums_kernel<T, decltype(a)::value><<<grid_for(work), c.threads, 0, s>>>(dy, x, gamma, beta, c, work,
-                                                                                          mean, rstd, partial);
+            chunk_sums_kernel<T, decltype(a)::value><<<grid_for(h.work), h.threads, 0, s>>>(dy, x, in, h, partial);
+        });
+        rc = hipGetLastError();
+        if (rc != hipSuccess)
+            return rc;
+        join_sums_kernel<<<grid_for(N * groups), SUM_THREADS, 0, s>>>(partial, h, in.gamma, totals, averages);
+        rc = hipGetLastError();
+        if (rc != hipSuccess)
+            return rc;
+        with_act(act, [&](auto a) {
+            backward_kernel<T, decltype(a)::value><<<grid_for(h.work), h.threads, 0, s>>>(dy, x, in, h, averages, dx);
         });
         rc = hipGetLastError();
         if (rc != hipSuccess)
             return rc;
     }
-    join_sums_kernel<<<grid_for(c.N * c.groups + ceil_div(c.C, SUM_COLS)), SUM_THREADS, 0, s>>>(partial, c, gamma,
-                                                                                                 averages, dgamma,
-                                                                                                 dbeta);
-    rc = hipGetLastError();
-    if (rc != hipSuccess || work == 0)
-        return rc;
-    with_act(act, [&](auto a) {
-        backward_kernel<T, decltype(a)::value><<<grid_for(work), c.threads, 0, s>>>(dy, x, gamma, beta, c, work, mean,
-                                                                                    rstd, averages, dx);
-    });
+    weights_kernel<<<static_cast<unsigned>(ceil_div(C, SUM_COLS)), SUM_THREADS, 0, s>>>(totals, N, C, dgamma, dbeta);
     return hipGetLastError();
 }
 
 }  // namespace
 
-int64_t group_norm_workspace(int32_t op, int64_t N, int64_t L, int64_t C, int64_t groups, int32_t)
+int64_t group_norm_workspace(int32_t op, int64_t N, int64_t L, int64_t C, int64_t groups, int32_t dtype)
 {
-    const Cut c = make_cut(N, L, C, groups);
-    return partial_bytes(c) + (op == POSEIDON_GROUP_NORM_BACKWARD ? N * groups * static_cast<int64_t>(sizeof(Pair)) : 0);
+    const bool backward = op == POSEIDON_GROUP_NORM_BACKWARD;
+    const int64_t totals = backward && N > 1 ? N * C : 0;
+    if (choose(op, N, L, C, groups, dtype).shape >= 0)
+        return totals * static_cast<int64_t>(sizeof(Pair));
+    const Map h = cut(N, L, C, groups);
+    return (N * h.chunks * C + (backward ? N * C + N * groups : 0)) * static_cast<int64_t>(sizeof(Pair));
 }
 
 hipError_t launch_group_norm_forward(const void* x, const float* gamma, const float* beta, int64_t N, int64_t L,
                                      int64_t C, int64_t groups, int32_t dtype, float eps, int32_t act, void* y,
                                      float* mean, float* rstd, void* ws, hipStream_t stream)
 {
-    const Cut c = make_cut(N, L, C, groups);
     if (dtype == POSEIDON_BF16)
-        return forward_typed(c, static_cast<const __bf16*>(x), gamma, beta, eps, act, static_cast<__bf16*>(y), mean,
-                             rstd, ws, stream);
-    return forward_typed(c, static_cast<const float*>(x), gamma, beta, eps, act, static_cast<float*>(y), mean, rstd,
-                         ws, stream);
+        return forward_typed(N, L, C, groups, static_cast<const __bf16*>(x), gamma, beta, eps, act,
+                             static_cast<__bf16*>(y), mean, rstd, ws, stream);
+    return forward_typed(N, L, C, groups, static_cast<const float*>(x), gamma, beta, eps, act, static_cast<float*>(y),
+                         mean, rstd, ws, stream);
 }
 
 hipError_t launch_group_norm_backward(const void* dy, const void* x, const float* gamma, const float* beta,
@@ -502,12 +1255,12 @@ hipError_t launch_group_norm_backward(const void* dy, const void* x, const float
                                       int64_t groups, int32_t dtype, int32_t act, void* dx, float* dgamma,
                                       float* dbeta, void* ws, hipStream_t stream)
 {
-    const Cut c = make_cut(N, L, C, groups);
+    const Inputs in{gamma, beta, mean, rstd};
     if (dtype == POSEIDON_BF16)
-        return backward_typed(c, static_cast<const __bf16*>(dy), static_cast<const __bf16*>(x), gamma, beta, mean,
-                              rstd, act, static_cast<__bf16*>(dx), dgamma, dbeta, ws, stream);
-    return backward_typed(c, static_cast<const float*>(dy), static_cast<const float*>(x), gamma, beta, mean, rstd,
-                          act, static_cast<float*>(dx), dgamma, dbeta, ws, stream);
+        return backward_typed(N, L, C, groups, static_cast<const __bf16*>(dy), static_cast<const __bf16*>(x), in, act,
+                              static_cast<__bf16*>(dx), dgamma, dbeta, ws, stream);
+    return backward_typed(N, L, C, groups, static_cast<const float*>(dy), static_cast<const float*>(x), in, act,
+                          static_cast<float*>(dx), dgamma, dbeta, ws, stream);
 }
 
 }  // namespace poseidon
