@@ -49,24 +49,27 @@ def test_workspace():
 def test_forward_refusals():
     for kw in WRONG + ({"eps": -1.0}, {"eps": NAN}, {"act": 3}, {"act": -1}, {"x": None}, {"gamma": None},
                        {"beta": None}, {"y": None}, {"mean": None}, {"rstd": None}, {"y": A}, {"y": B}, {"mean": C},
-                       {"rstd": E}, {"mean": D}, {"ws": D}, {"ws": A}):
+                       {"rstd": E}, {"mean": D}):
         assert fwd(**kw) == BAD, kw
-    need = size_of(L.GROUP_NORM_FORWARD, N=40, L_=5000)[1]
+    big = {"N": 40, "L_": 50000}
+    need = size_of(L.GROUP_NORM_FORWARD, **big)[1]
     assert need > 0
-    for kw in ({"ws": None}, {"ws": ctypes.c_void_p(0x7000008)}, {"bytes": need - 1}):
-        assert fwd(N=40, L_=5000, y=ctypes.c_void_p(0x40000000), x=ctypes.c_void_p(0x80000000), **{"bytes": need, **kw}) == BAD, kw
+    x, y = ctypes.c_void_p(0x80000000), ctypes.c_void_p(0x180000000)
+    for kw in ({"ws": None}, {"ws": ctypes.c_void_p(0x7000008)}, {"bytes": need - 1}, {"ws": x}, {"ws": y}, {"ws": E}):
+        assert fwd(**{**big, "x": x, "y": y, "bytes": need, **kw}) == BAD, kw
     assert fwd(x=None, gamma=None, beta=None, y=None, mean=None, rstd=None, ws=None, N=0) == L.OK
 
 
 def test_backward_refusals():
     for kw in WRONG + ({"act": 3}, {"dy": None}, {"x": None}, {"gamma": None}, {"beta": None}, {"mean": None},
                        {"rstd": None}, {"dx": None}, {"dgamma": None}, {"dbeta": None}, {"dx": A}, {"dx": H},
-                       {"dgamma": J}, {"dgamma": B}, {"dbeta": E}, {"dbeta": D}, {"ws": I}, {"ws": H}):
+                       {"dgamma": J}, {"dgamma": B}, {"dbeta": E}, {"dbeta": D}):
         assert bwd(**kw) == BAD, kw
-    need = size_of(L.GROUP_NORM_BACKWARD, N=40, L_=5000)[1]
-    big = {"dy": ctypes.c_void_p(0x40000000), "x": ctypes.c_void_p(0x80000000), "dx": ctypes.c_void_p(0xc0000000)}
-    for kw in ({"ws": None}, {"ws": ctypes.c_void_p(0x7000008)}, {"bytes": need - 1}):
-        assert bwd(N=40, L_=5000, **big, **{"bytes": need, **kw}) == BAD, kw
+    need = size_of(L.GROUP_NORM_BACKWARD, N=40, L_=50000)[1]
+    dy, x, dx = (ctypes.c_void_p(0x100000000 * k) for k in (1, 2, 3))
+    big = {"N": 40, "L_": 50000, "dy": dy, "x": x, "dx": dx}
+    for kw in ({"ws": None}, {"ws": ctypes.c_void_p(0x7000008)}, {"bytes": need - 1}, {"ws": dy}, {"ws": dx}, {"ws": I}):
+        assert bwd(**{**big, "bytes": need, **kw}) == BAD, kw
 
 
 def test_the_binding_refuses():
