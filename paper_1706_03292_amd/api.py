@@ -964,6 +964,7 @@ class AdamW:
         _check("poseidon_adamw_workspace", L.lib().poseidon_adamw_workspace(self._h, ctypes.byref(size)))
         self._ws_bytes = size.value
         self._rule = L.PoseidonAdamwRule(0.0, *self.betas, self.eps, 1, None, None, None, 0, 0)
+        self._sizes = [keep[0].numel() for keep in self._keep]
         self._kept_uses = _KeptUses([x for keep in self._keep for x in keep])
 
     @staticmethod
@@ -1037,11 +1038,15 @@ class AdamW:
                 out = [(torch.empty_like(k[0]), torch.empty_like(k[0])) for k in self._keep]
             if len(out) != len(self._keep):
                 raise ValueError(f"out needs one pair for each of the {len(self._keep)} tensors")
-            for i, (pair, k) in enumerate(zip(out, self._keep)):
-                for name, x in zip(("m", "v"), pair):
-                    if x is not None:
-                        _sized(i, name, x, torch.float32, dev, k[0].numel())
-            ptrs = [(ctypes.c_void_p * max(1, len(out)))(*[_ptr(pair[j]) for pair in out]) for j in (0, 1)]
+            ptrs = [(ctypes.c_void_p * max(1, len(out)))() for _ in range(2)]
+            for i, (pair, n) in enumerate(zip(out, self._sizes)):
+                for arr, name, x in zip(ptrs, ("m", "v"), pair):
+                    if x is None:
+                        continue
+                    if not (isinstance(x, torch.Tensor) and x.dtype is torch.float32 and x.get_device() == dev
+                            and x.numel() == n and x.is_contiguous()):
+                        _sized(i, name, x, torch.float32, dev, n)
+                    arr[i] = x.data_ptr()
             if stream is not None:
                 self._kept_uses(stream)
                 _uses(stream, *[x for pair in out for x in pair])

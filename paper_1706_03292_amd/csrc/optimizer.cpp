@@ -12,9 +12,9 @@ struct poseidon_adamw {
     std::vector<poseidon_adamw_tensor> tensors;   // all of them, the empty ones too
     std::vector<int64_t> first_group;
     std::vector<poseidon::Span> reads, writes;    // of all calls, sorted and disjoint
-    // what a step launches: fp32 and coded moments, from the shards and from the sums
-    std::vector<poseidon::AdamwGroup> plain, coded, plain_sums, coded_sums;
-    std::vector<poseidon::AdamwGroup> squares;    // what a clip launches
+    // what a step launches from the shards and from the sums, by kind (kind_of)
+    std::vector<poseidon::AdamwGroup> steps[4], sum_steps[4];
+    std::vector<poseidon::AdamwGroup> squares[2]; // what a clip launches: several rows of gradients, one
     int64_t chunk = 0;                            // values of a clip's workgroup
     int64_t parts = 0;                            // its workgroups
     int32_t dtype = 0;
@@ -26,9 +26,10 @@ namespace {
 
 constexpr int64_t MOST_VALUES = int64_t(1) << 34, MOST_STRIDE = int64_t(1) << 56;
 constexpr int32_t MOST_WORKERS = 1024;
-// Workgroups of a clip: eight a CU, enough loads in flight, few enough partial
-// sums that adding them costs little.
-constexpr int64_t CLIP_BLOCKS = 2048;
+// Workgroups of a clip: enough loads in flight, few enough partial sums that adding
+// them costs little (VGG19-22K's 229M values, fp32: 2048 of them 177 us, 4096 154, 8192
+// 142, 32768 148).
+constexpr int64_t CLIP_BLOCKS = 8192;
 
 int64_t value_size(int32_t dtype) { return dtype == POSEIDON_BF16 ? 2 : 4; }
 int64_t blocks_of(int64_t n, int64_t chunk) { return (n + chunk - 1) / chunk; }
@@ -49,7 +50,10 @@ void add(std::vector<AdamwGroup>& to, const AdamwItem& item, int64_t chunk)
     const int64_t blocks = blocks_of(item.n, chunk);
     if (to.empty() || to.back().count == ADAMW_GROUP || to.back().blocks + blocks > ADAMW_MOST_BLOCKS) {
         to.emplace_back();
-        to.back().count = to.back().blocks = 0;
+        AdamwGroup& g = to.back();
+        g.count = g.blocks = 0;
+        g.chunk = chunk;
+        std::fill(g.first_block, g.first_block + ADAMW_GROUP, INT32_MAX);
     }
     AdamwGroup& g = to.back();
     g.first_block[g.count] = g.blocks;
@@ -76,6 +80,9 @@ void merge(std::vector<Span>& v)
     }
     v.resize(n);
 }
+
+// A step's launches by what their tensors have in common.
+int kind_of(const poseidon_adamw_tensor& t, bool one) { return 2 * (t.exponents != nullptr) + one; }
 
 // Whether [p, p + bytes) meets one of the sorted, disjoint ranges.
 bool meets(const std::vector<Span>& sorted, const void* p, int64_t bytes)
@@ -117,23 +124,22 @@ int create(const poseidon_adamw_tensor* tensors, int32_t count, int32_t dtype, p
         return POSEIDON_ERR_INVALID_ARG;
     merge(o.writes);
     merge(o.reads);
-    const int64_t share = blocks_of(total, CLIP_BLOCKS);
-    o.chunk = std::max<int64_t>(1, blocks_of(share, ADAMW_CHUNK)) * ADAMW_CHUNK;
+    o.chunk = std::max<int64_t>(1, blocks_of(blocks_of(total, CLIP_BLOCKS), ADAMW_CHUNK)) * ADAMW_CHUNK;
     for (int32_t i = 0; i < count; ++i) {
         const poseidon_adamw_tensor& t = tensors[i];
         if (t.n == 0)
             continue;
         AdamwItem item = item_of(t, o.first_group[i]);
-        add(t.exponents ? o.coded : o.plain, item, ADAMW_CHUNK);
+        add(o.steps[kind_of(t, t.P == 1)], item, ADAMW_CHUNK);
         AdamwItem square = item;
         square.copy = t.sum;
-        add(o.squares, square, o.chunk);
+        add(o.squares[t.P == 1], square, o.chunk);
         o.parts += blocks_of(t.n, o.chunk);
         if (o.sums) {
             item.G = t.sum;
             item.stride = 0;
             item.P = 1;
-            add(t.exponents ? o.coded_sums : o.plain_sums, item, ADAMW_CHUNK);
+            add(o.sum_steps[kind_of(t, true)], item, ADAMW_CHUNK);
         }
     }
     return POSEIDON_OK;
@@ -142,14 +148,10 @@ int create(const poseidon_adamw_tensor* tensors, int32_t count, int32_t dtype, p
 int step(const poseidon_adamw& o, const poseidon_adamw_rule& r, hipStream_t stream)
 {
     const int32_t dtype = r.from_sums ? POSEIDON_F32 : o.dtype;
-    for (int coded = 0; coded < 2; ++coded) {
-        const auto& groups = coded ? (r.from_sums ? o.coded_sums : o.coded) : (r.from_sums ? o.plain_sums : o.plain);
-        for (const AdamwGroup& g : groups) {
-            const hipError_t rc = launch_adamw_step(g, dtype, coded != 0, r, stream);
-            if (rc != hipSuccess)
+    for (int kind = 0; kind < 4; ++kind)
+        for (const AdamwGroup& g : (r.from_sums ? o.sum_steps : o.steps)[kind])
+            if (launch_adamw_step(g, dtype, AdamwKind{(kind & 2) != 0, (kind & 1) != 0}, r, stream) != hipSuccess)
                 return POSEIDON_ERR_HIP;
-        }
-    }
     return POSEIDON_OK;
 }
 
@@ -263,11 +265,11 @@ extern "C" int poseidon_adamw_clip(const poseidon_adamw* optimizer, double max_n
         meets(o.writes, workspace, needed) || meets(o.reads, workspace, needed))
         return POSEIDON_ERR_INVALID_ARG;
     double* partial = static_cast<double*>(workspace);
-    for (const AdamwGroup& g : o.squares) {
-        const hipError_t rc = launch_adamw_squares(g, o.dtype, o.chunk, partial, stream);
-        if (rc != hipSuccess)
-            return POSEIDON_ERR_HIP;
-        partial += g.blocks;
-    }
+    for (int one = 0; one < 2; ++one)
+        for (const AdamwGroup& g : o.squares[one]) {
+            if (launch_adamw_squares(g, o.dtype, one != 0, partial, stream) != hipSuccess)
+                return POSEIDON_ERR_HIP;
+            partial += g.blocks;
+        }
     return status(launch_adamw_norm(static_cast<const double*>(workspace), o.parts, max_norm, result, stream));
 }

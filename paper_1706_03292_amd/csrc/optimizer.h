@@ -26,24 +26,32 @@ struct AdamwItem {
 // owns the workgroups [first_block[t], first_block[t+1]), `chunk` values each.
 constexpr int ADAMW_GROUP = 40;
 struct AdamwGroup {
-    int32_t first_block[ADAMW_GROUP];
+    int32_t first_block[ADAMW_GROUP];   // past the last tensor: INT32_MAX
     AdamwItem item[ADAMW_GROUP];
+    int64_t chunk;                      // a multiple of ADAMW_CHUNK
     int32_t count;
     int32_t blocks;
 };
+static_assert(ADAMW_GROUP % 8 == 0, "read eight by eight");
 static_assert(sizeof(AdamwGroup) <= 4000, "kernel arguments");
 
-// Values that a workgroup of the step (and of values) works on.
+// Values of a workgroup's turn.  A step's workgroup has one turn: with four, VGG19-22K's
+// 229M values take 1282 us against 1244 (fp32 moments), 687 against 654 (8 bits).
 constexpr int64_t ADAMW_CHUNK = 2048;
 constexpr int64_t ADAMW_MOST_BLOCKS = int64_t(1) << 23;   // of a launch: 2^31 threads
 
-// Kinds of arrays that a group's tensors have.
-hipError_t launch_adamw_step(const AdamwGroup& group, int32_t dtype, bool coded, const poseidon_adamw_rule& rule,
+// What a launch's tensors have in common for the step: 8-bit moments, one row of
+// gradients.
+struct AdamwKind {
+    bool coded, one;
+};
+
+hipError_t launch_adamw_step(const AdamwGroup& group, int32_t dtype, AdamwKind kind, const poseidon_adamw_rule& rule,
                              hipStream_t stream);
 hipError_t launch_adamw_values(const AdamwGroup& group, hipStream_t stream);
 // Sums of squares, one of each workgroup, to partial[0 .. group.blocks).
-hipError_t launch_adamw_squares(const AdamwGroup& group, int32_t dtype, int64_t chunk, double* partial,
-                                hipStream_t stream);
+// (`one`: one row of gradients each)
+hipError_t launch_adamw_squares(const AdamwGroup& group, int32_t dtype, bool one, double* partial, hipStream_t stream);
 hipError_t launch_adamw_norm(const double* partial, int64_t parts, double max_norm, float* result,
                              hipStream_t stream);
 
