@@ -903,31 +903,30 @@ __global__ __launch_bounds__(SUM_THREADS) void join_sums_kernel(const Pair* __re
     }
 }
 
-// dgamma and dbeta from the samples' totals, SUM_COLS channels a workgroup.
+// dgamma and dbeta from the samples' totals, SUM_COLS channels a workgroup of
+// `threads` (64 at least; lds: a pair for each).
 constexpr int SUM_COLS = 16;
 
 __device__ __forceinline__ void sum_samples(const Pair* __restrict__ totals, int64_t N, int64_t C, int64_t first,
-                                            double* lds, float* __restrict__ dgamma, float* __restrict__ dbeta)
+                                            int threads, double* lds, float* __restrict__ dgamma,
+                                            float* __restrict__ dbeta)
 {
-    constexpr int SLICES = SUM_THREADS / SUM_COLS;
+    const int slices = threads / SUM_COLS;
     const int lane = threadIdx.x % SUM_COLS, w = threadIdx.x / SUM_COLS;
     const int64_t channel = first + lane;
     double s1 = 0.0, s2 = 0.0;
-    if (w < SLICES && channel < C)
+    if (channel < C)
 #pragma unroll 4
-        for (int64_t i = w; i < N; i += SLICES) {
+        for (int64_t i = w; i < N; i += slices) {
             const Pair p = totals[i * C + channel];
             s1 += p.a;
             s2 += p.b;
         }
-    __syncthreads();
-    if (w < SLICES) {
-        lds[threadIdx.x * 2] = s1;
-        lds[threadIdx.x * 2 + 1] = s2;
-    }
+    lds[threadIdx.x * 2] = s1;
+    lds[threadIdx.x * 2 + 1] = s2;
     __syncthreads();
     if (w == 0 && channel < C) {
-        for (int i = 1; i < SLICES; ++i) {
+        for (int i = 1; i < slices; ++i) {
             s1 += lds[(i * SUM_COLS + lane) * 2];
             s2 += lds[(i * SUM_COLS + lane) * 2 + 1];
         }
@@ -940,15 +939,22 @@ __global__ __launch_bounds__(SUM_THREADS) void weights_kernel(const Pair* __rest
                                                               float* __restrict__ dgamma, float* __restrict__ dbeta)
 {
     __shared__ double lds[SUM_THREADS * 2];
-    sum_samples(totals, N, C, static_cast<int64_t>(blockIdx.x) * SUM_COLS, lds, dgamma, dbeta);
+    sum_samples(totals, N, C, static_cast<int64_t>(blockIdx.x) * SUM_COLS, SUM_THREADS, lds, dgamma, dbeta);
 }
 
 template <typename T, int ACT>
 __global__ __launch_bounds__(MOST_THREADS) void backward_kernel(const T* __restrict__ dy, const T* __restrict__ x,
                                                                 Inputs in, Map h, const Pair* __restrict__ averages,
-                                                                T* __restrict__ dx)
+                                                                T* __restrict__ dx, const Pair* __restrict__ totals,
+                                                                float* __restrict__ dgamma, float* __restrict__ dbeta,
+                                                                unsigned sums)
 {
-    for (int64_t b = blockIdx.x; b < h.work; b += gridDim.x) {
+    __shared__ double lds[MOST_THREADS * 2];
+    if (blockIdx.x < sums) {   // the first workgroups, not the last: theirs is a chain of loads
+        sum_samples(totals, h.N, h.C, static_cast<int64_t>(blockIdx.x) * SUM_COLS, h.threads, lds, dgamma, dbeta);
+        return;
+    }
+    for (int64_t b = blockIdx.x - sums; b < h.work; b += gridDim.x - sums) {
         const Spot s = spot_of(h, h.work - 1 - b);   // last read, first read again
         if (!s.active)
             continue;
@@ -1216,12 +1222,12 @@ hipError_t backward_typed(int64_t N, int64_t L, int64_t C, int64_t groups, const
         rc = hipGetLastError();
         if (rc != hipSuccess)
             return rc;
+        const unsigned sums = static_cast<unsigned>(ceil_div(C, SUM_COLS));
         with_act(act, [&](auto a) {
-            backward_kernel<T, decltype(a)::value><<<grid_for(h.work), h.threads, 0, s>>>(dy, x, in, h, averages, dx);
+            backward_kernel<T, decltype(a)::value><<<sums + grid_for(h.work), h.threads, 0, s>>>(
+                dy, x, in, h, averages, dx, totals, dgamma, dbeta, sums);
         });
-        rc = hipGetLastError();
-        if (rc != hipSuccess)
-            return rc;
+        return hipGetLastError();
     }
     weights_kernel<<<static_cast<unsigned>(ceil_div(C, SUM_COLS)), SUM_THREADS, 0, s>>>(totals, N, C, dgamma, dbeta);
     return hipGetLastError();
