@@ -6,12 +6,16 @@ pass), then the classifier with its softmax cross entropy.  The backward pass
 leaves its results where the synchronisation reads them: the normalisation's
 gradients in the workers' dense shards, the classifier's -- by Alg. 1's choice
 for its size -- either as this worker's rows of the sufficient factors or as its
-dense shard.  One ``SyncIteration`` then updates gamma, beta and the classifier.
+dense shard.  One ``SyncIteration`` then updates gamma, beta and the classifier by
+momentum SGD; or, asked for, one clipped AdamW step does, from the same payloads
+(factors rebuilt to the dense gradient first).
 
 ``python -m paper_1706_03292_amd.network_end`` trains it on drawn data and
 prints the loss of every tenth step.
 """
 from __future__ import annotations
+
+import argparse
 
 import torch
 
@@ -22,10 +26,13 @@ class NetworkEnd:
     """Dropout, residual, layer norm and classifier over ``features`` features
     and ``classes`` classes, trained by P workers of B rows each.  Parameters
     are fp32; with ``dtype`` bfloat16 the activations are bf16 and each step
-    works on a bf16 copy of the classifier."""
+    works on a bf16 copy of the classifier.  ``adamw`` (a dict, maybe empty)
+    trains it by AdamW instead of momentum SGD: ``betas``, ``eps``,
+    ``weight_decay`` (of the classifier), ``max_norm`` (of the gradient) and
+    ``bits`` (of the classifier's moments, 32 or 8)."""
 
     def __init__(self, classes: int, features: int, B: int, P: int, lr: float, momentum: float = 0.9, p: float = 0.1,
-                 dtype: torch.dtype = torch.float32, seed: int = 0, device=None):
+                 dtype: torch.dtype = torch.float32, seed: int = 0, device=None, adamw: dict | None = None):
         dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
         gen = torch.Generator(device=dev).manual_seed(seed)
         self.B, self.P, self.p, self.dtype = B, P, p, dtype
@@ -37,18 +44,45 @@ class NetworkEnd:
         empty = lambda *shape: torch.empty(shape, device=dev)  # noqa: E731
         zeros_like = torch.zeros_like
         self.dgamma, self.dbeta = empty(P, features), empty(P, features)
-        fc = {"fc": True, "W": self.W, "buf": zeros_like(self.W)}
+        self.lr, self.steps = lr, 0
         if self.scheme == api.SFB:
             self.U, self.V = empty(P * B, classes), empty(P * B, features)
-            fc.update(U=self.U, V=self.V)
         else:
             self.dW = empty(P, classes, features)
-            fc.update(shards=self.dW)
+        self.optimizer = self.pool = self.copy = None
+        if adamw is not None:
+            self._make_adamw(**adamw)
+            return
+        fc = {"fc": True, "W": self.W, "buf": zeros_like(self.W)}
+        fc.update({"U": self.U, "V": self.V} if self.scheme == api.SFB else {"shards": self.dW})
         self.pool = api.StreamPool(2, device=dev)
         self.sync = api.SyncIteration(
             self.pool, [{"fc": False, "W": self.gamma, "shards": self.dgamma, "buf": zeros_like(self.gamma)},
                         {"fc": False, "W": self.beta, "shards": self.dbeta, "buf": zeros_like(self.beta)}, fc],
             B, P, lr, momentum)
+
+    def _make_adamw(self, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0,
+                    max_norm: float = float("inf"), bits: int = 32) -> None:
+        self.max_norm = max_norm
+        # the classifier's gradient: the workers' shards, or the one rebuilt from their factors
+        self.rebuilt = torch.empty_like(self.W) if self.scheme == api.SFB else None
+        fc = {"W": self.W, "shards": self.dW if self.rebuilt is None else self.rebuilt[None],
+              "weight_decay": weight_decay, **api.AdamW.moments(self.W, bits)}
+        if self.dtype != torch.float32:
+            self.copy = fc["copy"] = self.W.to(self.dtype)
+        self.optimizer = api.AdamW(
+            [{"W": self.gamma, "shards": self.dgamma, **api.AdamW.moments(self.gamma)},
+             {"W": self.beta, "shards": self.dbeta, **api.AdamW.moments(self.beta)}, fc], betas, eps)
+        self.round_rng = self.rng[0].clone()   # of the 8-bit moments' rounding
+        self.round_rng[0] += self.P
+
+    def _adamw_step(self) -> None:
+        if self.rebuilt is not None:
+            self.rebuilt.zero_()
+            api.sf_apply(self.rebuilt, self.U, self.V, -1.0)   # 0 + U^T V
+        norm = self.optimizer.clip(self.max_norm)
+        self.optimizer.step(self.lr, self.steps, scale=norm[1:2], rng=self.round_rng)
+        self.round_rng[1] += 1
 
     def worker_step(self, w: int, x: torch.Tensor, residual: torch.Tensor, target: torch.Tensor,
                     dloss: torch.Tensor, W: torch.Tensor):
@@ -76,23 +110,33 @@ class NetworkEnd:
         # factors multiply those with the rows' values.
         x, residual = (torch.where(valid[:, None], v, torch.zeros_like(v)) for v in (x, residual))
         dloss = valid.float() / valid.sum().clamp(min=1)
-        W = self.W if self.dtype == torch.float32 else self.W.to(self.dtype)
+        W = self.W if self.dtype == torch.float32 else self.W.to(self.dtype) if self.copy is None else self.copy
         out = []
         for w in range(self.P):
             r = slice(w * self.B, (w + 1) * self.B)
             out.append(self.worker_step(w, x[r], residual[r], target[r], dloss[r], W))
-        self.sync()
+        self.steps += 1
+        if self.optimizer is None:
+            self.sync()
+        else:
+            self._adamw_step()
         self.rng[:, 1] += 1
         loss, dx, dresidual = (torch.cat(t) for t in zip(*out))
         return (loss * dloss).sum(), dx, dresidual
 
     def close(self) -> None:
-        self.pool.close()
+        (self.pool or self.optimizer).close()
 
 
 def main() -> None:
+    parser = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
+    parser.add_argument("--optimizer", choices=("sgd", "adamw", "adamw8"), default="sgd",
+                        help="momentum SGD, or AdamW with the classifier's moments in 32 or 8 bits")
+    optimizer = parser.parse_args().optimizer
+    adamw = None if optimizer == "sgd" else {"bits": 8 if optimizer == "adamw8" else 32, "weight_decay": 0.01,
+                                             "max_norm": 1.0}
     classes, features, B, P = 1000, 512, 32, 4
-    end = NetworkEnd(classes, features, B, P, lr=0.5, dtype=torch.bfloat16)
+    end = NetworkEnd(classes, features, B, P, lr=0.5 if adamw is None else 0.01, dtype=torch.bfloat16, adamw=adamw)
     gen = torch.Generator(device="cuda").manual_seed(1)
     centre = torch.randn(classes, features, generator=gen, device="cuda")
     for i in range(101):
