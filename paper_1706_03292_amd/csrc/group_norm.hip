@@ -1086,8 +1086,10 @@ Choice held_as(int op, int64_t N, int64_t L, int64_t C, int64_t groups, int shap
 }
 
 // Of the workgroups of whole groups that hold their share of a sample: the widest
-// (rows of up to 512 bytes) that still give every CU one, else the narrowest; of the
-// shapes for it, the first that fits.  What is left to three launches, us held and in
+// (rows of up to 512 bytes, or longer ones where threads would have none) that still
+// give every CU one, else the narrowest; of the shapes for it, the first that fits
+// (8192 x 1 x 4096 bf16 forward, an eighth of a workgroup's threads at work in rows of
+// 512 bytes 742 us, all of them in rows of 4 KB 117).  What is left to three launches, us held and in
 // three: rows below 64 bytes, which share memory lines with other workgroups, in more
 // than one round of workgroups (backward, bf16, 32 x 3136 x 256 in rows of 16 bytes
 // 93, 60); workgroups that fill a CU's registers, which load and store in turn, but
@@ -1105,7 +1107,7 @@ Choice choose(int op, int64_t N, int64_t L, int64_t C, int64_t groups, int32_t d
         if (all % cols)
             continue;
         const int64_t work = N * (all / cols), wide = cols * GROUP * bytes;
-        if (best.shape >= 0 && (work < 256 || wide > 512))
+        if (best.shape >= 0 && (work < 256 || (wide > 512 && best.h.teams <= L)))
             break;
         if (wide < 64 && cols < all && work > 256)
             continue;

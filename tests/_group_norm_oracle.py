@@ -2,9 +2,12 @@
 fp32 arithmetic may add (no test functions here).
 
 Bounds count roundings: u = 2^-24 each, relative, and half a step of the result's
-type for the last.  A thread sums at most 64 values in fp32 before the sums are
-joined by their means, so `k` = min(L, 64) + 8 roundings bound a mean of differences
-from a pivot that is itself one of the group's values."""
+type for the last.  Forward, a thread sums at most 64 rows of differences from one of
+the group's values or from a first mean.  Those sums are joined by their means in 64
+bits, or in fp32 in at most 3 + 64 / piece + 6 steps (eight channels, the partial
+sums that one of 64 lanes adds up, the lanes), piece >= 1.  So `k` = min(L, 64) + 80
+roundings bound a mean of such differences.  Backward, fp32 sums have a thread's at
+most 64 rows, six shuffles and at most 256 teams of a workgroup."""
 import torch
 
 U32, U16 = 2.0 ** -24, 2.0 ** -8
@@ -43,7 +46,7 @@ def forward(x, gamma, beta, groups, eps, act, u):
     var = c.square().mean((1, 3), keepdim=True)
     rstd = (var + eps) ** -0.5
     most = c.abs().amax((1, 3), keepdim=True)
-    k = min(L, 64) + 8
+    k = min(L, 64) + 80
     # differences from the pivot: at most 2 most, their mean square var + most^2
     d_mean = k * U32 * 2 * most + 2 * U32 * mean.abs()
     d_rstd = 0.5 * (2 * k * U32 * (var + most.square()) + d_mean.square()) / (var + eps) + 2 * U32   # relative
@@ -75,8 +78,8 @@ def backward(dy, x, gamma, beta, mean, rstd, act, u):
     g = dz * w
     count = L * D
     a1, a2 = (x_.sum((1, 3), keepdim=True) / count for x_ in (g, g * n))
-    # a thread's rows, then its workgroup's up to 256 teams; the rest in 64 bits
-    k = min(L, 64) + min(L, 256) + 4
+    # (a sum with 0 rounds nothing: no more teams count than rows)
+    k = min(L, 64) + min(L, 256) + 8
     e1 = (w.abs() * (d_dz + k * U32 * dz.abs())).sum((1, 3), keepdim=True) / count + 2 * U32 * a1.abs()
     e2 = (w.abs() * (d_dz * n.abs() + dz.abs() * d_n + k * U32 * (dz * n).abs())).sum((1, 3), keepdim=True) / count \
         + 2 * U32 * a2.abs()

@@ -300,3 +300,62 @@ def test_a_map_past_32_bits():
             # 2^-8 of the result's rounding, and 300 roundings of averages below 1
             assert ((dx[n, rows] - want).abs() <= O.U16 * want.abs() + 1e-4).all()
             assert ((y[n, rows] - z.clamp(min=0)).abs() <= O.U16 * z.abs() + 1e-5).all()
+
+
+def launched(call):
+    """The group norm kernels that `call` launches: names, with the threads and rows
+    of those that hold a map."""
+    import re
+
+    from _helpers import whole_kernel_names
+    out = []
+    for name in whole_kernel_names(call):
+        m = re.search(r"(held_\w+?_kernel)<[^>]*?, (\d+), (\d+)>", name)
+        if m:
+            out.append((m[1], int(m[2]), int(m[3])))
+        else:
+            m = re.search(r"(chunk_stats|chunk_sums|group_stats|join_sums|forward|backward|weights)_kernel", name)
+            if m:
+                out.append(m[1])
+    return out
+
+
+# (sizes, workgroup that holds them): one for each shape and, last, none.
+FORWARD_BF16 = [((1, 49, 512, 32), (256, 2)), ((1, 400, 512, 32), (256, 4)), ((1, 900, 512, 32), (256, 8)),
+                ((1, 1800, 512, 32), (512, 8)), ((4, 3500, 512, 32), (512, 16)), ((4, 8000, 512, 32), (512, 32)),
+                ((1, 8000, 512, 32), None), ((1, 3000, 100, 1), None), ((64, 1, 4096, 32), (256, 2))]
+FORWARD_F32 = [((1, 49, 512, 32), (256, 2)), ((1, 400, 512, 32), (256, 4)), ((1, 900, 512, 32), (256, 8)),
+               ((2, 1800, 512, 32), (512, 8)), ((4, 3500, 512, 32), (512, 16)), ((5, 3500, 520, 65), None)]
+BACKWARD_BF16 = [((1, 49, 512, 32), (256, 2)), ((1, 400, 512, 32), (256, 4)), ((1, 900, 512, 32), (256, 8)),
+                 ((2, 1800, 512, 32), (512, 8)), ((4, 3500, 512, 32), (512, 16)), ((1, 3500, 512, 32), None),
+                 ((3, 33, 57, 19), (256, 2))]
+BACKWARD_F32 = [((1, 49, 512, 32), (256, 2)), ((1, 400, 512, 32), (256, 4)), ((2, 900, 512, 32), (256, 8)),
+                ((4, 1800, 512, 32), (512, 8)), ((1, 1800, 512, 32), None)]
+
+
+@gpu
+@pytest.mark.parametrize("op,dtype,sizes,held", [(op, dt, s, h) for op, dt, rows in (
+    ("forward", BF16, FORWARD_BF16), ("forward", F32, FORWARD_F32), ("backward", BF16, BACKWARD_BF16),
+    ("backward", F32, BACKWARD_F32)) for s, h in rows])
+def test_each_workgroup(op, dtype, sizes, held):
+    """Every shape of workgroup that holds a map, and what is left to three launches:
+    that these sizes take it, and their results."""
+    N, L, C, groups = sizes
+    log(f"group norm workgroup {op} {dtype} {sizes}")
+    x, gamma, beta, dy = drawn(N, L, C, dtype, 11)
+    d = [t.to(dev()) for t in (x, gamma, beta, dy)]
+    y, mean, rstd = api().group_norm_forward(d[0], d[1], d[2], groups, EPS, act="relu")
+    if op == "forward":
+        names = launched(lambda: api().group_norm_forward(d[0], d[1], d[2], groups, EPS, act="relu"))
+        want = ["chunk_stats", "group_stats", "forward"] if held is None else [("held_forward_kernel", *held)]
+        checked, results = O.forward(x, gamma, beta, groups, EPS, "relu", rounding(dtype)), {"y": y, "mean": mean, "rstd": rstd}
+    else:
+        call = lambda: api().group_norm_backward(d[3], d[0], d[1], d[2], mean, rstd, act="relu")  # noqa: E731
+        names = launched(call)
+        want = ["chunk_sums", "join_sums", "backward"] if held is None else \
+            [("held_backward_kernel", *held)] + ["weights"] * (N > 1)
+        checked = O.backward(dy, x, gamma, beta, mean.cpu(), rstd.cpu(), "relu", rounding(dtype))
+        results = dict(zip(("dx", "dgamma", "dbeta"), call()))
+    assert names == want
+    for name, got in results.items():
+        within(got, checked[name], name)
