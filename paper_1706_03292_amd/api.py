@@ -1038,15 +1038,14 @@ class AdamW:
                 out = [(torch.empty_like(k[0]), torch.empty_like(k[0])) for k in self._keep]
             if len(out) != len(self._keep):
                 raise ValueError(f"out needs one pair for each of the {len(self._keep)} tensors")
-            ptrs = [(ctypes.c_void_p * max(1, len(out)))() for _ in range(2)]
-            for i, (pair, n) in enumerate(zip(out, self._sizes)):
-                for arr, name, x in zip(ptrs, ("m", "v"), pair):
-                    if x is None:
-                        continue
-                    if not (isinstance(x, torch.Tensor) and x.dtype is torch.float32 and x.get_device() == dev
-                            and x.numel() == n and x.is_contiguous()):
+            columns = tuple(zip(*out)) or ((), ())
+            for name, column in zip(("m", "v"), columns):
+                for i, (x, n) in enumerate(zip(column, self._sizes)):
+                    if x is not None and not (type(x) is torch.Tensor and x.dtype is torch.float32 and x.numel() == n
+                                              and x.get_device() == dev and x.is_contiguous()):
                         _sized(i, name, x, torch.float32, dev, n)
-                    arr[i] = x.data_ptr()
+            ptrs = [(ctypes.c_void_p * max(1, len(out)))(*[None if x is None else x.data_ptr() for x in column])
+                    for column in columns]
             if stream is not None:
                 self._kept_uses(stream)
                 _uses(stream, *[x for pair in out for x in pair])

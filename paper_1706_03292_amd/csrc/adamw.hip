@@ -533,9 +533,10 @@ __global__ __launch_bounds__(THREADS) void values_kernel(const AdamwGroup a)
 // The gradients' norm: each workgroup's sum of squares, then their sum, both in
 // a fixed order.
 // ---------------------------------------------------------------------------
+template <int N>
 __device__ __forceinline__ double workgroup_sum(double v)
 {
-    __shared__ double lds[THREADS / 64];
+    __shared__ double lds[N / 64];
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1)
         v += __shfl_xor(v, d);
@@ -544,7 +545,7 @@ __device__ __forceinline__ double workgroup_sum(double v)
     __syncthreads();
     v = 0.0;
 #pragma unroll
-    for (int i = 0; i < THREADS / 64; ++i)
+    for (int i = 0; i < N / 64; ++i)
         v += lds[i];
     return v;
 }
@@ -576,19 +577,21 @@ __global__ __launch_bounds__(THREADS) void squares_kernel(const AdamwGroup a, do
                 put<FULL>(static_cast<float*>(q.copy) + e + k * QUAD_GAP, left - k * QUAD_GAP, x);
         }
     });
-    sum = workgroup_sum(sum);
+    sum = workgroup_sum<THREADS>(sum);
     if (threadIdx.x == 0)
         partial[blockIdx.x] = sum;
 }
 
-__global__ __launch_bounds__(THREADS) void norm_kernel(const double* __restrict__ partial, int64_t parts,
-                                                       double max_norm, float* __restrict__ result)
+constexpr int NORM_THREADS = 1024;
+
+__global__ __launch_bounds__(NORM_THREADS) void norm_kernel(const double* __restrict__ partial, int64_t parts,
+                                                            double max_norm, float* __restrict__ result)
 {
     double sum = 0.0;
 #pragma unroll 8
-    for (int64_t i = threadIdx.x; i < parts; i += THREADS)
+    for (int64_t i = threadIdx.x; i < parts; i += NORM_THREADS)
         sum += partial[i];
-    sum = workgroup_sum(sum);
+    sum = workgroup_sum<NORM_THREADS>(sum);
     if (threadIdx.x == 0) {
         const double norm = sqrt(sum);
         result[0] = static_cast<float>(norm);
@@ -645,7 +648,7 @@ hipError_t launch_adamw_squares(const AdamwGroup& group, int32_t dtype, bool one
 
 hipError_t launch_adamw_norm(const double* partial, int64_t parts, double max_norm, float* result, hipStream_t stream)
 {
-    norm_kernel<<<1, THREADS, 0, stream>>>(partial, parts, max_norm, result);
+    norm_kernel<<<1, NORM_THREADS, 0, stream>>>(partial, parts, max_norm, result);
     return hipGetLastError();
 }
 

@@ -6,7 +6,7 @@
 // at eight neighbouring channels (a column), and walk the rows.  Maps whose groups
 // fit a workgroup's registers are read once (held_*_kernel).  Others take three
 // launches: sums of each chunk of rows and channel; each group's statistics from
-// them; the result, from a second read.
+// them (two launches for wide groups); the result, from a second read.
 //
 // A row that does not divide into eights has its last column end with it: that
 // thread's first `skip` channels belong to the column before, count for no sum and
@@ -696,9 +696,20 @@ __device__ __forceinline__ double team_sum(double v, double* lds)
     return v;
 }
 
-// TEAM threads a group, of at most TEAM * HELD pairs, which they hold; more pairs
-// (HELD = 0) are read twice.
-template <int TEAM, int HELD>
+// Sums of rows d and of the sums of squares about `from`, d a mean's distance from it:
+// of any pairs, whose mean and sum of squares about it they give, in 64 bits.
+struct Joined {
+    double s1 = 0.0, s2 = 0.0;
+    __device__ __forceinline__ void add(const Pair& p, double rows, double from)
+    {
+        const double d = p.a - from;
+        s1 += rows * d;
+        s2 += p.b + rows * d * d;
+    }
+};
+
+// TEAM threads a group.
+template <int TEAM>
 __global__ __launch_bounds__(SUM_THREADS) void group_stats_kernel(const Pair* __restrict__ partial, Map h, float eps,
                                                                   float* __restrict__ mean_out,
                                                                   float* __restrict__ rstd_out)
@@ -706,66 +717,76 @@ __global__ __launch_bounds__(SUM_THREADS) void group_stats_kernel(const Pair* __
     __shared__ double lds[SUM_THREADS / 64];
     constexpr int TEAMS = SUM_THREADS / TEAM;
     const int t = threadIdx.x % TEAM;
+    const uint32_t D = h.D;
     const int64_t pairs = h.chunks * h.D;
     const double count = static_cast<double>(h.L) * static_cast<double>(h.D);
-    const int64_t chunk_step = TEAM / h.D;
-    const int rest = TEAM - static_cast<int>(chunk_step) * h.D;
     for (int64_t q = static_cast<int64_t>(blockIdx.x) * TEAMS + threadIdx.x / TEAM; q < h.N * h.groups;
          q += static_cast<int64_t>(gridDim.x) * TEAMS) {
         const int64_t n = q / h.groups;
         const Pair* at = partial + n * h.chunks * h.C + (q - n * h.groups) * h.D;
-        int64_t chunk = t / h.D;
-        int c = t - static_cast<int>(chunk) * h.D;   // pair i: of chunk i / D, channel i % D
-        auto next = [&](double& rows) {
-            const Pair* p = at + chunk * h.C + c;
-            rows = static_cast<double>(chunk + 1 < h.chunks ? h.rows : h.L - chunk * h.rows);
-            chunk += chunk_step;
-            c += rest;
-            if (c >= h.D) {
-                c -= h.D;
-                ++chunk;
-            }
-            return p;
-        };
-        double s = 0.0, mean;
-        if constexpr (HELD > 0) {
-            Pair p[HELD];
-            double rows[HELD];
-#pragma unroll
-            for (int k = 0; k < HELD; ++k) {
-                const Pair* from = next(rows[k]);
-                const bool in = t + k * TEAM < pairs;
-                rows[k] = in ? rows[k] : 0.0;
-                p[k] = in ? *from : Pair{0.f, 0.f};
-            }
-#pragma unroll
-            for (int k = 0; k < HELD; ++k)
-                s += rows[k] * p[k].a;
-            mean = team_sum<TEAM>(s, lds) / count;
-            s = 0.0;
-#pragma unroll
-            for (int k = 0; k < HELD; ++k)
-                s += rows[k] > 0.0 ? p[k].b + rows[k] * (p[k].a - mean) * (p[k].a - mean) : 0.0;
-        } else {
-            double rows;
-            for (int64_t i = t; i < pairs; i += TEAM) {
-                const Pair p = *next(rows);
-                s += rows * p.a;
-            }
-            mean = team_sum<TEAM>(s, lds) / count;
-            s = 0.0;
-            chunk = t / h.D;
-            c = t - static_cast<int>(chunk) * h.D;
-            for (int64_t i = t; i < pairs; i += TEAM) {
-                const Pair p = *next(rows);
-                s += p.b + rows * (p.a - mean) * (p.a - mean);
-            }
+        const double from = at->a;
+        Joined j;
+#pragma unroll 4
+        for (int64_t i = t; i < pairs; i += TEAM) {
+            const uint32_t chunk = static_cast<uint32_t>(i) / D, c = static_cast<uint32_t>(i) - chunk * D;
+            j.add(at[chunk * h.C + c], static_cast<double>(chunk + 1 < h.chunks ? h.rows : h.L - chunk * h.rows), from);
         }
-        s = team_sum<TEAM>(s, lds);
+        j.s1 = team_sum<TEAM>(j.s1, lds) / count;
+        j.s2 = team_sum<TEAM>(j.s2, lds) / count - j.s1 * j.s1;
         if (t == 0) {
-            mean_out[q] = static_cast<float>(mean);
-            rstd_out[q] = static_cast<float>(1.0 / sqrt(s / count + eps));
+            mean_out[q] = static_cast<float>(from + j.s1);
+            rstd_out[q] = static_cast<float>(1.0 / sqrt((j.s2 < 0.0 ? 0.0 : j.s2) + eps));   // (NaN stays)
         }
+    }
+}
+
+// The chunks of one sample and TILE channels, TILE_SLICES threads a channel:
+// f(chunk, pair) for this thread's.
+constexpr int TILE = 16, TILE_SLICES = SUM_THREADS / TILE;
+
+template <typename F>
+__device__ __forceinline__ void each_chunk(const Pair* __restrict__ partial, const Map& h, int64_t n, int64_t channel,
+                                           F&& f)
+{
+    if (channel >= h.C)
+        return;
+#pragma unroll 4
+    for (int64_t k = threadIdx.x / TILE; k < h.chunks; k += TILE_SLICES)
+        f(k, partial[(n * h.chunks + k) * h.C + channel]);
+}
+
+// The sum over a channel's threads.
+__device__ __forceinline__ double slice_sum(double v, double* lds)
+{
+    __syncthreads();
+    lds[threadIdx.x] = v;
+    __syncthreads();
+    v = 0.0;
+#pragma unroll
+    for (int i = 0; i < TILE_SLICES; ++i)
+        v += lds[threadIdx.x % TILE + i * TILE];
+    return v;
+}
+
+// Each sample and channel's mean and sum of squares about it from those of its chunks:
+// where a group's pairs are many.
+__global__ __launch_bounds__(SUM_THREADS) void join_chunks_kernel(const Pair* __restrict__ partial, Map h,
+                                                                  Pair* __restrict__ joined)
+{
+    __shared__ double lds[SUM_THREADS];
+    const int64_t tiles = ceil_div(h.C, TILE);
+    for (int64_t q = blockIdx.x; q < h.N * tiles; q += gridDim.x) {
+        const int64_t n = q / tiles, channel = (q - n * tiles) * TILE + threadIdx.x % TILE;
+        const double from = channel < h.C ? partial[n * h.chunks * h.C + channel].a : 0.f;
+        Joined j;
+        each_chunk(partial, h, n, channel, [&](int64_t k, const Pair& p) {
+            j.add(p, static_cast<double>(k + 1 < h.chunks ? h.rows : h.L - k * h.rows), from);
+        });
+        j.s1 = slice_sum(j.s1, lds);
+        j.s2 = slice_sum(j.s2, lds) - j.s1 * j.s1 / static_cast<double>(h.L);
+        if (threadIdx.x < TILE && channel < h.C)
+            joined[n * h.C + channel] = Pair{static_cast<float>(from + j.s1 / static_cast<double>(h.L)),
+                                             static_cast<float>(j.s2 < 0.0 ? 0.0 : j.s2)};
     }
 }
 
@@ -855,51 +876,95 @@ __global__ __launch_bounds__(MOST_THREADS) void chunk_sums_kernel(const T* __res
     }
 }
 
-// One workgroup a group of one sample: its channels' sums over the chunks, a channel
-// a lane of `lanes`, and its averages.
+// Narrow groups (up to NARROW channels), one workgroup a group of one sample: its
+// channels' sums over the chunks, a channel a lane of `lanes`, and its averages.
+constexpr int NARROW = 64;
+
 __global__ __launch_bounds__(SUM_THREADS) void join_sums_kernel(const Pair* __restrict__ partial, Map h,
                                                                 const float* __restrict__ gamma,
                                                                 Pair* __restrict__ totals, Pair* __restrict__ averages)
 {
     __shared__ double lds[SUM_THREADS * 2];
     int lanes = 1;
-    while (lanes < 64 && lanes < h.D)
+    while (lanes < h.D)
         lanes *= 2;
     const int slices = SUM_THREADS / lanes, lane = threadIdx.x & (lanes - 1), slice = threadIdx.x / lanes;
     const double count = static_cast<double>(h.L) * static_cast<double>(h.D);
     for (int64_t q = blockIdx.x; q < h.N * h.groups; q += gridDim.x) {
+        const int64_t n = q / h.groups, channel = (q - n * h.groups) * h.D + lane;
+        double s1 = 0.0, s2 = 0.0;
+        if (lane < h.D)
+#pragma unroll 4
+            for (int64_t k = slice; k < h.chunks; k += slices) {
+                const Pair p = partial[(n * h.chunks + k) * h.C + channel];
+                s1 += p.a;
+                s2 += p.b;
+            }
+        __syncthreads();
+        lds[threadIdx.x * 2] = s1;
+        lds[threadIdx.x * 2 + 1] = s2;
+        __syncthreads();
+        if (slice != 0)
+            continue;   // (the rest within one wave)
+        for (int k = 1; k < slices; ++k) {
+            s1 += lds[(k * lanes + lane) * 2];
+            s2 += lds[(k * lanes + lane) * 2 + 1];
+        }
+        double a1 = 0.0, a2 = 0.0;
+        if (lane < h.D) {
+            totals[n * h.C + channel] = Pair{static_cast<float>(s1), static_cast<float>(s2)};
+            a1 = gamma[channel] * s1;
+            a2 = gamma[channel] * s2;
+        }
+        for (int m = 1; m < lanes; m <<= 1) {
+            a1 += __shfl_xor(a1, m);
+            a2 += __shfl_xor(a2, m);
+        }
+        if (lane == 0)
+            averages[q] = Pair{static_cast<float>(a1 / count), static_cast<float>(a2 / count)};
+    }
+}
+
+// Wide ones: the sums of each sample and channel, then a workgroup a group.
+__global__ __launch_bounds__(SUM_THREADS) void join_channels_kernel(const Pair* __restrict__ partial, Map h,
+                                                                    Pair* __restrict__ totals)
+{
+    __shared__ double lds[SUM_THREADS];
+    const int64_t tiles = ceil_div(h.C, TILE);
+    for (int64_t q = blockIdx.x; q < h.N * tiles; q += gridDim.x) {
+        const int64_t n = q / tiles, channel = (q - n * tiles) * TILE + threadIdx.x % TILE;
+        double s1 = 0.0, s2 = 0.0;
+        each_chunk(partial, h, n, channel, [&](int64_t, const Pair& p) {
+            s1 += p.a;
+            s2 += p.b;
+        });
+        s1 = slice_sum(s1, lds);
+        s2 = slice_sum(s2, lds);
+        if (threadIdx.x < TILE && channel < h.C)
+            totals[n * h.C + channel] = Pair{static_cast<float>(s1), static_cast<float>(s2)};
+    }
+}
+
+__global__ __launch_bounds__(SUM_THREADS) void average_kernel(const Pair* __restrict__ totals, Map h,
+                                                              const float* __restrict__ gamma,
+                                                              Pair* __restrict__ averages)
+{
+    __shared__ double lds[SUM_THREADS / 64];
+    const double count = static_cast<double>(h.L) * static_cast<double>(h.D);
+    for (int64_t q = blockIdx.x; q < h.N * h.groups; q += gridDim.x) {
         const int64_t n = q / h.groups, first = (q - n * h.groups) * h.D;
         double a1 = 0.0, a2 = 0.0;
-        for (int64_t c = lane; c - lane < h.D; c += lanes) {
-            double s1 = 0.0, s2 = 0.0;
-            if (c < h.D)
-                for (int64_t k = slice; k < h.chunks; k += slices) {
-                    const Pair p = partial[(n * h.chunks + k) * h.C + first + c];
-                    s1 += p.a;
-                    s2 += p.b;
-                }
-            lds[threadIdx.x * 2] = s1;
-            lds[threadIdx.x * 2 + 1] = s2;
-            __syncthreads();
-            if (slice == 0 && c < h.D) {
-                for (int k = 1; k < slices; ++k) {
-                    s1 += lds[(k * lanes + lane) * 2];
-                    s2 += lds[(k * lanes + lane) * 2 + 1];
-                }
-                totals[n * h.C + first + c] = Pair{static_cast<float>(s1), static_cast<float>(s2)};
-                a1 += gamma[first + c] * s1;
-                a2 += gamma[first + c] * s2;
-            }
-            __syncthreads();
+#pragma unroll 4
+        for (int64_t c = threadIdx.x; c < h.D; c += SUM_THREADS) {
+            const Pair p = totals[n * h.C + first + c];
+            const double w = gamma[first + c];
+            a1 += w * p.a;
+            a2 += w * p.b;
         }
-        if (slice == 0) {   // within one wave
-            for (int m = 1; m < lanes; m <<= 1) {
-                a1 += __shfl_xor(a1, m);
-                a2 += __shfl_xor(a2, m);
-            }
-            if (lane == 0)
-                averages[q] = Pair{static_cast<float>(a1 / count), static_cast<float>(a2 / count)};
-        }
+        a1 = team_sum<SUM_THREADS>(a1, lds);
+        a2 = team_sum<SUM_THREADS>(a2, lds);
+        if (threadIdx.x == 0)
+            averages[q] = Pair{static_cast<float>(a1 / count), static_cast<float>(a2 / count)};
     }
 }
 
@@ -1028,6 +1093,11 @@ Map cut(int64_t N, int64_t L, int64_t C, int64_t groups)
     h.work = N * h.chunks * h.sides;
     return h;
 }
+
+// Whether the forward pass joins each channel's chunks before its groups' channels:
+// where a workgroup's threads would walk more than MANY of a group's pairs.
+constexpr int64_t MANY = 16;
+bool joins_chunks(const Map& h) { return h.chunks > 1 && h.chunks * h.D > SUM_THREADS * MANY; }
 
 // Threads and held rows of a workgroup.
 template <int NT_, int K_>
@@ -1169,18 +1239,26 @@ hipError_t forward_typed(int64_t N, int64_t L, int64_t C, int64_t groups, const 
     hipError_t rc = hipGetLastError();
     if (rc != hipSuccess)
         return rc;
-    const int64_t pairs = h.chunks * h.D, all = N * groups;
+    const Pair* pairs_of = partial;
+    Map of = h;
+    if (joins_chunks(h)) {
+        Pair* joined = partial + N * h.chunks * C;
+        join_chunks_kernel<<<grid_for(N * ceil_div(C, TILE)), SUM_THREADS, 0, s>>>(partial, h, joined);
+        rc = hipGetLastError();
+        if (rc != hipSuccess)
+            return rc;
+        pairs_of = joined;
+        of.chunks = 1;
+        of.rows = L;
+    }
+    const int64_t pairs = of.chunks * of.D, all = N * groups;
     auto stats = [&](auto* kernel, int team) {
-        kernel<<<grid_for(ceil_div(all, SUM_THREADS / team)), SUM_THREADS, 0, s>>>(partial, h, eps, mean, rstd);
+        kernel<<<grid_for(ceil_div(all, SUM_THREADS / team)), SUM_THREADS, 0, s>>>(pairs_of, of, eps, mean, rstd);
     };
-    if (pairs <= 64 * 2)
-        stats(group_stats_kernel<64, 2>, 64);
-    else if (pairs <= 64 * 8)
-        stats(group_stats_kernel<64, 8>, 64);
-    else if (pairs <= SUM_THREADS * 8)
-        stats(group_stats_kernel<SUM_THREADS, 8>, SUM_THREADS);
+    if (pairs <= 64 * 8)
+        stats(group_stats_kernel<64>, 64);
     else
-        stats(group_stats_kernel<SUM_THREADS, 0>, SUM_THREADS);
+        stats(group_stats_kernel<SUM_THREADS>, SUM_THREADS);
     rc = hipGetLastError();
     if (rc != hipSuccess)
         return rc;
@@ -1220,7 +1298,15 @@ hipError_t backward_typed(int64_t N, int64_t L, int64_t C, int64_t groups, const
         rc = hipGetLastError();
         if (rc != hipSuccess)
             return rc;
-        join_sums_kernel<<<grid_for(N * groups), SUM_THREADS, 0, s>>>(partial, h, in.gamma, totals, averages);
+        if (h.D <= NARROW) {
+            join_sums_kernel<<<grid_for(N * groups), SUM_THREADS, 0, s>>>(partial, h, in.gamma, totals, averages);
+        } else {
+            join_channels_kernel<<<grid_for(N * ceil_div(C, TILE)), SUM_THREADS, 0, s>>>(partial, h, totals);
+            rc = hipGetLastError();
+            if (rc != hipSuccess)
+                return rc;
+            average_kernel<<<grid_for(N * groups), SUM_THREADS, 0, s>>>(totals, h, in.gamma, averages);
+        }
         rc = hipGetLastError();
         if (rc != hipSuccess)
             return rc;
@@ -1244,7 +1330,8 @@ int64_t group_norm_workspace(int32_t op, int64_t N, int64_t L, int64_t C, int64_
     if (choose(op, N, L, C, groups, dtype).shape >= 0)
         return totals * static_cast<int64_t>(sizeof(Pair));
     const Map h = cut(N, L, C, groups);
-    return (N * h.chunks * C + (backward ? N * C + N * groups : 0)) * static_cast<int64_t>(sizeof(Pair));
+    return (N * h.chunks * C + (backward ? N * C + N * groups : joins_chunks(h) ? N * C : 0)) *
+           static_cast<int64_t>(sizeof(Pair));
 }
 
 hipError_t launch_group_norm_forward(const void* x, const float* gamma, const float* beta, int64_t N, int64_t L,

@@ -314,21 +314,24 @@ def launched(call):
         if m:
             out.append((m[1], int(m[2]), int(m[3])))
         else:
-            m = re.search(r"(chunk_stats|chunk_sums|group_stats|join_sums|forward|backward|weights)_kernel", name)
+            m = re.search(r"(chunk_stats|chunk_sums|join_chunks|join_channels|group_stats|join_sums|average|forward|backward|weights)_kernel", name)
             if m:
                 out.append(m[1])
     return out
 
 
-# (sizes, workgroup that holds them): one for each shape and, last, none.
+# (sizes, workgroup that holds them): one for each shape, none, and none with groups
+# too wide for one workgroup's sums.
 FORWARD_BF16 = [((1, 49, 512, 32), (256, 2)), ((1, 400, 512, 32), (256, 4)), ((1, 900, 512, 32), (256, 8)),
                 ((1, 1800, 512, 32), (512, 8)), ((4, 3500, 512, 32), (512, 16)), ((4, 8000, 512, 32), (512, 32)),
-                ((1, 8000, 512, 32), None), ((1, 3000, 100, 1), None), ((64, 1, 4096, 32), (256, 2))]
+                ((1, 2000, 288, 32), None), ((1, 8000, 512, 32), "wide"), ((1, 3000, 100, 1), None), ((64, 1, 4096, 32), (256, 2)),
+                ((2, 4000, 1029, 3), "wide"), ((1, 9000, 520, 1), "wide")]
 FORWARD_F32 = [((1, 49, 512, 32), (256, 2)), ((1, 400, 512, 32), (256, 4)), ((1, 900, 512, 32), (256, 8)),
                ((2, 1800, 512, 32), (512, 8)), ((4, 3500, 512, 32), (512, 16)), ((5, 3500, 520, 65), None)]
 BACKWARD_BF16 = [((1, 49, 512, 32), (256, 2)), ((1, 400, 512, 32), (256, 4)), ((1, 900, 512, 32), (256, 8)),
                  ((2, 1800, 512, 32), (512, 8)), ((4, 3500, 512, 32), (512, 16)), ((1, 3500, 512, 32), None),
-                 ((3, 33, 57, 19), (256, 2))]
+                 ((3, 33, 57, 19), (256, 2)), ((2, 4000, 1029, 3), "wide"), ((1, 9000, 130, 2), "wide"),
+                 ((1, 9000, 128, 2), None)]
 BACKWARD_F32 = [((1, 49, 512, 32), (256, 2)), ((1, 400, 512, 32), (256, 4)), ((2, 900, 512, 32), (256, 8)),
                 ((4, 1800, 512, 32), (512, 8)), ((1, 1800, 512, 32), None)]
 
@@ -347,12 +350,14 @@ def test_each_workgroup(op, dtype, sizes, held):
     y, mean, rstd = api().group_norm_forward(d[0], d[1], d[2], groups, EPS, act="relu")
     if op == "forward":
         names = launched(lambda: api().group_norm_forward(d[0], d[1], d[2], groups, EPS, act="relu"))
-        want = ["chunk_stats", "group_stats", "forward"] if held is None else [("held_forward_kernel", *held)]
+        want = {None: ["chunk_stats", "group_stats", "forward"],
+                "wide": ["chunk_stats", "join_chunks", "group_stats", "forward"]}.get(held) or [("held_forward_kernel", *held)]
         checked, results = O.forward(x, gamma, beta, groups, EPS, "relu", rounding(dtype)), {"y": y, "mean": mean, "rstd": rstd}
     else:
         call = lambda: api().group_norm_backward(d[3], d[0], d[1], d[2], mean, rstd, act="relu")  # noqa: E731
         names = launched(call)
-        want = ["chunk_sums", "join_sums", "backward"] if held is None else \
+        want = {None: ["chunk_sums", "join_sums", "backward"],
+                "wide": ["chunk_sums", "join_channels", "average", "backward"]}.get(held) or \
             [("held_backward_kernel", *held)] + ["weights"] * (N > 1)
         checked = O.backward(dy, x, gamma, beta, mean.cpu(), rstd.cpu(), "relu", rounding(dtype))
         results = dict(zip(("dx", "dgamma", "dbeta"), call()))
