@@ -14,11 +14,12 @@
  *
  * General conventions
  *  - All array arguments are device pointers to fp32 data owned by the caller
- *    (the operators at a network's end name their own types).
+ *    (the operators from poseidon_dropout on name their own types).
  *    The library allocates no device memory and keeps no pointer past a call,
- *    except a KV store, which keeps its tensors' pointers for its lifetime and
- *    each received update's pointer until the work it triggers has been
- *    enqueued (and the caller keeps that memory valid until the work has run).
+ *    except a KV store and an AdamW optimizer, which keep their tensors'
+ *    pointers for their lifetime, the store also each received update's pointer
+ *    until the work it triggers has been enqueued (and the caller keeps that
+ *    memory valid until the work has run).
  *  - Work is enqueued asynchronously on `stream` (0 = the null stream).
  *    Argument errors are detected and reported synchronously, before anything
  *    is enqueued; a fault inside a kernel surfaces at the next synchronisation
