@@ -944,19 +944,20 @@ class AdamW:
                     raise TypeError(f"tensor {i}: shards must be a float32 or bfloat16 tensor")
                 dtype, dev = G.dtype, W.get_device()
             n = W.numel()
-            _dev("W", W, torch.float32, dev, W.shape)
+            _sized(i, "W", W, torch.float32, dev, n)
             P, stride = _rows_of(i, G, W, dtype, dev)
-            coded = t.get("exponents") is not None
-            for name in ("m", "v"):
-                _sized(i, name, t[name], torch.uint8 if coded else torch.float32, dev, n)
-            for name, kind, size in (("exponents", torch.uint8, 2 * (-(-n // ADAMW_BLOCK))),
-                                     ("copy", torch.bfloat16, n), ("sum", torch.float32, n)):
-                if t.get(name) is not None:
-                    _sized(i, name, t[name], kind, dev, size)
-            arr[i] = L.PoseidonAdamwTensor(W.data_ptr(), G.data_ptr(), t["m"].data_ptr(), t["v"].data_ptr(),
-                                           _ptr(t.get("exponents")), _ptr(t.get("copy")), _ptr(t.get("sum")), n,
-                                           stride, P, float(t.get("weight_decay", 0.0)))
-            self._keep.append((W, G, t["m"], t["v"], t.get("exponents"), t.get("copy"), t.get("sum")))
+            m, v, exponents, copy, total = t["m"], t["v"], t.get("exponents"), t.get("copy"), t.get("sum")
+            kind = torch.float32 if exponents is None else torch.uint8
+            _sized(i, "m", m, kind, dev, n), _sized(i, "v", v, kind, dev, n)
+            if exponents is not None:
+                _sized(i, "exponents", exponents, torch.uint8, dev, 2 * (-(-n // ADAMW_BLOCK)))
+            if copy is not None:
+                _sized(i, "copy", copy, torch.bfloat16, dev, n)
+            if total is not None:
+                _sized(i, "sum", total, torch.float32, dev, n)
+            arr[i] = L.PoseidonAdamwTensor(W.data_ptr(), G.data_ptr(), m.data_ptr(), v.data_ptr(), _ptr(exponents),
+                                           _ptr(copy), _ptr(total), n, stride, P, float(t.get("weight_decay", 0.0)))
+            self._keep.append((W, G, m, v, exponents, copy, total))
         self.device = torch.device("cuda", torch.cuda.current_device() if dev is None else dev)
         _check("poseidon_adamw_create", L.lib().poseidon_adamw_create(arr, len(tensors), _DTYPES[dtype],
                                                                       ctypes.byref(self._h)))
@@ -1067,9 +1068,11 @@ class AdamW:
 
 def _sized(i: int, name: str, t: torch.Tensor, dtype: torch.dtype, device: int, n: int) -> None:
     """Checks a contiguous tensor of n values of the given type on the device."""
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.numel() == n and t.get_device() == device
+            and t.is_contiguous()):
+        return
     _dev(f"tensor {i}: {name}", t, dtype, device, t.shape if isinstance(t, torch.Tensor) else ())
-    if t.numel() != n:
-        raise ValueError(f"tensor {i}: {name} must have {n} values, got {t.numel()}")
+    raise ValueError(f"tensor {i}: {name} must have {n} values, got {t.numel()}")
 
 
 def _rows_of(i: int, G: torch.Tensor, W: torch.Tensor, dtype: torch.dtype, device: int) -> tuple[int, int]:
@@ -1077,7 +1080,8 @@ def _rows_of(i: int, G: torch.Tensor, W: torch.Tensor, dtype: torch.dtype, devic
     if not isinstance(G, torch.Tensor):
         raise TypeError(f"tensor {i}: shards must be a torch.Tensor")
     P = G.shape[0] if G.dim() else 0
-    if P < 1 or G.shape[1:] not in (W.shape, (W.numel(),)):
+    shape = G.shape[1:]
+    if P < 1 or (shape != W.shape and shape != (W.numel(),)):
         raise ValueError(f"tensor {i}: shards must be P x {W.numel()} or P x {tuple(W.shape)}, got {tuple(G.shape)}")
-    _dev(f"tensor {i}: shards", G[0], dtype, device, G.shape[1:])
+    _dev("shards", G[0], dtype, device, shape)
     return P, G.stride(0)
