@@ -989,7 +989,8 @@ class AdamW:
         the device, multiplies the gradients (clip's result[1:2]; not finite: the
         step is left out); ``rng`` holds (seed, offset) as two int64 values on the
         device for the rounding of 8-bit moments, with another offset for every
-        step (None: to nearest); ``from_sums`` takes the gradients from the sums
+        step (None: to nearest, at which v all but stands still where beta2 is
+        near 1); ``from_sums`` takes the gradients from the sums
         that clip left."""
         rule = L.PoseidonAdamwRule.from_buffer_copy(self._rule)
         dev = self.device.index
