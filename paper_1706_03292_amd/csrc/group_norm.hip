@@ -9,7 +9,8 @@
 // at eight neighbouring channels (a column), and walk the rows.  Maps whose groups
 // fit a workgroup's registers are read once (held_*_kernel).  Others take three
 // launches: sums of each chunk of rows and channel; each group's statistics from
-// them (two launches for wide groups); the result, from a second read.
+// them (two launches for wide groups); the result, from a second read.  Where the
+// chunks are few, the first launch sums up groups too and the last one joins them: two.
 //
 // A row that does not divide into eights has its last column end with it: that
 // thread's first `skip` channels belong to the column before, count for no sum and
@@ -42,7 +43,8 @@ struct Map {
     int32_t shift;     // its logarithm
     int32_t fold;      // cols is a power of two up to 64: a wave's teams are joined by shuffles
     int32_t span;      // groups of a workgroup (held)
-    int32_t lanes;     // that add up one group (held): a power of two up to 64
+    int32_t lanes;     // that add up one group (held, chunk): a power of two up to 64
+    int32_t slices;    // threads that add up one group's chunks
     float inv_D;
 };
 
@@ -180,21 +182,27 @@ struct Lines {
     float mean[GROUP], scale[GROUP], shift[GROUP];
 };
 
-__device__ __forceinline__ void load_lines(const Map& h, const Spot& s, const Inputs& in, Lines& l, float (&rstd)[GROUP])
+// mean, rstd_of: of the sample's groups.
+__device__ __forceinline__ void load_lines(const Map& h, const Spot& s, const Inputs& in, const float* mean,
+                                           const float* rstd_of, Lines& l, float (&rstd)[GROUP])
 {
     load_weights(h, s, in.gamma, l.scale);
     load_weights(h, s, in.beta, l.shift);
     if (!s.active)
         return;
-    const float* mean = in.mean + s.n * h.groups;
-    const float* r = in.rstd + s.n * h.groups;
 #pragma unroll
     for (int i = 0; i < GROUP; ++i) {
         const int c = s.channel + i < h.C ? s.channel + i : static_cast<int>(h.C) - 1, g = group_of(h, c);
         l.mean[i] = mean[g];
-        rstd[i] = r[g];
+        rstd[i] = rstd_of[g];
         l.scale[i] *= rstd[i];
     }
+}
+
+__device__ __forceinline__ void load_lines(const Map& h, const Spot& s, const Inputs& in, Lines& l,
+                                           float (&rstd)[GROUP])
+{
+    load_lines(h, s, in, in.mean + s.n * h.groups, in.rstd + s.n * h.groups, l, rstd);
 }
 
 // dz = dy act'(z) of a thread's channels, v: x, d: x - mean.
@@ -563,8 +571,9 @@ __global__ __launch_bounds__(NT) void held_backward_kernel(const T* __restrict__
 }
 
 // ---------------------------------------------------------------------------
-// Three launches, forward: mean and sum of squares about it of each chunk and
-// channel; each group's mean and rstd; the result.
+// Two to four launches, forward: mean and sum of squares about it of each chunk and
+// channel; each group's mean and rstd; the result.  In two: of each chunk and group; the
+// result, each workgroup with its sample's statistics from those.
 // ---------------------------------------------------------------------------
 constexpr int MOST_THREADS = 256;
 constexpr int MOST_ROWS = 64;    // of a thread
@@ -597,7 +606,8 @@ __device__ __forceinline__ void walk(const Map& h, const Spot& s, const T* const
 // of any pairs, whose mean and sum of squares about it they give, in 64 bits.
 struct Joined {
     double s1 = 0.0, s2 = 0.0;
-    __device__ __forceinline__ void add(const Pair& p, double rows, double from)
+    template <typename P>
+    __device__ __forceinline__ void add(const P& p, double rows, double from)
     {
         const double d = p.a - from;
         s1 += rows * d;
@@ -605,9 +615,16 @@ struct Joined {
     }
 };
 
-template <typename T>
+// A chunk and group's mean and sum of squares about it.
+struct Wide {
+    double a, b;
+};
+
+// LATE: of each chunk and group (to `wide`), not channel (to `partial`).
+template <typename T, bool LATE>
 __global__ __launch_bounds__(MOST_THREADS) void chunk_stats_kernel(const T* __restrict__ x, Map h,
-                                                                   Pair* __restrict__ partial)
+                                                                   Pair* __restrict__ partial,
+                                                                   Wide* __restrict__ wide)
 {
     __shared__ Pair lds[MOST_THREADS * GROUP];
     __shared__ float counts[MOST_THREADS];
@@ -681,10 +698,28 @@ __global__ __launch_bounds__(MOST_THREADS) void chunk_stats_kernel(const T* __re
                 if (counts[w] > 0.f)
                     j.add(lds[w * channels + k], counts[w], from);
             const double off = j.s1 / all, q = j.s2 - j.s1 * off;
-            partial[(s.n * h.chunks + s.first_row / h.rows) * h.C + s.first + k] =
-                Pair{static_cast<float>(from + off), static_cast<float>(q < 0.0 ? 0.0 : q)};   // (NaN stays)
+            Pair* const to = LATE ? lds + k : partial + (s.n * h.chunks + s.first_row / h.rows) * h.C + s.first + k;
+            *to = Pair{static_cast<float>(from + off), static_cast<float>(q < 0.0 ? 0.0 : q)};   // (NaN stays)
         }
         __syncthreads();
+        if constexpr (LATE) {
+            const int lane = threadIdx.x & (h.lanes - 1), D = h.D;
+            for (int g = static_cast<int>(threadIdx.x) / h.lanes; g < h.groups; g += h.threads / h.lanes) {
+                const Pair* const of = lds + g * D;
+                const double from = of[0].a, count = all * D;
+                Joined j;
+                for (int c = lane; c < D; c += h.lanes)
+                    j.add(of[c], all, from);
+                for (int m = 1; m < h.lanes; m <<= 1) {
+                    j.s1 += __shfl_xor(j.s1, m);
+                    j.s2 += __shfl_xor(j.s2, m);
+                }
+                const double off = j.s1 / count, q = j.s2 - j.s1 * off;
+                if (lane == 0)
+                    wide[(s.n * h.chunks + s.first_row / h.rows) * h.groups + g] = Wide{from + off, q < 0.0 ? 0.0 : q};
+            }
+            __syncthreads();
+        }
     }
 }
 
@@ -790,17 +825,83 @@ __global__ __launch_bounds__(SUM_THREADS) void join_chunks_kernel(const Pair* __
     }
 }
 
-template <typename T, int ACT>
-__global__ __launch_bounds__(MOST_THREADS) void forward_kernel(const T* __restrict__ x, Inputs in, Map h,
-                                                               T* __restrict__ y)
+// What a sample's groups make of their chunks (`wide`), in each workgroup of the result:
+// a thread a group and one of `slices` of the chunks; add(sums, chunk's, k, from),
+// `from` being the first chunk's, and finish(group, sums, from) by one thread.
+constexpr int LATE_EACH = 8, LATE_ROUNDS = 2;   // chunks of a thread in flight together, times
+
+template <typename A, typename F>
+__device__ __forceinline__ void join_late(const Wide* __restrict__ wide, const Map& h, double* lds, A&& add, F&& finish)
 {
+    const int groups = static_cast<int>(h.groups), chunks = static_cast<int>(h.chunks);
+    const int slice = static_cast<int>(threadIdx.x) / groups, g = static_cast<int>(threadIdx.x) - slice * groups;
+    double from = 0.0;
+    Joined j;
+    if (slice < h.slices)
+        from = wide[g].a;
+    for (int first = slice; slice < h.slices && first < chunks; first += LATE_EACH * h.slices) {
+        Wide w[LATE_EACH];
+#pragma unroll
+        for (int i = 0; i < LATE_EACH; ++i)
+            if (first + i * h.slices < chunks)
+                w[i] = wide[(first + i * h.slices) * groups + g];
+#pragma unroll
+        for (int i = 0; i < LATE_EACH; ++i)
+            if (first + i * h.slices < chunks)
+                add(j, w[i], first + i * h.slices, from);
+    }
+    lds[2 * threadIdx.x] = j.s1;
+    lds[2 * threadIdx.x + 1] = j.s2;
+    __syncthreads();
+    if (slice == 0) {
+        for (int i = 1; i < h.slices; ++i) {
+            j.s1 += lds[2 * (i * groups + g)];
+            j.s2 += lds[2 * (i * groups + g) + 1];
+        }
+        finish(g, j, from);
+    }
+    __syncthreads();
+}
+
+// LATE: from the chunks' statistics; the workgroup of a sample's first rows writes the
+// groups'.
+template <typename T, int ACT, bool LATE>
+__global__ __launch_bounds__(MOST_THREADS) void forward_kernel(const T* __restrict__ x, Inputs in, Map h,
+                                                               T* __restrict__ y, const Wide* __restrict__ wide,
+                                                               float eps, float* __restrict__ mean_out,
+                                                               float* __restrict__ rstd_out)
+{
+    __shared__ double lds[LATE ? 2 * MOST_THREADS : 1];
+    __shared__ float mean[LATE ? MOST_THREADS : 1], of_rstd[LATE ? MOST_THREADS : 1];
     for (int64_t b = blockIdx.x; b < h.work; b += gridDim.x) {
         const Spot s = spot_of(h, h.work - 1 - b);   // last read, first read again
+        if constexpr (LATE) {
+            __syncthreads();   // what the last turn left has been read
+            const double D = h.D, inv = 1.0 / (static_cast<double>(h.L) * D);
+            const int last = static_cast<int>(h.chunks) - 1, rows = static_cast<int>(h.rows);
+            const int rest = static_cast<int>(h.L - last * h.rows);
+            join_late(wide + s.n * h.chunks * h.groups, h, lds,
+                      [&](Joined& j, const Wide& w, int k, double from) {
+                          j.add(w, D * static_cast<double>(k < last ? rows : rest), from);
+                      },
+                      [&](int g, const Joined& j, double from) {
+                          const double off = j.s1 * inv, var = j.s2 * inv - off * off;
+                          mean[g] = static_cast<float>(from + off);
+                          of_rstd[g] = static_cast<float>(1.0 / sqrt((var < 0.0 ? 0.0 : var) + eps));   // (NaN stays)
+                      });
+            if (s.first_row == 0 && threadIdx.x < h.groups) {
+                mean_out[s.n * h.groups + threadIdx.x] = mean[threadIdx.x];
+                rstd_out[s.n * h.groups + threadIdx.x] = of_rstd[threadIdx.x];
+            }
+        }
         if (!s.active)
             continue;
         Lines l;
         float rstd[GROUP];
-        load_lines(h, s, in, l, rstd);
+        if constexpr (LATE)
+            load_lines(h, s, in, mean, of_rstd, l, rstd);
+        else
+            load_lines(h, s, in, l, rstd);
         walk<1, T>(h, s, {x}, 0, [&](const Raw<T> (&r)[1], int64_t at) {
             float v[GROUP];
 #pragma unroll
@@ -812,12 +913,15 @@ __global__ __launch_bounds__(MOST_THREADS) void forward_kernel(const T* __restri
 }
 
 // ---------------------------------------------------------------------------
-// Three launches, backward: sums of dz and dz n of each chunk and channel; of each
-// sample and channel, and each group's averages; the result, and dgamma and dbeta.
+// Two to four launches, backward: sums of dz and dz n of each chunk and channel; of each
+// sample and channel, and each group's averages; the result, and dgamma and dbeta.  In
+// two, the chunks' groups are summed up where the chunks are, as in the forward pass.
 // ---------------------------------------------------------------------------
-template <typename T, int ACT>
+// LATE: of each chunk and group too, weighted by gamma (to `wide`).
+template <typename T, int ACT, bool LATE>
 __global__ __launch_bounds__(MOST_THREADS) void chunk_sums_kernel(const T* __restrict__ dy, const T* __restrict__ x,
-                                                                  Inputs in, Map h, Pair* __restrict__ partial)
+                                                                  Inputs in, Map h, Pair* __restrict__ partial,
+                                                                  Wide* __restrict__ wide)
 {
     __shared__ Pair lds[MOST_THREADS * GROUP];
     for (int64_t b = blockIdx.x; b < h.work; b += gridDim.x) {
@@ -871,8 +975,28 @@ __global__ __launch_bounds__(MOST_THREADS) void chunk_sums_kernel(const T* __res
                 t.b += lds[w * channels + k].b;
             }
             partial[(s.n * h.chunks + s.first_row / h.rows) * h.C + s.first + k] = t;
+            if (LATE)
+                lds[k] = t;
         }
         __syncthreads();
+        if constexpr (LATE) {
+            const int lane = threadIdx.x & (h.lanes - 1), D = h.D;
+            for (int g = static_cast<int>(threadIdx.x) / h.lanes; g < h.groups; g += h.threads / h.lanes) {
+                double s1 = 0.0, s2 = 0.0;
+                for (int c = g * D + lane; c < g * D + D; c += h.lanes) {
+                    const double w = in.gamma[c];
+                    s1 += w * lds[c].a;
+                    s2 += w * lds[c].b;
+                }
+                for (int m = 1; m < h.lanes; m <<= 1) {
+                    s1 += __shfl_xor(s1, m);
+                    s2 += __shfl_xor(s2, m);
+                }
+                if (lane == 0)
+                    wide[(s.n * h.chunks + s.first_row / h.rows) * h.groups + g] = Wide{s1, s2};
+            }
+            __syncthreads();
+        }
     }
 }
 
@@ -1007,20 +1131,35 @@ __global__ __launch_bounds__(SUM_THREADS) void weights_kernel(const Pair* __rest
     sum_samples(totals, N, C, static_cast<int64_t>(blockIdx.x) * SUM_COLS, SUM_THREADS, lds, dgamma, dbeta);
 }
 
-template <typename T, int ACT>
+// totals: of each sample and channel, or (LATE) chunk and channel.
+template <typename T, int ACT, bool LATE>
 __global__ __launch_bounds__(MOST_THREADS) void backward_kernel(const T* __restrict__ dy, const T* __restrict__ x,
                                                                 Inputs in, Map h, const Pair* __restrict__ averages,
                                                                 T* __restrict__ dx, const Pair* __restrict__ totals,
                                                                 float* __restrict__ dgamma, float* __restrict__ dbeta,
-                                                                unsigned sums)
+                                                                unsigned sums, const Wide* __restrict__ wide)
 {
     __shared__ double lds[MOST_THREADS * 2];
+    __shared__ Pair late[LATE ? MOST_THREADS : 1];
     if (blockIdx.x < sums) {   // the first workgroups, not the last: theirs is a chain of loads
-        sum_samples(totals, h.N, h.C, static_cast<int64_t>(blockIdx.x) * SUM_COLS, h.threads, lds, dgamma, dbeta);
+        sum_samples(totals, LATE ? h.N * h.chunks : h.N, h.C, static_cast<int64_t>(blockIdx.x) * SUM_COLS, h.threads,
+                    lds, dgamma, dbeta);
         return;
     }
     for (int64_t b = blockIdx.x - sums; b < h.work; b += gridDim.x - sums) {
         const Spot s = spot_of(h, h.work - 1 - b);   // last read, first read again
+        if constexpr (LATE) {
+            const double inv = 1.0 / (static_cast<double>(h.L) * static_cast<double>(h.D));
+            __syncthreads();   // what the last turn left has been read
+            join_late(wide + s.n * h.chunks * h.groups, h, lds,
+                      [](Joined& j, const Wide& w, int, double) {
+                          j.s1 += w.a;
+                          j.s2 += w.b;
+                      },
+                      [&](int g, const Joined& j, double) {
+                          late[g] = Pair{static_cast<float>(j.s1 * inv), static_cast<float>(j.s2 * inv)};
+                      });
+        }
         if (!s.active)
             continue;
         Lines l;
@@ -1029,7 +1168,7 @@ __global__ __launch_bounds__(MOST_THREADS) void backward_kernel(const T* __restr
 #pragma unroll
         for (int i = 0; i < GROUP; ++i) {
             const int c = s.channel + i < h.C ? s.channel + i : static_cast<int>(h.C) - 1;
-            const Pair a = averages[s.n * h.groups + group_of(h, c)];
+            const Pair a = LATE ? late[group_of(h, c)] : averages[s.n * h.groups + group_of(h, c)];
             k1[i] = -rstd[i] * a.a;
             k2[i] = -rstd[i] * rstd[i] * a.b;
         }
@@ -1093,7 +1232,29 @@ Map cut(int64_t N, int64_t L, int64_t C, int64_t groups)
     h.rows = std::min<int64_t>(L, each * teams);
     h.chunks = ceil_div(L, h.rows);
     h.work = N * h.chunks * h.sides;
+    h.lanes = 1;
+    while (h.lanes < 64 && 2 * h.lanes * groups <= h.threads)
+        h.lanes *= 2;
+    h.slices = static_cast<int32_t>(std::max<int64_t>(1, h.threads / groups));
     return h;
+}
+
+// Whether each workgroup of the result joins its sample's groups itself (join_late),
+// which leaves out a launch: where a row is one workgroup's and a group's chunks are few
+// to a thread.  Forward, three launches and two: 2 x 1225 x 288 fp32 in 32 groups 13.8
+// and 11.3 us, 17 x 1225 x 288 24.5 and 22.6, 4 x 9000 x 1000 fp32 in 8 99 and 90, 32 x
+// 50176 x 64 bf16 in 32 118 and 118; with 16 chunks a thread but in one round (more
+// registers) 128, with 131 chunks of 32 groups in three rounds (8 x 3136 x 320 fp32)
+// 29.6 and 32.5, with one group of 2048 chunks 16.7 and 25.9.  The backward pass has
+// more to do at both ends and takes it where the chip holds all workgroups at once: 60 x
+// 784 x 100 bf16 in 20 21.9 and 19.4, 2 x 1225 x 288 fp32 14.4 and 12.6, but 32 x 3136 x
+// 256 bf16 on 1792 workgroups 56 and 58.
+constexpr int64_t LATE_FEWEST = 8, LATE_WORK = 1024;   // groups; workgroups of a backward pass
+bool joins_late(int op, const Map& h)
+{
+    return h.sides == 1 && h.groups >= LATE_FEWEST && h.groups <= h.threads &&
+           h.chunks <= LATE_ROUNDS * LATE_EACH * h.slices &&
+           (op == POSEIDON_GROUP_NORM_FORWARD || h.work <= LATE_WORK);
 }
 
 // Whether the forward pass joins each channel's chunks before its groups' channels:
@@ -1161,10 +1322,10 @@ Choice held_as(int op, int64_t N, int64_t L, int64_t C, int64_t groups, int shap
 // (rows of up to 512 bytes, or longer ones where threads would have none) that still
 // give every CU one, else the narrowest; of the shapes for it, the first that fits
 // (8192 x 1 x 4096 bf16 forward, an eighth of a workgroup's threads at work in rows of
-// 512 bytes 742 us, all of them in rows of 4 KB 117).  What is left to three launches, us held and in
-// three: rows below 64 bytes, which share memory lines with other workgroups, in more
-// than one round of workgroups (backward, bf16, 32 x 3136 x 256 in rows of 16 bytes
-// 93, 60); workgroups that fill a CU's registers, which load and store in turn, but
+// 512 bytes 742 us, all of them in rows of 4 KB 117).  What is left to the other
+// launches, us held and in three of them: rows below 64 bytes, which share memory lines
+// with other workgroups, in more than one round of workgroups (backward, bf16, 32 x 3136
+// x 256 in rows of 16 bytes 93, 60); workgroups that fill a CU's registers, which load and store in turn, but
 // for one round of them over half of the chip or more (forward, 4 x 12544 x 128 on 64
 // CUs 36, 21, 32 x 3136 x 256 on 256 30, 38; backward, 2 x 1024 x 320 on 16 CUs 20,
 // 15, 16 x 3136 x 256 on 256 28, 37); those that fill half of them on fewer than 64
@@ -1236,8 +1397,21 @@ hipError_t forward_typed(int64_t N, int64_t L, int64_t C, int64_t groups, const 
             return hipGetLastError();
         });
     const Map h = cut(N, L, C, groups);
+    auto result = [&](auto late, const Wide* wide) {
+        with_act(act, [&](auto a) {
+            forward_kernel<T, decltype(a)::value, decltype(late)::value><<<grid_for(h.work), h.threads, 0, s>>>(
+                x, Inputs{gamma, beta, mean, rstd}, h, y, wide, eps, mean, rstd);
+        });
+        return hipGetLastError();
+    };
+    if (joins_late(POSEIDON_GROUP_NORM_FORWARD, h)) {
+        Wide* const wide = static_cast<Wide*>(ws);
+        chunk_stats_kernel<T, true><<<grid_for(h.work), h.threads, 0, s>>>(x, h, nullptr, wide);
+        const hipError_t rc = hipGetLastError();
+        return rc != hipSuccess ? rc : result(std::true_type(), wide);
+    }
     Pair* partial = static_cast<Pair*>(ws);
-    chunk_stats_kernel<T><<<grid_for(h.work), h.threads, 0, s>>>(x, h, partial);
+    chunk_stats_kernel<T, false><<<grid_for(h.work), h.threads, 0, s>>>(x, h, partial, nullptr);
     hipError_t rc = hipGetLastError();
     if (rc != hipSuccess)
         return rc;
@@ -1264,11 +1438,7 @@ hipError_t forward_typed(int64_t N, int64_t L, int64_t C, int64_t groups, const 
     rc = hipGetLastError();
     if (rc != hipSuccess)
         return rc;
-    with_act(act, [&](auto a) {
-        forward_kernel<T, decltype(a)::value><<<grid_for(h.work), h.threads, 0, s>>>(x, Inputs{gamma, beta, mean, rstd},
-                                                                                     h, y);
-    });
-    return hipGetLastError();
+    return result(std::false_type(), nullptr);
 }
 
 template <typename T>
@@ -1292,12 +1462,31 @@ hipError_t backward_typed(int64_t N, int64_t L, int64_t C, int64_t groups, const
             return rc;
     } else if (N > 0) {
         const Map h = cut(N, L, C, groups);
+        const unsigned sums = static_cast<unsigned>(ceil_div(C, SUM_COLS));
+        auto sums_of = [&](auto late, Pair* partial, Wide* wide) {
+            with_act(act, [&](auto a) {
+                chunk_sums_kernel<T, decltype(a)::value, decltype(late)::value><<<grid_for(h.work), h.threads, 0, s>>>(
+                    dy, x, in, h, partial, wide);
+            });
+            return hipGetLastError();
+        };
+        auto result = [&](auto late, const Pair* of, const Pair* averages, const Wide* wide) {
+            with_act(act, [&](auto a) {
+                backward_kernel<T, decltype(a)::value, decltype(late)::value>
+                    <<<sums + grid_for(h.work), h.threads, 0, s>>>(dy, x, in, h, averages, dx, of, dgamma, dbeta, sums,
+                                                                   wide);
+            });
+            return hipGetLastError();
+        };
+        if (joins_late(POSEIDON_GROUP_NORM_BACKWARD, h)) {
+            Wide* const wide = static_cast<Wide*>(ws);
+            Pair* const partial = reinterpret_cast<Pair*>(wide + N * h.chunks * groups);
+            rc = sums_of(std::true_type(), partial, wide);
+            return rc != hipSuccess ? rc : result(std::true_type(), partial, nullptr, wide);
+        }
         Pair* const averages = totals + N * C;
         Pair* const partial = averages + N * groups;
-        with_act(act, [&](auto a) {
-            chunk_sums_kernel<T, decltype(a)::value><<<grid_for(h.work), h.threads, 0, s>>>(dy, x, in, h, partial);
-        });
-        rc = hipGetLastError();
+        rc = sums_of(std::false_type(), partial, nullptr);
         if (rc != hipSuccess)
             return rc;
         if (h.D <= NARROW) {
@@ -1312,12 +1501,7 @@ hipError_t backward_typed(int64_t N, int64_t L, int64_t C, int64_t groups, const
         rc = hipGetLastError();
         if (rc != hipSuccess)
             return rc;
-        const unsigned sums = static_cast<unsigned>(ceil_div(C, SUM_COLS));
-        with_act(act, [&](auto a) {
-            backward_kernel<T, decltype(a)::value><<<sums + grid_for(h.work), h.threads, 0, s>>>(
-                dy, x, in, h, averages, dx, totals, dgamma, dbeta, sums);
-        });
-        return hipGetLastError();
+        return result(std::false_type(), totals, averages, nullptr);
     }
     weights_kernel<<<static_cast<unsigned>(ceil_div(C, SUM_COLS)), SUM_THREADS, 0, s>>>(totals, N, C, dgamma, dbeta);
     return hipGetLastError();
@@ -1332,6 +1516,9 @@ int64_t group_norm_workspace(int32_t op, int64_t N, int64_t L, int64_t C, int64_
     if (choose(op, N, L, C, groups, dtype).shape >= 0)
         return totals * static_cast<int64_t>(sizeof(Pair));
     const Map h = cut(N, L, C, groups);
+    if (joins_late(op, h))
+        return N * h.chunks * (groups * static_cast<int64_t>(sizeof(Wide)) +
+                               (backward ? C : 0) * static_cast<int64_t>(sizeof(Pair)));
     return (N * h.chunks * C + (backward ? N * C + N * groups : joins_chunks(h) ? N * C : 0)) *
            static_cast<int64_t>(sizeof(Pair));
 }

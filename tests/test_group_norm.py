@@ -320,20 +320,24 @@ def launched(call):
     return out
 
 
-# (sizes, workgroup that holds them): one for each shape, none, and none with groups
-# too wide for one workgroup's sums.
+# (sizes, workgroup that holds them): one for each shape, none, none with groups too
+# wide for one workgroup's sums, and none with few enough chunks for two launches.
 FORWARD_BF16 = [((1, 49, 512, 32), (256, 2)), ((1, 400, 512, 32), (256, 4)), ((1, 900, 512, 32), (256, 8)),
                 ((1, 1800, 512, 32), (512, 8)), ((4, 3500, 512, 32), (512, 16)), ((4, 8000, 512, 32), (512, 32)),
-                ((1, 2000, 288, 32), None), ((1, 8000, 512, 32), "wide"), ((1, 3000, 100, 1), None), ((64, 1, 4096, 32), (256, 2)),
-                ((2, 4000, 1029, 3), "wide"), ((1, 9000, 520, 1), "wide")]
+                ((1, 2000, 288, 32), "late"), ((1, 8000, 512, 32), "wide"), ((1, 3000, 100, 1), None), ((64, 1, 4096, 32), (256, 2)),
+                ((2, 4000, 1029, 3), "wide"), ((1, 9000, 520, 1), "wide"), ((1, 9000, 64, 32), "late"),
+                ((3, 1300, 1800, 8), "late"), ((17, 500, 249, 249), "late"), ((1, 2500, 57, 57), "late")]
 FORWARD_F32 = [((1, 49, 512, 32), (256, 2)), ((1, 400, 512, 32), (256, 4)), ((1, 900, 512, 32), (256, 8)),
-               ((2, 1800, 512, 32), (512, 8)), ((4, 3500, 512, 32), (512, 16)), ((5, 3500, 520, 65), None)]
+               ((2, 1800, 512, 32), (512, 8)), ((4, 3500, 512, 32), (512, 16)), ((5, 3500, 520, 65), None),
+               ((17, 700, 288, 32), "late"), ((3, 4000, 8, 8), "late")]
 BACKWARD_BF16 = [((1, 49, 512, 32), (256, 2)), ((1, 400, 512, 32), (256, 4)), ((1, 900, 512, 32), (256, 8)),
                  ((2, 1800, 512, 32), (512, 8)), ((4, 3500, 512, 32), (512, 16)), ((1, 3500, 512, 32), None),
                  ((3, 33, 57, 19), (256, 2)), ((2, 4000, 1029, 3), "wide"), ((1, 9000, 130, 2), "wide"),
-                 ((1, 9000, 128, 2), None)]
+                 ((1, 9000, 128, 2), None), ((24, 6000, 57, 19), None), ((3, 1300, 1800, 8), "late"), ((17, 500, 249, 249), "late"),
+                 ((1, 2500, 57, 57), "late")]
 BACKWARD_F32 = [((1, 49, 512, 32), (256, 2)), ((1, 400, 512, 32), (256, 4)), ((2, 900, 512, 32), (256, 8)),
-                ((4, 1800, 512, 32), (512, 8)), ((1, 1800, 512, 32), None)]
+                ((4, 1800, 512, 32), (512, 8)), ((1, 1800, 512, 32), "late"), ((1, 3500, 512, 32), None),
+                ((17, 700, 288, 32), "late"), ((3, 4000, 8, 8), "late")]
 
 
 @gpu
@@ -341,8 +345,8 @@ BACKWARD_F32 = [((1, 49, 512, 32), (256, 2)), ((1, 400, 512, 32), (256, 4)), ((2
     ("forward", BF16, FORWARD_BF16), ("forward", F32, FORWARD_F32), ("backward", BF16, BACKWARD_BF16),
     ("backward", F32, BACKWARD_F32)) for s, h in rows])
 def test_each_workgroup(op, dtype, sizes, held):
-    """Every shape of workgroup that holds a map, and what is left to three launches:
-    that these sizes take it, and their results."""
+    """Every shape of workgroup that holds a map, and what is left to two, three and four
+    launches: that these sizes take it, and their results."""
     N, L, C, groups = sizes
     log(f"group norm workgroup {op} {dtype} {sizes}")
     x, gamma, beta, dy = drawn(N, L, C, dtype, 11)
@@ -350,13 +354,13 @@ def test_each_workgroup(op, dtype, sizes, held):
     y, mean, rstd = api().group_norm_forward(d[0], d[1], d[2], groups, EPS, act="relu")
     if op == "forward":
         names = launched(lambda: api().group_norm_forward(d[0], d[1], d[2], groups, EPS, act="relu"))
-        want = {None: ["chunk_stats", "group_stats", "forward"],
+        want = {None: ["chunk_stats", "group_stats", "forward"], "late": ["chunk_stats", "forward"],
                 "wide": ["chunk_stats", "join_chunks", "group_stats", "forward"]}.get(held) or [("held_forward_kernel", *held)]
         checked, results = O.forward(x, gamma, beta, groups, EPS, "relu", rounding(dtype)), {"y": y, "mean": mean, "rstd": rstd}
     else:
         call = lambda: api().group_norm_backward(d[3], d[0], d[1], d[2], mean, rstd, act="relu")  # noqa: E731
         names = launched(call)
-        want = {None: ["chunk_sums", "join_sums", "backward"],
+        want = {None: ["chunk_sums", "join_sums", "backward"], "late": ["chunk_sums", "backward"],
                 "wide": ["chunk_sums", "join_channels", "average", "backward"]}.get(held) or \
             [("held_backward_kernel", *held)] + ["weights"] * (N > 1)
         checked = O.backward(dy, x, gamma, beta, mean.cpu(), rstd.cpu(), "relu", rounding(dtype))
