@@ -2,7 +2,7 @@
 // (include/poseidon.h gives the formulas).  A few operations per value, bound by
 // memory: x (and dy) read, y (dx) written once each is what it cannot do without.
 // bf16: forward 32 x 56 x 56 x 256 in one launch 30 us (3.4 TB/s of that), 32 x 224 x
-// 224 x 64 in three 113 us (3.6: x is read twice), backward 32 x 56 x 56 x 256 in
+// 224 x 64 in two 112 us (3.7: x is read twice), backward 32 x 56 x 56 x 256 in
 // three 55 us (2.8).
 //
 // A sample is L rows of C channels.  Threads stand in teams of a row each, a thread
