@@ -146,6 +146,37 @@ def test_what_is_not_finite_stays_in_its_group(bad, act):
     assert torch.isfinite(dx[~cells]).all()
 
 
+# Of maps that no workgroup holds: in two launches, three and four.
+SPREAD = [(3, 5000, 72, 9), (3, 5000, 70, 1), (2, 9000, 520, 1)]
+
+
+@gpu
+@pytest.mark.parametrize("N,L,C,groups", SPREAD)
+def test_far_means_and_bad_values_over_many_workgroups(N, L, C, groups):
+    """Spreads of a thousandth of the mean, then a NaN in the last chunk of a sample."""
+    log(f"group norm spread {N} {L} {C} {groups}")
+    x, gamma, beta, dy = drawn(N, L, C, F32, 12)
+    x = 1000.0 + x
+    want = O.forward(x, gamma, beta, groups, EPS, "relu", rounding(F32))
+    x, gamma, beta, dy = (t.to(dev()) for t in (x, gamma, beta, dy))
+    good = api().group_norm_forward(x, gamma, beta, groups, EPS, act="relu")
+    for got, name in zip(good, ("y", "mean", "rstd")):
+        within(got, want[name], name)
+    back = api().group_norm_backward(dy, x, gamma, beta, good[1], good[2], act="relu")
+    x[1, L - 1, C - 1] = float("nan")
+    y, mean, rstd = api().group_norm_forward(x, gamma, beta, groups, EPS, act="relu")
+    hit = torch.zeros(N, groups, dtype=torch.bool, device=dev())
+    hit[1, groups - 1] = True
+    assert torch.equal(mean[~hit], good[1][~hit]) and torch.equal(rstd[~hit], good[2][~hit])
+    assert torch.isnan(mean[hit]).all() and torch.isnan(rstd[hit]).all()
+    cells = hit[:, None, :, None].expand(N, L, groups, C // groups).reshape(N, L, C)
+    assert torch.equal(y[~cells], good[0][~cells]) and torch.isnan(y[cells]).all()
+    dx, dgamma, dbeta = api().group_norm_backward(dy, x, gamma, beta, mean, rstd, act="relu")
+    assert torch.equal(dx[~cells], back[0][~cells]) and torch.isnan(dx[cells]).all()
+    free = C - C // groups      # channels of the groups before the last
+    assert torch.equal(dgamma[:free], back[1][:free]) and torch.equal(dbeta[:free], back[2][:free])
+
+
 @gpu
 def test_relu_at_zero_passes_nothing():
     """gamma = 0 makes z = beta: the gradient passes where beta > 0 only."""
@@ -232,12 +263,13 @@ def test_channels_last_tensors_of_torch():
 
 @gpu
 @DTYPES
-def test_same_bits_on_another_stream_and_in_a_graph(dtype):
-    log(f"group norm streams {dtype}")
-    x, gamma, beta, dy = (t.to(dev()) for t in drawn(4, 999, 72, dtype, 9))
+@pytest.mark.parametrize("N,L,C,groups", [(4, 999, 72, 9)] + SPREAD)
+def test_same_bits_on_another_stream_and_in_a_graph(N, L, C, groups, dtype):
+    log(f"group norm streams {N} {L} {C} {groups} {dtype}")
+    x, gamma, beta, dy = (t.to(dev()) for t in drawn(N, L, C, dtype, 9))
 
     def both(stream=None):
-        y, mean, rstd = api().group_norm_forward(x, gamma, beta, 9, EPS, act="silu", stream=stream)
+        y, mean, rstd = api().group_norm_forward(x, gamma, beta, groups, EPS, act="silu", stream=stream)
         return [y, mean, rstd, *api().group_norm_backward(dy, x, gamma, beta, mean, rstd, act="silu", stream=stream)]
 
     first = both()
