@@ -17,9 +17,12 @@
 // are stored twice, alike.  So every access is of eight values (fewer channels than
 // eight in all are read one by one).
 //
-// Sums over a thread's rows are fp32, of differences from a value of the group or
-// from its mean, so that a mean far from 0 costs no accuracy; what joins chunks and
-// channels is in 64 bits.  Every order is fixed: nothing depends on timing.
+// Sums over a thread's rows and a workgroup's teams are fp32 (a held group's over its
+// channels too), what joins chunks, and channels elsewhere, is in 64 bits.  Forward,
+// they are sums of differences from a value of the group or from a first mean, and the
+// result counts with what the mean's rounding to fp32 leaves (as part of beta), so that
+// a mean far from 0 costs y no accuracy.  The backward pass takes the mean as it is
+// handed over.  Every order is fixed: nothing depends on timing.
 #include "elements.h"
 
 namespace poseidon {
@@ -182,14 +185,15 @@ struct Lines {
     float mean[GROUP], scale[GROUP], shift[GROUP];
 };
 
-// mean, rstd_of: of the sample's groups.
-__device__ __forceinline__ void load_lines(const Map& h, const Spot& s, const Inputs& in, const float* mean,
-                                           const float* rstd_of, Lines& l, float (&rstd)[GROUP])
+__device__ __forceinline__ void load_lines(const Map& h, const Spot& s, const Inputs& in, Lines& l,
+                                           float (&rstd)[GROUP])
 {
     load_weights(h, s, in.gamma, l.scale);
     load_weights(h, s, in.beta, l.shift);
     if (!s.active)
         return;
+    const float* const mean = in.mean + s.n * h.groups;
+    const float* const rstd_of = in.rstd + s.n * h.groups;
 #pragma unroll
     for (int i = 0; i < GROUP; ++i) {
         const int c = s.channel + i < h.C ? s.channel + i : static_cast<int>(h.C) - 1, g = group_of(h, c);
@@ -197,12 +201,6 @@ __device__ __forceinline__ void load_lines(const Map& h, const Spot& s, const In
         rstd[i] = rstd_of[g];
         l.scale[i] *= rstd[i];
     }
-}
-
-__device__ __forceinline__ void load_lines(const Map& h, const Spot& s, const Inputs& in, Lines& l,
-                                           float (&rstd)[GROUP])
-{
-    load_lines(h, s, in, in.mean + s.n * h.groups, in.rstd + s.n * h.groups, l, rstd);
 }
 
 // dz = dy act'(z) of a thread's channels, v: x, d: x - mean.
@@ -420,13 +418,17 @@ __global__ __launch_bounds__(NT) void held_forward_kernel(const T* __restrict__ 
         g = g < most ? g : most;
         const float off = sums[2 * g] * inv, var = sums[2 * g + 1] * inv - off * off;
         const float rstd = 1.f / sqrtf((var < 0.f ? 0.f : var) + eps);   // (NaN stays)
-        mean[i] += off;
+        // the mean rounded to fp32, and what that leaves of it (the exact error of the sum)
+        const float sum = mean[i] + off, part = sum - mean[i];
+        const float low = (mean[i] - (sum - part)) + (off - part);
+        mean[i] = sum;
         if (s.active && s.team == 0 && s.channel + i < h.C && i >= s.skip && (local + i) - g * h.D == 0) {
             const int64_t at = s.n * h.groups + s.first / h.D + g;
             mean_out[at] = mean[i];
             rstd_out[at] = rstd;
         }
         scale[i] *= rstd;
+        shift[i] = fmaf(-low, scale[i], shift[i]);
     }
     if (!s.active)
         return;
@@ -620,7 +622,30 @@ struct Wide {
     double a, b;
 };
 
+// A group as the result takes it: its mean, what the mean's rounding leaves, and rstd.
+// (One load.)
+struct Stat {
+    float mean, low, rstd;
+};
+
+__device__ __forceinline__ Stat stat_of(double mean, double var, float eps)
+{
+    const float m = static_cast<float>(mean);
+    return Stat{m, static_cast<float>(mean - m), static_cast<float>(1.0 / sqrt((var < 0.0 ? 0.0 : var) + eps))};   // (NaN stays)
+}
+
+// A sample's middle row.
+template <typename T>
+__device__ __forceinline__ const T* middle_of(const T* x, const Map& h, int64_t n)
+{
+    return x + (n * h.L + h.L / 2) * h.C;
+}
+
 // LATE: of each chunk and group (to `wide`), not channel (to `partial`).
+//
+// A mean in fp32 is its distance from a value of the group, its first channel's in the
+// chunk's first row (LATE) or in the sample's middle row: rounding it costs nothing where
+// the group's values lie together, far from 0.
 template <typename T, bool LATE>
 __global__ __launch_bounds__(MOST_THREADS) void chunk_stats_kernel(const T* __restrict__ x, Map h,
                                                                    Pair* __restrict__ partial,
@@ -631,11 +656,18 @@ __global__ __launch_bounds__(MOST_THREADS) void chunk_stats_kernel(const T* __re
     for (int64_t b = blockIdx.x; b < h.work; b += gridDim.x) {
         const Spot s = spot_of(h, b);
         const int local = s.channel - s.first, channels = h.cols * GROUP;
+        const T* const near = LATE ? x + (s.n * h.L + s.first_row) * h.C : middle_of(x, h, s.n);
         float mean[GROUP] = {}, m2[GROUP] = {}, count = 0.f;
         if (s.active && s.first_row + s.team < s.end_row) {
             // differences from the thread's own first value
             Raw<T> first;
             load_row(h, x + s.base, first);
+            float pivot[GROUP];
+#pragma unroll
+            for (int i = 0; i < GROUP; ++i) {
+                const int c = s.channel + i < h.C ? s.channel + i : static_cast<int>(h.C) - 1;
+                pivot[i] = static_cast<float>(near[group_of(h, c) * h.D]);
+            }
             float s1[GROUP] = {};
             walk<1, T>(h, s, {x}, 1, [&](const Raw<T> (&r)[1], int64_t) {
 #pragma unroll
@@ -650,7 +682,7 @@ __global__ __launch_bounds__(MOST_THREADS) void chunk_stats_kernel(const T* __re
 #pragma unroll
             for (int i = 0; i < GROUP; ++i) {
                 const float m = s1[i] * inv, q = fmaf(-m, s1[i], m2[i]);
-                mean[i] = raw_value(first, i) + m;
+                mean[i] = (raw_value(first, i) - pivot[i]) + m;
                 m2[i] = q < 0.f ? 0.f : q;   // (NaN stays)
             }
         }
@@ -716,7 +748,8 @@ __global__ __launch_bounds__(MOST_THREADS) void chunk_stats_kernel(const T* __re
                 }
                 const double off = j.s1 / count, q = j.s2 - j.s1 * off;
                 if (lane == 0)
-                    wide[(s.n * h.chunks + s.first_row / h.rows) * h.groups + g] = Wide{from + off, q < 0.0 ? 0.0 : q};
+                    wide[(s.n * h.chunks + s.first_row / h.rows) * h.groups + g] =
+                        Wide{static_cast<float>(near[g * D]) + (from + off), q < 0.0 ? 0.0 : q};
             }
             __syncthreads();
         }
@@ -744,8 +777,10 @@ __device__ __forceinline__ double team_sum(double v, double* lds)
 }
 
 // TEAM threads a group.
-template <int TEAM>
-__global__ __launch_bounds__(SUM_THREADS) void group_stats_kernel(const Pair* __restrict__ partial, Map h, float eps,
+template <int TEAM, typename T>
+__global__ __launch_bounds__(SUM_THREADS) void group_stats_kernel(const Pair* __restrict__ partial,
+                                                                  const T* __restrict__ x, Map h, float eps,
+                                                                  Stat* __restrict__ stats,
                                                                   float* __restrict__ mean_out,
                                                                   float* __restrict__ rstd_out)
 {
@@ -759,7 +794,7 @@ __global__ __launch_bounds__(SUM_THREADS) void group_stats_kernel(const Pair* __
          q += static_cast<int64_t>(gridDim.x) * TEAMS) {
         const int64_t n = q / h.groups;
         const Pair* at = partial + n * h.chunks * h.C + (q - n * h.groups) * h.D;
-        const double from = at->a;
+        const double from = at->a, middle = static_cast<float>(middle_of(x, h, n)[(q - n * h.groups) * h.D]);
         Joined j;
 #pragma unroll 4
         for (int64_t i = t; i < pairs; i += TEAM) {
@@ -769,8 +804,10 @@ __global__ __launch_bounds__(SUM_THREADS) void group_stats_kernel(const Pair* __
         j.s1 = team_sum<TEAM>(j.s1, lds) / count;
         j.s2 = team_sum<TEAM>(j.s2, lds) / count - j.s1 * j.s1;
         if (t == 0) {
-            mean_out[q] = static_cast<float>(from + j.s1);
-            rstd_out[q] = static_cast<float>(1.0 / sqrt((j.s2 < 0.0 ? 0.0 : j.s2) + eps));   // (NaN stays)
+            const Stat stat = stat_of(middle + (from + j.s1), j.s2, eps);
+            stats[q] = stat;
+            mean_out[q] = stat.mean;
+            rstd_out[q] = stat.rstd;
         }
     }
 }
@@ -866,13 +903,16 @@ __device__ __forceinline__ void join_late(const Wide* __restrict__ wide, const M
 // LATE: from the chunks' statistics; the workgroup of a sample's first rows writes the
 // groups'.
 template <typename T, int ACT, bool LATE>
-__global__ __launch_bounds__(MOST_THREADS) void forward_kernel(const T* __restrict__ x, Inputs in, Map h,
+__global__ __launch_bounds__(MOST_THREADS) void forward_kernel(const T* __restrict__ x,
+                                                               const float* __restrict__ gamma,
+                                                               const float* __restrict__ beta, Map h,
                                                                T* __restrict__ y, const Wide* __restrict__ wide,
-                                                               float eps, float* __restrict__ mean_out,
+                                                               const Stat* __restrict__ stats, float eps,
+                                                               float* __restrict__ mean_out,
                                                                float* __restrict__ rstd_out)
 {
     __shared__ double lds[LATE ? 2 * MOST_THREADS : 1];
-    __shared__ float mean[LATE ? MOST_THREADS : 1], of_rstd[LATE ? MOST_THREADS : 1];
+    __shared__ Stat late[LATE ? MOST_THREADS : 1];
     for (int64_t b = blockIdx.x; b < h.work; b += gridDim.x) {
         const Spot s = spot_of(h, h.work - 1 - b);   // last read, first read again
         if constexpr (LATE) {
@@ -886,22 +926,26 @@ __global__ __launch_bounds__(MOST_THREADS) void forward_kernel(const T* __restri
                       },
                       [&](int g, const Joined& j, double from) {
                           const double off = j.s1 * inv, var = j.s2 * inv - off * off;
-                          mean[g] = static_cast<float>(from + off);
-                          of_rstd[g] = static_cast<float>(1.0 / sqrt((var < 0.0 ? 0.0 : var) + eps));   // (NaN stays)
+                          late[g] = stat_of(from + off, var, eps);
                       });
             if (s.first_row == 0 && threadIdx.x < h.groups) {
-                mean_out[s.n * h.groups + threadIdx.x] = mean[threadIdx.x];
-                rstd_out[s.n * h.groups + threadIdx.x] = of_rstd[threadIdx.x];
+                mean_out[s.n * h.groups + threadIdx.x] = late[threadIdx.x].mean;
+                rstd_out[s.n * h.groups + threadIdx.x] = late[threadIdx.x].rstd;
             }
         }
         if (!s.active)
             continue;
         Lines l;
-        float rstd[GROUP];
-        if constexpr (LATE)
-            load_lines(h, s, in, mean, of_rstd, l, rstd);
-        else
-            load_lines(h, s, in, l, rstd);
+        load_weights(h, s, gamma, l.scale);
+        load_weights(h, s, beta, l.shift);
+#pragma unroll
+        for (int i = 0; i < GROUP; ++i) {
+            const int c = s.channel + i < h.C ? s.channel + i : static_cast<int>(h.C) - 1, g = group_of(h, c);
+            const Stat t = LATE ? late[g] : stats[s.n * h.groups + g];
+            l.mean[i] = t.mean;
+            l.scale[i] *= t.rstd;
+            l.shift[i] = fmaf(-t.low, l.scale[i], l.shift[i]);
+        }
         walk<1, T>(h, s, {x}, 0, [&](const Raw<T> (&r)[1], int64_t at) {
             float v[GROUP];
 #pragma unroll
@@ -1397,10 +1441,10 @@ hipError_t forward_typed(int64_t N, int64_t L, int64_t C, int64_t groups, const 
             return hipGetLastError();
         });
     const Map h = cut(N, L, C, groups);
-    auto result = [&](auto late, const Wide* wide) {
+    auto result = [&](auto late, const Wide* wide, const Stat* stats) {
         with_act(act, [&](auto a) {
             forward_kernel<T, decltype(a)::value, decltype(late)::value><<<grid_for(h.work), h.threads, 0, s>>>(
-                x, Inputs{gamma, beta, mean, rstd}, h, y, wide, eps, mean, rstd);
+                x, gamma, beta, h, y, wide, stats, eps, mean, rstd);
         });
         return hipGetLastError();
     };
@@ -1408,9 +1452,10 @@ hipError_t forward_typed(int64_t N, int64_t L, int64_t C, int64_t groups, const 
         Wide* const wide = static_cast<Wide*>(ws);
         chunk_stats_kernel<T, true><<<grid_for(h.work), h.threads, 0, s>>>(x, h, nullptr, wide);
         const hipError_t rc = hipGetLastError();
-        return rc != hipSuccess ? rc : result(std::true_type(), wide);
+        return rc != hipSuccess ? rc : result(std::true_type(), wide, nullptr);
     }
-    Pair* partial = static_cast<Pair*>(ws);
+    Pair* const partial = static_cast<Pair*>(ws);
+    Stat* const stats_of = reinterpret_cast<Stat*>(partial + N * h.chunks * C + (joins_chunks(h) ? N * C : 0));
     chunk_stats_kernel<T, false><<<grid_for(h.work), h.threads, 0, s>>>(x, h, partial, nullptr);
     hipError_t rc = hipGetLastError();
     if (rc != hipSuccess)
@@ -1418,7 +1463,7 @@ hipError_t forward_typed(int64_t N, int64_t L, int64_t C, int64_t groups, const 
     const Pair* pairs_of = partial;
     Map of = h;
     if (joins_chunks(h)) {
-        Pair* joined = partial + N * h.chunks * C;
+        Pair* const joined = partial + N * h.chunks * C;
         join_chunks_kernel<<<grid_for(N * ceil_div(C, TILE)), SUM_THREADS, 0, s>>>(partial, h, joined);
         rc = hipGetLastError();
         if (rc != hipSuccess)
@@ -1429,16 +1474,17 @@ hipError_t forward_typed(int64_t N, int64_t L, int64_t C, int64_t groups, const 
     }
     const int64_t pairs = of.chunks * of.D, all = N * groups;
     auto stats = [&](auto* kernel, int team) {
-        kernel<<<grid_for(ceil_div(all, SUM_THREADS / team)), SUM_THREADS, 0, s>>>(pairs_of, of, eps, mean, rstd);
+        kernel<<<grid_for(ceil_div(all, SUM_THREADS / team)), SUM_THREADS, 0, s>>>(pairs_of, x, of, eps, stats_of, mean,
+                                                                                   rstd);
     };
     if (pairs <= 64 * 8)
-        stats(group_stats_kernel<64>, 64);
+        stats(group_stats_kernel<64, T>, 64);
     else
-        stats(group_stats_kernel<SUM_THREADS>, SUM_THREADS);
+        stats(group_stats_kernel<SUM_THREADS, T>, SUM_THREADS);
     rc = hipGetLastError();
     if (rc != hipSuccess)
         return rc;
-    return result(std::false_type(), nullptr);
+    return result(std::false_type(), nullptr, stats_of);
 }
 
 template <typename T>
@@ -1519,8 +1565,8 @@ int64_t group_norm_workspace(int32_t op, int64_t N, int64_t L, int64_t C, int64_
     if (joins_late(op, h))
         return N * h.chunks * (groups * static_cast<int64_t>(sizeof(Wide)) +
                                (backward ? C : 0) * static_cast<int64_t>(sizeof(Pair)));
-    return (N * h.chunks * C + (backward ? N * C + N * groups : joins_chunks(h) ? N * C : 0)) *
-           static_cast<int64_t>(sizeof(Pair));
+    const int64_t pairs = N * h.chunks * C + (backward ? N * C + N * groups : joins_chunks(h) ? N * C : 0);
+    return pairs * static_cast<int64_t>(sizeof(Pair)) + (backward ? 0 : N * groups * static_cast<int64_t>(sizeof(Stat)));
 }
 
 hipError_t launch_group_norm_forward(const void* x, const float* gamma, const float* beta, int64_t N, int64_t L,
