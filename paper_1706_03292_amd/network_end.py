@@ -49,7 +49,7 @@ class NetworkEnd:
             self.U, self.V = empty(P * B, classes), empty(P * B, features)
         else:
             self.dW = empty(P, classes, features)
-        self.optimizer = self.pool = self.copy = None
+        self.optimizer = self.pool = None
         if adamw is not None:
             self._make_adamw(**adamw)
             return
@@ -68,13 +68,17 @@ class NetworkEnd:
         self.rebuilt = torch.empty_like(self.W) if self.scheme == api.SFB else None
         fc = {"W": self.W, "shards": self.dW if self.rebuilt is None else self.rebuilt[None],
               "weight_decay": weight_decay, **api.AdamW.moments(self.W, bits)}
-        if self.dtype != torch.float32:
-            self.copy = fc["copy"] = self.W.to(self.dtype)
         self.optimizer = api.AdamW(
             [{"W": self.gamma, "shards": self.dgamma, **api.AdamW.moments(self.gamma)},
              {"W": self.beta, "shards": self.dbeta, **api.AdamW.moments(self.beta)}, fc], betas, eps)
         self.round_rng = self.rng[0].clone()   # of the 8-bit moments' rounding
         self.round_rng[0] += self.P
+
+    @property
+    def copy(self) -> torch.Tensor:
+        """The classifier in the activations' type, as a step's passes read it: W itself,
+        or made from it anew, since W may have been written from outside."""
+        return self.W.to(self.dtype)
 
     def _adamw_step(self) -> None:
         if self.rebuilt is not None:
@@ -110,7 +114,7 @@ class NetworkEnd:
         # factors multiply those with the rows' values.
         x, residual = (torch.where(valid[:, None], v, torch.zeros_like(v)) for v in (x, residual))
         dloss = valid.float() / valid.sum().clamp(min=1)
-        W = self.W if self.dtype == torch.float32 else self.W.to(self.dtype) if self.copy is None else self.copy
+        W = self.copy
         out = []
         for w in range(self.P):
             r = slice(w * self.B, (w + 1) * self.B)
