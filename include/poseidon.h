@@ -847,7 +847,9 @@ typedef struct poseidon_adamw_tensor {
  * 1 counts as 1) takes the place of lr and step where it is given, so that a
  * captured graph's replays can each have their own.  scale (one value in device
  * memory, NULL for 1) is poseidon_adamw_clip's result[1] as a rule; where it is
- * infinite or NaN the step is left out: everything keeps its value. */
+ * infinite or NaN the step is left out: everything keeps its value.  t is the
+ * caller's: m and v have not seen a step that was left out, so it is not to be
+ * counted, which a clock advanced on the device where scale is finite sees to. */
 typedef struct poseidon_adamw_rule {
     double         lr;
     double         beta1;

@@ -987,7 +987,8 @@ class AdamW:
         ``step`` (counted from 1), or ``clock``, the two as float64 values on the
         device for steps that are replayed from a graph; ``scale``, one float32 on
         the device, multiplies the gradients (clip's result[1:2]; not finite: the
-        step is left out); ``rng`` holds (seed, offset) as two int64 values on the
+        step is left out, and does not count: ``clock[1:] += scale.isfinite()``
+        before each step keeps t right); ``rng`` holds (seed, offset) as two int64 values on the
         device for the rounding of 8-bit moments, with another offset for every
         step (None: to nearest, at which v all but stands still where beta2 is
         near 1); ``from_sums`` takes the gradients from the sums

@@ -71,6 +71,9 @@ class NetworkEnd:
         self.optimizer = api.AdamW(
             [{"W": self.gamma, "shards": self.dgamma, **api.AdamW.moments(self.gamma)},
              {"W": self.beta, "shards": self.dbeta, **api.AdamW.moments(self.beta)}, fc], betas, eps)
+        # lr and the number of steps that were taken: one whose norm is not finite is left
+        # out on the device, and only there it is known
+        self.clock = torch.tensor([self.lr, 0.0], dtype=torch.float64, device=self.W.device)
         self.round_rng = self.rng[0].clone()   # of the 8-bit moments' rounding
         self.round_rng[0] += self.P
 
@@ -85,7 +88,9 @@ class NetworkEnd:
             self.rebuilt.zero_()
             api.sf_apply(self.rebuilt, self.U, self.V, -1.0)   # 0 + U^T V
         norm = self.optimizer.clip(self.max_norm)
-        self.optimizer.step(self.lr, self.steps, scale=norm[1:2], rng=self.round_rng)
+        self.clock[0] = self.lr
+        self.clock[1:] += norm[1:2].isfinite()
+        self.optimizer.step(clock=self.clock, scale=norm[1:2], rng=self.round_rng)
         self.round_rng[1] += 1
 
     def worker_step(self, w: int, x: torch.Tensor, residual: torch.Tensor, target: torch.Tensor,
