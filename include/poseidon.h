@@ -912,7 +912,8 @@ int poseidon_adamw_workspace(const poseidon_adamw* optimizer, int64_t* bytes);
  * (1 for norm 0, NaN for an infinite or NaN norm: poseidon_adamw_step then leaves
  * the step out).  All sums are formed in 64 bits.  A tensor with a `sum` array
  * gets sum_{p<P} G_p there, rounded to fp32, so that the step need not read the
- * workers' shards again (from_sums).  Returns POSEIDON_OK,
+ * workers' shards again (from_sums); a sum that is infinite in fp32 makes the norm
+ * infinite.  Returns POSEIDON_OK,
  * POSEIDON_ERR_INVALID_ARG (NULL arguments; max_norm not above 0 or NaN; result
  * or workspace overlapping each other or an array of the optimizer; a workspace
  * too small or off its boundary) or POSEIDON_ERR_HIP.

@@ -563,6 +563,7 @@ __global__ __launch_bounds__(THREADS) void squares_kernel(const AdamwGroup a, do
     const AdamwItem& q = a.item[t];
     const Range range = range_of(q, blockIdx.x - a.first_block[t], a.chunk);
     double sum = 0.0;
+    float most = 0.f;   // of the sums as fp32
     turns(range, [&](auto full, int64_t at) {
         constexpr bool FULL = decltype(full)::value;
         const int64_t e = at + threadIdx.x * QUAD, left = q.n - e;
@@ -578,11 +579,17 @@ __global__ __launch_bounds__(THREADS) void squares_kernel(const AdamwGroup a, do
             for (int i = 0; i < QUAD; ++i) {
                 sum = fma(s[k][i], s[k][i], sum);
                 x[i] = static_cast<float>(s[k][i]);
+                if (!ONE)
+                    most = fmaxf(most, fabsf(x[i]));
             }
             if (q.copy)
                 put<FULL>(static_cast<float*>(q.copy) + e + k * QUAD_GAP, left - k * QUAD_GAP, x);
         }
     });
+    // A kept sum that is infinite in fp32 makes the norm infinite: the step from the sums
+    // would be wrong, so it is left out.
+    if (!ONE && q.copy && most == INFINITY)
+        sum = INFINITY;
     sum = workgroup_sum<THREADS>(sum);
     if (threadIdx.x == 0)
         partial[blockIdx.x] = sum;
