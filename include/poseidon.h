@@ -804,7 +804,9 @@ int poseidon_group_norm_backward(const void* dy, const void* x, const float* gam
  *     copy <- W rounded to bf16                         (where a copy is asked for)
  *
  * The sum over the workers is formed in 64 bits.  The moments m and v are fp32
- * or, for a tensor with an exponents array, 8 bits a value:
+ * (where a change below half of a moment's last bit is lost: betas above about
+ * 1 - 2^-20 lose most of them) or, for a tensor with an exponents array, 8 bits a
+ * value:
  *
  * A block of 128 consecutive values of a tensor (the last one shorter) shares
  * one exponent byte for m and one for v, exponents[2 b] and exponents[2 b + 1]:
@@ -815,11 +817,15 @@ int poseidon_group_norm_backward(const void* dy, const void* x, const float* gam
  * bit 7; v has top 255.  So all-zero arrays are zero moments.  A moment is
  * computed in 64 bits, from the values that the codes stand for, and rounded
  * between its two neighbouring codes by 16 random bits r: upwards when its share
- * of the way from the lower one is at least 1 - r / 65536, so that the rounding
- * is right on average (v changes by a thousandth a step at beta2 = 0.999, a code
- * is a tenth: rounded to nearest it would stand still).  The step itself uses the
- * moments before that rounding.  m becomes 0 below its codes; v, which divides,
- * stays at code 1 there; values below 2^-126 are 0.  A block with an infinite or
+ * of the way from the lower one is at least 1 - r / 65536, so that between codes
+ * the rounding is right on average (v changes by a thousandth a step at beta2 =
+ * 0.999, a code is a tenth: rounded to nearest it would stand still).  The step
+ * itself uses the moments before that rounding.  Below code 1 it is not: m becomes
+ * 0 there, and v, which divides, stays at code 1; values below 2^-126 are 0.  m's
+ * code 1 is between 1.25 * 2^-16 and 1.25 * 2^-15 of its block's largest m, so an m
+ * that is 0 stays 0 while (1 - beta1) |g| is smaller than that (at beta1 = 0.9:
+ * |g| below 2 to 4 ten-thousandths of it), and the value steps by that one
+ * gradient's share of m alone.  A block with an infinite or
  * NaN moment gets the exponent byte 255 and all of its moments read as NaN.
  *
  * The random bits are poseidon_dropout's: rng holds the key and the counter's
