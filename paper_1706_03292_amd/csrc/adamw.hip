@@ -200,10 +200,7 @@ __device__ __forceinline__ void read_clock(Rates& r)
 }
 
 // W - lr (decay W + (m / c1) / (sqrt(v / c2) + eps)).  The square root and the
-// reciprocal are the instructions' (1 ulp each); they take denormals for 0, which
-// eps hides unless it is below SMALL_EPS itself.
-constexpr float SMALL_EPS = 1e-12f;
-
+// reciprocal are the instructions' (1 ulp each) unless CAREFUL (needs_care).
 template <bool CAREFUL>
 __device__ __forceinline__ float stepped(float w, float m, float v, float decay, const Rates& r)
 {
@@ -622,6 +619,15 @@ static float part_of(double b)
     return f < b || f == 0.f ? f : nextafterf(f, 0.f);
 }
 
+// The instructions take denormals for 0.  Of a v below 2^-126 the denominator then lacks
+// up to 2^-63 root, root = (1 - beta2^t)^-1/2 <= (1 - beta2)^-1/2: less than a rounding of
+// eps where that is 2^24 times as large.  And the reciprocal is 0 above 2^126, which only
+// eps can bring about (v's root ends at 2^64, root at 2^27).
+static bool needs_care(const Rates& r)
+{
+    return !(r.eps >= 0x1p-39 / sqrt(r.one_beta2) && r.eps < 0x1p125f);
+}
+
 hipError_t launch_adamw_step(const AdamwGroup& group, int32_t dtype, AdamwKind kind, const poseidon_adamw_rule& rule,
                              hipStream_t stream)
 {
@@ -652,7 +658,7 @@ hipError_t launch_adamw_step(const AdamwGroup& group, int32_t dtype, AdamwKind k
     };
     constexpr std::true_type yes{};
     constexpr std::false_type no{};
-    auto* k = r.eps < SMALL_EPS ? (kind.one ? pick(yes, yes) : pick(yes, no)) : (kind.one ? pick(no, yes) : pick(no, no));
+    auto* k = needs_care(r) ? (kind.one ? pick(yes, yes) : pick(yes, no)) : (kind.one ? pick(no, yes) : pick(no, no));
     k<<<group.blocks, THREADS, 0, stream>>>(group, r);
     return hipGetLastError();
 }
