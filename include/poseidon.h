@@ -752,7 +752,9 @@ int poseidon_xent_factor(const void* X, const void* W, const int64_t* target, co
  *     z = (x - mean) * rstd * gamma + beta,  y = act(z)
  *
  * x and y are of `dtype`; gamma and beta have C values, mean and rstd N * groups.
- * act: z itself, max(z, 0), or z / (1 + e^-z).
+ * act: z itself, max(z, 0), or z / (1 + e^-z).  The squares of x - mean are fp32: a
+ * group's have to add up to less than 3e38 (above, rstd is 0), and with eps = 0 to
+ * stay above 1e-38.
  */
 #define POSEIDON_ACT_NONE 0
 #define POSEIDON_ACT_RELU 1
@@ -777,8 +779,9 @@ int poseidon_group_norm_forward(const void* x, const float* gamma, const float* 
                                 float* rstd, void* workspace, int64_t workspace_bytes, hipStream_t stream);
 
 /*
- * Its backward pass, from mean and rstd as the forward pass left them; with
- * n = (x - mean) * rstd, dz = dy * act'(n * gamma + beta) and g = dz * gamma:
+ * Its backward pass, from mean and rstd as the forward pass left them (rounded to
+ * fp32, which moves n by up to 2^-24 |mean| rstd; the forward pass's own y is
+ * without that); with n = (x - mean) * rstd, dz = dy * act'(n * gamma + beta) and g = dz * gamma:
  *
  *     dx = rstd * (g - avg(g) - n * avg(g * n))       (averages over sample and group)
  *     dgamma = sum over samples and positions of dz * n,   dbeta = the same of dz

@@ -925,8 +925,8 @@ class AdamW:
     slices of one flat buffer per worker) and the moments ``m`` and ``v``: fp32 of
     W's size, or uint8 of W's size together with ``exponents``, uint8 of
     2 * ceil(n / 128).  All-zero arrays are zero moments (``moments`` makes them).
-    (8 bits: an m below 2^-15 of the largest in its block of 128 is lost, and one that
-    is 0 stays 0 while its (1 - beta1) |g| is below that.)
+    (8 bits: an m below 1.25 * 2^-15 or less of the largest in its block of 128 is lost,
+    and one that is 0 stays 0 while its (1 - beta1) |g| is below that.)
     Optional: ``weight_decay`` (0), ``copy`` (bf16 of W's size, receives the new
     weights), ``sum`` (fp32 of W's size, receives the summed gradient in
     ``clip``).  The shards of all entries have one type, fp32 or bf16.  The

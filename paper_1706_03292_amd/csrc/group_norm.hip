@@ -2,7 +2,7 @@
 // (include/poseidon.h gives the formulas).  A few operations per value, bound by
 // memory: x (and dy) read, y (dx) written once each is what it cannot do without.
 // bf16: forward 32 x 56 x 56 x 256 in one launch 30 us (3.4 TB/s of that), 32 x 224 x
-// 224 x 64 in two 112 us (3.7: x is read twice), backward 32 x 56 x 56 x 256 in
+// 224 x 64 in two 113 us (3.6: x is read twice), backward 32 x 56 x 56 x 256 in
 // three 55 us (2.8).
 //
 // A sample is L rows of C channels.  Threads stand in teams of a row each, a thread
@@ -1285,11 +1285,11 @@ Map cut(int64_t N, int64_t L, int64_t C, int64_t groups)
 
 // Whether each workgroup of the result joins its sample's groups itself (join_late),
 // which leaves out a launch: where a row is one workgroup's and a group's chunks are few
-// to a thread.  Forward, three launches and two: 2 x 1225 x 288 fp32 in 32 groups 13.8
-// and 11.3 us, 17 x 1225 x 288 24.5 and 22.6, 4 x 9000 x 1000 fp32 in 8 99 and 90, 32 x
-// 50176 x 64 bf16 in 32 118 and 118; with 16 chunks a thread but in one round (more
+// to a thread.  Forward, three launches and two: 2 x 1225 x 288 fp32 in 32 groups 14.9
+// and 12.1 us, 17 x 1225 x 288 26.0 and 22.9, 4 x 9000 x 1000 fp32 in 8 98 and 89, 32 x
+// 50176 x 64 bf16 in 32 116 and 114; with 16 chunks a thread but in one round (more
 // registers) 128, with 131 chunks of 32 groups in three rounds (8 x 3136 x 320 fp32)
-// 29.6 and 32.5, with one group of 2048 chunks 16.7 and 25.9.  The backward pass has
+// 31.7 and 32.0, with one group of 2048 chunks 16.7 and 25.9.  The backward pass has
 // more to do at both ends and takes it where the chip holds all workgroups at once: 60 x
 // 784 x 100 bf16 in 20 21.9 and 19.4, 2 x 1225 x 288 fp32 14.4 and 12.6, but 32 x 3136 x
 // 256 bf16 on 1792 workgroups 56 and 58.
